@@ -26,8 +26,8 @@
  *   - Return value: EMOE_OK or a negative emoe_status.  Arguments are checked
  *     on the host before anything is enqueued; on a validation error nothing
  *     is enqueued and no output is touched.  T == 0 is a successful no-op.
- *   - Limits: 1 <= k <= S <= E <= 64; d_model and d_ff multiples of 8;
- *     (T*k + 2) * max(d_model, d_ff) <= 2^31.
+ *   - Limits of the layer's calls: 1 <= k <= S <= E <= 64; d_model and d_ff multiples of 8;
+ *     (T*k + 2) * max(d_model, d_ff) <= 2^31.  The cache's and the attention's stand with them.
  */
 #ifndef EMOE_H
 #define EMOE_H
@@ -407,6 +407,126 @@ int emoe_expected_latency(int32_t n_running, const emoe_request *running, int32_
 int emoe_schedule(int32_t n_waiting, const emoe_request *waiting, int32_t n_scheduled,
                   const emoe_request *scheduled, int64_t t_max, double c, int32_t *admitted, int32_t *n_admitted);
 int emoe_generation_tick(emoe_request *request, int32_t completed, double reset_fraction);
+
+/*
+ * ---- Paged key/value cache in 4 bits, and attention over it ---------------------------------------
+ *
+ * What stands between two MoE layers of a model that serves: the HBM that absent experts leave free goes
+ * to longer contexts and larger batches (Section 5.5), that is, to the cache of keys and values.
+ *
+ * Cache: `pages` pages of `page_size` tokens, [pages][kv_heads][page_size * head_dim * 17 / 16 bytes] uint8
+ * dev, 16-byte aligned; one tensor per attention layer, all layers of a model sharing the tables.  A page of
+ * one head holds, in this order, the codes of its keys [page_size][head_dim / 2], the codes of its values
+ * (same), the scales of its keys [page_size][head_dim / 32], the scales of its values.  32 consecutive
+ * elements of a row form a block: element = code value * 2^(scale byte - 127); code values (4 bits, sign in
+ * bit 3): 0, 0.5, 1, 1.5, 2, 3, 4, 6; the even element of a byte in its low half.  These are the element
+ * and scale types of the OCP microscaling format MXFP4, which the matrix cores and converters of gfx950 read.
+ * Memory that was never written, NaN patterns included, does not reach any result.
+ *
+ * Requests have a row each (rows = R) in the per-request arrays and in the block table [R][table_width]
+ * int32 dev, whose entry b is the page of the request's tokens b * page_size on.  The slot of a token is
+ * page * page_size + place in the page.  Entries and slots outside the cache (-1) belong to nobody: such
+ * tokens are not written and not seen.
+ *
+ * Limits: page_size 16, 32, 64, 128 or 256; head_dim 64 or 128; kv_heads 1..256; pages * page_size <
+ * 2^31 and table_width * page_size < 2^31; rows 0..65536; T * kv_heads * head_dim <= 2^33.
+ */
+typedef struct {
+    int32_t pages;       /* pages of the cache                    */
+    int32_t page_size;   /* tokens of a page                      */
+    int32_t kv_heads;    /* heads of keys and values              */
+    int32_t head_dim;    /* elements of a head's row              */
+    int32_t rows;        /* R: requests of this batch             */
+    int32_t table_width; /* entries of a row of the block table   */
+} emoe_kv_desc;
+
+/* Bytes of a cache of desc->pages pages.  Pure host arithmetic. */
+int emoe_kv_cache_bytes(const emoe_kv_desc *desc, size_t *bytes);
+
+/*
+ * The tables of one step, from the requests' lengths.  Request r holds len[r] tokens and brings new_len[r]
+ * (negative: none); its tokens are the next new_len[r] of the step's T, in row order.  Pages come from a
+ * ring of free ones: free_pages [pages] int32, of which the entries head .. tail-1 (modulo pages) are
+ * free, counters = {head, tail}, two int64 that only ever grow.  have = ceil(len / page_size), want = ceil((len +
+ * new_len) / page_size); the pages b = have .. want-1 of the rows are taken in row order, from head on.
+ *   block_table[r][b]  the pages taken (other entries are not touched)
+ *   cu_new [R+1]       exclusive prefix sum of new_len (at most 2^31-1)
+ *   slot [T], position [T]  of every token: its slot, and its place len + i in its request
+ *   seq_len [R]        len + new_len
+ *   counters_out [2]   {head + pages taken, tail}
+ *   refused [1]        number of refused rows
+ * A row is refused, and takes nothing, if want > table_width, if its tokens end beyond T, or if it needs pages
+ * and the rows up to it need more than tail - head together.  Its tokens have slot -1 and their positions, its
+ * seq_len is 0 (nothing is seen); it keeps what it held: the caller passes the same len again later.
+ * Tokens from cu_new[R] on, up to T, have slot -1 and position -1.  All pointers dev int32 but the
+ * counters; counters_out is not counters.  Nothing that is read is written (but for the table's new entries): the
+ * same call again gives the same result.
+ */
+int emoe_kv_plan(const emoe_kv_desc *desc, int32_t T, const int32_t *len, const int32_t *new_len, int32_t *block_table,
+                 const int32_t *free_pages, const int64_t *counters, int32_t *cu_new, int32_t *slot, int32_t *position,
+                 int32_t *seq_len, int64_t *counters_out, int32_t *refused, void *stream);
+
+/*
+ * Pages that nobody will read any more, back to the ring: between two steps, when request r has grown from
+ * len_before[r] to len[r] tokens since the last release.  With a sliding window (see emoe_kv_attention) the
+ * pages b that hold no sink and no token that a query at position len[r] or later sees, that is
+ * ceil(sinks / page_size) <= b < floor((len - window + 1) / page_size), leave; those that had left at len_before
+ * have done so already.  Without one (window 0) no page leaves before its request ends, and len_before may be
+ * NULL.  ended[r] != 0 (NULL: none): all pages that are left go back.  Pages go into the ring from tail on, in row order and
+ * ascending within a row; counters_out = {head, tail + pages returned}.  The table is not touched.  As emoe_kv_plan,
+ * counters_out is not counters.
+ */
+int emoe_kv_release(const emoe_kv_desc *desc, const int32_t *len_before, const int32_t *len, const int32_t *ended,
+                    int32_t window, int32_t sinks, const int32_t *block_table, int32_t *free_pages, const int64_t *counters,
+                    int64_t *counters_out, void *stream);
+
+/*
+ * Keys and values of T tokens into their slots.  k, v: dev, element type dtype (emoe_dtype), row t of head h
+ * at element t * stride + h * head_dim (strides of at least kv_heads * head_dim, multiples of 8: a slice of a fused
+ * projection's output will do); 16-byte aligned.  slot [T] int32 dev, all different where >= 0.  A block's scale
+ * is the smallest power of two s >= 2^-126 with max|x| <= 7 s; its codes are the values nearest to x / s, ties to
+ * the even code, beyond 6 the 6: all of it exact, so that the bits depend on nothing but the input.  A block
+ * that holds an infinity or a NaN is stored as NaN (scale byte 255).
+ */
+int emoe_kv_append(const emoe_kv_desc *desc, int32_t T, int32_t dtype, const void *k, int64_t k_stride, const void *v,
+                   int64_t v_stride, const int32_t *slot, void *cache, void *stream);
+
+/* The numbers that T slots hold: k, v [T][kv_heads][head_dim] of dtype dev (out), dense; zeros where slot < 0. */
+int emoe_kv_read(const emoe_kv_desc *desc, int32_t T, int32_t dtype, const void *cache, const int32_t *slot, void *k,
+                 void *v, void *stream);
+
+typedef struct {
+    int32_t T;          /* query tokens in this call                                             */
+    int32_t q_heads;    /* a multiple of kv_heads: consecutive q_heads / kv_heads share a kv head */
+    int32_t dtype;      /* emoe_dtype of q and out                                               */
+    int32_t max_new;    /* no request brings more query tokens than this                         */
+    int32_t window;     /* 0: all earlier tokens are seen; else the last `window`, itself included */
+    int32_t sinks;      /* with a window: the first `sinks` tokens stay visible                   */
+    float scale;        /* of the scores, head_dim^-0.5 as a rule                                */
+    int32_t reserved;   /* 0                                                                     */
+    int64_t q_stride;   /* elements from one token's q to the next, a multiple of 8              */
+    int64_t out_stride; /* the same of out                                                       */
+} emoe_attention_desc;
+
+/* Bytes of device workspace of emoe_kv_attention: at most 64 MiB, whatever the extents.  Needs no initialising, and nothing in
+ * it outlives a call. */
+int emoe_kv_attention_workspace_bytes(const emoe_kv_desc *desc, const emoe_attention_desc *attention, size_t *bytes);
+
+/*
+ * Attention of a step's queries over the cache, their own tokens included (append first).  Request r has the queries
+ * cu_new[r] .. cu_new[r+1]-1 and seq_len[r] tokens in the cache; its i-th of n queries stands at position p = seq_len -
+ * n + i and sees the tokens j <= p with window == 0, j > p - window, or j < sinks.
+ *   out[t][h] = sum_j softmax_j(scale * q[t][h] . k_j) v_j, fp32 sums; zeros where nothing is seen (p < 0).
+ * q [T][q_heads][head_dim] and out dev, dtype, rows as the strides say, 16-byte aligned; block_table, seq_len, cu_new as
+ * emoe_kv_plan leaves them.  Lengths are read on the device only.  bf16: the weights of the softmax are rounded to
+ * bf16 for the product with the values, fp32: nothing is rounded below fp32.  NaN or infinite tokens make NaN of what sees them,
+ * and of nothing else.  Rows of out from cu_new[R] on are not written.  Results do not depend on the order of
+ * execution.  ws dev, 16-byte aligned, not shared with a call that may run at the same time.
+ * Limits: q_heads / kv_heads <= 256, T * q_heads < 2^31 / 16, max_new <= T.
+ */
+int emoe_kv_attention(const emoe_kv_desc *desc, const emoe_attention_desc *attention, const void *q, const void *cache,
+                      const int32_t *block_table, const int32_t *seq_len, const int32_t *cu_new, void *out, void *ws,
+                      size_t ws_bytes, void *stream);
 
 /*
  * Measurement aids (no step of the layer; for the benchmark's measured ceilings beside the

@@ -30,13 +30,25 @@ EXPORTS = ("emoe_status_string", "emoe_workspace_bytes", "emoe_route", "emoe_rou
            "emoe_loader_next_prompt", "emoe_loader_update", "emoe_loader_layer_begin", "emoe_loader_layer_end",
            "emoe_loader_layer_ready", "emoe_loader_residents", "emoe_loader_synchronize", "emoe_expected_latency", "emoe_schedule",
            "emoe_generation_tick", "emoe_measure_mfma_loop", "emoe_measure_read_stream",
-           "emoe_measure_copy_stream", "emoe_measure_scatter_combine")
+           "emoe_measure_copy_stream", "emoe_measure_scatter_combine", "emoe_kv_cache_bytes", "emoe_kv_plan", "emoe_kv_release",
+           "emoe_kv_append", "emoe_kv_read", "emoe_kv_attention_workspace_bytes", "emoe_kv_attention")
 
 
 class EmoeLayerDesc(ctypes.Structure):
     _fields_ = [("T", ctypes.c_int32), ("d_model", ctypes.c_int32), ("d_ff", ctypes.c_int32),
                 ("E", ctypes.c_int32), ("k", ctypes.c_int32), ("S", ctypes.c_int32),
                 ("dtype", ctypes.c_int32), ("act", ctypes.c_int32)]
+
+
+class EmoeKvDesc(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("rows", ctypes.c_int32), ("table_width", ctypes.c_int32)]
+
+
+class EmoeAttentionDesc(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("dtype", ctypes.c_int32), ("max_new", ctypes.c_int32),
+                ("window", ctypes.c_int32), ("sinks", ctypes.c_int32), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32),
+                ("q_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64)]
 
 
 class EmoeError(RuntimeError):
@@ -77,6 +89,15 @@ def lib() -> ctypes.CDLL:
         L.emoe_expert_ffn_gather_combine.argtypes = [dp] + [vp] * 11 + [sz, vp]
         L.emoe_layer_forward.argtypes = [dp] + [vp] * 15 + [vp, sz, vp, sz, vp]
         L.emoe_load_experts.argtypes = [dp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        i64 = ctypes.c_int64
+        kp, ap = ctypes.POINTER(EmoeKvDesc), ctypes.POINTER(EmoeAttentionDesc)
+        L.emoe_kv_cache_bytes.argtypes = [kp, ctypes.POINTER(sz)]
+        L.emoe_kv_plan.argtypes = [kp, i32] + [vp] * 12
+        L.emoe_kv_release.argtypes = [kp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp]
+        L.emoe_kv_append.argtypes = [kp, i32, i32, vp, i64, vp, i64, vp, vp, vp]
+        L.emoe_kv_read.argtypes = [kp, i32, i32, vp, vp, vp, vp, vp]
+        L.emoe_kv_attention_workspace_bytes.argtypes = [kp, ap, ctypes.POINTER(sz)]
+        L.emoe_kv_attention.argtypes = [kp, ap] + [vp] * 7 + [sz, vp]
         for name in EXPORTS[1:]:
             getattr(L, name).restype = ctypes.c_int
         _lib = L
@@ -281,6 +302,68 @@ def emoe_layer_forward(desc, x, w_gate, gate_bias, slot_of_expert, w1_slots, w3_
                                   _addr(out), _addr(permute_ws), int(permute_ws_bytes), _addr(ffn_ws), int(ffn_ws_bytes),
                                   _stream_addr(stream))
     return _check(rc, "emoe_layer_forward", check)
+
+
+def make_kv_desc(pages: int, page_size: int, kv_heads: int, head_dim: int, rows: int, table_width: int) -> EmoeKvDesc:
+    return EmoeKvDesc(pages, page_size, kv_heads, head_dim, rows, table_width)
+
+
+def make_attention_desc(T: int, q_heads: int, head_dim: int, dtype, max_new: int, window: int = 0, sinks: int = 0,
+                        scale: Optional[float] = None, q_stride: Optional[int] = None,
+                        out_stride: Optional[int] = None) -> EmoeAttentionDesc:
+    """`scale`: head_dim ** -0.5 if not given; strides in elements from token to token, dense if not given."""
+    row = q_heads * head_dim
+    return EmoeAttentionDesc(T, q_heads, DTYPES.get(dtype, dtype), max_new, window, sinks, head_dim ** -0.5 if scale is None else scale, 0,
+                             row if q_stride is None else q_stride, row if out_stride is None else out_stride)
+
+
+def emoe_kv_cache_bytes(kv: EmoeKvDesc, check=True) -> int:
+    n = ctypes.c_size_t(0)
+    rc = lib().emoe_kv_cache_bytes(ctypes.byref(kv), ctypes.byref(n))
+    _check(rc, "emoe_kv_cache_bytes", check)
+    return n.value if rc == EMOE_OK else rc
+
+
+def emoe_kv_plan(kv, T, length, new_len, block_table, free_pages, counters, cu_new, slot, position, seq_len, counters_out, refused,
+                 stream=None, check=True) -> int:
+    rc = lib().emoe_kv_plan(ctypes.byref(kv), T, _addr(length), _addr(new_len), _addr(block_table), _addr(free_pages), _addr(counters),
+                            _addr(cu_new), _addr(slot), _addr(position), _addr(seq_len), _addr(counters_out), _addr(refused),
+                            _stream_addr(stream))
+    return _check(rc, "emoe_kv_plan", check)
+
+
+def emoe_kv_release(kv, len_before, length, ended, window, sinks, block_table, free_pages, counters, counters_out, stream=None,
+                    check=True) -> int:
+    rc = lib().emoe_kv_release(ctypes.byref(kv), _addr(len_before), _addr(length), _addr(ended), window, sinks, _addr(block_table),
+                               _addr(free_pages), _addr(counters), _addr(counters_out), _stream_addr(stream))
+    return _check(rc, "emoe_kv_release", check)
+
+
+def emoe_kv_append(kv, T, dtype, k, v, slot, cache, k_stride=None, v_stride=None, stream=None, check=True) -> int:
+    """`k_stride`, `v_stride`: elements from one token's row to the next, kv_heads * head_dim if not given."""
+    row = kv.kv_heads * kv.head_dim
+    rc = lib().emoe_kv_append(ctypes.byref(kv), T, DTYPES.get(dtype, dtype), _addr(k), row if k_stride is None else k_stride, _addr(v),
+                              row if v_stride is None else v_stride, _addr(slot), _addr(cache), _stream_addr(stream))
+    return _check(rc, "emoe_kv_append", check)
+
+
+def emoe_kv_read(kv, T, dtype, cache, slot, k, v, stream=None, check=True) -> int:
+    rc = lib().emoe_kv_read(ctypes.byref(kv), T, DTYPES.get(dtype, dtype), _addr(cache), _addr(slot), _addr(k), _addr(v),
+                            _stream_addr(stream))
+    return _check(rc, "emoe_kv_read", check)
+
+
+def emoe_kv_attention_workspace_bytes(kv, attention, check=True) -> int:
+    n = ctypes.c_size_t(0)
+    rc = lib().emoe_kv_attention_workspace_bytes(ctypes.byref(kv), ctypes.byref(attention), ctypes.byref(n))
+    _check(rc, "emoe_kv_attention_workspace_bytes", check)
+    return n.value if rc == EMOE_OK else rc
+
+
+def emoe_kv_attention(kv, attention, q, cache, block_table, seq_len, cu_new, out, ws, ws_bytes, stream=None, check=True) -> int:
+    rc = lib().emoe_kv_attention(ctypes.byref(kv), ctypes.byref(attention), _addr(q), _addr(cache), _addr(block_table), _addr(seq_len),
+                                 _addr(cu_new), _addr(out), _addr(ws), int(ws_bytes), _stream_addr(stream))
+    return _check(rc, "emoe_kv_attention", check)
 
 
 def _i32_array(values: Optional[Sequence[int]]):

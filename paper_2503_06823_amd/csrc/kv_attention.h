@@ -1,0 +1,113 @@
+// What the attention kernels share: which tokens a row of queries sees, how the work is cut, the fragments of the matrix
+// instructions.
+#pragma once
+#include "kv_cache.h"
+
+namespace emoe {
+namespace {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short shortx4 __attribute__((ext_vector_type(4)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLowest = -3.0e38f;  // of a running maximum: finite, so that nothing minus it is a NaN
+
+// A request's queries and keys, from the lengths on the device, whatever these hold.
+struct Request {
+    int first;  // its first query's token
+    int n;      // query tokens
+    int seq;    // tokens that can be seen, positions 0 .. seq-1
+    int len;    // of the whole request: query i stands at len - n + i
+};
+__device__ __forceinline__ Request request(const AttentionArgs& a, int r) {
+    Request q;
+    int begin = a.cu_new[r], end = a.cu_new[r + 1];
+    begin = begin < 0 ? 0 : begin < a.T ? begin : a.T;
+    end = end < begin ? begin : end < a.T ? end : a.T;
+    q.first = begin;
+    q.n = end - begin < a.max_new ? end - begin : a.max_new;
+    q.len = a.seq_len[r];
+    const int most = a.width << a.page.log2_size;
+    q.seq = q.len < 0 ? 0 : q.len < most ? q.len : most;
+    return q;
+}
+
+// The key tiles that queries at positions first .. last see: 0 .. sinks-1 and from .. to-1, the i-th of them.
+struct Tiles {
+    int sinks, from, to;
+    __device__ int count() const { return sinks + (to > from ? to - from : 0); }
+    __device__ int tile(int i) const { return i < sinks ? i : i - sinks + from; }
+};
+template <int SIZE>
+__device__ __forceinline__ Tiles tiles(const AttentionArgs& a, int seq, int first, int last) {
+    Tiles t;
+    const int end = last + 1 < seq ? last + 1 : seq;
+    t.to = end > 0 ? (end + SIZE - 1) / SIZE : 0;
+    t.sinks = t.from = 0;
+    if (a.window > 0) {
+        const long long lo = (long long)first - a.window + 1;
+        t.from = lo > 0 ? (int)(lo / SIZE) : 0;
+        const int s = a.sinks < end ? a.sinks : end;
+        t.sinks = s > 0 ? (s + SIZE - 1) / SIZE : 0;
+        if (t.sinks >= t.from) t.sinks = t.from = 0;  // one piece
+    }
+    return t;
+}
+
+__device__ __forceinline__ int wave_inclusive(int v) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) {
+        const int o = __shfl_up(v, s);
+        if (lane >= s) v += o;
+    }
+    return v;
+}
+
+// x over the four lanes that hold one query (lane, lane ^ 16, ^ 32, ^ 48).
+template <class F>
+__device__ __forceinline__ float over_groups(float x, F f) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = f(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// Eight elements of 4 bits as bf16: exact, a code has two significant bits.
+__device__ __forceinline__ bf16x8 from_codes(uint32_t codes, float scale) {
+    union {
+        bf16x2 two[4];
+        bf16x8 eight;
+    } u;
+    u.two[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0);
+    u.two[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1);
+    u.two[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2);
+    u.two[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3);
+    return u.eight;
+}
+
+// Eight fp32 numbers as one bf16 operand or, with PIECES 3, as three whose sum is exact to 24 bits.
+template <int PIECES>
+__device__ __forceinline__ void to_operands(const float* x, bf16x8* out) {
+    float rest[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rest[i] = x[i];
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            out[p][i] = (__bf16)rest[i];
+            if (p + 1 < PIECES) rest[i] -= (float)out[p][i];
+        }
+}
+
+// Four rows (tokens) of one column (element) from row-major bf16 in LDS: of the 16 lanes of a group, lane j names the eight
+// bytes of columns 4 (j % 4) on of row j / 4, and receives column j of the four rows.
+__device__ __forceinline__ shortx4 read_transposed(const bf16_t* p) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)p);
+}
+
+}  // namespace
+}  // namespace emoe

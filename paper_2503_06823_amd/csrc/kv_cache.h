@@ -1,0 +1,62 @@
+// The paged 4-bit cache of keys and values: layout, and what its kernels share.
+#pragma once
+#include "common.h"
+
+namespace emoe {
+
+constexpr int kKvBlock = 32;                        // elements that share a scale
+constexpr size_t kAttentionWsBytes = 64ull << 20;   // no call needs more
+
+// Host-side checks; EMOE_OK or an error.
+int validate_kv_desc(const emoe_kv_desc* d);
+int validate_attention(const emoe_kv_desc* d, const emoe_attention_desc* a);
+
+inline int log2_of(int v) {
+    int n = 0;
+    while ((1 << n) < v) ++n;
+    return n;
+}
+
+// Bytes of one head's part of a page, and where its sections begin.
+struct KvPage {
+    int log2_size;   // tokens
+    int codes;       // bytes of the codes of its keys, and of its values
+    int scales;      // the same of the scales
+    __host__ __device__ int bytes() const { return 2 * (codes + scales); }
+};
+inline KvPage kv_page(const emoe_kv_desc& d) {
+    return {log2_of(d.page_size), d.page_size * d.head_dim / 2, d.page_size * d.head_dim / kKvBlock};
+}
+
+// A scale byte as the factor that the converters take: they look at the exponent alone; 255 becomes a NaN.
+__device__ __forceinline__ float scale_of_byte(uint32_t b) { return __uint_as_float(__umul24(b, 0x808000u)); }
+
+hipError_t launch_kv_plan(const emoe_kv_desc& d, int T, const int32_t* len, const int32_t* new_len, int32_t* table,
+                          const int32_t* free_pages, const int64_t* counters, int32_t* cu_new, int32_t* slot, int32_t* position,
+                          int32_t* seq_len, int64_t* counters_out, int32_t* refused, hipStream_t st);
+hipError_t launch_kv_release(const emoe_kv_desc& d, const int32_t* len_before, const int32_t* len, const int32_t* ended, int window,
+                             int sinks, const int32_t* table, int32_t* free_pages, const int64_t* counters, int64_t* counters_out,
+                             hipStream_t st);
+hipError_t launch_kv_append(const emoe_kv_desc& d, int T, int dtype, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                            const int32_t* slot, void* cache, hipStream_t st);
+hipError_t launch_kv_read(const emoe_kv_desc& d, int T, int dtype, const void* cache, const int32_t* slot, void* k, void* v,
+                          hipStream_t st);
+
+// What the attention kernels are told.
+struct AttentionArgs {
+    const void* q;
+    const uint8_t* cache;
+    const int32_t* table;
+    const int32_t* seq_len;
+    const int32_t* cu_new;
+    void* out;
+    uint8_t* ws;
+    int64_t q_stride, out_stride;
+    float scale_log2;  // scale * log2(e): the exponentials are powers of two
+    int T, R, max_new, q_heads, kv_heads, group, width, pages, window, sinks;
+    KvPage page;
+};
+size_t attention_ws_bytes(const emoe_kv_desc& d, const emoe_attention_desc& a);
+hipError_t launch_attention(const emoe_kv_desc& d, const emoe_attention_desc& a, const AttentionArgs& args, hipStream_t st);
+
+}  // namespace emoe

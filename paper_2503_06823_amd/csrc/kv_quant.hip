@@ -1,0 +1,164 @@
+// Rows of keys and values into the 4-bit cache, and back.
+//
+// Four lanes hold a block of 32 elements, eight each: one 16-byte load of bf16, the largest magnitude by two steps over the
+// lanes (as integers: a NaN is larger than all numbers), a power of two as scale, and the converters of gfx950, whose rounding is to
+// nearest even.  With the scale a power of two x / s is exact, so the codes depend on the input alone.  Bound by HBM at
+// many tokens: 2 + 17/32 bytes per bf16 element in, the same out; by the launch at a decode step's.
+#include "kv_cache.h"
+
+namespace emoe {
+namespace {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
+
+constexpr int kThreads = 256;
+
+// Eight elements of a row as fp32.
+__device__ __forceinline__ void load8(const float* p, float* x) {
+    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+}
+__device__ __forceinline__ void load8(const bf16_t* p, float* x) {
+    const uint4 a = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(w[i] << 16);
+        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+}
+
+// The larger of this lane's value and that of the lane CTRL leads to (quad_perm).
+template <int CTRL>
+__device__ __forceinline__ uint32_t larger(uint32_t v) {
+    const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
+    return v > o ? v : o;
+}
+
+// Where a slot's row of one head lies: codes, scales.
+struct RowAt {
+    size_t codes, scales;
+};
+__device__ __forceinline__ RowAt row_at(int slot, int head, int kv_heads, KvPage page, bool values, int dim) {
+    const int p = slot >> page.log2_size, in_page = slot & ((1 << page.log2_size) - 1);
+    const size_t base = ((size_t)p * kv_heads + head) * (size_t)(2 * (page.codes + page.scales));
+    return {base + (values ? page.codes : 0) + (size_t)in_page * (dim / 2),
+            base + 2 * page.codes + (values ? page.scales : 0) + (size_t)in_page * (dim / kKvBlock)};
+}
+
+// blockIdx.y: 0 the keys, 1 the values.  A thread: eight elements.
+template <class E>
+__global__ __launch_bounds__(kThreads) void kv_append_kernel(const E* __restrict__ k, int64_t k_stride, const E* __restrict__ v,
+                                                             int64_t v_stride, const int32_t* __restrict__ slots, uint8_t* __restrict__ cache,
+                                                             int T, int kv_heads, int dim, int n_slots, KvPage page) {
+    const bool values = blockIdx.y != 0;
+    const int per_row = kv_heads * dim / 8, per_head = dim / 8;
+    const long long n = (long long)T * per_row;
+    const long long i = (long long)blockIdx.x * kThreads + threadIdx.x;
+    if (i >= n) return;  // whole blocks of four lanes: per_row is a multiple of 8
+    const long long t = i / per_row;
+    const int e = (int)(i - t * per_row), head = e / per_head, piece = e % per_head;
+    const int slot = slots[t];
+    if ((unsigned)slot >= (unsigned)n_slots) return;
+    float x[8];
+    load8((values ? v + t * v_stride : k + t * k_stride) + (size_t)e * 8, x);
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t a = __float_as_uint(x[j]) & 0x7fffffffu;
+        top = a > top ? a : top;
+    }
+    top = larger<0xB1>(top);  // lanes 1 0 3 2
+    top = larger<0x4E>(top);  // lanes 2 3 0 1
+    const bool finite = top < 0x7f800000u;
+    // amax = 1.m * 2^(e - 127) <= 7 * 2^k = 1.75 * 2^(k + 2)
+    int byte = (int)(top >> 23) - 2 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
+    byte = byte < 1 ? 1 : byte;
+    byte = finite ? byte : 255;
+    const float scale = __uint_as_float((uint32_t)byte << 23);
+    uint32_t codes = 0;
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[0], x[1], scale, 0);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[2], x[3], scale, 1);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[4], x[5], scale, 2);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[6], x[7], scale, 3);
+    const RowAt at = row_at(slot, head, kv_heads, page, values, dim);
+    *reinterpret_cast<uint32_t*>(cache + at.codes + piece * 4) = finite ? codes : 0u;
+    if ((piece & 3) == 0) cache[at.scales + piece / 4] = (uint8_t)byte;
+}
+
+__device__ __forceinline__ void store8(float* p, uint32_t codes, float scale) {
+    floatx2 f[4];
+    f[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 0);
+    f[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 1);
+    f[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 2);
+    f[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 3);
+    reinterpret_cast<float4*>(p)[0] = float4{f[0][0], f[0][1], f[1][0], f[1][1]};
+    reinterpret_cast<float4*>(p)[1] = float4{f[2][0], f[2][1], f[3][0], f[3][1]};
+}
+__device__ __forceinline__ void store8(bf16_t* p, uint32_t codes, float scale) {
+    uint4 o;
+    o.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0));
+    o.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1));
+    o.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2));
+    o.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
+    *reinterpret_cast<uint4*>(p) = o;
+}
+
+template <class E>
+__global__ __launch_bounds__(kThreads) void kv_read_kernel(const uint8_t* __restrict__ cache, const int32_t* __restrict__ slots,
+                                                           E* __restrict__ k, E* __restrict__ v, int T, int kv_heads, int dim, int n_slots,
+                                                           KvPage page) {
+    const bool values = blockIdx.y != 0;
+    const int per_row = kv_heads * dim / 8, per_head = dim / 8;
+    const long long n = (long long)T * per_row;
+    const long long i = (long long)blockIdx.x * kThreads + threadIdx.x;
+    if (i >= n) return;
+    const long long t = i / per_row;
+    const int e = (int)(i - t * per_row), head = e / per_head, piece = e % per_head;
+    const int slot = slots[t];
+    uint32_t codes = 0, byte = 127;
+    if ((unsigned)slot < (unsigned)n_slots) {
+        const RowAt at = row_at(slot, head, kv_heads, page, values, dim);
+        codes = *reinterpret_cast<const uint32_t*>(cache + at.codes + piece * 4);
+        byte = cache[at.scales + piece / 4];
+    }
+    store8((values ? v : k) + i * 8, codes, scale_of_byte(byte));
+}
+
+template <class F>
+hipError_t over_rows(const emoe_kv_desc& d, int T, F launch) {
+    const long long n = (long long)T * (d.kv_heads * d.head_dim / 8), groups = (n + kThreads - 1) / kThreads;
+    if (groups > 0x7fffffff) return hipErrorInvalidValue;
+    launch(dim3((unsigned)groups, 2));
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_kv_append(const emoe_kv_desc& d, int T, int dtype, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                            const int32_t* slot, void* cache, hipStream_t st) {
+    auto run = [&](auto* kp, auto* vp) {
+        return over_rows(d, T, [&](dim3 grid) {
+            kv_append_kernel<<<grid, kThreads, 0, st>>>(kp, k_stride, vp, v_stride, slot, static_cast<uint8_t*>(cache), T, d.kv_heads, d.head_dim,
+                                                        d.pages * d.page_size, kv_page(d));
+        });
+    };
+    if (dtype == EMOE_F32) return run(static_cast<const float*>(k), static_cast<const float*>(v));
+    return run(static_cast<const bf16_t*>(k), static_cast<const bf16_t*>(v));
+}
+
+hipError_t launch_kv_read(const emoe_kv_desc& d, int T, int dtype, const void* cache, const int32_t* slot, void* k, void* v,
+                          hipStream_t st) {
+    auto run = [&](auto* kp, auto* vp) {
+        return over_rows(d, T, [&](dim3 grid) {
+            kv_read_kernel<<<grid, kThreads, 0, st>>>(static_cast<const uint8_t*>(cache), slot, kp, vp, T, d.kv_heads, d.head_dim,
+                                                      d.pages * d.page_size, kv_page(d));
+        });
+    };
+    if (dtype == EMOE_F32) return run(static_cast<float*>(k), static_cast<float*>(v));
+    return run(static_cast<bf16_t*>(k), static_cast<bf16_t*>(v));
+}
+
+}  // namespace emoe
