@@ -14,6 +14,10 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLowest = -3.0e38f;  // of a running maximum: finite, so that nothing minus it is a NaN
 
+// A value that all lanes hold alike, in a scalar register: what is computed from it costs no vector instruction, and addresses made of it
+// no vector registers.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
 // A request's queries and keys, from the lengths on the device, whatever these hold.
 struct Request {
     int first;  // its first query's token
@@ -40,6 +44,8 @@ struct Tiles {
     __device__ int count() const { return sinks + (to > from ? to - from : 0); }
     __device__ int tile(int i) const { return i < sinks ? i : i - sinks + from; }
 };
+__device__ __forceinline__ Request uniform(Request q) { return {uniform(q.first), uniform(q.n), uniform(q.seq), uniform(q.len)}; }
+__device__ __forceinline__ Tiles uniform(Tiles t) { return {uniform(t.sinks), uniform(t.from), uniform(t.to)}; }
 template <int SIZE>
 __device__ __forceinline__ Tiles tiles(const AttentionArgs& a, int seq, int first, int last) {
     Tiles t;

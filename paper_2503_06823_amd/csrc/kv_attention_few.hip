@@ -7,16 +7,21 @@
 // its four wavefronts take tiles of 32 tokens in turn, each with a maximum, a sum and an output of its own, so that nothing waits in
 // the walk; they meet once, at its end.  The matrix instructions' token and element orders are free as long as both operands
 // agree, and are chosen so that no data moves between lanes but V's:
-//   - K: lane (row = lane % 16, group = lane / 16) holds D / 4 consecutive elements of one token, one 16-byte load (D = 128),
-//     which all lie in one block and share one scale; step s multiplies its eight elements s, of all groups, with q's.
+//   - K: lane (row = lane % 16, group = lane / 16) holds D / 4 consecutive elements of one token, 16 bytes (D = 128), which all
+//     lie in one block and share one scale; step s multiplies its eight elements s, of all groups, with q's.
 //   - P^T comes out of S^T in the registers in which the second product wants it: lane (query, group) holds tokens 4 group .. +3
 //     of each 16, and V's rows are taken in that order.
 //   - V: converted to bf16 where its scale is one per lane, through LDS (a wavefront's own), read back transposed.
 // fp32 queries and weights are three bf16 operands each, which is exact to fp32; a 4-bit number is exact in bf16.
 //
-// Split: pieces of c tiles, so that all requests and heads together are about as many pieces as the chip holds workgroups; c
-// follows from the lengths, which every wavefront reads for itself.  A row that is cut leaves its pieces (fp32 output, maximum, sum) in
-// the workspace, and a second launch adds them in the pieces' order.
+// Split: all rows' key tiles make one line, of which every workgroup that the chip holds takes an equal part (Stretch).  A row that is cut
+// leaves its pieces (fp32 output, maximum, sum) in the workspace, and a second launch adds them in the pieces' order.
+//
+// Keys and values are loaded in the order of memory: 16 bytes a lane at the stride of a token's row took an L1 access a lane.  What is alike in
+// a wavefront is held in scalar registers (page numbers, addresses): in vector registers it took 16 of them and half the
+// instructions, and the lookup of a page waited for the tiles on their way.
+#include <math.h>
+
 #include "kv_attention.h"
 
 namespace emoe {
@@ -25,12 +30,19 @@ namespace {
 constexpr int kTok = 32;      // tokens of a tile
 constexpr int kRows = 16;     // rows of a workgroup
 constexpr int kWaves = 4;
-constexpr int kLeastTiles = 8;  // of a piece
+// See Stretch.
+constexpr int kFixed = 2;       // units that a stretch's beginning and end take time for
+constexpr int kLeastUnits = 3;  // of a workgroup's share
+constexpr int kSnap = 1;
 constexpr float kLazy = 8.0f;   // log2 of what a weight may grow to before the maximum is taken up
 
-// Workspace: [0] number of pieces, records, maxima and sums, outputs.
+// Workspace: two pieces of rows that are cut for every workgroup, the one that its share begins in (slot 2 w) and the one that it ends in
+// (slot 2 w + 1): records, maxima and sums, outputs.
 struct Piece {
-    int token0, row0, rows, kv_head, piece, count, pad0, pad1;
+    int token0, row0, rows, kv_head;
+    int piece, count;  // the how many-th of how many pieces; count 0: there is none in this slot
+    int group0;        // the workgroup of the first piece
+    int pad;
 };
 struct FewWs {
     size_t records, sums, outputs, total;
@@ -47,6 +59,10 @@ FewWs few_ws(int most_pieces, int dim) {
 template <class E> struct Pieces { static constexpr int n = 1; };
 template <> struct Pieces<float> { static constexpr int n = 3; };
 
+template <class E, int D> struct WavesPerSimd { static constexpr int n = 3; };
+template <> struct WavesPerSimd<float, 128> { static constexpr int n = 2; };
+template <> struct WavesPerSimd<float, 64> { static constexpr int n = 3; };
+
 __device__ __forceinline__ void load8(const float* p, float* x) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = p[i];
@@ -59,375 +75,443 @@ __device__ __forceinline__ void load8(const bf16_t* p, float* x) {
 __device__ __forceinline__ void store4(float* p, floatx4 v) { *reinterpret_cast<floatx4*>(p) = v; }
 __device__ __forceinline__ void store4(bf16_t* p, floatx4 v) { *reinterpret_cast<bf16x4*>(p) = __builtin_convertvector(v, bf16x4); }
 
-// The piece of work of a workgroup.
-struct Job {
-    int r, row_tile, kv_head, piece, pieces, tiles_each, slot;
+// The work as one line of units: requests in order, of a request its kv heads, of a head its tiles of 16 rows, of those (a stretch) kFixed
+// units for its beginning and end and then the rounds of kWaves key tiles that the longest row sees, at least one.  Every workgroup takes an
+// equal part of the line, so that all of them end together whatever the lengths; a boundary within kSnap rounds of a stretch's beginning or
+// end moves there, or nothing would be left whole.
+struct Stretch {
+    int row_tiles;  // of a request
+    int rounds;     // of one of its stretches
+    __device__ long long all(int kv_heads) const { return (long long)row_tiles * kv_heads * (kFixed + rounds); }
 };
-
-// Finds job `want` of the requests with at most most_rows rows; every wavefront by itself, 64 requests a trip.  false: there is none.
-// all_slots (if not null) receives the number of pieces of rows that are cut.
-__device__ bool find_job(const AttentionArgs& a, int most_rows, int at_once, int want, Job* job, int* all_slots) {
-    const int lane = threadIdx.x & 63;
-    auto of_row = [&](int r, int* tiles_r, int* row_tiles) {
-        *tiles_r = *row_tiles = 0;
-        if (r >= a.R) return;
-        const Request q = request(a, r);
-        const long long rows = (long long)q.n * a.group;
-        if (rows == 0 || rows > most_rows) return;
-        *row_tiles = (int)((rows + kRows - 1) / kRows);
-        *tiles_r = tiles<kTok>(a, q.seq, q.len - q.n, q.len - 1).count();
-    };
-    int tiles_r, row_tiles;
-    long long units = 0;
-    for (int r0 = 0; r0 < a.R; r0 += 64) {
-        of_row(r0 + lane, &tiles_r, &row_tiles);
-        units += (long long)tiles_r * row_tiles * a.kv_heads;
-    }
-#pragma unroll
-    for (int s = 32; s > 0; s /= 2) {
-        const int lo = __shfl_xor((int)units, s), hi = __shfl_xor((int)(units >> 32), s);
-        units += ((long long)hi << 32) | (uint32_t)lo;
-    }
-    long long c = (units + at_once - 1) / at_once;
-    c = (c + kWaves - 1) / kWaves * kWaves;
-    const int each = c < kLeastTiles ? kLeastTiles : (int)c;
-    int jobs = 0, slots = 0;
-    bool found = false;
-    for (int r0 = 0; r0 < a.R; r0 += 64) {
-        if (a.R > 64) of_row(r0 + lane, &tiles_r, &row_tiles);
-        const int pieces = tiles_r > each ? (tiles_r + each - 1) / each : 1;
-        const int mine = row_tiles * a.kv_heads * pieces, cut = pieces > 1 ? mine : 0;
-        const int upto = wave_inclusive(mine), cut_upto = wave_inclusive(cut);
-        const int total = __builtin_amdgcn_readlane(upto, 63);
-        if (!found && want - jobs < total) {
-            const int at = __builtin_ctzll(__ballot(upto > want - jobs));
-            const int p = __builtin_amdgcn_readlane(pieces, at), rt = __builtin_amdgcn_readlane(row_tiles, at);
-            int local = want - jobs - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(mine, at));
-            job->r = r0 + at;
-            job->pieces = p;
-            job->tiles_each = each;
-            job->row_tile = local % rt;
-            local /= rt;
-            job->kv_head = local % a.kv_heads;
-            job->piece = local / a.kv_heads;
-            job->slot = slots + __builtin_amdgcn_readlane(cut_upto, at) - __builtin_amdgcn_readlane(cut, at) +
-                        (job->kv_head * rt + job->row_tile) * p + job->piece;
-            found = true;
-        }
-        jobs += total;
-        slots += __builtin_amdgcn_readlane(cut_upto, 63);
-        if (found && all_slots == nullptr) break;
-    }
-    if (all_slots != nullptr) *all_slots = slots;
-    return found;
+__device__ __forceinline__ Stretch stretch(const AttentionArgs& a, const Request& q, int most_rows) {
+    const long long rows = (long long)q.n * a.group;
+    if (rows == 0 || rows > most_rows) return {0, 0};
+    const int n = (tiles<kTok>(a, q.seq, q.len - q.n, q.len - 1).count() + kWaves - 1) / kWaves;
+    return {(int)((rows + kRows - 1) / kRows), n > 0 ? n : 1};
 }
 
-template <int D> struct KeyLoad { typedef uint4 type; };
-template <> struct KeyLoad<64> { typedef uint2 type; };
+__device__ __forceinline__ long long readlane(long long v, int lane) {
+    const int lo = __builtin_amdgcn_readlane((int)v, lane), hi = __builtin_amdgcn_readlane((int)(v >> 32), lane);
+    return ((long long)hi << 32) | (uint32_t)lo;
+}
 
-// A tile on its way: what one lane loads of it.
-template <int D>
-struct Tile {
-    static constexpr int V_LOADS = kTok * D / 2 / 1024;  // 16 bytes a lane
-    union {
-        typename KeyLoad<D>::type load;
-        uint32_t step[D / 32];
-    } k[2];
-    uint4 v[V_LOADS];
-    uint32_t k_scale[2], v_scale[V_LOADS];
+// total units in `groups` shares, the first `longer` of them one unit longer.
+struct Shares {
+    long long total, each, longer;
+    int groups;
+    __device__ __forceinline__ static long long divide(long long x, long long y) {  // mostly small: 32 bits are five times as fast
+        return (((unsigned long long)x | (unsigned long long)y) >> 32) == 0 ? (long long)((uint32_t)x / (uint32_t)y) : x / y;
+    }
+    __device__ __forceinline__ long long begin(int w) const { return w * each + (w < longer ? w : longer); }
+    __device__ __forceinline__ int owner(long long u) const {
+        const long long of_longer = longer * (each + 1);
+        return (int)(u < of_longer ? divide(u, each + 1) : longer + divide(u - of_longer, each));
+    }
 };
 
+// The shares, and the request in which this workgroup's begins; every wavefront by itself, 64 requests a trip.
+struct Start {
+    Shares shares;
+    int r;
+    long long before;  // units of the requests before r
+    Request request;
+};
+__device__ __forceinline__ bool find_start(const AttentionArgs& a, int most_rows, Start* s) {
+    const int lane = threadIdx.x & 63;
+    Request mine;
+    auto units_of = [&](int r) {
+        mine = {0, 0, 0, 0};
+        if (r < a.R) mine = request(a, r);
+        return stretch(a, mine, most_rows).all(a.kv_heads);
+    };
+    auto inclusive = [&](long long v) {
+#pragma unroll
+        for (int k = 1; k < 64; k *= 2) {
+            const int lo = __shfl_up((int)v, k), hi = __shfl_up((int)(v >> 32), k);
+            v += lane >= k ? (((long long)hi << 32) | (uint32_t)lo) : 0ll;
+        }
+        return v;
+    };
+    long long upto = 0, total = 0;  // of a trip, of all
+    for (int r0 = 0; r0 < a.R; r0 += 64) {
+        upto = inclusive(units_of(r0 + lane));
+        total += readlane(upto, 63);
+    }
+    const long long most = Shares::divide(total + kLeastUnits - 1, kLeastUnits);
+    s->shares.total = total;
+    s->shares.groups = most < gridDim.x ? (int)most : (int)gridDim.x;
+    if ((int)blockIdx.x >= s->shares.groups) return false;
+    s->shares.each = Shares::divide(total, s->shares.groups);
+    s->shares.longer = total - s->shares.each * s->shares.groups;
+    const long long begin = s->shares.begin(blockIdx.x);
+    s->before = 0;
+    for (int r0 = 0; r0 < a.R; r0 += 64) {
+        if (a.R > 64) upto = inclusive(units_of(r0 + lane));
+        const long long sum = readlane(upto, 63);
+        if (begin - s->before < sum) {
+            const int at = __builtin_ctzll(__ballot(upto > begin - s->before));
+            s->r = r0 + at;
+            if (at > 0) s->before += readlane(upto, at - 1);
+            s->request = {__builtin_amdgcn_readlane(mine.first, at), __builtin_amdgcn_readlane(mine.n, at),
+                          __builtin_amdgcn_readlane(mine.seq, at), __builtin_amdgcn_readlane(mine.len, at)};
+            return true;
+        }
+        s->before += sum;
+    }
+    return false;
+}
+
+// What a lane loads of 16 tokens' keys or values, D / 4 elements of one row: a word holds eight.
+template <int D> struct Quarter { typedef uint32_t type __attribute__((ext_vector_type(4))); };
+template <> struct Quarter<64> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
+
 template <class E, int D>
-__global__ __launch_bounds__(64 * kWaves) void attention_few_kernel(AttentionArgs a, int most_rows, int at_once, int most_pieces, FewWs lay) {
+__global__ __launch_bounds__(64 * kWaves, (WavesPerSimd<E, D>::n)) void attention_few_kernel(AttentionArgs a, int most_rows, FewWs lay) {
     constexpr int PIECES = Pieces<E>::n, STEPS = D / 32, BLOCKS = D / 16;
     constexpr int V_STRIDE = D + 16;  // elements; 32 bytes past the row: 16 rows of 32 bytes fall on all banks alike
-    constexpr int V_PER_TOKEN = D / 32;
-    constexpr int WAVE_BYTES = kTok * V_STRIDE * 2;
-    static_assert(BLOCKS * 1024 <= WAVE_BYTES, "the outputs take V's place at the end");
+    constexpr int V_BYTES = kTok * V_STRIDE * 2, WAVE_BYTES = V_BYTES + kTok * D / 2;  // V as bf16, K as it comes
+    static_assert(WAVE_BYTES % 16 == 0 && BLOCKS * 1024 <= WAVE_BYTES, "the outputs take V's place at the end");
     __shared__ __align__(16) char lds[kWaves * WAVE_BYTES];
     __shared__ float sums[kWaves][kRows][2];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const int col = lane & 15, group = lane >> 4;
 
-    Job job;
-    int slots = 0;
-    const bool found = find_job(a, most_rows, at_once, blockIdx.x, &job, blockIdx.x == 0 ? &slots : nullptr);
-    if (blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<int*>(a.ws) = slots;
-    if (!found) return;
-    const int r = __builtin_amdgcn_readfirstlane(job.r), kv_head = __builtin_amdgcn_readfirstlane(job.kv_head);
-    const Request q = request(a, r);
-    const int rows = q.n * a.group, row0 = job.row_tile * kRows;
-    const int row = row0 + col, token = row / a.group, head = kv_head * a.group + row % a.group;
-    const int position = row < rows ? q.len - q.n + token : -1;  // -1 sees nothing
-    const int last_row = row0 + kRows < rows ? row0 + kRows - 1 : rows - 1;
-    const int p_first = q.len - q.n + row0 / a.group, p_last = q.len - q.n + last_row / a.group;
-
-    bf16x8 query[PIECES][STEPS];
-    {
-        float x[8];
-        const E* at = static_cast<const E*>(a.q) + (int64_t)(q.first + token) * a.q_stride + (int64_t)head * D + group * (D / 4);
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = 0.0f;
-            if (row < rows) load8(at + s * 8, x);
-            bf16x8 o[PIECES];
-            to_operands<PIECES>(x, o);
-#pragma unroll
-            for (int p = 0; p < PIECES; ++p) query[p][s] = o[p];
+    Start start;
+    const bool some = find_start(a, most_rows, &start);
+    Piece* records = reinterpret_cast<Piece*>(a.ws + lay.records) + 2 * (size_t)blockIdx.x;
+    bool used[2] = {false, false};
+    const long long share_end = some ? start.shares.begin(blockIdx.x + 1) : 0;
+    int r = uniform(start.r);
+    long long before = start.before;
+    Request q = start.request;
+    for (long long unit = some ? start.shares.begin(blockIdx.x) : 0; unit < share_end;) {
+        const Stretch here = stretch(a, q, most_rows);
+        const long long all_here = here.all(a.kv_heads);
+        if (unit - before >= all_here) {
+            before += all_here;
+            q = uniform(request(a, ++r));
+            continue;
         }
-    }
-
-    const Tiles seen = tiles<kTok>(a, q.seq, q.len - q.n, q.len - 1);
-    int i_end = (job.piece + 1) * job.tiles_each, i_all = seen.count();
-    i_end = i_end < i_all ? i_end : i_all;
-    while (i_end > 0 && seen.tile(i_end - 1) * kTok > p_last) --i_end;  // no row of this tile sees so far
-    const int32_t* table = a.table + (size_t)r * a.width;
-    const size_t page_bytes = (size_t)a.page.bytes();
-    bf16_t* v_lds = reinterpret_cast<bf16_t*>(lds + wave * WAVE_BYTES);
-
-    auto page_of = [&](int i, int half) {
-        const int b = (seen.tile(i) * kTok + 16 * half) >> a.page.log2_size;
-        return b < a.width ? __builtin_amdgcn_readfirstlane(table[b]) : -1;
-    };
-    auto load = [&](Tile<D>& t, int i, const int* pages) {
-        const uint8_t* base[2];
-        int in_page[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int pg = (unsigned)pages[h] < (unsigned)a.pages ? pages[h] : 0;
-            base[h] = a.cache + ((size_t)pg * a.kv_heads + kv_head) * page_bytes;
-            in_page[h] = (seen.tile(i) * kTok + 16 * h) & ((1 << a.page.log2_size) - 1);
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int tk = in_page[h] + col;
-            t.k[h].load = *reinterpret_cast<const typename KeyLoad<D>::type*>(base[h] + tk * (D / 2) + group * (D / 8));
-            t.k_scale[h] = base[h][2 * a.page.codes + tk * (D / 32) + group * (D / 4) / 32];
-        }
-#pragma unroll
-        for (int n = 0; n < Tile<D>::V_LOADS; ++n) {
-            const int chunk = n * 64 + lane, tok = chunk / V_PER_TOKEN, h = D == 128 ? n : tok / 16;
-            const uint8_t* from = D == 128 ? base[n] : h ? base[1] : base[0];
-            const int tk = (D == 128 ? in_page[n] : h ? in_page[1] : in_page[0]) + tok % 16;
-            t.v[n] = *reinterpret_cast<const uint4*>(from + a.page.codes + tk * (D / 2) + chunk % V_PER_TOKEN * 16);
-            t.v_scale[n] = from[2 * a.page.codes + a.page.scales + tk * (D / 32) + chunk % V_PER_TOKEN];
-        }
-    };
-
-    floatx4 out[BLOCKS];
-#pragma unroll
-    for (int b = 0; b < BLOCKS; ++b) out[b] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-    float most = kLowest, sum = 0.0f;
-
-    auto multiply = [&](const Tile<D>& t, int i, const int* pages) {
-        const int t0 = seen.tile(i) * kTok;
-        const bool owned[2] = {(unsigned)pages[0] < (unsigned)a.pages, (unsigned)pages[1] < (unsigned)a.pages};
-        // every row sees every token of the tile
-        const bool whole = owned[0] && owned[1] && t0 + kTok - 1 <= p_first &&
-                           (a.window == 0 || t0 > p_last - a.window || t0 + kTok <= a.sinks);
-        bool nan = false;
-#pragma unroll
-        for (int n = 0; n < Tile<D>::V_LOADS; ++n) {
-            const int chunk = n * 64 + lane, tok = chunk / V_PER_TOKEN;
-            uint32_t byte = t.v_scale[n];
-            if (!whole && (t0 + tok >= q.seq || !(tok < 16 ? owned[0] : owned[1]))) byte = 127;  // never written: any number will do
-            nan |= byte == 255;
-            const float scale = scale_of_byte(byte);
-            bf16_t* to = v_lds + tok * V_STRIDE + chunk % V_PER_TOKEN * 32;
-            *reinterpret_cast<bf16x8*>(to) = from_codes(t.v[n].x, scale);
-            *reinterpret_cast<bf16x8*>(to + 8) = from_codes(t.v[n].y, scale);
-            *reinterpret_cast<bf16x8*>(to + 16) = from_codes(t.v[n].z, scale);
-            *reinterpret_cast<bf16x8*>(to + 24) = from_codes(t.v[n].w, scale);
-        }
-        float z[8];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            floatx4 s = {0.0f, 0.0f, 0.0f, 0.0f};
-            const float scale = scale_of_byte(t.k_scale[h]);
-#pragma unroll
-            for (int st = 0; st < STEPS; ++st) {
-                const bf16x8 key = from_codes(t.k[h].step[st], scale);
-#pragma unroll
-                for (int p = PIECES - 1; p >= 0; --p) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, query[p][st], s, 0, 0, 0);
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) z[4 * h + e] = s[e] * a.scale_log2;
-        }
-        if (!whole) {
-            const int from = a.window > 0 && position >= a.window ? position - a.window + 1 : 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int j = t0 + 16 * (e / 4) + 4 * group + e % 4;
-                const bool sees = j <= position && (j >= from || j < a.sinks) && owned[e / 4];
-                z[e] = sees ? z[e] : -INFINITY;
-            }
-        }
-        float top = z[0];
-#pragma unroll
-        for (int e = 1; e < 8; ++e) top = fmaxf(top, z[e]);
-        top = over_groups(top, [](float x, float y) { return fmaxf(x, y); });
-        if (__any(top > most + kLazy)) {  // the weights stay below 2^8: a maximum that rises by less is not worth a pass over the output
-            const float next = fmaxf(most, top), f = __builtin_amdgcn_exp2f(most - next);
-            most = next;
-            sum *= f;
-#pragma unroll
-            for (int b = 0; b < BLOCKS; ++b) out[b] *= f;
-        }
-        float w[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            w[e] = __builtin_amdgcn_exp2f(z[e] - most);
-            sum += w[e];
-        }
-        bf16x8 weight[PIECES];
-        to_operands<PIECES>(w, weight);
-        const bf16_t* v_at = v_lds + (4 * group + (col >> 2)) * V_STRIDE + 4 * (col & 3);
-        union VFragment {
-            shortx4 half[2];
-            bf16x8 all;
+        const int rounds = uniform(here.rounds), units = kFixed + rounds, nth = uniform((int)Shares::divide(unit - before, units));
+        const long long first_unit = before + (long long)nth * units;
+        const int snap = kSnap < rounds / 2 ? kSnap : rounds / 2;
+        auto round_at = [&](long long u) {
+            const int k = u - first_unit < units ? (int)(u - first_unit) - kFixed : rounds;
+            return uniform(k <= snap ? 0 : k >= rounds - snap ? rounds : k);
         };
-        if (__any(nan)) {
-            // blocks of NaN: what sees them becomes NaN, what does not stays as it is
-            bf16x8 sees;
+        const int u_begin = round_at(unit), u_end = round_at(share_end);
+        unit = first_unit + units;
+        if (u_begin >= u_end) continue;
+        const int kv_head = nth / here.row_tiles, row_tile = nth % here.row_tiles;
+        const int rows = q.n * a.group, row0 = row_tile * kRows, last_row = row0 + kRows < rows ? row0 + kRows - 1 : rows - 1;
+        const int p_first = q.len - q.n + row0 / a.group, p_last = q.len - q.n + last_row / a.group;
+
+        const Tiles seen = uniform(tiles<kTok>(a, q.seq, q.len - q.n, q.len - 1));
+        const int i_all = seen.count();
+        int i_end = u_end * kWaves < i_all ? u_end * kWaves : i_all;
+        while (i_end > 0 && seen.tile(i_end - 1) * kTok > p_last) --i_end;  // no row of this tile sees so far
+        // read through the scalar cache: a vector load here would wait for the tiles on their way
+        typedef const __attribute__((address_space(4))) int32_t* ScalarTable;
+        const ScalarTable table = (ScalarTable)(a.table + (size_t)r * a.width);
+        const int page_mask = (1 << a.page.log2_size) - 1;
+        const uint32_t head_bytes = (uint32_t)a.page.bytes(), page_stride = head_bytes * (uint32_t)a.kv_heads;
+        const uint8_t* cache = a.cache + (size_t)kv_head * head_bytes;
+        bf16_t* v_lds = reinterpret_cast<bf16_t*>(lds + wave * WAVE_BYTES);
+        char* k_lds = lds + wave * WAVE_BYTES + V_BYTES;
+
+        // Both are loaded in the order of memory, quarter lane % 4 of token lane / 4 (16 bytes a lane at a stride of 64 took an access of the
+        // L1 cache per lane).  Keys go through LDS, where quarter q of token t lies in place q ^ swizzle(t), to lane (token, quarter).
+        const int in_tok = lane >> 2, quarter = lane & 3;
+        const uint32_t in_at = in_tok * (D / 2) + quarter * (D / 8), v_scale_at = in_tok * (D / 32) + quarter * (D / 4) / 32;
+        const uint32_t k_scale_at = col * (D / 32) + group * (D / 4) / 32;
+        auto swizzle = [](int t) { return (t >> (D == 128 ? 2 : 3)) & 3; };
+        char* k_to = k_lds + in_tok * (D / 2) + (quarter ^ swizzle(in_tok)) * (D / 8);
+        const char* k_from = k_lds + col * (D / 2) + (group ^ swizzle(col)) * (D / 8);
+        bf16_t* v_to = v_lds + in_tok * V_STRIDE + quarter * (D / 4);
+        const bf16_t* v_from = v_lds + (4 * group + (col >> 2)) * V_STRIDE + 4 * (col & 3);
+
+        // Where a tile's two halves of 16 tokens lie: codes and scales of their keys.  Pages of nobody are read as page 0, and masked.
+        struct Place {
+            const uint8_t *codes0, *codes1, *scales0, *scales1;
+            int t0;
+            bool owned0, owned1;
+        };
+        auto place = [&](int i) {
+            Place p;
+            p.t0 = seen.tile(i) * kTok;
+            auto half = [&](int t, const uint8_t*& codes, const uint8_t*& scales, bool& owned) {
+                const int b = t >> a.page.log2_size, in_page = t & page_mask;
+                const uint32_t page = (uint32_t)table[b < a.width ? b : a.width - 1];
+                owned = page < (uint32_t)a.pages && b < a.width;
+                const uint8_t* head = cache + (uint64_t)(owned ? page : 0u) * page_stride;
+                codes = head + in_page * (D / 2);
+                scales = head + 2 * a.page.codes + in_page * (D / 32);
+            };
+            half(p.t0, p.codes0, p.scales0, p.owned0);
+            half(p.t0 + 16, p.codes1, p.scales1, p.owned1);
+            return p;
+        };
+        typedef typename Quarter<D>::type Words;
+        Words k0, k1, v0, v1;
+        uint32_t k_scale0, k_scale1, v_scale0, v_scale1;
+        auto load_keys = [&](const Place& p) {
+            k0 = *reinterpret_cast<const Words*>(p.codes0 + in_at);
+            k1 = *reinterpret_cast<const Words*>(p.codes1 + in_at);
+            k_scale0 = p.scales0[k_scale_at];
+            k_scale1 = p.scales1[k_scale_at];
+        };
+        auto load_values = [&](const Place& p) {
+            v0 = *reinterpret_cast<const Words*>(p.codes0 + a.page.codes + in_at);
+            v1 = *reinterpret_cast<const Words*>(p.codes1 + a.page.codes + in_at);
+            v_scale0 = (p.scales0 + a.page.scales)[v_scale_at];
+            v_scale1 = (p.scales1 + a.page.scales)[v_scale_at];
+        };
+
+        floatx4 out[BLOCKS];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sees[e] = (__bf16)(z[e] == -INFINITY ? 0.0f : 1.0f);
+        for (int b = 0; b < BLOCKS; ++b) out[b] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+        float most = kLowest, sum = 0.0f;
+        uint32_t bad = 0;  // quarters of this lane's query that a block of NaN values among its tokens has reached
+
+        // Tile i + 4's values and keys are on their way from where tile i's have been used on, and its page is looked up a tile earlier.  The first
+        // tile's are sent for before the queries are.
+        int i = u_begin * kWaves + wave;
+        const int last = i_end - 1;  // past the end: the last tile again, unused
+        Place now, next;
+        if (i < i_end) {
+            now = place(i);
+            load_values(now);
+            load_keys(now);
+            next = place(i + kWaves < i_end ? i + kWaves : last);
+        }
+        const int row = row0 + col, token = row / a.group, head = kv_head * a.group + row % a.group;
+        const int position = row < rows ? q.len - q.n + token : -1;  // -1 sees nothing
+
+        bf16x8 query[PIECES][STEPS];
+        {
+            float x[8];
+            const E* at = static_cast<const E*>(a.q) + (int64_t)(q.first + token) * a.q_stride + (int64_t)head * D + group * (D / 4);
 #pragma unroll
-            for (int b = 0; b < BLOCKS; ++b) {
-                VFragment f;
-                f.half[0] = read_transposed(v_at + 16 * b);
-                f.half[1] = read_transposed(v_at + 16 * V_STRIDE + 16 * b);
-                bf16x8 bad;
+            for (int s = 0; s < STEPS; ++s) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = 0.0f;
+                if (row < rows) load8(at + s * 8, x);
+                bf16x8 o[PIECES];
+                to_operands<PIECES>(x, o);
+#pragma unroll
+                for (int p = 0; p < PIECES; ++p) query[p][s] = o[p];
+            }
+        }
+
+        for (; i < i_end; i += kWaves) {
+            const Place after = place(i + 2 * kWaves < i_end ? i + 2 * kWaves : last);
+            const int t0 = now.t0;
+            // every row sees every token of the tile
+            const bool whole = now.owned0 & now.owned1 & (t0 + kTok - 1 <= p_first) &
+                               ((a.window == 0) | (t0 > p_last - a.window) | (t0 + kTok <= a.sinks));
+            if (!whole) {  // what was never written: any number will do
+                if (!(t0 + in_tok < q.seq && now.owned0)) v_scale0 = 127;
+                if (!(t0 + 16 + in_tok < q.seq && now.owned1)) v_scale1 = 127;
+            }
+            const unsigned long long nan0 = __ballot(v_scale0 == 255), nan1 = __ballot(v_scale1 == 255);
+            auto write_values = [&](const Words& words, uint32_t byte, bf16_t* to) {
+                const float scale = scale_of_byte(byte == 255 ? 127 : byte);
+#pragma unroll
+                for (int e = 0; e < D / 32; ++e) *reinterpret_cast<bf16x8*>(to + 8 * e) = from_codes(words[e], scale);
+            };
+            write_values(v0, v_scale0, v_to);
+            write_values(v1, v_scale1, v_to + 16 * V_STRIDE);
+            load_values(next);
+            *reinterpret_cast<Words*>(k_to) = k0;
+            *reinterpret_cast<Words*>(k_to + 16 * D / 2) = k1;
+            const float scale0 = scale_of_byte(k_scale0), scale1 = scale_of_byte(k_scale1);
+            load_keys(next);
+            auto scores = [&](const char* from, float scale) {
+                const Words words = *reinterpret_cast<const Words*>(from);
+                floatx4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int st = 0; st < STEPS; ++st) {
+                    const bf16x8 key = from_codes(words[st], scale);
+#pragma unroll
+                    for (int p = PIECES - 1; p >= 0; --p) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, query[p][st], s, 0, 0, 0);
+                }
+                return s * a.scale_log2;
+            };
+            const floatx4 z0 = scores(k_from, scale0), z1 = scores(k_from + 16 * D / 2, scale1);
+            float z[8] = {z0[0], z0[1], z0[2], z0[3], z1[0], z1[1], z1[2], z1[3]};
+            if (!whole) {
+                const int from = a.window > 0 && position >= a.window ? position - a.window + 1 : 0;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const bool is = f.all[e] != f.all[e];
-                    bad[e] = (__bf16)(is ? 1.0f : 0.0f);
-                    f.all[e] = is ? (__bf16)0.0f : f.all[e];
+                    const int j = t0 + 16 * (e / 4) + 4 * group + e % 4;
+                    const bool sees = (j <= position) & ((j >= from) | (j < a.sinks)) & (e < 4 ? now.owned0 : now.owned1);
+                    z[e] = sees ? z[e] : -INFINITY;
                 }
-                floatx4 hit = {0.0f, 0.0f, 0.0f, 0.0f};
-                hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bad, sees, hit, 0, 0, 0);
+            }
+            if ((nan0 | nan1) != 0) {
+                // bit 4 t + quarter of nan0: the value of token t.  V holds numbers there; what sees it becomes NaN at the end
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    bad |= z[e] != -INFINITY ? (uint32_t)((e < 4 ? nan0 : nan1) >> (16 * group + 4 * (e % 4))) & 15u : 0u;
+            }
+            float top = z[0];
+#pragma unroll
+            for (int e = 1; e < 8; ++e) top = fmaxf(top, z[e]);
+            top = over_groups(top, [](float x, float y) { return fmaxf(x, y); });
+            if (__any(top > most + kLazy)) {  // the weights stay below 2^8: a maximum that rises by less is not worth a pass over the output
+                const float up = fmaxf(most, top), f = __builtin_amdgcn_exp2f(most - up);
+                most = up;
+                sum *= f;
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b) out[b] *= f;
+            }
+            float w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                w[e] = __builtin_amdgcn_exp2f(z[e] - most);
+                sum += w[e];
+            }
+            bf16x8 weight[PIECES];
+            to_operands<PIECES>(w, weight);
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) {
+                union {
+                    shortx4 half[2];
+                    bf16x8 all;
+                } f;
+                f.half[0] = read_transposed(v_from + 16 * b);
+                f.half[1] = read_transposed(v_from + 16 * V_STRIDE + 16 * b);
 #pragma unroll
                 for (int p = PIECES - 1; p >= 0; --p) out[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.all, weight[p], out[b], 0, 0, 0);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) out[b][e] = hit[e] > 0.0f ? __uint_as_float(0x7fc00000u) : out[b][e];
             }
-            return;
-        }
-#pragma unroll
-        for (int b = 0; b < BLOCKS; ++b) {
-            VFragment f;
-            f.half[0] = read_transposed(v_at + 16 * b);
-            f.half[1] = read_transposed(v_at + 16 * V_STRIDE + 16 * b);
-#pragma unroll
-            for (int p = PIECES - 1; p >= 0; --p) out[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.all, weight[p], out[b], 0, 0, 0);
-        }
-    };
-
-    // tile i + 4 is on its way while tile i is multiplied, and the page of tile i + 8 is looked up
-    int i = job.piece * job.tiles_each + wave;
-    if (i < i_end) {
-        Tile<D> now;
-        int pages[2], pages_next[2] = {-1, -1};
-#pragma unroll
-        for (int h = 0; h < 2; ++h) pages[h] = page_of(i, h);
-        if (i + kWaves < i_end) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) pages_next[h] = page_of(i + kWaves, h);
-        }
-        load(now, i, pages);
-        for (; i < i_end; i += kWaves) {
-            Tile<D> next = now;
-            int pages_after[2] = {-1, -1};
-            if (i + kWaves < i_end) load(next, i + kWaves, pages_next);
-            if (i + 2 * kWaves < i_end) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) pages_after[h] = page_of(i + 2 * kWaves, h);
-            }
-            multiply(now, i, pages);
             now = next;
+            next = after;
+        }
+
+        // the four wavefronts' outputs, to the largest of their maxima
+        sum = over_groups(sum, [](float x, float y) { return x + y; });
+        if (__any(bad != 0)) {
+            bad |= (uint32_t)__shfl_xor((int)bad, 16);
+            bad |= (uint32_t)__shfl_xor((int)bad, 32);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                pages[h] = pages_next[h];
-                pages_next[h] = pages_after[h];
+            for (int b = 0; b < BLOCKS; ++b)
+                if (bad >> (b * 16 / (D / 4)) & 1u) out[b] = floatx4{NAN, NAN, NAN, NAN};
+        }
+        floatx4* part = reinterpret_cast<floatx4*>(lds);
+        constexpr int WAVE_PARTS = WAVE_BYTES / 16;
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b) part[wave * WAVE_PARTS + b * 64 + lane] = out[b];
+        if (group == 0) {
+            sums[wave][col][0] = most;
+            sums[wave][col][1] = sum;
+        }
+        __syncthreads();
+        float top = kLowest, all = 0.0f, factor[kWaves];
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sums[w][col][0]);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            factor[w] = __builtin_amdgcn_exp2f(sums[w][col][0] - top);
+            all += sums[w][col][1] * factor[w];
+        }
+        const bool cut = u_begin > 0 || u_end < rounds;
+        const int which = u_begin == 0 ? 1 : 0;
+        const size_t slot = 2 * (size_t)blockIdx.x + which;
+#pragma unroll
+        for (int n = 0; n < BLOCKS / kWaves; ++n) {
+            const int b = wave * (BLOCKS / kWaves) + n;
+            floatx4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) v += part[w * WAVE_PARTS + b * 64 + lane] * factor[w];
+            const int d = 16 * b + 4 * group;
+            if (row >= rows) continue;
+            if (cut) {
+                float* to = reinterpret_cast<float*>(a.ws + lay.outputs) + (slot * kRows + col) * D + d;
+                *reinterpret_cast<floatx4*>(to) = v;
+            } else {
+                const float by = all == 0.0f ? 0.0f : 1.0f / all;
+                store4(static_cast<E*>(a.out) + (int64_t)(q.first + token) * a.out_stride + (int64_t)head * D + d, v * by);
             }
         }
-    }
-
-    // the four wavefronts' outputs, to the largest of their maxima
-    sum = over_groups(sum, [](float x, float y) { return x + y; });
-    floatx4* part = reinterpret_cast<floatx4*>(lds);
-    constexpr int WAVE_PARTS = WAVE_BYTES / 16;
-#pragma unroll
-    for (int b = 0; b < BLOCKS; ++b) part[wave * WAVE_PARTS + b * 64 + lane] = out[b];
-    if (group == 0) {
-        sums[wave][col][0] = most;
-        sums[wave][col][1] = sum;
-    }
-    __syncthreads();
-    float top = kLowest, all = 0.0f, factor[kWaves];
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sums[w][col][0]);
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        factor[w] = __builtin_amdgcn_exp2f(sums[w][col][0] - top);
-        all += sums[w][col][1] * factor[w];
-    }
-    const bool cut = job.pieces > 1;
-    if (row >= rows && !cut) return;
-    const int slot = job.slot < most_pieces ? job.slot : most_pieces - 1;
-#pragma unroll
-    for (int n = 0; n < BLOCKS / kWaves; ++n) {
-        const int b = wave * (BLOCKS / kWaves) + n;
-        floatx4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) v += part[w * WAVE_PARTS + b * 64 + lane] * factor[w];
-        const int d = 16 * b + 4 * group;
         if (cut) {
-            float* to = reinterpret_cast<float*>(a.ws + lay.outputs) + ((size_t)slot * kRows + col) * D + d;
-            if (row < rows) *reinterpret_cast<floatx4*>(to) = v;
-        } else {
-            const float by = all == 0.0f ? 0.0f : 1.0f / all;
-            store4(static_cast<E*>(a.out) + (int64_t)(q.first + token) * a.out_stride + (int64_t)head * D + d, v * by);
+            used[which] = true;
+            if (wave == 0 && group == 0) {
+                float* to = reinterpret_cast<float*>(a.ws + lay.sums) + (slot * kRows + col) * 2;
+                to[0] = top;
+                to[1] = all;
+                if (col == 0) {
+                    // whose share holds a unit, boundaries as they are after snapping
+                    const int w0 = start.shares.owner(first_unit + kFixed + snap), w1 = start.shares.owner(first_unit + units - snap - 1);
+                    records[which] = Piece{q.first, row0, rows - row0 < kRows ? rows - row0 : kRows, kv_head, (int)blockIdx.x - w0, w1 - w0 + 1, w0, 0};
+                }
+            }
         }
+        __syncthreads();  // the outputs are read: the next stretch's tiles may take their place
     }
-    if (cut && wave == 0 && group == 0) {
-        float* to = reinterpret_cast<float*>(a.ws + lay.sums) + ((size_t)slot * kRows + col) * 2;
-        to[0] = top;
-        to[1] = all;
-        if (col == 0) {
-            const int n = rows - row0 < kRows ? rows - row0 : kRows;
-            reinterpret_cast<Piece*>(a.ws + lay.records)[slot] = Piece{q.first, row0, n, kv_head, job.piece, job.pieces, 0, 0};
-        }
+    if (threadIdx.x == 0) {
+        if (!used[0]) records[0].count = 0;
+        if (!used[1]) records[1].count = 0;
     }
 }
 
-// The pieces of rows that were cut, in the pieces' order.  A workgroup for every piece; those of one row share its elements.
+// The pieces of rows that were cut, in the pieces' order.  A workgroup for every piece; those of one cut take its rows in turn.  A team of
+// lanes has four elements of a row each; teams share a row's pieces, as many as there are pieces for, so that the many pieces of a long
+// context are read side by side, and the rows of a short one.
+constexpr int kJoinThreads = 256;
 template <class E, int D>
-__global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a, FewWs lay) {
-    const int slots = *reinterpret_cast<const int*>(a.ws);
-    if ((int)blockIdx.x >= slots) return;
+__global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(AttentionArgs a, FewWs lay) {
+    constexpr int LANES = D / 4, TEAMS = kJoinThreads / LANES;
+    __shared__ floatx4 part[TEAMS][LANES];
+    __shared__ float2 part_sums[TEAMS];
     const Piece p = reinterpret_cast<const Piece*>(a.ws + lay.records)[blockIdx.x];
-    const size_t first = blockIdx.x - p.piece;
-    const float* sums = reinterpret_cast<const float*>(a.ws + lay.sums) + first * kRows * 2;
-    const float* outputs = reinterpret_cast<const float*>(a.ws + lay.outputs) + first * kRows * D;
-    for (int e = p.piece * 256 + threadIdx.x; e < p.rows * D; e += p.count * 256) {
-        const int row = e / D, d = e % D;
-        float top = kLowest;
-        for (int n = 0; n < p.count; ++n) top = fmaxf(top, sums[(n * kRows + row) * 2]);
-        float all = 0.0f, v = 0.0f;
+    if (p.count == 0) return;
+    // the first piece is the end of its workgroup's share, the others are the beginnings of theirs
+    auto row_of = [&](int n, int row) { return (size_t)(2 * (p.group0 + n) + (n == 0 ? 1 : 0)) * kRows + row; };
+    const float2* sums = reinterpret_cast<const float2*>(a.ws + lay.sums);
+    const float* outputs = reinterpret_cast<const float*>(a.ws + lay.outputs);
+    const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES;
+    int shares = 2;  // teams of a row
+    while (shares < TEAMS && shares < p.count) shares *= 2;
+    const int share = team % shares, side = team / shares, step = p.count * (TEAMS / shares);
+    for (int row0 = p.piece; row0 < p.rows; row0 += step) {
+        const int row = row0 + side * p.count;
+        floatx4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+        float top = kLowest, all = 0.0f;
+        if (row < p.rows) {
 #pragma unroll 4
-        for (int n = 0; n < p.count; ++n) {
-            const float f = __builtin_amdgcn_exp2f(sums[(n * kRows + row) * 2] - top);
-            all += sums[(n * kRows + row) * 2 + 1] * f;
-            v += outputs[((size_t)n * kRows + row) * D + d] * f;
+            for (int n = share; n < p.count; n += shares) {  // one pass: nothing is loaded that waits for another load but the record
+                const size_t at = row_of(n, row);
+                const float2 s = sums[at];
+                const floatx4 o = *reinterpret_cast<const floatx4*>(outputs + at * D + 4 * lane);
+                const float up = fmaxf(top, s.x), f = __builtin_amdgcn_exp2f(top - up), g = __builtin_amdgcn_exp2f(s.x - up);
+                top = up;
+                all = all * f + s.y * g;
+                v = v * f + o * g;
+            }
         }
-        const int m = p.row0 + row;
-        store_from_f32(static_cast<E*>(a.out), (size_t)((int64_t)(p.token0 + m / a.group) * a.out_stride +
-                                                        (int64_t)(p.kv_head * a.group + m % a.group) * D + d), all == 0.0f ? 0.0f : v / all);
+        part[team][lane] = v;
+        if (lane == 0) part_sums[team] = float2{top, all};
+        __syncthreads();
+        if (share == 0 && row < p.rows) {
+            for (int s = 1; s < shares; ++s) top = fmaxf(top, part_sums[team + s].x);
+            v = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+            all = 0.0f;
+            for (int s = 0; s < shares; ++s) {
+                const float f = __builtin_amdgcn_exp2f(part_sums[team + s].x - top);
+                all += part_sums[team + s].y * f;
+                v += part[team + s][lane] * f;
+            }
+            const int m = p.row0 + row;
+            const float by = all == 0.0f ? 0.0f : 1.0f / all;
+            store4(static_cast<E*>(a.out) + (int64_t)(p.token0 + m / a.group) * a.out_stride +
+                       (int64_t)(p.kv_head * a.group + m % a.group) * D + 4 * lane, v * by);
+        }
+        __syncthreads();  // the sums are read
     }
 }
 
-constexpr int kPerCu = 4;  // workgroups that a CU holds
+constexpr int kPerCu = 3;  // workgroups that a CU holds
 
 }  // namespace
 
@@ -437,21 +521,22 @@ hipError_t launch_attention_few(const emoe_kv_desc& d, const emoe_attention_desc
     DeviceShape shape;
     hipError_t e = device_shape(&shape);
     if (e != hipSuccess) return e;
-    const int at_once = kPerCu * shape.groups, most_pieces = 2 * at_once;
-    const FewWs lay = few_ws(most_pieces, d.head_dim);
-    // row tiles that there can be, by the tokens and by the requests
-    const long long per_request = ((long long)(a.max_new * (long long)a.group < most_rows ? a.max_new * (long long)a.group : most_rows) + kRows - 1) / kRows;
+    // As many workgroups as the chip holds at once, or as many as there can be shares for, by the tokens and the requests.
+    const long long per_request = ((long long)a.max_new * a.group < most_rows ? (long long)a.max_new * a.group : most_rows) + kRows - 1;
     const long long by_tokens = (long long)a.T * a.group / kRows + a.R;
-    const long long row_tiles = per_request * a.R < by_tokens ? per_request * a.R : by_tokens;
-    const long long groups = row_tiles * a.kv_heads + at_once;  // no more pieces than that
-    if (groups > 0x7fffffff / 256) return hipErrorInvalidValue;
+    const long long row_tiles = per_request / kRows * a.R < by_tokens ? per_request / kRows * a.R : by_tokens;
+    const long long most_rounds = (((long long)a.width << a.page.log2_size) + kTok * kWaves - 1) / (kTok * kWaves);
+    const long long line = row_tiles * a.kv_heads * (kFixed + most_rounds), shares = (line + kLeastUnits - 1) / kLeastUnits;
+    const int groups = shares < kPerCu * shape.groups ? (int)shares : kPerCu * shape.groups;
+    const FewWs lay = few_ws(2 * kPerCu * kMaxGroups, d.head_dim);
     auto run = [&](auto element, auto dim) {
         typedef decltype(element) E;
         constexpr int D = decltype(dim)::value;
-        attention_few_kernel<E, D><<<(unsigned)groups, 64 * kWaves, 0, st>>>(a, most_rows, at_once, most_pieces, lay);
+        attention_few_kernel<E, D><<<(unsigned)groups, 64 * kWaves, 0, st>>>(a, most_rows, lay);
         hipError_t err = hipGetLastError();
         if (err != hipSuccess) return err;
-        attention_join_kernel<E, D><<<(unsigned)most_pieces, 256, 0, st>>>(a, lay);
+        if (most_rounds <= 2 * kSnap + 1) return err;  // no stretch is long enough to be cut
+        attention_join_kernel<E, D><<<2u * (unsigned)groups, kJoinThreads, 0, st>>>(a, lay);
         return hipGetLastError();
     };
     if (at.dtype == EMOE_F32)
