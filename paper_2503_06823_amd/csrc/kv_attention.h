@@ -4,6 +4,29 @@
 #include "kv_cache.h"
 
 namespace emoe {
+
+// Work that is cut along the keys: pieces leave their outputs (fp32, not divided by the sum), maxima and sums in slots of the workspace, and
+// a launch at the end adds them.
+constexpr int kFewRows = 16;      // rows of a slot of the kernel for few queries
+constexpr int kFewPerCu = 3;      // workgroups of it that a CU holds, two slots each
+constexpr int kFewSlots = 2 * kFewPerCu * kMaxGroups;
+constexpr int kTileRows = 128;    // of the kernel for many
+constexpr int kTileSlots = 768;
+struct Piece {
+    int token0, row0, rows, kv_head;
+    int piece, count;         // the how many-th of how many pieces; count 0: there is none in this slot
+    int first, second, step;  // slots of the row's pieces: first, second, second + step, ...
+    int pad[3];
+};
+struct AttentionWs {
+    size_t few_records, few_sums, few_outputs;
+    size_t tile_count, tile_records, tile_sums, tile_outputs;  // tile_count: slots in use
+    size_t total;
+};
+hipError_t launch_attention_few(const emoe_kv_desc& d, int dtype, const AttentionArgs& a, int most_rows, const AttentionWs& ws, int* slots,
+                                hipStream_t st);
+hipError_t launch_attention_tile(const emoe_kv_desc& d, const AttentionArgs& a, int least_rows, const AttentionWs& ws, hipStream_t st);
+
 namespace {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -114,6 +137,9 @@ __device__ __forceinline__ void to_operands(const float* x, bf16x8* out) {
 __device__ __forceinline__ shortx4 read_transposed(const bf16_t* p) {
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)p);
 }
+
+__device__ __forceinline__ void store4(float* p, floatx4 v) { *reinterpret_cast<floatx4*>(p) = v; }
+__device__ __forceinline__ void store4(bf16_t* p, floatx4 v) { *reinterpret_cast<bf16x4*>(p) = __builtin_convertvector(v, bf16x4); }
 
 }  // namespace
 }  // namespace emoe

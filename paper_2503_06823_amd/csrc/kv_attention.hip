@@ -1,0 +1,117 @@
+// Attention over the paged 4-bit cache: which kernel takes which requests, the workspace, and the sum of pieces.
+#include "kv_attention.h"
+
+namespace emoe {
+namespace {
+
+// The pieces of rows that were cut, in the pieces' order.  A workgroup for every piece; those of one cut take its rows in turn.  A team of
+// lanes has four elements of a row each; teams share a row's pieces, as many as there are pieces for, so that the many pieces of a long
+// context are read side by side, and the rows of a short one.
+constexpr int kJoinThreads = 256;
+template <class E, int D>
+__global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(AttentionArgs a, AttentionWs lay, int few_slots) {
+    constexpr int LANES = D / 4, TEAMS = kJoinThreads / LANES;
+    __shared__ floatx4 part[TEAMS][LANES];
+    __shared__ float2 part_sums[TEAMS];
+    const bool few = (int)blockIdx.x < few_slots;
+    const int slot = few ? blockIdx.x : blockIdx.x - few_slots, rows = few ? kFewRows : kTileRows;
+    if (!few && slot >= *reinterpret_cast<const int*>(a.ws + lay.tile_count)) return;
+    const Piece p = reinterpret_cast<const Piece*>(a.ws + (few ? lay.few_records : lay.tile_records))[slot];
+    if (p.count == 0) return;
+    auto row_of = [&](int n, int row) { return (size_t)(n == 0 ? p.first : p.second + (n - 1) * p.step) * rows + row; };
+    const float2* sums = reinterpret_cast<const float2*>(a.ws + (few ? lay.few_sums : lay.tile_sums));
+    const float* outputs = reinterpret_cast<const float*>(a.ws + (few ? lay.few_outputs : lay.tile_outputs));
+    const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES;
+    int shares = 2;  // teams of a row
+    while (shares < TEAMS && shares < p.count) shares *= 2;
+    const int share = team % shares, side = team / shares, step = p.count * (TEAMS / shares);
+    for (int row0 = p.piece; row0 < p.rows; row0 += step) {
+        const int row = row0 + side * p.count;
+        floatx4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+        float top = kLowest, all = 0.0f;
+        if (row < p.rows) {
+#pragma unroll 4
+            for (int n = share; n < p.count; n += shares) {  // one pass: nothing is loaded that waits for another load but the record
+                const size_t at = row_of(n, row);
+                const float2 s = sums[at];
+                const floatx4 o = *reinterpret_cast<const floatx4*>(outputs + at * D + 4 * lane);
+                const float up = fmaxf(top, s.x), f = __builtin_amdgcn_exp2f(top - up), g = __builtin_amdgcn_exp2f(s.x - up);
+                top = up;
+                all = all * f + s.y * g;
+                v = v * f + o * g;
+            }
+        }
+        part[team][lane] = v;
+        if (lane == 0) part_sums[team] = float2{top, all};
+        __syncthreads();
+        if (share == 0 && row < p.rows) {
+            for (int s = 1; s < shares; ++s) top = fmaxf(top, part_sums[team + s].x);
+            v = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+            all = 0.0f;
+            for (int s = 0; s < shares; ++s) {
+                const float f = __builtin_amdgcn_exp2f(part_sums[team + s].x - top);
+                all += part_sums[team + s].y * f;
+                v += part[team + s][lane] * f;
+            }
+            const int m = p.row0 + row;
+            const float by = all == 0.0f ? 0.0f : 1.0f / all;
+            store4(static_cast<E*>(a.out) + (int64_t)(p.token0 + m / a.group) * a.out_stride +
+                       (int64_t)(p.kv_head * a.group + m % a.group) * D + 4 * lane, v * by);
+        }
+        __syncthreads();  // the sums are read
+    }
+}
+
+size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
+
+AttentionWs attention_ws(int dim, bool tiles) {
+    AttentionWs w;
+    w.few_records = 0;
+    w.few_sums = align256(kFewSlots * sizeof(Piece));
+    w.few_outputs = align256(w.few_sums + (size_t)kFewSlots * kFewRows * 8);
+    w.tile_count = align256(w.few_outputs + (size_t)kFewSlots * kFewRows * dim * 4);
+    w.tile_records = w.tile_count + 256;
+    w.tile_sums = align256(w.tile_records + kTileSlots * sizeof(Piece));
+    w.tile_outputs = align256(w.tile_sums + (size_t)kTileSlots * kTileRows * 8);
+    w.total = tiles ? align256(w.tile_outputs + (size_t)kTileSlots * kTileRows * dim * 4) : w.tile_count;
+    return w;
+}
+
+// Requests of up to this many rows (query tokens times the heads of a kv head) go to the kernel for few queries.
+constexpr int kMostFewRows = 32;
+
+// The tile kernel is for bf16: fp32 queries would take three times the matrix work and registers there, and are for verification.
+bool with_tiles(const emoe_attention_desc& a, int group) { return a.dtype == EMOE_BF16 && (long long)a.max_new * group > kMostFewRows; }
+
+}  // namespace
+
+size_t attention_ws_bytes(const emoe_kv_desc& d, const emoe_attention_desc& a) {
+    return attention_ws(d.head_dim, with_tiles(a, a.q_heads / d.kv_heads)).total;
+}
+
+hipError_t launch_attention(const emoe_kv_desc& d, const emoe_attention_desc& at, const AttentionArgs& a, hipStream_t st) {
+    const bool tiles = with_tiles(at, a.group), few = !tiles || a.R > 1;
+    const AttentionWs ws = attention_ws(d.head_dim, tiles);
+    static_assert((size_t)kFewSlots * (sizeof(Piece) + kFewRows * (8 + 128 * 4)) + (size_t)kTileSlots * (sizeof(Piece) + kTileRows * (8 + 128 * 4)) +
+                          8 * 256 <= kAttentionWsBytes, "as include/emoe.h promises");
+    int few_slots = 0;
+    if (tiles) {  // one request alone goes there whatever it brings: the lengths are on the device
+        hipError_t e = launch_attention_tile(d, a, few ? kMostFewRows + 1 : 0, ws, st);
+        if (e != hipSuccess) return e;
+    }
+    if (few) {
+        hipError_t e = launch_attention_few(d, at.dtype, a, tiles ? kMostFewRows : 0x7fffffff, ws, &few_slots, st);
+        if (e != hipSuccess) return e;
+    }
+    const int slots = few_slots + (tiles ? kTileSlots : 0);
+    if (slots == 0) return hipSuccess;
+    auto join = [&](auto element, auto dim) {
+        attention_join_kernel<decltype(element), decltype(dim)::value><<<(unsigned)slots, kJoinThreads, 0, st>>>(a, ws, few_slots);
+        return hipGetLastError();
+    };
+    if (at.dtype == EMOE_F32)
+        return d.head_dim == 64 ? join(float(), std::integral_constant<int, 64>()) : join(float(), std::integral_constant<int, 128>());
+    return d.head_dim == 64 ? join(bf16_t(), std::integral_constant<int, 64>()) : join(bf16_t(), std::integral_constant<int, 128>());
+}
+
+}  // namespace emoe

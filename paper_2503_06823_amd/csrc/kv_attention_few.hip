@@ -14,6 +14,8 @@
 //   - V: converted to bf16 where its scale is one per lane, through LDS (a wavefront's own), read back transposed.
 // fp32 queries and weights are three bf16 operands each, which is exact to fp32; a 4-bit number is exact in bf16.
 //
+// A workgroup has two slots of the workspace: the piece that its share ends in is the first of its row, the one that it begins in is not.
+//
 // Split: all rows' key tiles make one line, of which every workgroup that the chip holds takes an equal part (Stretch).  A row that is cut
 // leaves its pieces (fp32 output, maximum, sum) in the workspace, and a second launch adds them in the pieces' order.
 //
@@ -28,33 +30,13 @@ namespace emoe {
 namespace {
 
 constexpr int kTok = 32;      // tokens of a tile
-constexpr int kRows = 16;     // rows of a workgroup
+constexpr int kRows = kFewRows;  // of a workgroup
 constexpr int kWaves = 4;
 // See Stretch.
 constexpr int kFixed = 2;       // units that a stretch's beginning and end take time for
 constexpr int kLeastUnits = 3;  // of a workgroup's share
 constexpr int kSnap = 1;
 constexpr float kLazy = 8.0f;   // log2 of what a weight may grow to before the maximum is taken up
-
-// Workspace: two pieces of rows that are cut for every workgroup, the one that its share begins in (slot 2 w) and the one that it ends in
-// (slot 2 w + 1): records, maxima and sums, outputs.
-struct Piece {
-    int token0, row0, rows, kv_head;
-    int piece, count;  // the how many-th of how many pieces; count 0: there is none in this slot
-    int group0;        // the workgroup of the first piece
-    int pad;
-};
-struct FewWs {
-    size_t records, sums, outputs, total;
-};
-FewWs few_ws(int most_pieces, int dim) {
-    FewWs w;
-    w.records = 256;
-    w.sums = w.records + (size_t)most_pieces * sizeof(Piece);
-    w.outputs = w.sums + (size_t)most_pieces * kRows * 8;
-    w.total = w.outputs + (size_t)most_pieces * kRows * dim * 4;
-    return w;
-}
 
 template <class E> struct Pieces { static constexpr int n = 1; };
 template <> struct Pieces<float> { static constexpr int n = 3; };
@@ -72,9 +54,6 @@ __device__ __forceinline__ void load8(const bf16_t* p, float* x) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = (float)v[i];
 }
-__device__ __forceinline__ void store4(float* p, floatx4 v) { *reinterpret_cast<floatx4*>(p) = v; }
-__device__ __forceinline__ void store4(bf16_t* p, floatx4 v) { *reinterpret_cast<bf16x4*>(p) = __builtin_convertvector(v, bf16x4); }
-
 // The work as one line of units: requests in order, of a request its kv heads, of a head its tiles of 16 rows, of those (a stretch) kFixed
 // units for its beginning and end and then the rounds of kWaves key tiles that the longest row sees, at least one.  Every workgroup takes an
 // equal part of the line, so that all of them end together whatever the lengths; a boundary within kSnap rounds of a stretch's beginning or
@@ -167,7 +146,7 @@ template <int D> struct Quarter { typedef uint32_t type __attribute__((ext_vecto
 template <> struct Quarter<64> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
 
 template <class E, int D>
-__global__ __launch_bounds__(64 * kWaves, (WavesPerSimd<E, D>::n)) void attention_few_kernel(AttentionArgs a, int most_rows, FewWs lay) {
+__global__ __launch_bounds__(64 * kWaves, (WavesPerSimd<E, D>::n)) void attention_few_kernel(AttentionArgs a, int most_rows, AttentionWs lay) {
     constexpr int PIECES = Pieces<E>::n, STEPS = D / 32, BLOCKS = D / 16;
     constexpr int V_STRIDE = D + 16;  // elements; 32 bytes past the row: 16 rows of 32 bytes fall on all banks alike
     constexpr int V_BYTES = kTok * V_STRIDE * 2, WAVE_BYTES = V_BYTES + kTok * D / 2;  // V as bf16, K as it comes
@@ -179,7 +158,7 @@ __global__ __launch_bounds__(64 * kWaves, (WavesPerSimd<E, D>::n)) void attentio
 
     Start start;
     const bool some = find_start(a, most_rows, &start);
-    Piece* records = reinterpret_cast<Piece*>(a.ws + lay.records) + 2 * (size_t)blockIdx.x;
+    Piece* records = reinterpret_cast<Piece*>(a.ws + lay.few_records) + 2 * (size_t)blockIdx.x;
     bool used[2] = {false, false};
     const long long share_end = some ? start.shares.begin(blockIdx.x + 1) : 0;
     int r = uniform(start.r);
@@ -427,7 +406,7 @@ __global__ __launch_bounds__(64 * kWaves, (WavesPerSimd<E, D>::n)) void attentio
             const int d = 16 * b + 4 * group;
             if (row >= rows) continue;
             if (cut) {
-                float* to = reinterpret_cast<float*>(a.ws + lay.outputs) + (slot * kRows + col) * D + d;
+                float* to = reinterpret_cast<float*>(a.ws + lay.few_outputs) + (slot * kRows + col) * D + d;
                 *reinterpret_cast<floatx4*>(to) = v;
             } else {
                 const float by = all == 0.0f ? 0.0f : 1.0f / all;
@@ -437,13 +416,14 @@ __global__ __launch_bounds__(64 * kWaves, (WavesPerSimd<E, D>::n)) void attentio
         if (cut) {
             used[which] = true;
             if (wave == 0 && group == 0) {
-                float* to = reinterpret_cast<float*>(a.ws + lay.sums) + (slot * kRows + col) * 2;
+                float* to = reinterpret_cast<float*>(a.ws + lay.few_sums) + (slot * kRows + col) * 2;
                 to[0] = top;
                 to[1] = all;
                 if (col == 0) {
                     // whose share holds a unit, boundaries as they are after snapping
                     const int w0 = start.shares.owner(first_unit + kFixed + snap), w1 = start.shares.owner(first_unit + units - snap - 1);
-                    records[which] = Piece{q.first, row0, rows - row0 < kRows ? rows - row0 : kRows, kv_head, (int)blockIdx.x - w0, w1 - w0 + 1, w0, 0};
+                    records[which] = Piece{q.first, row0, rows - row0 < kRows ? rows - row0 : kRows, kv_head, (int)blockIdx.x - w0, w1 - w0 + 1,
+                                           2 * w0 + 1, 2 * (w0 + 1), 2, {}};
                 }
             }
         }
@@ -455,99 +435,29 @@ __global__ __launch_bounds__(64 * kWaves, (WavesPerSimd<E, D>::n)) void attentio
     }
 }
 
-// The pieces of rows that were cut, in the pieces' order.  A workgroup for every piece; those of one cut take its rows in turn.  A team of
-// lanes has four elements of a row each; teams share a row's pieces, as many as there are pieces for, so that the many pieces of a long
-// context are read side by side, and the rows of a short one.
-constexpr int kJoinThreads = 256;
-template <class E, int D>
-__global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(AttentionArgs a, FewWs lay) {
-    constexpr int LANES = D / 4, TEAMS = kJoinThreads / LANES;
-    __shared__ floatx4 part[TEAMS][LANES];
-    __shared__ float2 part_sums[TEAMS];
-    const Piece p = reinterpret_cast<const Piece*>(a.ws + lay.records)[blockIdx.x];
-    if (p.count == 0) return;
-    // the first piece is the end of its workgroup's share, the others are the beginnings of theirs
-    auto row_of = [&](int n, int row) { return (size_t)(2 * (p.group0 + n) + (n == 0 ? 1 : 0)) * kRows + row; };
-    const float2* sums = reinterpret_cast<const float2*>(a.ws + lay.sums);
-    const float* outputs = reinterpret_cast<const float*>(a.ws + lay.outputs);
-    const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES;
-    int shares = 2;  // teams of a row
-    while (shares < TEAMS && shares < p.count) shares *= 2;
-    const int share = team % shares, side = team / shares, step = p.count * (TEAMS / shares);
-    for (int row0 = p.piece; row0 < p.rows; row0 += step) {
-        const int row = row0 + side * p.count;
-        floatx4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-        float top = kLowest, all = 0.0f;
-        if (row < p.rows) {
-#pragma unroll 4
-            for (int n = share; n < p.count; n += shares) {  // one pass: nothing is loaded that waits for another load but the record
-                const size_t at = row_of(n, row);
-                const float2 s = sums[at];
-                const floatx4 o = *reinterpret_cast<const floatx4*>(outputs + at * D + 4 * lane);
-                const float up = fmaxf(top, s.x), f = __builtin_amdgcn_exp2f(top - up), g = __builtin_amdgcn_exp2f(s.x - up);
-                top = up;
-                all = all * f + s.y * g;
-                v = v * f + o * g;
-            }
-        }
-        part[team][lane] = v;
-        if (lane == 0) part_sums[team] = float2{top, all};
-        __syncthreads();
-        if (share == 0 && row < p.rows) {
-            for (int s = 1; s < shares; ++s) top = fmaxf(top, part_sums[team + s].x);
-            v = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-            all = 0.0f;
-            for (int s = 0; s < shares; ++s) {
-                const float f = __builtin_amdgcn_exp2f(part_sums[team + s].x - top);
-                all += part_sums[team + s].y * f;
-                v += part[team + s][lane] * f;
-            }
-            const int m = p.row0 + row;
-            const float by = all == 0.0f ? 0.0f : 1.0f / all;
-            store4(static_cast<E*>(a.out) + (int64_t)(p.token0 + m / a.group) * a.out_stride +
-                       (int64_t)(p.kv_head * a.group + m % a.group) * D + 4 * lane, v * by);
-        }
-        __syncthreads();  // the sums are read
-    }
-}
-
-constexpr int kPerCu = 3;  // workgroups that a CU holds
-
 }  // namespace
 
-size_t attention_few_ws_bytes(const emoe_kv_desc& d) { return few_ws(2 * kPerCu * kMaxGroups, d.head_dim).total; }
-
-hipError_t launch_attention_few(const emoe_kv_desc& d, const emoe_attention_desc& at, const AttentionArgs& a, int most_rows, hipStream_t st) {
+// *slots: of the workspace that can hold a piece.
+hipError_t launch_attention_few(const emoe_kv_desc& d, int dtype, const AttentionArgs& a, int most_rows, const AttentionWs& ws, int* slots,
+                                hipStream_t st) {
     DeviceShape shape;
     hipError_t e = device_shape(&shape);
     if (e != hipSuccess) return e;
     // As many workgroups as the chip holds at once, or as many as there can be shares for, by the tokens and the requests.
-    const long long per_request = ((long long)a.max_new * a.group < most_rows ? (long long)a.max_new * a.group : most_rows) + kRows - 1;
-    const long long by_tokens = (long long)a.T * a.group / kRows + a.R;
-    const long long row_tiles = per_request / kRows * a.R < by_tokens ? per_request / kRows * a.R : by_tokens;
+    const long long rows = (long long)a.max_new * a.group < most_rows ? (long long)a.max_new * a.group : most_rows;
+    const long long per_request = (rows + kRows - 1) / kRows, by_tokens = (long long)a.T * a.group / kRows + a.R;
+    const long long row_tiles = per_request * a.R < by_tokens ? per_request * a.R : by_tokens;
     const long long most_rounds = (((long long)a.width << a.page.log2_size) + kTok * kWaves - 1) / (kTok * kWaves);
     const long long line = row_tiles * a.kv_heads * (kFixed + most_rounds), shares = (line + kLeastUnits - 1) / kLeastUnits;
-    const int groups = shares < kPerCu * shape.groups ? (int)shares : kPerCu * shape.groups;
-    const FewWs lay = few_ws(2 * kPerCu * kMaxGroups, d.head_dim);
+    const int groups = shares < kFewPerCu * shape.groups ? (int)shares : kFewPerCu * shape.groups;
+    *slots = most_rounds > 2 * kSnap + 1 ? 2 * groups : 0;  // none if no stretch is long enough to be cut
     auto run = [&](auto element, auto dim) {
-        typedef decltype(element) E;
-        constexpr int D = decltype(dim)::value;
-        attention_few_kernel<E, D><<<(unsigned)groups, 64 * kWaves, 0, st>>>(a, most_rows, lay);
-        hipError_t err = hipGetLastError();
-        if (err != hipSuccess) return err;
-        if (most_rounds <= 2 * kSnap + 1) return err;  // no stretch is long enough to be cut
-        attention_join_kernel<E, D><<<2u * (unsigned)groups, kJoinThreads, 0, st>>>(a, lay);
+        attention_few_kernel<decltype(element), decltype(dim)::value><<<(unsigned)groups, 64 * kWaves, 0, st>>>(a, most_rows, ws);
         return hipGetLastError();
     };
-    if (at.dtype == EMOE_F32)
+    if (dtype == EMOE_F32)
         return d.head_dim == 64 ? run(float(), std::integral_constant<int, 64>()) : run(float(), std::integral_constant<int, 128>());
     return d.head_dim == 64 ? run(bf16_t(), std::integral_constant<int, 64>()) : run(bf16_t(), std::integral_constant<int, 128>());
-}
-
-size_t attention_ws_bytes(const emoe_kv_desc& d, const emoe_attention_desc&) { return attention_few_ws_bytes(d); }
-
-hipError_t launch_attention(const emoe_kv_desc& d, const emoe_attention_desc& at, const AttentionArgs& a, hipStream_t st) {
-    return launch_attention_few(d, at, a, 0x7fffffff, st);
 }
 
 }  // namespace emoe

@@ -1,0 +1,465 @@
+// Attention over the paged 4-bit cache for bf16 requests of many queries: prompts, and pieces of them.
+//
+//   S^T = K Q^T,  P^T = exp2(S^T - max),  O^T += V^T P^T,  one pass over the keys and values, as for few queries.
+//
+// Bound by the matrix cores (4 * D flop a query, head and visible token), next to them by the exponentials and by LDS.  A workgroup
+// has 128 rows (query token, query head) of one kv head, 32 a wavefront, and walks the keys in tiles of 64; two workgroups share a
+// CU, so that one's exponentials run under the other's products.
+//   - K stays in 4 bits all the way: v_mfma_scale_f32_32x32x64_f8f6f4 takes it as it lies in the cache, with its scales, and q as two
+//     8-bit operands, the nearest e4m3 and 16 times what it leaves.  A bf16 number has eight significant bits, four for each,
+//     so their sum is q up to 2^-21 of the row's largest element.  The product's sums are off by 8e-7 (rms; 2.5e-5 at worst) of the
+//     sum of magnitudes.  It takes the time of a product in bf16, but a quarter of the LDS bytes for K, and no conversion: with K as
+//     bf16 the fragment reads of 32 rows a wavefront take LDS as long as the products take the matrix cores.
+//   - V is converted to bf16 once for the workgroup on its way into LDS and read back transposed.
+//   - P^T comes out of S^T in the registers in which the second product wants it.
+// The tile after the next is on its way from memory while a tile is multiplied, the next one is written to the other half of LDS; one barrier a
+// tile.
+//
+// Split: a workgroup takes a row tile's keys whole, the longest first, where there are enough row tiles; else pieces of them (plan_tiles), which
+// leave fp32 outputs, maxima and sums in the workspace for a second launch to add.
+#include <math.h>
+
+#include "kv_attention.h"
+
+namespace emoe {
+namespace {
+
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef int intx8 __attribute__((ext_vector_type(8)));
+
+constexpr int kTok = 64;    // tokens of a tile
+constexpr int kRows = kTileRows;
+constexpr int kWaves = 4;
+constexpr float kLazy = 8.0f;  // log2 of what a weight may grow to before the maximum is taken up
+
+// A request's row tiles and the key tiles of the longest and the shortest of them.
+struct Rows {
+    int row_tiles, longest, shortest;
+};
+__device__ __forceinline__ Rows rows_of(const AttentionArgs& a, const Request& q, int least_rows) {
+    const long long rows = (long long)q.n * a.group;
+    if (rows == 0 || rows < least_rows) return {0, 0, 0};
+    const int n = (int)((rows + kRows - 1) / kRows);
+    const int p0 = q.len - q.n, first = kRows / a.group < q.n ? kRows / a.group : q.n;
+    const int whole = tiles<kTok>(a, q.seq, p0, q.len - 1).count(), start = tiles<kTok>(a, q.seq, p0, p0 + first - 1).count();
+    return {n, whole > 0 ? whole : 1, start > 0 ? start : 1};
+}
+
+// A piece of work: a row tile, and the how many-th of its pieces of `each` key tiles.
+struct Job {
+    int r, row_tile, kv_head, piece, pieces, each, slot, all_slots;
+    bool found;
+    Request q;
+};
+
+// The longest piece is chosen so that the work is over soonest: the longest request's tiles over 1 to 64 pieces, an estimate a lane.  With
+// pieces of c tiles there are n = sum of ceil(tiles / c), and they take ceil(n / places) rounds of c + kFixed, or, in any
+// order, no longer than an equal share and one piece.  Every wavefront by itself, 64 requests a trip.
+constexpr int kFixed = 4;  // key tiles that a piece's beginning and end take time for
+__device__ __forceinline__ Job find_job(const AttentionArgs& a, int least_rows, int places, int want, bool to_the_end) {
+    const int lane = threadIdx.x & 63;
+    Request mine;
+    auto rows_at = [&](int r) {
+        mine = {0, 0, 0, 0};
+        if (r < a.R) mine = request(a, r);
+        return rows_of(a, mine, least_rows);
+    };
+    Rows rows;
+    int longest = 0;
+    for (int r0 = 0; r0 < a.R; r0 += 64) {
+        rows = rows_at(r0 + lane);
+        int n = rows.longest;
+#pragma unroll
+        for (int s = 32; s > 0; s /= 2) {
+            const int o = __shfl_xor(n, s);
+            n = o > n ? o : n;
+        }
+        longest = n > longest ? n : longest;
+    }
+    Job job;
+    job.found = false;
+    job.all_slots = 0;
+    if (longest == 0) return job;
+    const int c = (longest + lane) / (lane + 1);  // this lane's estimate
+    float pieces = 0.0f, cut = 0.0f, work = 0.0f;
+    for (int r0 = 0; r0 < a.R; r0 += 64) {
+        if (a.R > 64) rows = rows_at(r0 + lane);
+        for (unsigned long long some = __ballot(rows.row_tiles > 0); some != 0; some &= some - 1) {
+            const int at = __builtin_ctzll(some);
+            const float stretches = (float)__builtin_amdgcn_readlane(rows.row_tiles, at) * (float)a.kv_heads;
+            const int n = __builtin_amdgcn_readlane(rows.longest, at), k = (n + c - 1) / c;
+            pieces += stretches * (float)k;
+            cut += k > 1 ? stretches * (float)k : 0.0f;
+            work += stretches * 0.5f * (float)(n + __builtin_amdgcn_readlane(rows.shortest, at));
+        }
+    }
+    const float rounds = ceilf(pieces / (float)places) * (float)(c + kFixed);
+    const float any_order = (work + pieces * (float)kFixed) / (float)places + (float)c;
+    float best = cut > (float)kTileSlots ? INFINITY : fminf(rounds, any_order);
+    int each = c;
+#pragma unroll
+    for (int s = 32; s > 0; s /= 2) {
+        const float o = __shfl_xor(best, s);
+        const int e = __shfl_xor(each, s);
+        if (o < best || (o == best && e > each)) {
+            best = o;
+            each = e;
+        }
+    }
+    each = uniform(each);
+
+    int jobs = 0, slots = 0;
+    for (int r0 = 0; r0 < a.R; r0 += 64) {
+        if (a.R > 64) rows = rows_at(r0 + lane);
+        const int k = rows.row_tiles > 0 ? (rows.longest + each - 1) / each : 0;
+        const int here = rows.row_tiles * a.kv_heads * k, cut_here = k > 1 ? here : 0;
+        const int upto = wave_inclusive(here), cut_upto = wave_inclusive(cut_here);
+        const int total = __builtin_amdgcn_readlane(upto, 63);
+        if (!job.found && want - jobs < total) {
+            const int at = __builtin_ctzll(__ballot(upto > want - jobs));
+            const int row_tiles = __builtin_amdgcn_readlane(rows.row_tiles, at);
+            int local = want - jobs - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(here, at));
+            // kv heads side by side: workgroups of one head then share an XCD's L2 where the heads are a multiple of the XCDs; the longest row
+            // tiles first, for the short ones fill the gaps at the end
+            job.kv_head = local % a.kv_heads;
+            local /= a.kv_heads;
+            job.row_tile = row_tiles - 1 - local % row_tiles;
+            job.piece = local / row_tiles;
+            job.r = r0 + at;
+            job.pieces = __builtin_amdgcn_readlane(k, at);
+            job.each = each;
+            job.slot = slots + __builtin_amdgcn_readlane(cut_upto, at) - __builtin_amdgcn_readlane(cut_here, at) +
+                       (job.row_tile * a.kv_heads + job.kv_head) * job.pieces + job.piece;
+            job.q = {__builtin_amdgcn_readlane(mine.first, at), __builtin_amdgcn_readlane(mine.n, at), __builtin_amdgcn_readlane(mine.seq, at),
+                     __builtin_amdgcn_readlane(mine.len, at)};
+            job.found = true;
+        }
+        jobs += total;
+        slots += __builtin_amdgcn_readlane(cut_upto, 63);
+        if (job.found && !to_the_end) break;
+    }
+    job.all_slots = slots;
+    return job;
+}
+
+template <int D> struct Quarter { typedef uint32_t type __attribute__((ext_vector_type(4))); };
+template <> struct Quarter<64> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
+
+template <int D>
+__global__ __launch_bounds__(64 * kWaves, 2) void attention_tile_kernel(AttentionArgs a, int least_rows, int places, AttentionWs lay) {
+    constexpr int STEPS = D / 64, BLOCKS = D / 32, SCALES = D / 32;
+    constexpr int V_ROW = 2 * D, K_ROW = D / 2;
+    typedef typename Quarter<D>::type Words;
+    struct Half {
+        __attribute__((aligned(16))) char v[kTok * V_ROW];  // bf16
+        __attribute__((aligned(16))) char k[kTok * K_ROW];
+        __attribute__((aligned(16))) uint8_t k_scale[kTok * SCALES], v_scale[kTok * SCALES];
+        __attribute__((aligned(16))) int odd[kWaves];  // of a wavefront's 16 tokens: 1, some block of values is NaN; 2, their page is nobody's
+    };
+    __shared__ Half halves[2];
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const int col = lane & 31, group = lane >> 5;
+
+    const Job job = find_job(a, least_rows, places, blockIdx.x, blockIdx.x == 0);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<int*>(a.ws + lay.tile_count) = job.all_slots;
+    if (!job.found) return;
+    const int r = uniform(job.r), kv_head = uniform(job.kv_head), row_tile = uniform(job.row_tile), pieces = uniform(job.pieces);
+    const Request q = uniform(job.q);
+    const int rows = q.n * a.group, row0 = row_tile * kRows, p0 = q.len - q.n;
+    const int last_row = row0 + kRows < rows ? row0 + kRows - 1 : rows - 1;
+    // the wavefront's own rows
+    const int w_row0 = row0 + 32 * wave, w_last = w_row0 + 31 < rows ? w_row0 + 31 : rows - 1;
+    const bool w_any = w_row0 < rows;
+    const int w_first_p = uniform(p0 + w_row0 / a.group), w_last_p = uniform(p0 + w_last / a.group);
+
+    const Tiles seen = uniform(tiles<kTok>(a, q.seq, p0 + row0 / a.group, p0 + last_row / a.group));
+    const int i_all = seen.count(), each = uniform(job.each);
+    const int i_begin = uniform(job.piece) * each;
+    int i_end = i_begin + each < i_all ? i_begin + each : i_all;
+    if (job.piece + 1 == job.pieces) i_end = i_all;
+
+    typedef const __attribute__((address_space(4))) int32_t* ScalarTable;
+    const ScalarTable table = (ScalarTable)(a.table + (size_t)r * a.width);
+    const int page_mask = (1 << a.page.log2_size) - 1;
+    const uint32_t head_bytes = (uint32_t)a.page.bytes(), page_stride = head_bytes * (uint32_t)a.kv_heads;
+    const uint8_t* cache = a.cache + (size_t)kv_head * head_bytes;
+
+    // A wavefront brings 16 tokens of a tile, which lie in one page: quarter lane % 4 of token lane / 4, in the order of memory.
+    const int in_tok = 16 * wave + (lane >> 2), quarter = lane & 3;
+    const uint32_t in_at = (lane >> 2) * (D / 2) + quarter * (D / 8), scale_at = (lane >> 2) * SCALES + quarter * (D / 4) / 32;
+    struct Place {
+        const uint8_t *codes, *scales;
+        int t0;
+        bool owned;
+    };
+    auto place = [&](int i) {
+        Place p;
+        p.t0 = seen.tile(i) * kTok;
+        const int t = p.t0 + 16 * wave, b = t >> a.page.log2_size;
+        const uint32_t page = (uint32_t)table[b < a.width ? b : a.width - 1];
+        p.owned = page < (uint32_t)a.pages && b < a.width;
+        const uint8_t* head = cache + (uint64_t)(p.owned ? page : 0u) * page_stride;
+        p.codes = head + (t & page_mask) * (D / 2);
+        p.scales = head + 2 * a.page.codes + (t & page_mask) * SCALES;
+        return p;
+    };
+    Words k_in, v_in;
+    uint32_t k_byte, v_byte;
+    auto load = [&](const Place& p) {
+        k_in = *reinterpret_cast<const Words*>(p.codes + in_at);
+        v_in = *reinterpret_cast<const Words*>(p.codes + a.page.codes + in_at);
+        k_byte = p.scales[scale_at];
+        v_byte = (p.scales + a.page.scales)[scale_at];
+    };
+    // In LDS the 64-byte piece b of V's row t lies in place b ^ v_swizzle(t), so that the four rows of a transposed read fall on all banks;
+    // the 16-byte chunk c of K's row t in c ^ k_swizzle(t).
+    auto v_swizzle = [](int t) { return D == 128 ? t & 3 : (t >> 1) & 1; };
+    auto k_swizzle = [](int t) { return D == 128 ? (t >> 2) & 3 : 0; };
+    const int v_to = in_tok * V_ROW + (((quarter * (D / 4) / 32) ^ v_swizzle(in_tok)) * 64) + (D == 128 ? 0 : (quarter & 1) * 32);
+    const int k_to = in_tok * K_ROW + (((quarter * (D / 8) / 16) ^ k_swizzle(in_tok)) * 16) + (D == 128 ? 0 : (quarter & 1) * 8);
+    auto write = [&](Half& h, const Place& p) {
+        const bool there = p.owned & (p.t0 + in_tok < q.seq);
+        uint32_t byte = there ? v_byte : 127u;  // never written: any number will do
+        const unsigned long long nan = __ballot(byte == 255);
+        if (lane == 0) h.odd[wave] = (nan != 0 ? 1 : 0) | (p.owned ? 0 : 2);
+        if (D == 128 || (quarter & 1) == 0) {
+            h.k_scale[in_tok * SCALES + quarter * (D / 4) / 32] = (uint8_t)k_byte;
+            h.v_scale[in_tok * SCALES + quarter * (D / 4) / 32] = (uint8_t)byte;
+        }
+        *reinterpret_cast<Words*>(h.k + k_to) = k_in;
+        const float scale = scale_of_byte(byte == 255 ? 127u : byte);
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) *reinterpret_cast<bf16x8*>(h.v + v_to + 16 * e) = from_codes(v_in[e], scale);
+    };
+
+    floatx16 out[BLOCKS];
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) out[b][e] = 0.0f;
+    float most = kLowest, sum = 0.0f;
+    uint32_t bad = 0;  // blocks of this lane's query that a block of NaN values has reached
+
+    Place ahead, after;
+    if (i_begin < i_end) {
+        const Place first = place(i_begin);
+        load(first);
+        ahead = place(i_begin + 1 < i_end ? i_begin + 1 : i_begin);
+        write(halves[0], first);
+        load(ahead);
+        after = place(i_begin + 2 < i_end ? i_begin + 2 : i_end - 1);
+    }
+
+    // q as two e4m3 operands.  Lane (col, group) holds elements 64 s + 16 group .. +15 and 32 further on of its row; one scale a row.
+    const int row = w_row0 + col, token = row / a.group, head = kv_head * a.group + row % a.group;
+    const int position = row < rows ? p0 + token : -1;  // -1 sees nothing
+    intx8 q_hi[STEPS], q_lo[STEPS];
+    int q_scale;
+    {
+        float x[STEPS][32];
+        const bf16_t* at = static_cast<const bf16_t*>(a.q) + (int64_t)(q.first + token) * a.q_stride + (int64_t)head * D + group * 16;
+        uint32_t top = 0;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                bf16x8 v;
+                if (row < rows) v = *reinterpret_cast<const bf16x8*>(at + 64 * s + 32 * (c / 2) + 8 * (c % 2));
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    x[s][8 * c + e] = row < rows ? (float)v[e] : 0.0f;
+                    const uint32_t m = __float_as_uint(x[s][8 * c + e]) & 0x7fffffffu;
+                    top = m > top ? m : top;
+                }
+            }
+        const uint32_t other = (uint32_t)__shfl_xor((int)top, 32);
+        top = other > top ? other : top;
+        // the largest below 2^8 (e4m3 reaches 448), what is left below 2^4, times 16
+        int e = (int)(top >> 23) - 127 - 7;
+        e = e < -118 ? -118 : e;
+        const float down = __uint_as_float((uint32_t)(127 - e) << 23);
+        q_scale = (e + 127) | ((e + 127 - 4) << 8);
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+            for (int w = 0; w < 8; ++w) {
+                float y[4], rest[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) y[k] = x[s][4 * w + k] * down;
+                int hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+                hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], hi, true);
+                rest[0] = (y[0] - __builtin_amdgcn_cvt_f32_fp8(hi, 0)) * 16.0f;
+                rest[1] = (y[1] - __builtin_amdgcn_cvt_f32_fp8(hi, 1)) * 16.0f;
+                rest[2] = (y[2] - __builtin_amdgcn_cvt_f32_fp8(hi, 2)) * 16.0f;
+                rest[3] = (y[3] - __builtin_amdgcn_cvt_f32_fp8(hi, 3)) * 16.0f;
+                int lo = __builtin_amdgcn_cvt_pk_fp8_f32(rest[0], rest[1], 0, false);
+                lo = __builtin_amdgcn_cvt_pk_fp8_f32(rest[2], rest[3], lo, true);
+                q_hi[s][w] = hi;
+                q_lo[s][w] = lo;
+            }
+    }
+
+    // fragment addresses: K's row is the lane's column index; V's rows 4 group + (lane % 16) / 4 of every eight, four columns each
+    const int sub = (lane >> 4) & 1, v_row = 4 * group + ((lane & 15) >> 2);
+    int k_from[STEPS], v_from[BLOCKS];
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) k_from[s] = col * K_ROW + (((2 * s + group) ^ k_swizzle(col)) * 16);
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) v_from[b] = v_row * V_ROW + ((b ^ v_swizzle(v_row)) * 64) + sub * 32 + (lane & 3) * 8;
+
+    auto barrier = [] {
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    };
+    barrier();
+
+    for (int i = i_begin; i < i_end; ++i) {
+        const Half& h = halves[(i - i_begin) & 1];
+        const int t0 = seen.tile(i) * kTok;
+        if (i + 1 < i_end) {
+            write(halves[(i - i_begin + 1) & 1], ahead);
+            load(after);
+            ahead = after;
+            after = place(i + 3 < i_end ? i + 3 : i_end - 1);
+        }
+        const bool some = w_any & (t0 <= w_last_p) & ((a.window == 0) | (t0 + kTok > w_first_p - a.window + 1) | (t0 < a.sinks));
+        if (some) {
+            floatx16 z[2];
+#pragma unroll
+            for (int tb = 0; tb < 2; ++tb) {
+                int scale;
+                if (D == 128) scale = (int)(*reinterpret_cast<const uint32_t*>(h.k_scale + (32 * tb + col) * SCALES) >> (8 * group));
+                else scale = h.k_scale[(32 * tb + col) * SCALES + group];
+                floatx16 s;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[e] = 0.0f;
+#pragma unroll
+                for (int st = 0; st < STEPS; ++st) {
+                    const int4 w = *reinterpret_cast<const int4*>(h.k + k_from[st] + 32 * tb * K_ROW);
+                    const intx8 key = {w.x, w.y, w.z, w.w, 0, 0, 0, 0};
+                    if (st == 0) {
+                        s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(key, q_lo[st], s, 4, 0, 0, scale, 1, q_scale);
+                        s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(key, q_hi[st], s, 4, 0, 0, scale, 0, q_scale);
+                    } else {
+                        s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(key, q_lo[st], s, 4, 0, 2, scale, 1, q_scale);
+                        s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(key, q_hi[st], s, 4, 0, 2, scale, 0, q_scale);
+                    }
+                }
+                z[tb] = s * a.scale_log2;
+            }
+            const int4 odd4 = *reinterpret_cast<const int4*>(h.odd);
+            const int odd[4] = {odd4.x, odd4.y, odd4.z, odd4.w}, any_odd = uniform(odd4.x | odd4.y | odd4.z | odd4.w);
+            // every row of this wavefront sees every token of the tile
+            const bool whole = ((any_odd & 2) == 0) & (t0 + kTok - 1 <= w_first_p) &
+                               ((a.window == 0) | (t0 > w_last_p - a.window) | (t0 + kTok <= a.sinks));
+            if (!whole) {
+                const int from = a.window > 0 && position >= a.window ? position - a.window + 1 : 0;
+#pragma unroll
+                for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int j = t0 + 32 * tb + 8 * (e / 4) + 4 * group + e % 4;
+                        const bool sees = (j <= position) & ((j >= from) | (j < a.sinks)) & ((odd[2 * tb + e / 8] & 2) == 0);
+                        z[tb][e] = sees ? z[tb][e] : -INFINITY;
+                    }
+            }
+            if ((any_odd & 1) != 0) {
+                // V holds numbers where its blocks are NaN; what sees such a token becomes NaN at the end
+#pragma unroll
+                for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int t = 32 * tb + 8 * (e / 4) + 4 * group + e % 4;
+                        uint32_t w;
+                        if (D == 128) w = *reinterpret_cast<const uint32_t*>(h.v_scale + t * SCALES);
+                        else w = *reinterpret_cast<const uint16_t*>(h.v_scale + t * SCALES);
+                        const uint32_t all_ones = ((w & 0x7f7f7f7fu) + 0x01010101u) & w & 0x80808080u;  // bytes of 255
+                        const uint32_t blocks = (all_ones >> 7 & 1) | (all_ones >> 14 & 2) | (all_ones >> 21 & 4) | (all_ones >> 28 & 8);
+                        bad |= z[tb][e] != -INFINITY ? blocks : 0u;
+                    }
+            }
+            float top = z[0][0];
+#pragma unroll
+            for (int e = 1; e < 32; ++e) top = fmaxf(top, z[e / 16][e % 16]);
+            {
+                const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+                top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+            }
+            if (__any(top > most + kLazy)) {  // the weights stay below 2^8: a maximum that rises by less is not worth a pass over the output
+                const float up = fmaxf(most, top), f = __builtin_amdgcn_exp2f(most - up);
+                most = up;
+                sum *= f;
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b) out[b] *= f;
+            }
+            bf16x8 weight[4];
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+                const float w = __builtin_amdgcn_exp2f(z[e / 16][e % 16] - most);
+                sum += w;
+                weight[e / 8][e % 8] = (__bf16)w;
+            }
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    union {
+                        shortx4 half[2];
+                        bf16x8 all;
+                    } f;
+                    f.half[0] = read_transposed(reinterpret_cast<const bf16_t*>(h.v + v_from[b] + (16 * k) * V_ROW));
+                    f.half[1] = read_transposed(reinterpret_cast<const bf16_t*>(h.v + v_from[b] + (16 * k + 8) * V_ROW));
+                    out[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.all, weight[k], out[b], 0, 0, 0);
+                }
+        }
+        barrier();
+    }
+
+    if (row >= rows) return;
+    {
+        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
+        sum = __uint_as_float(both[0]) + __uint_as_float(both[1]);
+    }
+    bad |= (uint32_t)__shfl_xor((int)bad, 32);
+    const bool cut = pieces > 1;
+    const float by = cut ? 1.0f : sum == 0.0f ? 0.0f : 1.0f / sum;
+    const size_t slot_row = (size_t)uniform(job.slot) * kRows + 32 * wave + col;
+    float* piece_to = reinterpret_cast<float*>(a.ws + lay.tile_outputs) + slot_row * D;
+    bf16_t* to = static_cast<bf16_t*>(a.out) + (int64_t)(q.first + token) * a.out_stride + (int64_t)head * D;
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int d = 32 * b + 8 * e + 4 * group;
+            floatx4 v = {out[b][4 * e], out[b][4 * e + 1], out[b][4 * e + 2], out[b][4 * e + 3]};
+            v *= by;
+            if (bad >> b & 1u) v = floatx4{NAN, NAN, NAN, NAN};
+            if (cut) *reinterpret_cast<floatx4*>(piece_to + d) = v;
+            else *reinterpret_cast<bf16x4*>(to + d) = __builtin_convertvector(v, bf16x4);
+        }
+    if (cut && group == 0) {
+        *reinterpret_cast<float2*>(a.ws + lay.tile_sums + slot_row * 8) = float2{most, sum};
+        if (threadIdx.x == 0) {
+            const int n = rows - row0 < kRows ? rows - row0 : kRows;
+            const int first = uniform(job.slot) - uniform(job.piece);
+            reinterpret_cast<Piece*>(a.ws + lay.tile_records)[uniform(job.slot)] =
+                Piece{q.first, row0, n, kv_head, uniform(job.piece), pieces, first, first + 1, 1};
+        }
+    }
+}
+
+}  // namespace
+
+hipError_t launch_attention_tile(const emoe_kv_desc& d, const AttentionArgs& a, int least_rows, const AttentionWs& lay, hipStream_t st) {
+    DeviceShape shape;
+    hipError_t e = device_shape(&shape);
+    if (e != hipSuccess) return e;
+    const long long per_request = ((long long)a.max_new * a.group + kRows - 1) / kRows, by_tokens = (long long)a.T * a.group / kRows + a.R;
+    const long long row_tiles = per_request * a.R < by_tokens ? per_request * a.R : by_tokens;
+    const long long groups = row_tiles * a.kv_heads + kTileSlots;  // no more pieces than that
+    if (groups > 0x7fffffff / 256) return hipErrorInvalidValue;
+    if (d.head_dim == 64) attention_tile_kernel<64><<<(unsigned)groups, 64 * kWaves, 0, st>>>(a, least_rows, 2 * shape.cus, lay);
+    else attention_tile_kernel<128><<<(unsigned)groups, 64 * kWaves, 0, st>>>(a, least_rows, 2 * shape.cus, lay);
+    return hipGetLastError();
+}
+
+}  // namespace emoe
