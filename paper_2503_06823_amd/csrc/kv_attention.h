@@ -11,7 +11,7 @@ constexpr int kFewRows = 16;      // rows of a slot of the kernel for few querie
 constexpr int kFewPerCu = 3;      // workgroups of it that a CU holds, two slots each
 constexpr int kFewSlots = 2 * kFewPerCu * kMaxGroups;
 constexpr int kTileRows = 128;    // of the kernel for many
-constexpr int kTileSlots = 768;
+constexpr int kTileSlots = 2 * kMaxGroups;  // as many as run at the same time
 struct Piece {
     int token0, row0, rows, kv_head;
     int piece, count;         // the how many-th of how many pieces; count 0: there is none in this slot

@@ -5,9 +5,10 @@ namespace emoe {
 namespace {
 
 // The pieces of rows that were cut, in the pieces' order.  A workgroup for every piece; those of one cut take its rows in turn.  A team of
-// lanes has four elements of a row each; teams share a row's pieces, as many as there are pieces for, so that the many pieces of a long
-// context are read side by side, and the rows of a short one.
+// lanes has four elements of a row each; where there are many pieces all teams share a row's, so that those of a long context are read side by
+// side, else every team has a row of its own.
 constexpr int kJoinThreads = 256;
+constexpr int kOneTeam = 8;  // pieces that a team adds alone
 template <class E, int D>
 __global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(AttentionArgs a, AttentionWs lay, int few_slots) {
     constexpr int LANES = D / 4, TEAMS = kJoinThreads / LANES;
@@ -22,8 +23,7 @@ __global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(AttentionA
     const float2* sums = reinterpret_cast<const float2*>(a.ws + (few ? lay.few_sums : lay.tile_sums));
     const float* outputs = reinterpret_cast<const float*>(a.ws + (few ? lay.few_outputs : lay.tile_outputs));
     const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES;
-    int shares = 2;  // teams of a row
-    while (shares < TEAMS && shares < p.count) shares *= 2;
+    const int shares = p.count > kOneTeam ? TEAMS : 1;  // teams of a row
     const int share = team % shares, side = team / shares, step = p.count * (TEAMS / shares);
     for (int row0 = p.piece; row0 < p.rows; row0 += step) {
         const int row = row0 + side * p.count;
@@ -41,24 +41,28 @@ __global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(AttentionA
                 v = v * f + o * g;
             }
         }
-        part[team][lane] = v;
-        if (lane == 0) part_sums[team] = float2{top, all};
-        __syncthreads();
-        if (share == 0 && row < p.rows) {
-            for (int s = 1; s < shares; ++s) top = fmaxf(top, part_sums[team + s].x);
-            v = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-            all = 0.0f;
-            for (int s = 0; s < shares; ++s) {
-                const float f = __builtin_amdgcn_exp2f(part_sums[team + s].x - top);
-                all += part_sums[team + s].y * f;
-                v += part[team + s][lane] * f;
+        if (shares > 1) {
+            part[team][lane] = v;
+            if (lane == 0) part_sums[team] = float2{top, all};
+            __syncthreads();
+            if (share == 0) {
+                for (int s = 1; s < TEAMS; ++s) top = fmaxf(top, part_sums[s].x);
+                v = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+                all = 0.0f;
+                for (int s = 0; s < TEAMS; ++s) {
+                    const float f = __builtin_amdgcn_exp2f(part_sums[s].x - top);
+                    all += part_sums[s].y * f;
+                    v += part[s][lane] * f;
+                }
             }
+            __syncthreads();  // the sums are read
+        }
+        if (share == 0 && row < p.rows) {
             const int m = p.row0 + row;
             const float by = all == 0.0f ? 0.0f : 1.0f / all;
             store4(static_cast<E*>(a.out) + (int64_t)(p.token0 + m / a.group) * a.out_stride +
                        (int64_t)(p.kv_head * a.group + m % a.group) * D + 4 * lane, v * by);
         }
-        __syncthreads();  // the sums are read
     }
 }
 

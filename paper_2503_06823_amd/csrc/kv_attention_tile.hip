@@ -12,8 +12,8 @@
 //     bf16 the fragment reads of 32 rows a wavefront take LDS as long as the products take the matrix cores.
 //   - V is converted to bf16 once for the workgroup on its way into LDS and read back transposed.
 //   - P^T comes out of S^T in the registers in which the second product wants it.
-// The tile after the next is on its way from memory while a tile is multiplied, the next one is written to the other half of LDS; one barrier a
-// tile.
+// The tile after the next is on its way from memory while a tile is multiplied, the next one is written to the other half of LDS under the
+// scores' products; one barrier a tile.
 //
 // Split: a workgroup takes a row tile's keys whole, the longest first, where there are enough row tiles; else pieces of them (plan_tiles), which
 // leave fp32 outputs, maxima and sums in the workspace for a second launch to add.
@@ -30,7 +30,7 @@ typedef int intx8 __attribute__((ext_vector_type(8)));
 constexpr int kTok = 64;    // tokens of a tile
 constexpr int kRows = kTileRows;
 constexpr int kWaves = 4;
-constexpr float kLazy = 8.0f;  // log2 of what a weight may grow to before the maximum is taken up
+constexpr float kMostSum = 1.15e18f;  // 2^60: of weights, before the maximum is looked for again
 
 // A request's row tiles and the key tiles of the longest and the shortest of them.
 struct Rows {
@@ -52,10 +52,11 @@ struct Job {
     Request q;
 };
 
-// The longest piece is chosen so that the work is over soonest: the longest request's tiles over 1 to 64 pieces, an estimate a lane.  With
-// pieces of c tiles there are n = sum of ceil(tiles / c), and they take ceil(n / places) rounds of c + kFixed, or, in any
-// order, no longer than an equal share and one piece.  Every wavefront by itself, 64 requests a trip.
-constexpr int kFixed = 4;  // key tiles that a piece's beginning and end take time for
+// The longest piece is chosen so that the work is over soonest.  Row tiles stay whole where an equal share of all of them is twice the longest
+// or the longest is short; else the longest's key tiles are divided by 1 to 64, an estimate a lane: with pieces of c tiles there are n =
+// sum of ceil(tiles / c), which have to find places at the same time, and take c and kFixed for a beginning and an end, and kJoin
+// for the sum of pieces.  Every wavefront by itself, 64 requests a trip.
+constexpr int kFixed = 4, kJoin = 5;  // in key tiles
 __device__ __forceinline__ Job find_job(const AttentionArgs& a, int least_rows, int places, int want, bool to_the_end) {
     const int lane = threadIdx.x & 63;
     Request mine;
@@ -66,47 +67,49 @@ __device__ __forceinline__ Job find_job(const AttentionArgs& a, int least_rows, 
     };
     Rows rows;
     int longest = 0;
+    float work = 0.0f;
     for (int r0 = 0; r0 < a.R; r0 += 64) {
         rows = rows_at(r0 + lane);
         int n = rows.longest;
+        float w = (float)rows.row_tiles * 0.5f * (float)(rows.longest + rows.shortest);
 #pragma unroll
         for (int s = 32; s > 0; s /= 2) {
             const int o = __shfl_xor(n, s);
             n = o > n ? o : n;
+            w += __shfl_xor(w, s);
         }
         longest = n > longest ? n : longest;
+        work += w * (float)a.kv_heads;
     }
     Job job;
     job.found = false;
     job.all_slots = 0;
+    longest = uniform(longest);
     if (longest == 0) return job;
-    const int c = (longest + lane) / (lane + 1);  // this lane's estimate
-    float pieces = 0.0f, cut = 0.0f, work = 0.0f;
-    for (int r0 = 0; r0 < a.R; r0 += 64) {
-        if (a.R > 64) rows = rows_at(r0 + lane);
-        for (unsigned long long some = __ballot(rows.row_tiles > 0); some != 0; some &= some - 1) {
-            const int at = __builtin_ctzll(some);
-            const float stretches = (float)__builtin_amdgcn_readlane(rows.row_tiles, at) * (float)a.kv_heads;
-            const int n = __builtin_amdgcn_readlane(rows.longest, at), k = (n + c - 1) / c;
-            pieces += stretches * (float)k;
-            cut += k > 1 ? stretches * (float)k : 0.0f;
-            work += stretches * 0.5f * (float)(n + __builtin_amdgcn_readlane(rows.shortest, at));
+    int each = longest;
+    if (longest > kFixed + kJoin && work < 2.0f * (float)longest * (float)places) {
+        const int c = (longest + lane) / (lane + 1);  // this lane's estimate
+        long long pieces = 0;
+        for (int r0 = 0; r0 < a.R; r0 += 64) {
+            if (a.R > 64) rows = rows_at(r0 + lane);
+            for (unsigned long long some = __ballot(rows.row_tiles > 0); some != 0; some &= some - 1) {
+                const int at = __builtin_ctzll(some);
+                pieces += (long long)(__builtin_amdgcn_readlane(rows.row_tiles, at) * a.kv_heads) *
+                          ((__builtin_amdgcn_readlane(rows.longest, at) + c - 1) / c);
+            }
         }
-    }
-    const float rounds = ceilf(pieces / (float)places) * (float)(c + kFixed);
-    const float any_order = (work + pieces * (float)kFixed) / (float)places + (float)c;
-    float best = cut > (float)kTileSlots ? INFINITY : fminf(rounds, any_order);
-    int each = c;
+        int best = lane == 0 ? (int)((pieces + places - 1) / places) * longest + kFixed : pieces <= places ? c + kFixed + kJoin : 0x7fffffff;
+        each = c;
 #pragma unroll
-    for (int s = 32; s > 0; s /= 2) {
-        const float o = __shfl_xor(best, s);
-        const int e = __shfl_xor(each, s);
-        if (o < best || (o == best && e > each)) {
-            best = o;
-            each = e;
+        for (int s = 32; s > 0; s /= 2) {
+            const int o = __shfl_xor(best, s), e = __shfl_xor(each, s);
+            if (o < best || (o == best && e > each)) {
+                best = o;
+                each = e;
+            }
         }
+        each = uniform(each);
     }
-    each = uniform(each);
 
     int jobs = 0, slots = 0;
     for (int r0 = 0; r0 < a.R; r0 += 64) {
@@ -153,8 +156,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_tile_kernel(Attentio
     struct Half {
         __attribute__((aligned(16))) char v[kTok * V_ROW];  // bf16
         __attribute__((aligned(16))) char k[kTok * K_ROW];
-        __attribute__((aligned(16))) uint8_t k_scale[kTok * SCALES], v_scale[kTok * SCALES];
-        __attribute__((aligned(16))) int odd[kWaves];  // of a wavefront's 16 tokens: 1, some block of values is NaN; 2, their page is nobody's
+        __attribute__((aligned(16))) uint8_t k_scale[kTok * SCALES];
+        // of a wavefront's 16 tokens: 1, some block of values is NaN; 2, their page is nobody's.  Which blocks: bit 4 t + quarter.  Eight copies,
+        // so that all lanes can write without a branch.
+        __attribute__((aligned(16))) int odd[8][kWaves];
+        unsigned long long nan[8][kWaves];
     };
     __shared__ Half halves[2];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
@@ -211,40 +217,32 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_tile_kernel(Attentio
         k_byte = p.scales[scale_at];
         v_byte = (p.scales + a.page.scales)[scale_at];
     };
-    // In LDS the 64-byte piece b of V's row t lies in place b ^ v_swizzle(t), so that the four rows of a transposed read fall on all banks;
-    // the 16-byte chunk c of K's row t in c ^ k_swizzle(t).
+    // In LDS the 64-byte piece b of V's row t lies in place b ^ v_swizzle(t), so that the four rows of a transposed read fall on all banks, and
+    // in odd rows the 16-byte pieces of a pair are swapped, so that the two rows that eight lanes write do; the 16-byte chunk c of K's
+    // row t lies in c ^ k_swizzle(t).
     auto v_swizzle = [](int t) { return D == 128 ? t & 3 : (t >> 1) & 1; };
     auto k_swizzle = [](int t) { return D == 128 ? (t >> 2) & 3 : 0; };
     const int v_to = in_tok * V_ROW + (((quarter * (D / 4) / 32) ^ v_swizzle(in_tok)) * 64) + (D == 128 ? 0 : (quarter & 1) * 32);
+    const int v_even = v_to + (in_tok & 1) * 16, v_odd = v_to + 16 - (in_tok & 1) * 16;
     const int k_to = in_tok * K_ROW + (((quarter * (D / 8) / 16) ^ k_swizzle(in_tok)) * 16) + (D == 128 ? 0 : (quarter & 1) * 8);
     auto write = [&](Half& h, const Place& p) {
         const bool there = p.owned & (p.t0 + in_tok < q.seq);
         uint32_t byte = there ? v_byte : 127u;  // never written: any number will do
         const unsigned long long nan = __ballot(byte == 255);
-        if (lane == 0) h.odd[wave] = (nan != 0 ? 1 : 0) | (p.owned ? 0 : 2);
-        if (D == 128 || (quarter & 1) == 0) {
-            h.k_scale[in_tok * SCALES + quarter * (D / 4) / 32] = (uint8_t)k_byte;
-            h.v_scale[in_tok * SCALES + quarter * (D / 4) / 32] = (uint8_t)byte;
-        }
+        h.nan[lane & 7][wave] = nan;
+        h.odd[lane & 7][wave] = (nan != 0 ? 1 : 0) | (p.owned ? 0 : 2);
+        h.k_scale[in_tok * SCALES + quarter * (D / 4) / 32] = (uint8_t)k_byte;
         *reinterpret_cast<Words*>(h.k + k_to) = k_in;
         const float scale = scale_of_byte(byte == 255 ? 127u : byte);
 #pragma unroll
-        for (int e = 0; e < D / 32; ++e) *reinterpret_cast<bf16x8*>(h.v + v_to + 16 * e) = from_codes(v_in[e], scale);
+        for (int e = 0; e < D / 32; ++e) *reinterpret_cast<bf16x8*>(h.v + (e % 2 == 0 ? v_even : v_odd) + 32 * (e / 2)) = from_codes(v_in[e], scale);
     };
-
-    floatx16 out[BLOCKS];
-#pragma unroll
-    for (int b = 0; b < BLOCKS; ++b)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) out[b][e] = 0.0f;
-    float most = kLowest, sum = 0.0f;
-    uint32_t bad = 0;  // blocks of this lane's query that a block of NaN values has reached
 
     Place ahead, after;
     if (i_begin < i_end) {
         const Place first = place(i_begin);
         load(first);
-        ahead = place(i_begin + 1 < i_end ? i_begin + 1 : i_begin);
+        ahead = place(i_begin + 1 < i_end ? i_begin + 1 : i_end - 1);
         write(halves[0], first);
         load(ahead);
         after = place(i_begin + 2 < i_end ? i_begin + 2 : i_end - 1);
@@ -256,19 +254,19 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_tile_kernel(Attentio
     intx8 q_hi[STEPS], q_lo[STEPS];
     int q_scale;
     {
-        float x[STEPS][32];
+        uint4 raw[STEPS][4];
         const bf16_t* at = static_cast<const bf16_t*>(a.q) + (int64_t)(q.first + token) * a.q_stride + (int64_t)head * D + group * 16;
         uint32_t top = 0;
 #pragma unroll
         for (int s = 0; s < STEPS; ++s)
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                bf16x8 v;
-                if (row < rows) v = *reinterpret_cast<const bf16x8*>(at + 64 * s + 32 * (c / 2) + 8 * (c % 2));
+                raw[s][c] = uint4{0, 0, 0, 0};
+                if (row < rows) raw[s][c] = *reinterpret_cast<const uint4*>(at + 64 * s + 32 * (c / 2) + 8 * (c % 2));
+                const uint32_t words[4] = {raw[s][c].x, raw[s][c].y, raw[s][c].z, raw[s][c].w};
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    x[s][8 * c + e] = row < rows ? (float)v[e] : 0.0f;
-                    const uint32_t m = __float_as_uint(x[s][8 * c + e]) & 0x7fffffffu;
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t lower = words[e] << 16 & 0x7fff0000u, upper = words[e] & 0x7fff0000u, m = lower > upper ? lower : upper;
                     top = m > top ? m : top;
                 }
             }
@@ -277,15 +275,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_tile_kernel(Attentio
         // the largest below 2^8 (e4m3 reaches 448), what is left below 2^4, times 16
         int e = (int)(top >> 23) - 127 - 7;
         e = e < -118 ? -118 : e;
-        const float down = __uint_as_float((uint32_t)(127 - e) << 23);
+        const float down = copysignf(__uint_as_float((uint32_t)(127 - e) << 23), a.scale_log2);
         q_scale = (e + 127) | ((e + 127 - 4) << 8);
 #pragma unroll
         for (int s = 0; s < STEPS; ++s)
 #pragma unroll
             for (int w = 0; w < 8; ++w) {
-                float y[4], rest[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) y[k] = x[s][4 * w + k] * down;
+                const uint32_t* words = reinterpret_cast<const uint32_t*>(&raw[s][w / 2]) + 2 * (w % 2);
+                const float y[4] = {__uint_as_float(words[0] << 16) * down, __uint_as_float(words[0] & 0xffff0000u) * down,
+                                    __uint_as_float(words[1] << 16) * down, __uint_as_float(words[1] & 0xffff0000u) * down};
+                float rest[4];
                 int hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
                 hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], hi, true);
                 rest[0] = (y[0] - __builtin_amdgcn_cvt_f32_fp8(hi, 0)) * 16.0f;
@@ -299,119 +298,162 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_tile_kernel(Attentio
             }
     }
 
+    floatx16 out[BLOCKS];
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) out[b][e] = 0.0f;
+    float most = kLowest, sum = 0.0f;  // the weights are 2^(scaled score - most)
+    uint32_t bad = 0;  // quarters of this lane's query that a block of NaN values has reached
+
     // fragment addresses: K's row is the lane's column index; V's rows 4 group + (lane % 16) / 4 of every eight, four columns each
     const int sub = (lane >> 4) & 1, v_row = 4 * group + ((lane & 15) >> 2);
     int k_from[STEPS], v_from[BLOCKS];
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) k_from[s] = col * K_ROW + (((2 * s + group) ^ k_swizzle(col)) * 16);
 #pragma unroll
-    for (int b = 0; b < BLOCKS; ++b) v_from[b] = v_row * V_ROW + ((b ^ v_swizzle(v_row)) * 64) + sub * 32 + (lane & 3) * 8;
+    for (int b = 0; b < BLOCKS; ++b) v_from[b] = v_row * V_ROW + ((b ^ v_swizzle(v_row)) * 64) + sub * 32 + ((((lane & 3) >> 1) ^ (v_row & 1)) * 16) + (lane & 1) * 8;
 
     auto barrier = [] {
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     };
     barrier();
 
-    for (int i = i_begin; i < i_end; ++i) {
-        const Half& h = halves[(i - i_begin) & 1];
-        const int t0 = seen.tile(i) * kTok;
-        if (i + 1 < i_end) {
-            write(halves[(i - i_begin + 1) & 1], ahead);
-            load(after);
-            ahead = after;
-            after = place(i + 3 < i_end ? i + 3 : i_end - 1);
+    // Scores are compared before they are scaled: the scale is positive, its sign went into q.  A scale of zero becomes next to nothing, so
+    // that it does not meet an infinity.
+    const float scale = fmaxf(fabsf(a.scale_log2), 1e-37f);
+    auto scores = [&](const Half& h, int tb) {
+        int byte;
+        if (D == 128) byte = (int)(*reinterpret_cast<const uint32_t*>(h.k_scale + (32 * tb + col) * SCALES) >> (8 * group));
+        else byte = h.k_scale[(32 * tb + col) * SCALES + group];
+        floatx16 z;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) z[e] = 0.0f;
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st) {
+            const int4 w = *reinterpret_cast<const int4*>(h.k + k_from[st] + 32 * tb * K_ROW);
+            const intx8 key = {w.x, w.y, w.z, w.w, 0, 0, 0, 0};
+            if (st == 0) {
+                z = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(key, q_lo[st], z, 4, 0, 0, byte, 1, q_scale);
+                z = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(key, q_hi[st], z, 4, 0, 0, byte, 0, q_scale);
+            } else {
+                z = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(key, q_lo[st], z, 4, 0, 2, byte, 1, q_scale);
+                z = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(key, q_hi[st], z, 4, 0, 2, byte, 0, q_scale);
+            }
         }
-        const bool some = w_any & (t0 <= w_last_p) & ((a.window == 0) | (t0 + kTok > w_first_p - a.window + 1) | (t0 < a.sinks));
-        if (some) {
-            floatx16 z[2];
+        return z;
+    };
+    // masks 32 tokens' scores, and notes blocks of NaN values among the tokens seen: V holds numbers there
+    auto look_closely = [&](floatx16& z, const Half& h, int4 odd4, int t0, int tb) {
+        const int odd[2] = {tb == 0 ? odd4.x : odd4.z, tb == 0 ? odd4.y : odd4.w};
+        // token 8 (e / 4) + 4 group + e % 4 of these 32, compared as 8 (e / 4) + e % 4: numbers that an instruction holds
+        const int base = t0 + 32 * tb + 4 * group, last = position - base, first_sink = a.sinks - base;
+        const int first = a.window > 0 && position >= a.window ? position - a.window + 1 - base : -base;
 #pragma unroll
-            for (int tb = 0; tb < 2; ++tb) {
-                int scale;
-                if (D == 128) scale = (int)(*reinterpret_cast<const uint32_t*>(h.k_scale + (32 * tb + col) * SCALES) >> (8 * group));
-                else scale = h.k_scale[(32 * tb + col) * SCALES + group];
-                floatx16 s;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[e] = 0.0f;
-#pragma unroll
-                for (int st = 0; st < STEPS; ++st) {
-                    const int4 w = *reinterpret_cast<const int4*>(h.k + k_from[st] + 32 * tb * K_ROW);
-                    const intx8 key = {w.x, w.y, w.z, w.w, 0, 0, 0, 0};
-                    if (st == 0) {
-                        s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(key, q_lo[st], s, 4, 0, 0, scale, 1, q_scale);
-                        s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(key, q_hi[st], s, 4, 0, 0, scale, 0, q_scale);
-                    } else {
-                        s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(key, q_lo[st], s, 4, 0, 2, scale, 1, q_scale);
-                        s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(key, q_hi[st], s, 4, 0, 2, scale, 0, q_scale);
-                    }
-                }
-                z[tb] = s * a.scale_log2;
-            }
-            const int4 odd4 = *reinterpret_cast<const int4*>(h.odd);
-            const int odd[4] = {odd4.x, odd4.y, odd4.z, odd4.w}, any_odd = uniform(odd4.x | odd4.y | odd4.z | odd4.w);
-            // every row of this wavefront sees every token of the tile
-            const bool whole = ((any_odd & 2) == 0) & (t0 + kTok - 1 <= w_first_p) &
-                               ((a.window == 0) | (t0 > w_last_p - a.window) | (t0 + kTok <= a.sinks));
-            if (!whole) {
-                const int from = a.window > 0 && position >= a.window ? position - a.window + 1 : 0;
-#pragma unroll
-                for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int j = t0 + 32 * tb + 8 * (e / 4) + 4 * group + e % 4;
-                        const bool sees = (j <= position) & ((j >= from) | (j < a.sinks)) & ((odd[2 * tb + e / 8] & 2) == 0);
-                        z[tb][e] = sees ? z[tb][e] : -INFINITY;
-                    }
-            }
-            if ((any_odd & 1) != 0) {
-                // V holds numbers where its blocks are NaN; what sees such a token becomes NaN at the end
-#pragma unroll
-                for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int t = 32 * tb + 8 * (e / 4) + 4 * group + e % 4;
-                        uint32_t w;
-                        if (D == 128) w = *reinterpret_cast<const uint32_t*>(h.v_scale + t * SCALES);
-                        else w = *reinterpret_cast<const uint16_t*>(h.v_scale + t * SCALES);
-                        const uint32_t all_ones = ((w & 0x7f7f7f7fu) + 0x01010101u) & w & 0x80808080u;  // bytes of 255
-                        const uint32_t blocks = (all_ones >> 7 & 1) | (all_ones >> 14 & 2) | (all_ones >> 21 & 4) | (all_ones >> 28 & 8);
-                        bad |= z[tb][e] != -INFINITY ? blocks : 0u;
-                    }
-            }
-            float top = z[0][0];
-#pragma unroll
-            for (int e = 1; e < 32; ++e) top = fmaxf(top, z[e / 16][e % 16]);
-            {
-                const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-                top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
-            }
-            if (__any(top > most + kLazy)) {  // the weights stay below 2^8: a maximum that rises by less is not worth a pass over the output
-                const float up = fmaxf(most, top), f = __builtin_amdgcn_exp2f(most - up);
-                most = up;
-                sum *= f;
-#pragma unroll
-                for (int b = 0; b < BLOCKS; ++b) out[b] *= f;
-            }
-            bf16x8 weight[4];
-#pragma unroll
-            for (int e = 0; e < 32; ++e) {
-                const float w = __builtin_amdgcn_exp2f(z[e / 16][e % 16] - most);
-                sum += w;
-                weight[e / 8][e % 8] = (__bf16)w;
-            }
-#pragma unroll
-            for (int b = 0; b < BLOCKS; ++b)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    union {
-                        shortx4 half[2];
-                        bf16x8 all;
-                    } f;
-                    f.half[0] = read_transposed(reinterpret_cast<const bf16_t*>(h.v + v_from[b] + (16 * k) * V_ROW));
-                    f.half[1] = read_transposed(reinterpret_cast<const bf16_t*>(h.v + v_from[b] + (16 * k + 8) * V_ROW));
-                    out[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.all, weight[k], out[b], 0, 0, 0);
-                }
+        for (int e = 0; e < 16; ++e) {
+            const int j = 8 * (e / 4) + e % 4;
+            const bool sees = (j <= last) & ((j >= first) | (j < first_sink)) & ((odd[e / 8] & 2) == 0);
+            z[e] = sees ? z[e] : -INFINITY;
         }
-        barrier();
+        if (((odd[0] | odd[1]) & 1) != 0) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const uint32_t* eights = reinterpret_cast<const uint32_t*>(&h.nan[0][2 * tb + e / 8]);
+                const uint32_t tokens = (uint32_t)uniform((int)eights[e / 4 % 2]) >> (16 * group);
+                bad |= z[e] != -INFINITY ? tokens >> (4 * (e % 4)) & 15u : 0u;
+            }
+        }
+    };
+    auto largest = [&](const floatx16& z) {
+        float top = z[0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) top = fmaxf(top, z[e]);
+        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+        return fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+    };
+    // The weights are taken against the largest score of the row's first tile, whatever comes later: they are floating-point numbers, and none
+    // loses a bit until their sum comes near the end of the range.  Only then is the maximum looked for.
+    auto weigh = [&](const floatx16* z, bf16x8* w) {
+        union {
+            bf16x2 two[16];
+            bf16x8 eight[4];
+        } u;
+#pragma unroll
+        for (int e = 0; e < 32; ++e) u.eight[e / 8][e % 8] = (__bf16)__builtin_amdgcn_exp2f(fmaf(z[e / 16][e % 16], scale, -most));
+        const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+        float added[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int e = 0; e < 16; ++e) added[e % 2] = __builtin_amdgcn_fdot2_f32_bf16(u.two[e], ones, added[e % 2], false);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = u.eight[k];
+        return added[0] + added[1];
+    };
+    // One tile.  `under` runs under the scores' products: no branch between it and them.
+    auto step = [&](const Half& here, int t0, bool closely, int4 odd, auto under) {
+        floatx16 z[2];
+        z[0] = scores(here, 0);
+        z[1] = scores(here, 1);
+        under();
+        if (closely) {
+            look_closely(z[0], here, odd, t0, 0);
+            look_closely(z[1], here, odd, t0, 1);
+        }
+        bf16x8 w[4];
+        float added = weigh(z, w);
+        if (__any(sum + added > kMostSum)) {
+            const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
+            const float so_far = most + __builtin_amdgcn_logf(fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])));
+            const float up = fmaxf(fmaxf(most, fmaxf(largest(z[0]), largest(z[1])) * scale), so_far), f = __builtin_amdgcn_exp2f(most - up);
+            most = up;
+            sum *= f;
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) out[b] *= f;
+            added = weigh(z, w);
+        }
+        sum += added;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) {
+                union {
+                    shortx4 half[2];
+                    bf16x8 all;
+                } f;
+                f.half[0] = read_transposed(reinterpret_cast<const bf16_t*>(here.v + v_from[b] + (16 * k) * V_ROW));
+                f.half[1] = read_transposed(reinterpret_cast<const bf16_t*>(here.v + v_from[b] + (16 * k + 8) * V_ROW));
+                out[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.all, w[k], out[b], 0, 0, 0);
+            }
+    };
+    int at = 0;
+    // the next tile into the half that held the one before: all have passed the barrier after it
+    auto stage = [&](int i, int next_at) {
+        write(halves[next_at], ahead);
+        load(after);
+        const int next_t0 = ahead.t0;
+        ahead = after;
+        after = place(i + 3 < i_end ? i + 3 : i_end - 1);
+        return next_t0;
+    };
+    if (w_any && i_begin < i_end) {
+        int t0 = seen.tile(i_begin) * kTok;
+        for (int i = i_begin; i < i_end; ++i) {
+            const int next_at = at ^ 1;
+            const Half& h = halves[at];
+            const int4 odd = *reinterpret_cast<const int4*>(h.odd[0]);
+            const bool closely = (uniform(odd.x | odd.y | odd.z | odd.w) != 0) | (t0 + kTok - 1 > w_first_p) |
+                                 ((a.window > 0) & (t0 <= w_last_p - a.window) & (t0 + kTok > a.sinks));
+            int next_t0;
+            step(h, t0, closely, odd, [&] { next_t0 = stage(i, next_at); });
+            barrier();
+            t0 = next_t0;
+            at = next_at;
+        }
+    } else {
+        for (int i = i_begin; i < i_end; ++i) {  // a wavefront without rows brings its part of the tiles
+            at ^= 1;
+            stage(i, at);
+            barrier();
+        }
     }
 
     if (row >= rows) return;
@@ -432,7 +474,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_tile_kernel(Attentio
             const int d = 32 * b + 8 * e + 4 * group;
             floatx4 v = {out[b][4 * e], out[b][4 * e + 1], out[b][4 * e + 2], out[b][4 * e + 3]};
             v *= by;
-            if (bad >> b & 1u) v = floatx4{NAN, NAN, NAN, NAN};
+            if (bad >> (D == 128 ? b : 2 * b) & (D == 128 ? 1u : 3u)) v = floatx4{NAN, NAN, NAN, NAN};
             if (cut) *reinterpret_cast<floatx4*>(piece_to + d) = v;
             else *reinterpret_cast<bf16x4*>(to + d) = __builtin_convertvector(v, bf16x4);
         }
@@ -455,10 +497,13 @@ hipError_t launch_attention_tile(const emoe_kv_desc& d, const AttentionArgs& a, 
     if (e != hipSuccess) return e;
     const long long per_request = ((long long)a.max_new * a.group + kRows - 1) / kRows, by_tokens = (long long)a.T * a.group / kRows + a.R;
     const long long row_tiles = per_request * a.R < by_tokens ? per_request * a.R : by_tokens;
-    const long long groups = row_tiles * a.kv_heads + kTileSlots;  // no more pieces than that
+    // whole row tiles, or pieces of them that find places at the same time
+    const int places = 2 * shape.groups;
+    static_assert(2 * kMaxGroups <= kTileSlots, "a slot for every piece");
+    const long long groups = row_tiles * a.kv_heads > places ? row_tiles * a.kv_heads : places;
     if (groups > 0x7fffffff / 256) return hipErrorInvalidValue;
-    if (d.head_dim == 64) attention_tile_kernel<64><<<(unsigned)groups, 64 * kWaves, 0, st>>>(a, least_rows, 2 * shape.cus, lay);
-    else attention_tile_kernel<128><<<(unsigned)groups, 64 * kWaves, 0, st>>>(a, least_rows, 2 * shape.cus, lay);
+    if (d.head_dim == 64) attention_tile_kernel<64><<<(unsigned)groups, 64 * kWaves, 0, st>>>(a, least_rows, places, lay);
+    else attention_tile_kernel<128><<<(unsigned)groups, 64 * kWaves, 0, st>>>(a, least_rows, places, lay);
     return hipGetLastError();
 }
 
