@@ -23,9 +23,21 @@ struct AttentionWs {
     size_t tile_count, tile_records, tile_sums, tile_outputs;  // tile_count: slots in use
     size_t total;
 };
-hipError_t launch_attention_few(const emoe_kv_desc& d, int dtype, const AttentionArgs& a, int most_rows, const AttentionWs& ws, int* slots,
+// Which requests the kernel for few queries takes, by their rows (query tokens times the heads of a kv head): up to `always`, and up to `small` if
+// the work of all that have more than `always` is small.  The kernel for many takes the others.
+struct FewRule {
+    int always, small;
+};
+hipError_t launch_attention_few(const emoe_kv_desc& d, int dtype, const AttentionArgs& a, FewRule rule, const AttentionWs& ws, int* slots,
                                 hipStream_t st);
-hipError_t launch_attention_tile(const emoe_kv_desc& d, const AttentionArgs& a, int least_rows, const AttentionWs& ws, hipStream_t st);
+hipError_t launch_attention_tile(const emoe_kv_desc& d, const AttentionArgs& a, FewRule rule, const AttentionWs& ws, hipStream_t st);
+
+// Rows of 16 times the tokens that they see, kFewStart more for a beginning and an end, up to which the kernel for few queries is faster whatever
+// the request's rows (us, few / many queries' kernel, 32 heads on 8: 128 rows on 2000 tokens 17 / 23, on 16000 35 / 36; 256 rows on 2000
+// 21 / 32, on 16000 52 / 40; four times 256 rows on 2000 32 / 46, on 16000 131 / 82): it starts sooner and cuts finer, but reads the
+// keys anew for every 16 rows.
+constexpr long long kFewWork = 1400000;
+constexpr int kFewStart = 256;
 
 namespace {
 
@@ -83,6 +95,25 @@ __device__ __forceinline__ Tiles tiles(const AttentionArgs& a, int seq, int firs
         if (t.sinks >= t.from) t.sinks = t.from = 0;  // one piece
     }
     return t;
+}
+
+// The most rows of a request that the kernel for few queries takes; every wavefront by itself, alike in both kernels.
+__device__ __forceinline__ int few_rows(const AttentionArgs& a, FewRule rule) {
+    if (rule.small <= rule.always) return rule.always;
+    const int lane = threadIdx.x & 63;
+    long long work = 0;
+    for (int r = lane; r < a.R; r += 64) {
+        const Request q = request(a, r);
+        const long long rows = (long long)q.n * a.group, reach = (long long)a.window + a.sinks + q.n;
+        const long long seen = a.window > 0 && reach < q.seq ? reach : q.seq;
+        if (rows > rule.always) work += (rows + 15) / 16 * a.kv_heads * (seen + kFewStart);
+    }
+#pragma unroll
+    for (int s = 32; s > 0; s /= 2) {
+        const int lo = __shfl_xor((int)work, s), hi = __shfl_xor((int)(work >> 32), s);
+        work += ((long long)hi << 32) | (uint32_t)lo;
+    }
+    return work <= kFewWork ? rule.small : rule.always;
 }
 
 __device__ __forceinline__ int wave_inclusive(int v) {

@@ -81,30 +81,47 @@ AttentionWs attention_ws(int dim, bool tiles) {
     return w;
 }
 
-// Requests of up to this many rows (query tokens times the heads of a kv head) go to the kernel for few queries.
-constexpr int kMostFewRows = 32;
+// Requests of up to this many rows go to the kernel for few queries always, of up to the other where there is little work.
+constexpr int kAlwaysFewRows = 32, kSmallFewRows = 512;
 
-// The tile kernel is for bf16: fp32 queries would take three times the matrix work and registers there, and are for verification.
-bool with_tiles(const emoe_attention_desc& a, int group) { return a.dtype == EMOE_BF16 && (long long)a.max_new * group > kMostFewRows; }
+// The tile kernel is for bf16: fp32 queries would take three times the matrix work and registers there, and are for verification.  Work that is
+// small at the table's full width is small.
+bool with_tiles(const emoe_kv_desc& d, const emoe_attention_desc& a) {
+    const long long rows = (long long)a.max_new * (a.q_heads / d.kv_heads);
+    if (a.dtype != EMOE_BF16 || rows <= kAlwaysFewRows) return false;
+    const long long row_tiles = ((long long)a.T * a.q_heads / d.kv_heads + 15) / 16 + d.rows;  // at most, of 16 rows
+    return rows > kSmallFewRows || row_tiles * d.kv_heads * ((long long)d.table_width * d.page_size + kFewStart) > kFewWork;
+}
 
 }  // namespace
 
 size_t attention_ws_bytes(const emoe_kv_desc& d, const emoe_attention_desc& a) {
-    return attention_ws(d.head_dim, with_tiles(a, a.q_heads / d.kv_heads)).total;
+    return attention_ws(d.head_dim, with_tiles(d, a)).total;
 }
 
 hipError_t launch_attention(const emoe_kv_desc& d, const emoe_attention_desc& at, const AttentionArgs& a, hipStream_t st) {
-    const bool tiles = with_tiles(at, a.group), few = !tiles || a.R > 1;
+    // Lengths are on the device: both kernels are launched unless the host knows that one will find nothing.
+    const bool tiles = with_tiles(d, at);
+    FewRule rule = {0x7fffffff, 0};
+    bool few = true;
+    if (tiles) {
+        const bool large = (long long)a.T * a.q_heads / 16 * kFewStart > 2 * kFewWork;  // if all the tokens are there
+        rule = {kAlwaysFewRows, large ? 0 : kSmallFewRows};
+        if (a.R == 1 && (large || a.max_new * (long long)a.group > kSmallFewRows)) {  // one request, which goes there whatever it brings
+            rule = {0, 0};
+            few = false;
+        }
+    }
     const AttentionWs ws = attention_ws(d.head_dim, tiles);
     static_assert((size_t)kFewSlots * (sizeof(Piece) + kFewRows * (8 + 128 * 4)) + (size_t)kTileSlots * (sizeof(Piece) + kTileRows * (8 + 128 * 4)) +
                           8 * 256 <= kAttentionWsBytes, "as include/emoe.h promises");
     int few_slots = 0;
-    if (tiles) {  // one request alone goes there whatever it brings: the lengths are on the device
-        hipError_t e = launch_attention_tile(d, a, few ? kMostFewRows + 1 : 0, ws, st);
+    if (tiles) {
+        hipError_t e = launch_attention_tile(d, a, rule, ws, st);
         if (e != hipSuccess) return e;
     }
     if (few) {
-        hipError_t e = launch_attention_few(d, at.dtype, a, tiles ? kMostFewRows : 0x7fffffff, ws, &few_slots, st);
+        hipError_t e = launch_attention_few(d, at.dtype, a, rule, ws, &few_slots, st);
         if (e != hipSuccess) return e;
     }
     const int slots = few_slots + (tiles ? kTileSlots : 0);

@@ -146,7 +146,7 @@ template <int D> struct Quarter { typedef uint32_t type __attribute__((ext_vecto
 template <> struct Quarter<64> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
 
 template <class E, int D>
-__global__ __launch_bounds__(64 * kWaves, (WavesPerSimd<E, D>::n)) void attention_few_kernel(AttentionArgs a, int most_rows, AttentionWs lay) {
+__global__ __launch_bounds__(64 * kWaves, (WavesPerSimd<E, D>::n)) void attention_few_kernel(AttentionArgs a, FewRule rule, AttentionWs lay) {
     constexpr int PIECES = Pieces<E>::n, STEPS = D / 32, BLOCKS = D / 16;
     constexpr int V_STRIDE = D + 16;  // elements; 32 bytes past the row: 16 rows of 32 bytes fall on all banks alike
     constexpr int V_BYTES = kTok * V_STRIDE * 2, WAVE_BYTES = V_BYTES + kTok * D / 2;  // V as bf16, K as it comes
@@ -156,6 +156,7 @@ __global__ __launch_bounds__(64 * kWaves, (WavesPerSimd<E, D>::n)) void attentio
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const int col = lane & 15, group = lane >> 4;
 
+    const int most_rows = uniform(few_rows(a, rule));
     Start start;
     const bool some = find_start(a, most_rows, &start);
     Piece* records = reinterpret_cast<Piece*>(a.ws + lay.few_records) + 2 * (size_t)blockIdx.x;
@@ -438,12 +439,13 @@ __global__ __launch_bounds__(64 * kWaves, (WavesPerSimd<E, D>::n)) void attentio
 }  // namespace
 
 // *slots: of the workspace that can hold a piece.
-hipError_t launch_attention_few(const emoe_kv_desc& d, int dtype, const AttentionArgs& a, int most_rows, const AttentionWs& ws, int* slots,
+hipError_t launch_attention_few(const emoe_kv_desc& d, int dtype, const AttentionArgs& a, FewRule rule, const AttentionWs& ws, int* slots,
                                 hipStream_t st) {
     DeviceShape shape;
     hipError_t e = device_shape(&shape);
     if (e != hipSuccess) return e;
     // As many workgroups as the chip holds at once, or as many as there can be shares for, by the tokens and the requests.
+    const int most_rows = rule.always > rule.small ? rule.always : rule.small;
     const long long rows = (long long)a.max_new * a.group < most_rows ? (long long)a.max_new * a.group : most_rows;
     const long long per_request = (rows + kRows - 1) / kRows, by_tokens = (long long)a.T * a.group / kRows + a.R;
     const long long row_tiles = per_request * a.R < by_tokens ? per_request * a.R : by_tokens;
@@ -452,7 +454,7 @@ hipError_t launch_attention_few(const emoe_kv_desc& d, int dtype, const Attentio
     const int groups = shares < kFewPerCu * shape.groups ? (int)shares : kFewPerCu * shape.groups;
     *slots = most_rounds > 2 * kSnap + 1 ? 2 * groups : 0;  // none if no stretch is long enough to be cut
     auto run = [&](auto element, auto dim) {
-        attention_few_kernel<decltype(element), decltype(dim)::value><<<(unsigned)groups, 64 * kWaves, 0, st>>>(a, most_rows, ws);
+        attention_few_kernel<decltype(element), decltype(dim)::value><<<(unsigned)groups, 64 * kWaves, 0, st>>>(a, rule, ws);
         return hipGetLastError();
     };
     if (dtype == EMOE_F32)

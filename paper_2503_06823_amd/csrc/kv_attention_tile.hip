@@ -149,7 +149,7 @@ template <int D> struct Quarter { typedef uint32_t type __attribute__((ext_vecto
 template <> struct Quarter<64> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
 
 template <int D>
-__global__ __launch_bounds__(64 * kWaves, 2) void attention_tile_kernel(AttentionArgs a, int least_rows, int places, AttentionWs lay) {
+__global__ __launch_bounds__(64 * kWaves, 2) void attention_tile_kernel(AttentionArgs a, FewRule rule, int places, AttentionWs lay) {
     constexpr int STEPS = D / 64, BLOCKS = D / 32, SCALES = D / 32;
     constexpr int V_ROW = 2 * D, K_ROW = D / 2;
     typedef typename Quarter<D>::type Words;
@@ -166,7 +166,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_tile_kernel(Attentio
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const int col = lane & 31, group = lane >> 5;
 
-    const Job job = find_job(a, least_rows, places, blockIdx.x, blockIdx.x == 0);
+    const Job job = find_job(a, uniform(few_rows(a, rule)) + 1, places, blockIdx.x, blockIdx.x == 0);
     if (blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<int*>(a.ws + lay.tile_count) = job.all_slots;
     if (!job.found) return;
     const int r = uniform(job.r), kv_head = uniform(job.kv_head), row_tile = uniform(job.row_tile), pieces = uniform(job.pieces);
@@ -491,7 +491,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_tile_kernel(Attentio
 
 }  // namespace
 
-hipError_t launch_attention_tile(const emoe_kv_desc& d, const AttentionArgs& a, int least_rows, const AttentionWs& lay, hipStream_t st) {
+hipError_t launch_attention_tile(const emoe_kv_desc& d, const AttentionArgs& a, FewRule rule, const AttentionWs& lay, hipStream_t st) {
     DeviceShape shape;
     hipError_t e = device_shape(&shape);
     if (e != hipSuccess) return e;
@@ -502,8 +502,8 @@ hipError_t launch_attention_tile(const emoe_kv_desc& d, const AttentionArgs& a, 
     static_assert(2 * kMaxGroups <= kTileSlots, "a slot for every piece");
     const long long groups = row_tiles * a.kv_heads > places ? row_tiles * a.kv_heads : places;
     if (groups > 0x7fffffff / 256) return hipErrorInvalidValue;
-    if (d.head_dim == 64) attention_tile_kernel<64><<<(unsigned)groups, 64 * kWaves, 0, st>>>(a, least_rows, places, lay);
-    else attention_tile_kernel<128><<<(unsigned)groups, 64 * kWaves, 0, st>>>(a, least_rows, places, lay);
+    if (d.head_dim == 64) attention_tile_kernel<64><<<(unsigned)groups, 64 * kWaves, 0, st>>>(a, rule, places, lay);
+    else attention_tile_kernel<128><<<(unsigned)groups, 64 * kWaves, 0, st>>>(a, rule, places, lay);
     return hipGetLastError();
 }
 
