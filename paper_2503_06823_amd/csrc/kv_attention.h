@@ -108,22 +108,8 @@ __device__ __forceinline__ int few_rows(const AttentionArgs& a, FewRule rule) {
         const long long seen = a.window > 0 && reach < q.seq ? reach : q.seq;
         if (rows > rule.always) work += (rows + 15) / 16 * a.kv_heads * (seen + kFewStart);
     }
-#pragma unroll
-    for (int s = 32; s > 0; s /= 2) {
-        const int lo = __shfl_xor((int)work, s), hi = __shfl_xor((int)(work >> 32), s);
-        work += ((long long)hi << 32) | (uint32_t)lo;
-    }
+    work = readlane(wave_inclusive(work), 63);
     return work <= kFewWork ? rule.small : rule.always;
-}
-
-__device__ __forceinline__ int wave_inclusive(int v) {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int s = 1; s < 64; s *= 2) {
-        const int o = __shfl_up(v, s);
-        if (lane >= s) v += o;
-    }
-    return v;
 }
 
 // x over the four lanes that hold one query (lane, lane ^ 16, ^ 32, ^ 48).

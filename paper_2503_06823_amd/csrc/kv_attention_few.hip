@@ -70,11 +70,6 @@ __device__ __forceinline__ Stretch stretch(const AttentionArgs& a, const Request
     return {(int)((rows + kRows - 1) / kRows), n > 0 ? n : 1};
 }
 
-__device__ __forceinline__ long long readlane(long long v, int lane) {
-    const int lo = __builtin_amdgcn_readlane((int)v, lane), hi = __builtin_amdgcn_readlane((int)(v >> 32), lane);
-    return ((long long)hi << 32) | (uint32_t)lo;
-}
-
 // total units in `groups` shares, the first `longer` of them one unit longer.
 struct Shares {
     long long total, each, longer;
@@ -104,17 +99,9 @@ __device__ __forceinline__ bool find_start(const AttentionArgs& a, int most_rows
         if (r < a.R) mine = request(a, r);
         return stretch(a, mine, most_rows).all(a.kv_heads);
     };
-    auto inclusive = [&](long long v) {
-#pragma unroll
-        for (int k = 1; k < 64; k *= 2) {
-            const int lo = __shfl_up((int)v, k), hi = __shfl_up((int)(v >> 32), k);
-            v += lane >= k ? (((long long)hi << 32) | (uint32_t)lo) : 0ll;
-        }
-        return v;
-    };
     long long upto = 0, total = 0;  // of a trip, of all
     for (int r0 = 0; r0 < a.R; r0 += 64) {
-        upto = inclusive(units_of(r0 + lane));
+        upto = wave_inclusive(units_of(r0 + lane));
         total += readlane(upto, 63);
     }
     const long long most = Shares::divide(total + kLeastUnits - 1, kLeastUnits);
@@ -126,7 +113,7 @@ __device__ __forceinline__ bool find_start(const AttentionArgs& a, int most_rows
     const long long begin = s->shares.begin(blockIdx.x);
     s->before = 0;
     for (int r0 = 0; r0 < a.R; r0 += 64) {
-        if (a.R > 64) upto = inclusive(units_of(r0 + lane));
+        if (a.R > 64) upto = wave_inclusive(units_of(r0 + lane));
         const long long sum = readlane(upto, 63);
         if (begin - s->before < sum) {
             const int at = __builtin_ctzll(__ballot(upto > begin - s->before));

@@ -116,7 +116,7 @@ __device__ __forceinline__ Job find_job(const AttentionArgs& a, int least_rows, 
         if (a.R > 64) rows = rows_at(r0 + lane);
         const int k = rows.row_tiles > 0 ? (rows.longest + each - 1) / each : 0;
         const int here = rows.row_tiles * a.kv_heads * k, cut_here = k > 1 ? here : 0;
-        const int upto = wave_inclusive(here), cut_upto = wave_inclusive(cut_here);
+        const int upto = (int)wave_inclusive((long long)here), cut_upto = (int)wave_inclusive((long long)cut_here);
         const int total = __builtin_amdgcn_readlane(upto, 63);
         if (!job.found && want - jobs < total) {
             const int at = __builtin_ctzll(__ballot(upto > want - jobs));

@@ -3,7 +3,7 @@
 // Four lanes hold a block of 32 elements, eight each: one 16-byte load of bf16, the largest magnitude by two steps over the
 // lanes (as integers: a NaN is larger than all numbers), a power of two as scale, and the converters of gfx950, whose rounding is to
 // nearest even.  With the scale a power of two x / s is exact, so the codes depend on the input alone.  Bound by HBM at
-// many tokens: 2 + 17/32 bytes per bf16 element in, the same out; by the launch at a decode step's.
+// many tokens: 2 bytes of bf16 in and 17/32 out per element, or the other way round; by the launch at a decode step's.
 #include "kv_cache.h"
 
 namespace emoe {
@@ -48,22 +48,8 @@ __device__ __forceinline__ RowAt row_at(int slot, int head, int kv_heads, KvPage
             base + 2 * page.codes + (values ? page.scales : 0) + (size_t)in_page * (dim / kKvBlock)};
 }
 
-// blockIdx.y: 0 the keys, 1 the values.  A thread: eight elements.
-template <class E>
-__global__ __launch_bounds__(kThreads) void kv_append_kernel(const E* __restrict__ k, int64_t k_stride, const E* __restrict__ v,
-                                                             int64_t v_stride, const int32_t* __restrict__ slots, uint8_t* __restrict__ cache,
-                                                             int T, int kv_heads, int dim, int n_slots, KvPage page) {
-    const bool values = blockIdx.y != 0;
-    const int per_row = kv_heads * dim / 8, per_head = dim / 8;
-    const long long n = (long long)T * per_row;
-    const long long i = (long long)blockIdx.x * kThreads + threadIdx.x;
-    if (i >= n) return;  // whole blocks of four lanes: per_row is a multiple of 8
-    const long long t = i / per_row;
-    const int e = (int)(i - t * per_row), head = e / per_head, piece = e % per_head;
-    const int slot = slots[t];
-    if ((unsigned)slot >= (unsigned)n_slots) return;
-    float x[8];
-    load8((values ? v + t * v_stride : k + t * k_stride) + (size_t)e * 8, x);
+// The four lanes of a block: their codes, and its scale byte.
+__device__ __forceinline__ uint32_t quantise(const float* x, uint32_t* scale_byte) {
     uint32_t top = 0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -83,9 +69,32 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(const E* __restrict
     codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[2], x[3], scale, 1);
     codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[4], x[5], scale, 2);
     codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[6], x[7], scale, 3);
-    const RowAt at = row_at(slot, head, kv_heads, page, values, dim);
-    *reinterpret_cast<uint32_t*>(cache + at.codes + piece * 4) = finite ? codes : 0u;
-    if ((piece & 3) == 0) cache[at.scales + piece / 4] = (uint8_t)byte;
+    *scale_byte = (uint32_t)byte;
+    return finite ? codes : 0u;
+}
+
+// A thread: eight elements of a token's keys and the same of its values.  Pieces are numbered through, per_row of them a token; 32 bits hold them.
+// Two or four tokens' pieces a thread were no faster.
+template <class E>
+__global__ __launch_bounds__(kThreads) void kv_append_kernel(const E* __restrict__ k, int64_t k_stride, const E* __restrict__ v,
+                                                             int64_t v_stride, const int32_t* __restrict__ slots, uint8_t* __restrict__ cache,
+                                                             uint32_t n, int kv_heads, int dim, int n_slots, KvPage page) {
+    const uint32_t per_row = (uint32_t)(kv_heads * dim / 8), per_head = (uint32_t)dim / 8, i = blockIdx.x * kThreads + threadIdx.x;
+    if (i >= n) return;  // alike in the four lanes of a block: per_row is a multiple of 8
+    const uint32_t t = i / per_row, e = i - t * per_row, head = e / per_head, piece = e % per_head;
+    const int slot = slots[t];
+    float x[2][8];
+    load8(k + (int64_t)t * k_stride + e * 8, x[0]);
+    load8(v + (int64_t)t * v_stride + e * 8, x[1]);
+    if ((unsigned)slot >= (unsigned)n_slots) return;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        uint32_t byte;
+        const uint32_t codes = quantise(x[w], &byte);
+        const RowAt at = row_at(slot, head, kv_heads, page, w == 1, dim);
+        *reinterpret_cast<uint32_t*>(cache + at.codes + piece * 4) = codes;
+        if ((piece & 3) == 0) cache[at.scales + piece / 4] = (uint8_t)byte;
+    }
 }
 
 __device__ __forceinline__ void store8(float* p, uint32_t codes, float scale) {
@@ -108,30 +117,29 @@ __device__ __forceinline__ void store8(bf16_t* p, uint32_t codes, float scale) {
 
 template <class E>
 __global__ __launch_bounds__(kThreads) void kv_read_kernel(const uint8_t* __restrict__ cache, const int32_t* __restrict__ slots,
-                                                           E* __restrict__ k, E* __restrict__ v, int T, int kv_heads, int dim, int n_slots,
+                                                           E* __restrict__ k, E* __restrict__ v, uint32_t n, int kv_heads, int dim, int n_slots,
                                                            KvPage page) {
-    const bool values = blockIdx.y != 0;
-    const int per_row = kv_heads * dim / 8, per_head = dim / 8;
-    const long long n = (long long)T * per_row;
-    const long long i = (long long)blockIdx.x * kThreads + threadIdx.x;
+    const uint32_t per_row = (uint32_t)(kv_heads * dim / 8), per_head = (uint32_t)dim / 8, i = blockIdx.x * kThreads + threadIdx.x;
     if (i >= n) return;
-    const long long t = i / per_row;
-    const int e = (int)(i - t * per_row), head = e / per_head, piece = e % per_head;
+    const uint32_t t = i / per_row, e = i - t * per_row, head = e / per_head, piece = e % per_head;
     const int slot = slots[t];
-    uint32_t codes = 0, byte = 127;
+    uint32_t codes[2] = {0, 0}, byte[2] = {127, 127};
     if ((unsigned)slot < (unsigned)n_slots) {
-        const RowAt at = row_at(slot, head, kv_heads, page, values, dim);
-        codes = *reinterpret_cast<const uint32_t*>(cache + at.codes + piece * 4);
-        byte = cache[at.scales + piece / 4];
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            const RowAt at = row_at(slot, head, kv_heads, page, w == 1, dim);
+            codes[w] = *reinterpret_cast<const uint32_t*>(cache + at.codes + piece * 4);
+            byte[w] = cache[at.scales + piece / 4];
+        }
     }
-    store8((values ? v : k) + i * 8, codes, scale_of_byte(byte));
+    store8(k + (size_t)i * 8, codes[0], scale_of_byte(byte[0]));
+    store8(v + (size_t)i * 8, codes[1], scale_of_byte(byte[1]));
 }
 
 template <class F>
 hipError_t over_rows(const emoe_kv_desc& d, int T, F launch) {
-    const long long n = (long long)T * (d.kv_heads * d.head_dim / 8), groups = (n + kThreads - 1) / kThreads;
-    if (groups > 0x7fffffff) return hipErrorInvalidValue;
-    launch(dim3((unsigned)groups, 2));
+    const long long n = (long long)T * (d.kv_heads * d.head_dim / 8);  // at most 2^30
+    launch((unsigned)((n + kThreads - 1) / kThreads), (uint32_t)n);
     return hipGetLastError();
 }
 
@@ -140,9 +148,9 @@ hipError_t over_rows(const emoe_kv_desc& d, int T, F launch) {
 hipError_t launch_kv_append(const emoe_kv_desc& d, int T, int dtype, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                             const int32_t* slot, void* cache, hipStream_t st) {
     auto run = [&](auto* kp, auto* vp) {
-        return over_rows(d, T, [&](dim3 grid) {
-            kv_append_kernel<<<grid, kThreads, 0, st>>>(kp, k_stride, vp, v_stride, slot, static_cast<uint8_t*>(cache), T, d.kv_heads, d.head_dim,
-                                                        d.pages * d.page_size, kv_page(d));
+        return over_rows(d, T, [&](unsigned groups, uint32_t n) {
+            kv_append_kernel<<<groups, kThreads, 0, st>>>(
+                kp, k_stride, vp, v_stride, slot, static_cast<uint8_t*>(cache), n, d.kv_heads, d.head_dim, d.pages * d.page_size, kv_page(d));
         });
     };
     if (dtype == EMOE_F32) return run(static_cast<const float*>(k), static_cast<const float*>(v));
@@ -152,9 +160,9 @@ hipError_t launch_kv_append(const emoe_kv_desc& d, int T, int dtype, const void*
 hipError_t launch_kv_read(const emoe_kv_desc& d, int T, int dtype, const void* cache, const int32_t* slot, void* k, void* v,
                           hipStream_t st) {
     auto run = [&](auto* kp, auto* vp) {
-        return over_rows(d, T, [&](dim3 grid) {
-            kv_read_kernel<<<grid, kThreads, 0, st>>>(static_cast<const uint8_t*>(cache), slot, kp, vp, T, d.kv_heads, d.head_dim,
-                                                      d.pages * d.page_size, kv_page(d));
+        return over_rows(d, T, [&](unsigned groups, uint32_t n) {
+            kv_read_kernel<<<groups, kThreads, 0, st>>>(
+                static_cast<const uint8_t*>(cache), slot, kp, vp, n, d.kv_heads, d.head_dim, d.pages * d.page_size, kv_page(d));
         });
     };
     if (dtype == EMOE_F32) return run(static_cast<float*>(k), static_cast<float*>(v));

@@ -14,31 +14,24 @@ namespace {
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kReleaseRows = kWaves;
 
-__device__ __forceinline__ long long shfl_up(long long v, int by) {
-    const int lo = __shfl_up((int)v, by), hi = __shfl_up((int)(v >> 32), by);
-    return ((long long)hi << 32) | (uint32_t)lo;
-}
-
-// Inclusive prefix sum over the workgroup, and the sum of all.
-__device__ long long block_scan(long long v, long long* totals, long long* sum) {
+// Inclusive prefix sums over the workgroup of N values a thread, and the sums of all.
+template <int N>
+__device__ __forceinline__ void block_scan(long long (&v)[N], long long (*totals)[kWaves], long long (&sums)[N]) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
-    for (int s = 1; s < 64; s *= 2) {
-        const long long o = shfl_up(v, s);
-        if (lane >= s) v += o;
-    }
+    for (int n = 0; n < N; ++n) v[n] = wave_inclusive(v[n]);
     __syncthreads();  // the totals of an earlier scan are read
-    if (lane == 63) totals[wave] = v;
-    __syncthreads();
-    long long before = 0, all = 0;
-#pragma unroll 4
-    for (int w = 0; w < kWaves; ++w) {
-        const long long t = totals[w];
-        all += t;
-        before += w < wave ? t : 0;
+    if (lane == 63) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) totals[n][wave] = v[n];
     }
-    *sum = all;
-    return before + v;
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < N; ++n) {  // 16 wavefronts' totals in 16 lanes
+        const long long all = wave_inclusive(lane < kWaves ? totals[n][lane < kWaves ? lane : 0] : 0ll);
+        sums[n] = readlane(all, kWaves - 1);
+        v[n] += wave > 0 ? readlane(all, wave > 0 ? wave - 1 : 0) : 0ll;
+    }
 }
 
 __device__ __forceinline__ int ring_index(int start, long long by, int pages) {
@@ -54,10 +47,10 @@ __global__ __launch_bounds__(kThreads) void kv_plan_kernel(int R, int T, int pag
                                                            int32_t* __restrict__ slot, int32_t* __restrict__ position,
                                                            int32_t* __restrict__ seq_len, int64_t* __restrict__ counters_out,
                                                            int32_t* __restrict__ refused) {
-    __shared__ long long totals[kWaves];
+    __shared__ long long totals[2][kWaves];
     __shared__ int row_at[kThreads], pos0_at[kThreads], have_at[kThreads], base_at[kThreads];  // of the row that begins at this token
     __shared__ int last_of_wave[kWaves], refusals;
-    const int i = threadIdx.x, lane = i & 63, wave = i >> 6;
+    const int i = threadIdx.x, lane = i & 63, wave = __builtin_amdgcn_readfirstlane(i >> 6);
     const int s0 = blockIdx.x * kThreads;
     const long long s1 = (long long)s0 + kThreads;
     const bool rows_too = blockIdx.x == 0;  // this workgroup writes what there is one of per row
@@ -65,26 +58,38 @@ __global__ __launch_bounds__(kThreads) void kv_plan_kernel(int R, int T, int pag
     if (i == 0) refusals = 0;
     const long long head = counters[0], tail = counters[1];
     const long long free_now = tail - head < 0 ? 0 : tail - head > pages ? pages : tail - head;
-    const int start = (int)((unsigned long long)head % (unsigned)pages);
     const long long P = 1ll << log2_page;
 
     long long tokens = 0, wanted = 0, taken = 0;  // of the rows of the trips before
     for (int r0 = 0; r0 < R && (rows_too || tokens < s1); r0 += kThreads) {
         const int r = r0 + i;
         const bool there = r < R;
-        const long long l = there && len[r] > 0 ? len[r] : 0, n = there && new_len[r] > 0 ? new_len[r] : 0;
-        long long sum;
-        const long long cu_end = tokens + block_scan(n, totals, &sum), cu = cu_end - n;
-        tokens += sum;
+        const int l_in = there ? len[r] : 0, n_in = there ? new_len[r] : 0;
+        const long long l = l_in > 0 ? l_in : 0, n = n_in > 0 ? n_in : 0;
         const long long have = (l + P - 1) >> log2_page, want = (l + n + P - 1) >> log2_page;
-        const bool fits = want <= width && cu_end <= T;
-        const long long need = there && fits ? want - have : 0;
-        const long long upto = wanted + block_scan(need, totals, &sum), base = upto - need;
-        wanted += sum;
-        const bool ok = fits && (need == 0 || upto <= free_now);
+        bool fits = want <= width;
+        // tokens and pages in one go, as if all tokens found a place: a second scan only where some do not
+        long long upto[2] = {n, fits ? want - have : 0}, sum[2];
+        block_scan<2>(upto, totals, sum);
+        const long long cu_end = tokens + upto[0], cu = cu_end - n;
+        if (tokens + sum[0] > T) {
+            fits &= cu_end <= T;
+            long long again[1] = {fits ? want - have : 0}, again_sum[1];
+            block_scan<1>(again, totals, again_sum);
+            upto[1] = again[0];
+            sum[1] = again_sum[0];
+        }
+        tokens += sum[0];
+        const long long need = fits ? want - have : 0, all_upto = wanted + upto[1], base = all_upto - need;
+        wanted += sum[1];
+        const bool ok = fits && (need == 0 || all_upto <= free_now);
         if (rows_too) {
-            block_scan(ok ? need : 0, totals, &sum);
-            taken += sum;
+            if (wanted <= free_now) taken = wanted;
+            else {
+                long long got[1] = {ok ? need : 0}, got_sum[1];
+                block_scan<1>(got, totals, got_sum);
+                taken += got_sum[0];
+            }
             if (there) {
                 constexpr long long most = 0x7fffffff;
                 if (r == 0) cu_new[0] = 0;
@@ -125,6 +130,7 @@ __global__ __launch_bounds__(kThreads) void kv_plan_kernel(int R, int T, int pag
         return;
     }
     const int row = row_at[from], have = have_at[from], pos = pos0_at[from] + (int)t;
+    const int start = (int)((unsigned long long)head % (unsigned)pages);
     position[t] = pos;
     if (have < 0) {
         slot[t] = -1;
@@ -165,10 +171,10 @@ __global__ __launch_bounds__(kThreads) void kv_release_kernel(int R, int pages, 
                                                               const int32_t* __restrict__ ended, const int32_t* __restrict__ table,
                                                               int32_t* __restrict__ free_pages, const int64_t* __restrict__ counters,
                                                               int64_t* __restrict__ counters_out) {
-    __shared__ long long totals[kWaves];
+    __shared__ long long totals[1][kWaves];
     __shared__ long long base_of[kReleaseRows];
     __shared__ Leaving rows[kReleaseRows];
-    const int i = threadIdx.x, lane = i & 63, wave = i >> 6;
+    const int i = threadIdx.x, lane = i & 63, wave = __builtin_amdgcn_readfirstlane(i >> 6);
     const int own = blockIdx.x * kReleaseRows;
     const bool last = blockIdx.x == gridDim.x - 1;
     const long long tail = counters[1];
@@ -181,13 +187,13 @@ __global__ __launch_bounds__(kThreads) void kv_release_kernel(int R, int pages, 
             if (l.to > width) l.to = width;  // a length that the table cannot hold
             if (l.first > width) l.first = width;
         }
-        long long sum;
-        const long long n = l.count(), upto = before + block_scan(n, totals, &sum);
-        before += sum;
+        long long upto[1] = {l.count()}, sum[1];
+        block_scan<1>(upto, totals, sum);
         if (r >= own && r < own + kReleaseRows) {
             rows[r - own] = l;
-            base_of[r - own] = upto - n;
+            base_of[r - own] = before + upto[0] - l.count();
         }
+        before += sum[0];
     }
     __syncthreads();
     if (last && i == 0) {
