@@ -9,13 +9,15 @@ namespace {
 // side, else every team has a row of its own.
 constexpr int kJoinThreads = 256;
 constexpr int kOneTeam = 8;  // pieces that a team adds alone
+constexpr int kTileJoiners = 2;  // workgroups of a piece of the kernel for many, which has eight times the rows
 template <class E, int D>
 __global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(AttentionArgs a, AttentionWs lay, int few_slots) {
     constexpr int LANES = D / 4, TEAMS = kJoinThreads / LANES;
     __shared__ floatx4 part[TEAMS][LANES];
     __shared__ float2 part_sums[TEAMS];
     const bool few = (int)blockIdx.x < few_slots;
-    const int slot = few ? blockIdx.x : blockIdx.x - few_slots, rows = few ? kFewRows : kTileRows;
+    const int of_tiles = (int)blockIdx.x - few_slots, rows = few ? kFewRows : kTileRows;
+    const int slot = few ? blockIdx.x : of_tiles / kTileJoiners, joiner = few ? 0 : of_tiles % kTileJoiners, joiners = few ? 1 : kTileJoiners;
     if (!few && slot >= *reinterpret_cast<const int*>(a.ws + lay.tile_count)) return;
     const Piece p = reinterpret_cast<const Piece*>(a.ws + (few ? lay.few_records : lay.tile_records))[slot];
     if (p.count == 0) return;
@@ -25,7 +27,7 @@ __global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(AttentionA
     const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES;
     const int shares = p.count > kOneTeam ? TEAMS : 1;  // teams of a row
     const int share = team % shares, side = team / shares, step = p.count * (TEAMS / shares);
-    for (int row0 = p.piece; row0 < p.rows; row0 += step) {
+    for (int row0 = p.piece + joiner * step; row0 < p.rows; row0 += step * joiners) {
         const int row = row0 + side * p.count;
         floatx4 v = {0.0f, 0.0f, 0.0f, 0.0f};
         float top = kLowest, all = 0.0f;
@@ -124,10 +126,10 @@ hipError_t launch_attention(const emoe_kv_desc& d, const emoe_attention_desc& at
         hipError_t e = launch_attention_few(d, at.dtype, a, rule, ws, &few_slots, st);
         if (e != hipSuccess) return e;
     }
-    const int slots = few_slots + (tiles ? kTileSlots : 0);
-    if (slots == 0) return hipSuccess;
+    const int groups = few_slots + (tiles ? kTileSlots * kTileJoiners : 0);
+    if (groups == 0) return hipSuccess;
     auto join = [&](auto element, auto dim) {
-        attention_join_kernel<decltype(element), decltype(dim)::value><<<(unsigned)slots, kJoinThreads, 0, st>>>(a, ws, few_slots);
+        attention_join_kernel<decltype(element), decltype(dim)::value><<<(unsigned)groups, kJoinThreads, 0, st>>>(a, ws, few_slots);
         return hipGetLastError();
     };
     if (at.dtype == EMOE_F32)
