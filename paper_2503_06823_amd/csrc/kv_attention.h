@@ -46,6 +46,7 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef int intx8 __attribute__((ext_vector_type(8)));
 
 constexpr float kLowest = -3.0e38f;  // of a running maximum: finite, so that nothing minus it is a NaN
 
@@ -114,11 +115,17 @@ __device__ __forceinline__ int few_rows(const AttentionArgs& a, FewRule rule) {
 
 // x over the four lanes that hold one query (lane, lane ^ 16, ^ 32, ^ 48).
 template <class F>
+__device__ __forceinline__ uint32_t over_groups(uint32_t x, F f) {
+    const auto a = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    x = f(a[0], a[1]);
+    const auto b = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    return f(b[0], b[1]);
+}
+template <class F>
 __device__ __forceinline__ float over_groups(float x, F f) {
-    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = f(__uint_as_float(a[0]), __uint_as_float(a[1]));
-    const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
+    return __uint_as_float(over_groups(__float_as_uint(x), [&](uint32_t x, uint32_t y) {
+        return __float_as_uint(f(__uint_as_float(x), __uint_as_float(y)));
+    }));
 }
 
 // Eight elements of 4 bits as bf16: exact, a code has two significant bits.
@@ -147,6 +154,43 @@ __device__ __forceinline__ void to_operands(const float* x, bf16x8* out) {
             out[p][i] = (__bf16)rest[i];
             if (p + 1 < PIECES) rest[i] -= (float)out[p][i];
         }
+}
+
+// bf16 queries as two e4m3 operands of the scaled matrix instructions: the nearest, and 16 times what it leaves.  A bf16 number has eight
+// significant bits, four for each, so that their sum is the number up to 2^-21 of the largest of its row.
+// The bits of the largest magnitude of eight numbers, and of `top`:
+__device__ __forceinline__ uint32_t largest_bits(const uint4& eight, uint32_t top) {
+    const uint32_t words[4] = {eight.x, eight.y, eight.z, eight.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t lower = words[e] << 16 & 0x7fff0000u, upper = words[e] & 0x7fff0000u, m = lower > upper ? lower : upper;
+        top = m > top ? m : top;
+    }
+    return top;
+}
+// A row's scale from its largest: that comes below 2^8 (e4m3 reaches 448), what is left of it below 2^4.  `byte`: the scales of the two operands
+// as the instruction takes them; `down`: what a number is multiplied with, with the sign of the scores' scale.
+struct QueryScale {
+    float down;
+    int nearest, rest;
+};
+__device__ __forceinline__ QueryScale query_scale(uint32_t top, float scale) {
+    int e = (int)(top >> 23) - 127 - 7;
+    e = e < -118 ? -118 : e;
+    return {copysignf(__uint_as_float((uint32_t)(127 - e) << 23), scale), e + 127, e + 127 - 4};
+}
+// Four numbers, two a word.
+__device__ __forceinline__ void to_e4m3(uint32_t w0, uint32_t w1, float down, int* nearest, int* rest) {
+    const float y[4] = {__uint_as_float(w0 << 16) * down, __uint_as_float(w0 & 0xffff0000u) * down, __uint_as_float(w1 << 16) * down,
+                        __uint_as_float(w1 & 0xffff0000u) * down};
+    int hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+    hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], hi, true);
+    const float left[4] = {(y[0] - __builtin_amdgcn_cvt_f32_fp8(hi, 0)) * 16.0f, (y[1] - __builtin_amdgcn_cvt_f32_fp8(hi, 1)) * 16.0f,
+                           (y[2] - __builtin_amdgcn_cvt_f32_fp8(hi, 2)) * 16.0f, (y[3] - __builtin_amdgcn_cvt_f32_fp8(hi, 3)) * 16.0f};
+    int lo = __builtin_amdgcn_cvt_pk_fp8_f32(left[0], left[1], 0, false);
+    lo = __builtin_amdgcn_cvt_pk_fp8_f32(left[2], left[3], lo, true);
+    *nearest = hi;
+    *rest = lo;
 }
 
 // Four rows (tokens) of one column (element) from row-major bf16 in LDS: of the 16 lanes of a group, lane j names the eight

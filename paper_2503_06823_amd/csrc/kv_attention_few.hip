@@ -45,15 +45,6 @@ template <class E, int D> struct WavesPerSimd { static constexpr int n = 3; };
 template <> struct WavesPerSimd<float, 128> { static constexpr int n = 2; };
 template <> struct WavesPerSimd<float, 64> { static constexpr int n = 3; };
 
-__device__ __forceinline__ void load8(const float* p, float* x) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = p[i];
-}
-__device__ __forceinline__ void load8(const bf16_t* p, float* x) {
-    const bf16x8 v = *reinterpret_cast<const bf16x8*>(p);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = (float)v[i];
-}
 // The work as one line of units: requests in order, of a request its kv heads, of a head its tiles of 16 rows, of those (a stretch) kFixed
 // units for its beginning and end and then the rounds of kWaves key tiles that the longest row sees, at least one.  Every workgroup takes an
 // equal part of the line, so that all of them end together whatever the lengths; a boundary within kSnap rounds of a stretch's beginning or
@@ -135,6 +126,7 @@ template <> struct Quarter<64> { typedef uint32_t type __attribute__((ext_vector
 template <class E, int D>
 __global__ __launch_bounds__(64 * kWaves, (WavesPerSimd<E, D>::n)) void attention_few_kernel(AttentionArgs a, FewRule rule, AttentionWs lay) {
     constexpr int PIECES = Pieces<E>::n, STEPS = D / 32, BLOCKS = D / 16;
+    constexpr bool SCALED = sizeof(E) == 2;  // K stays in 4 bits
     constexpr int V_STRIDE = D + 16;  // elements; 32 bytes past the row: 16 rows of 32 bytes fall on all banks alike
     constexpr int V_BYTES = kTok * V_STRIDE * 2, WAVE_BYTES = V_BYTES + kTok * D / 2;  // V as bf16, K as it comes
     static_assert(WAVE_BYTES % 16 == 0 && BLOCKS * 1024 <= WAVE_BYTES, "the outputs take V's place at the end");
@@ -191,10 +183,14 @@ __global__ __launch_bounds__(64 * kWaves, (WavesPerSimd<E, D>::n)) void attentio
         // L1 cache per lane).  Keys go through LDS, where quarter q of token t lies in place q ^ swizzle(t), to lane (token, quarter).
         const int in_tok = lane >> 2, quarter = lane & 3;
         const uint32_t in_at = in_tok * (D / 2) + quarter * (D / 8), v_scale_at = in_tok * (D / 32) + quarter * (D / 4) / 32;
-        const uint32_t k_scale_at = col * (D / 32) + group * (D / 4) / 32;
-        auto swizzle = [](int t) { return (t >> (D == 128 ? 2 : 3)) & 3; };
-        char* k_to = k_lds + in_tok * (D / 2) + (quarter ^ swizzle(in_tok)) * (D / 8);
-        const char* k_from = k_lds + col * (D / 2) + (group ^ swizzle(col)) * (D / 8);
+        // In fp32 lane (token, group) takes quarter `group` of the token's keys; in bf16 the 32 elements of block `group`, for D = 64 of
+        // block group % 2.
+        constexpr int K_WORDS = SCALED ? 4 : D / 32, K_PARTS = D / 8 / K_WORDS;
+        const int k_part = group % K_PARTS;
+        const uint32_t k_scale_at = col * (D / 32) + k_part * K_WORDS * 8 / 32;
+        auto swizzle = [](int t) { return (t >> (D == 128 ? 2 : 3)) & (K_PARTS - 1); };
+        char* k_to = k_lds + in_tok * (D / 2) + ((quarter * K_PARTS / 4) ^ swizzle(in_tok)) * (4 * K_WORDS) + quarter % (4 / K_PARTS) * (D / 8);
+        const char* k_from = k_lds + col * (D / 2) + (k_part ^ swizzle(col)) * (4 * K_WORDS);
         bf16_t* v_to = v_lds + in_tok * V_STRIDE + quarter * (D / 4);
         const bf16_t* v_from = v_lds + (4 * group + (col >> 2)) * V_STRIDE + 4 * (col & 3);
 
@@ -255,15 +251,46 @@ __global__ __launch_bounds__(64 * kWaves, (WavesPerSimd<E, D>::n)) void attentio
         const int row = row0 + col, token = row / a.group, head = kv_head * a.group + row % a.group;
         const int position = row < rows ? q.len - q.n + token : -1;  // -1 sees nothing
 
-        bf16x8 query[PIECES][STEPS];
-        {
+        // Scores are compared before they are scaled: the scale is positive, its sign goes into q.  A scale of zero becomes next to nothing, so
+        // that it does not meet an infinity.
+        const float scale = fmaxf(fabsf(a.scale_log2), 1e-37f);
+        bf16x8 query[SCALED ? 1 : PIECES][SCALED ? 1 : STEPS];
+        intx8 q_hi, q_lo;  // for D = 64 both are in q_hi
+        int q_scale;
+        const E* q_at = static_cast<const E*>(a.q) + (int64_t)(q.first + token) * a.q_stride + (int64_t)head * D;
+        if constexpr (SCALED) {
+            // a lane's bytes 0 .. 15 are elements 16 group on of the 128 of a product, 16 .. 31 those 64 further on; its scale is of elements 32 group on
+            constexpr int LOADS = D / 32;
+            uint4 raw[LOADS];
+            uint32_t top = 0;
+#pragma unroll
+            for (int c = 0; c < LOADS; ++c) {
+                raw[c] = uint4{0, 0, 0, 0};
+                if (row < rows) raw[c] = *reinterpret_cast<const uint4*>(q_at + 16 * group + 64 * (c / 2) + 8 * (c % 2));
+                top = largest_bits(raw[c], top);
+            }
+            top = over_groups(top, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
+            const QueryScale by = query_scale(top, a.scale_log2);
+            q_scale = D == 128 ? by.nearest | by.rest << 8 : group < 2 ? by.nearest : by.rest;
+#pragma unroll
+            for (int w = 0; w < 2 * LOADS; ++w) {
+                const uint32_t words[4] = {raw[w / 2].x, raw[w / 2].y, raw[w / 2].z, raw[w / 2].w};
+                int nearest, rest;
+                to_e4m3(words[2 * (w % 2)], words[2 * (w % 2) + 1], by.down, &nearest, &rest);
+                q_hi[w] = nearest;
+                if (D == 128) q_lo[w] = rest;
+                else q_hi[4 + w] = rest;
+            }
+        } else {
             float x[8];
-            const E* at = static_cast<const E*>(a.q) + (int64_t)(q.first + token) * a.q_stride + (int64_t)head * D + group * (D / 4);
 #pragma unroll
             for (int s = 0; s < STEPS; ++s) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[i] = 0.0f;
-                if (row < rows) load8(at + s * 8, x);
+                if (row < rows) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i] = q_at[group * (D / 4) + s * 8 + i] * (a.scale_log2 < 0.0f ? -1.0f : 1.0f);
+                }
                 bf16x8 o[PIECES];
                 to_operands<PIECES>(x, o);
 #pragma unroll
@@ -292,20 +319,28 @@ __global__ __launch_bounds__(64 * kWaves, (WavesPerSimd<E, D>::n)) void attentio
             load_values(next);
             *reinterpret_cast<Words*>(k_to) = k0;
             *reinterpret_cast<Words*>(k_to + 16 * D / 2) = k1;
-            const float scale0 = scale_of_byte(k_scale0), scale1 = scale_of_byte(k_scale1);
+            const uint32_t byte0 = k_scale0, byte1 = k_scale1;
             load_keys(next);
-            auto scores = [&](const char* from, float scale) {
-                const Words words = *reinterpret_cast<const Words*>(from);
+            auto scores = [&](const char* from, uint32_t byte) {
                 floatx4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+                if constexpr (SCALED) {
+                    const int4 w = *reinterpret_cast<const int4*>(from);
+                    const intx8 key = {w.x, w.y, w.z, w.w, 0, 0, 0, 0};
+                    if constexpr (D == 128) s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(key, q_lo, s, 4, 0, 0, (int)byte, 1, q_scale);
+                    s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(key, q_hi, s, 4, 0, 0, (int)byte, 0, q_scale);
+                } else {
+                    const Words words = *reinterpret_cast<const Words*>(from);
+                    const float by = scale_of_byte(byte);
 #pragma unroll
-                for (int st = 0; st < STEPS; ++st) {
-                    const bf16x8 key = from_codes(words[st], scale);
+                    for (int st = 0; st < STEPS; ++st) {
+                        const bf16x8 key = from_codes(words[st], by);
 #pragma unroll
-                    for (int p = PIECES - 1; p >= 0; --p) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, query[p][st], s, 0, 0, 0);
+                        for (int p = PIECES - 1; p >= 0; --p) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, query[p][st], s, 0, 0, 0);
+                    }
                 }
-                return s * a.scale_log2;
+                return s;
             };
-            const floatx4 z0 = scores(k_from, scale0), z1 = scores(k_from + 16 * D / 2, scale1);
+            const floatx4 z0 = scores(k_from, byte0), z1 = scores(k_from + 16 * D / 2, byte1);
             float z[8] = {z0[0], z0[1], z0[2], z0[3], z1[0], z1[1], z1[2], z1[3]};
             if (!whole) {
                 const int from = a.window > 0 && position >= a.window ? position - a.window + 1 : 0;
@@ -325,7 +360,7 @@ __global__ __launch_bounds__(64 * kWaves, (WavesPerSimd<E, D>::n)) void attentio
             float top = z[0];
 #pragma unroll
             for (int e = 1; e < 8; ++e) top = fmaxf(top, z[e]);
-            top = over_groups(top, [](float x, float y) { return fmaxf(x, y); });
+            top = over_groups(top, [](float x, float y) { return fmaxf(x, y); }) * scale;
             if (__any(top > most + kLazy)) {  // the weights stay below 2^8: a maximum that rises by less is not worth a pass over the output
                 const float up = fmaxf(most, top), f = __builtin_amdgcn_exp2f(most - up);
                 most = up;
@@ -335,12 +370,22 @@ __global__ __launch_bounds__(64 * kWaves, (WavesPerSimd<E, D>::n)) void attentio
             }
             float w[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                w[e] = __builtin_amdgcn_exp2f(z[e] - most);
-                sum += w[e];
-            }
+            for (int e = 0; e < 8; ++e) w[e] = __builtin_amdgcn_exp2f(fmaf(z[e], scale, -most));
             bf16x8 weight[PIECES];
             to_operands<PIECES>(w, weight);
+            if constexpr (PIECES == 1) {  // as they are multiplied with: what rounding does to all alike is divided out
+                union {
+                    bf16x8 all;
+                    bf16x2 two[4];
+                } u;
+                u.all = weight[0];
+                const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum = __builtin_amdgcn_fdot2_f32_bf16(u.two[e], ones, sum, false);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum += w[e];
+            }
 #pragma unroll
             for (int b = 0; b < BLOCKS; ++b) {
                 union {

@@ -25,12 +25,11 @@ namespace emoe {
 namespace {
 
 typedef float floatx16 __attribute__((ext_vector_type(16)));
-typedef int intx8 __attribute__((ext_vector_type(8)));
 
 constexpr int kTok = 64;    // tokens of a tile
 constexpr int kRows = kTileRows;
 constexpr int kWaves = 4;
-constexpr float kMostSum = 1.15e18f;  // 2^60: of weights, before the maximum is looked for again
+constexpr float kMostSum = 4294967296.0f;  // of weights, before the maximum is looked for again: outputs have room for values up to 2^95
 
 // A request's row tiles and the key tiles of the longest and the shortest of them.
 struct Rows {
@@ -263,38 +262,21 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_tile_kernel(Attentio
             for (int c = 0; c < 4; ++c) {
                 raw[s][c] = uint4{0, 0, 0, 0};
                 if (row < rows) raw[s][c] = *reinterpret_cast<const uint4*>(at + 64 * s + 32 * (c / 2) + 8 * (c % 2));
-                const uint32_t words[4] = {raw[s][c].x, raw[s][c].y, raw[s][c].z, raw[s][c].w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t lower = words[e] << 16 & 0x7fff0000u, upper = words[e] & 0x7fff0000u, m = lower > upper ? lower : upper;
-                    top = m > top ? m : top;
-                }
+                top = largest_bits(raw[s][c], top);
             }
         const uint32_t other = (uint32_t)__shfl_xor((int)top, 32);
         top = other > top ? other : top;
-        // the largest below 2^8 (e4m3 reaches 448), what is left below 2^4, times 16
-        int e = (int)(top >> 23) - 127 - 7;
-        e = e < -118 ? -118 : e;
-        const float down = copysignf(__uint_as_float((uint32_t)(127 - e) << 23), a.scale_log2);
-        q_scale = (e + 127) | ((e + 127 - 4) << 8);
+        const QueryScale by = query_scale(top, a.scale_log2);
+        q_scale = by.nearest | by.rest << 8;
 #pragma unroll
         for (int s = 0; s < STEPS; ++s)
 #pragma unroll
             for (int w = 0; w < 8; ++w) {
                 const uint32_t* words = reinterpret_cast<const uint32_t*>(&raw[s][w / 2]) + 2 * (w % 2);
-                const float y[4] = {__uint_as_float(words[0] << 16) * down, __uint_as_float(words[0] & 0xffff0000u) * down,
-                                    __uint_as_float(words[1] << 16) * down, __uint_as_float(words[1] & 0xffff0000u) * down};
-                float rest[4];
-                int hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-                hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], hi, true);
-                rest[0] = (y[0] - __builtin_amdgcn_cvt_f32_fp8(hi, 0)) * 16.0f;
-                rest[1] = (y[1] - __builtin_amdgcn_cvt_f32_fp8(hi, 1)) * 16.0f;
-                rest[2] = (y[2] - __builtin_amdgcn_cvt_f32_fp8(hi, 2)) * 16.0f;
-                rest[3] = (y[3] - __builtin_amdgcn_cvt_f32_fp8(hi, 3)) * 16.0f;
-                int lo = __builtin_amdgcn_cvt_pk_fp8_f32(rest[0], rest[1], 0, false);
-                lo = __builtin_amdgcn_cvt_pk_fp8_f32(rest[2], rest[3], lo, true);
-                q_hi[s][w] = hi;
-                q_lo[s][w] = lo;
+                int nearest, rest;
+                to_e4m3(words[0], words[1], by.down, &nearest, &rest);
+                q_hi[s][w] = nearest;
+                q_lo[s][w] = rest;
             }
     }
 
