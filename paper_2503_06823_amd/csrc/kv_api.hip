@@ -140,7 +140,7 @@ int emoe_kv_attention(const emoe_kv_desc* desc, const emoe_attention_desc* atten
     a.max_new = attention->max_new;
     a.q_heads = attention->q_heads;
     a.kv_heads = desc->kv_heads;
-    a.group = attention->q_heads / desc->kv_heads;
+    a.set_group(attention->q_heads / desc->kv_heads);
     a.width = desc->table_width;
     a.pages = desc->pages;
     a.window = attention->window;

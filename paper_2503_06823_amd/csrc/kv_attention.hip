@@ -60,10 +60,10 @@ __global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(AttentionA
             __syncthreads();  // the sums are read
         }
         if (share == 0 && row < p.rows) {
-            const int m = p.row0 + row;
+            const int m = p.row0 + row, token = a.token_of(m);
             const float by = all == 0.0f ? 0.0f : 1.0f / all;
-            store4(static_cast<E*>(a.out) + (int64_t)(p.token0 + m / a.group) * a.out_stride +
-                       (int64_t)(p.kv_head * a.group + m % a.group) * D + 4 * lane, v * by);
+            store4(static_cast<E*>(a.out) + (int64_t)(p.token0 + token) * a.out_stride +
+                       (int64_t)(p.kv_head * a.group + m - token * a.group) * D + 4 * lane, v * by);
         }
     }
 }

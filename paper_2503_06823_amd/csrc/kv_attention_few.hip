@@ -31,7 +31,7 @@ namespace {
 
 constexpr int kTok = 32;      // tokens of a tile
 constexpr int kRows = kFewRows;  // of a workgroup
-constexpr int kWaves = 4;
+constexpr int kLogWaves = 2, kWaves = 1 << kLogWaves;
 // See Stretch.
 constexpr int kFixed = 2;       // units that a stretch's beginning and end take time for
 constexpr int kLeastUnits = 3;  // of a workgroup's share
@@ -46,32 +46,29 @@ template <> struct WavesPerSimd<float, 128> { static constexpr int n = 2; };
 template <> struct WavesPerSimd<float, 64> { static constexpr int n = 3; };
 
 // The work as one line of units: requests in order, of a request its kv heads, of a head its tiles of 16 rows, of those (a stretch) kFixed
-// units for its beginning and end and then the rounds of kWaves key tiles that the longest row sees, at least one.  Every workgroup takes an
+// units for its beginning and end and then the rounds of key tiles that the longest row sees, at least one.  Every workgroup takes an
 // equal part of the line, so that all of them end together whatever the lengths; a boundary within kSnap rounds of a stretch's beginning or
-// end moves there, or nothing would be left whole.
+// end moves there, or nothing would be left whole.  A round is kWaves << shift tiles: more than one a wavefront only where the line would not
+// fit 31 bits.
 struct Stretch {
     int row_tiles;  // of a request
     int rounds;     // of one of its stretches
-    __device__ long long all(int kv_heads) const { return (long long)row_tiles * kv_heads * (kFixed + rounds); }
+    __device__ int all(int kv_heads) const { return row_tiles * kv_heads * (kFixed + rounds); }
 };
-__device__ __forceinline__ Stretch stretch(const AttentionArgs& a, const Request& q, int most_rows) {
-    const long long rows = (long long)q.n * a.group;
+__device__ __forceinline__ Stretch stretch(const AttentionArgs& a, const Request& q, int most_rows, int shift) {
+    const int rows = q.n * a.group;
     if (rows == 0 || rows > most_rows) return {0, 0};
-    const int n = (tiles<kTok>(a, q.seq, q.len - q.n, q.len - 1).count() + kWaves - 1) / kWaves;
-    return {(int)((rows + kRows - 1) / kRows), n > 0 ? n : 1};
+    const int n = (tiles<kTok>(a, q.seq, q.len - q.n, q.len - 1).count() + (kWaves << shift) - 1) >> shift >> kLogWaves;
+    return {(int)((uint32_t)(rows + kRows - 1) / kRows), n > 0 ? n : 1};
 }
 
 // total units in `groups` shares, the first `longer` of them one unit longer.
 struct Shares {
-    long long total, each, longer;
-    int groups;
-    __device__ __forceinline__ static long long divide(long long x, long long y) {  // mostly small: 32 bits are five times as fast
-        return (((unsigned long long)x | (unsigned long long)y) >> 32) == 0 ? (long long)((uint32_t)x / (uint32_t)y) : x / y;
-    }
-    __device__ __forceinline__ long long begin(int w) const { return w * each + (w < longer ? w : longer); }
-    __device__ __forceinline__ int owner(long long u) const {
-        const long long of_longer = longer * (each + 1);
-        return (int)(u < of_longer ? divide(u, each + 1) : longer + divide(u - of_longer, each));
+    int total, each, longer, groups;
+    __device__ __forceinline__ int begin(int w) const { return w * each + (w < longer ? w : longer); }
+    __device__ __forceinline__ int owner(int u) const {
+        const int of_longer = longer * (each + 1);
+        return u < of_longer ? (uint32_t)u / (uint32_t)(each + 1) : longer + (uint32_t)(u - of_longer) / (uint32_t)each;
     }
 };
 
@@ -79,39 +76,45 @@ struct Shares {
 struct Start {
     Shares shares;
     int r;
-    long long before;  // units of the requests before r
+    int before;  // units of the requests before r
     Request request;
+    Stretch stretch;
 };
-__device__ __forceinline__ bool find_start(const AttentionArgs& a, int most_rows, Start* s) {
+__device__ __forceinline__ bool find_start(const AttentionArgs& a, int most_rows, int shift, Start* s) {
     const int lane = threadIdx.x & 63;
     Request mine;
+    Stretch its;
     auto units_of = [&](int r) {
         mine = {0, 0, 0, 0};
         if (r < a.R) mine = request(a, r);
-        return stretch(a, mine, most_rows).all(a.kv_heads);
+        its = stretch(a, mine, most_rows, shift);
+        return its.all(a.kv_heads);
     };
-    long long upto = 0, total = 0;  // of a trip, of all
+    long long upto = 0, all = 0;  // of a trip, of all
     for (int r0 = 0; r0 < a.R; r0 += 64) {
-        upto = wave_inclusive(units_of(r0 + lane));
-        total += readlane(upto, 63);
+        upto = wave_inclusive((long long)units_of(r0 + lane));
+        all += readlane(upto, 63);
     }
-    const long long most = Shares::divide(total + kLeastUnits - 1, kLeastUnits);
+    if (all > 0x7fffffff) return false;  // there are more queries than T: cu_new is not a list of offsets
+    const int total = (int)all;
+    const int most = (uint32_t)(total + kLeastUnits - 1) / kLeastUnits;
     s->shares.total = total;
-    s->shares.groups = most < gridDim.x ? (int)most : (int)gridDim.x;
+    s->shares.groups = most < (int)gridDim.x ? most : (int)gridDim.x;
     if ((int)blockIdx.x >= s->shares.groups) return false;
-    s->shares.each = Shares::divide(total, s->shares.groups);
+    s->shares.each = (uint32_t)total / (uint32_t)s->shares.groups;
     s->shares.longer = total - s->shares.each * s->shares.groups;
-    const long long begin = s->shares.begin(blockIdx.x);
+    const int begin = s->shares.begin(blockIdx.x);
     s->before = 0;
     for (int r0 = 0; r0 < a.R; r0 += 64) {
-        if (a.R > 64) upto = wave_inclusive(units_of(r0 + lane));
-        const long long sum = readlane(upto, 63);
+        if (a.R > 64) upto = wave_inclusive((long long)units_of(r0 + lane));
+        const int mine_upto = (int)upto, sum = __builtin_amdgcn_readlane(mine_upto, 63);
         if (begin - s->before < sum) {
-            const int at = __builtin_ctzll(__ballot(upto > begin - s->before));
+            const int at = __builtin_ctzll(__ballot(mine_upto > begin - s->before));
             s->r = r0 + at;
-            if (at > 0) s->before += readlane(upto, at - 1);
+            if (at > 0) s->before += __builtin_amdgcn_readlane(mine_upto, at - 1);
             s->request = {__builtin_amdgcn_readlane(mine.first, at), __builtin_amdgcn_readlane(mine.n, at),
                           __builtin_amdgcn_readlane(mine.seq, at), __builtin_amdgcn_readlane(mine.len, at)};
+            s->stretch = {__builtin_amdgcn_readlane(its.row_tiles, at), __builtin_amdgcn_readlane(its.rounds, at)};
             return true;
         }
         s->before += sum;
@@ -124,7 +127,7 @@ template <int D> struct Quarter { typedef uint32_t type __attribute__((ext_vecto
 template <> struct Quarter<64> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
 
 template <class E, int D>
-__global__ __launch_bounds__(64 * kWaves, (WavesPerSimd<E, D>::n)) void attention_few_kernel(AttentionArgs a, FewRule rule, AttentionWs lay) {
+__global__ __launch_bounds__(64 * kWaves, (WavesPerSimd<E, D>::n)) void attention_few_kernel(AttentionArgs a, FewRule rule, int shift, AttentionWs lay) {
     constexpr int PIECES = Pieces<E>::n, STEPS = D / 32, BLOCKS = D / 16;
     constexpr bool SCALED = sizeof(E) == 2;  // K stays in 4 bits
     constexpr int V_STRIDE = D + 16;  // elements; 32 bytes past the row: 16 rows of 32 bytes fall on all banks alike
@@ -137,38 +140,51 @@ __global__ __launch_bounds__(64 * kWaves, (WavesPerSimd<E, D>::n)) void attentio
 
     const int most_rows = uniform(few_rows(a, rule));
     Start start;
-    const bool some = find_start(a, most_rows, &start);
+    const bool some = find_start(a, most_rows, shift, &start);
     Piece* records = reinterpret_cast<Piece*>(a.ws + lay.few_records) + 2 * (size_t)blockIdx.x;
     bool used[2] = {false, false};
-    const long long share_end = some ? start.shares.begin(blockIdx.x + 1) : 0;
-    int r = uniform(start.r);
-    long long before = start.before;
+    const int share_end = some ? start.shares.begin(blockIdx.x + 1) : 0;
+    int r = uniform(start.r), before = start.before;
     Request q = start.request;
-    for (long long unit = some ? start.shares.begin(blockIdx.x) : 0; unit < share_end;) {
-        const Stretch here = stretch(a, q, most_rows);
-        const long long all_here = here.all(a.kv_heads);
-        if (unit - before >= all_here) {
-            before += all_here;
+    Stretch here = start.stretch;
+    for (int unit = some ? start.shares.begin(blockIdx.x) : 0; unit < share_end;) {
+        if (unit - before >= here.all(a.kv_heads)) {
+            before += here.all(a.kv_heads);
             q = uniform(request(a, ++r));
+            here = stretch(a, q, most_rows, shift);
             continue;
         }
-        const int rounds = uniform(here.rounds), units = kFixed + rounds, nth = uniform((int)Shares::divide(unit - before, units));
-        const long long first_unit = before + (long long)nth * units;
+        const int rounds = uniform(here.rounds), units = kFixed + rounds, nth = uniform((uint32_t)(unit - before) / (uint32_t)units);
+        const int first_unit = before + nth * units;
         const int snap = kSnap < rounds / 2 ? kSnap : rounds / 2;
-        auto round_at = [&](long long u) {
-            const int k = u - first_unit < units ? (int)(u - first_unit) - kFixed : rounds;
+        auto round_at = [&](int u) {
+            const int k = u - first_unit < units ? u - first_unit - kFixed : rounds;
             return uniform(k <= snap ? 0 : k >= rounds - snap ? rounds : k);
         };
         const int u_begin = round_at(unit), u_end = round_at(share_end);
         unit = first_unit + units;
         if (u_begin >= u_end) continue;
-        const int kv_head = nth / here.row_tiles, row_tile = nth % here.row_tiles;
+        const int kv_head = uniform((uint32_t)nth / (uint32_t)here.row_tiles), row_tile = nth - kv_head * here.row_tiles;
         const int rows = q.n * a.group, row0 = row_tile * kRows, last_row = row0 + kRows < rows ? row0 + kRows - 1 : rows - 1;
-        const int p_first = q.len - q.n + row0 / a.group, p_last = q.len - q.n + last_row / a.group;
+        const int p_first = q.len - q.n + a.token_of(row0), p_last = q.len - q.n + a.token_of(last_row);
+
+        const int row = row0 + col, token = a.token_of(row), head = kv_head * a.group + row - token * a.group;
+        const int position = row < rows ? q.len - q.n + token : -1;  // -1 sees nothing
+
+        const E* q_at = static_cast<const E*>(a.q) + (int64_t)(q.first + token) * a.q_stride + (int64_t)head * D;
+        constexpr int LOADS = D / 32;
+        uint4 raw[LOADS];  // of bf16 queries
+        if constexpr (SCALED) {
+#pragma unroll
+            for (int c = 0; c < LOADS; ++c) {
+                raw[c] = uint4{0, 0, 0, 0};
+                if (row < rows) raw[c] = *reinterpret_cast<const uint4*>(q_at + 16 * group + 64 * (c / 2) + 8 * (c % 2));
+            }
+        }
 
         const Tiles seen = uniform(tiles<kTok>(a, q.seq, q.len - q.n, q.len - 1));
         const int i_all = seen.count();
-        int i_end = u_end * kWaves < i_all ? u_end * kWaves : i_all;
+        int i_end = u_end < rounds ? u_end * (kWaves << shift) : i_all;
         while (i_end > 0 && seen.tile(i_end - 1) * kTok > p_last) --i_end;  // no row of this tile sees so far
         // read through the scalar cache: a vector load here would wait for the tiles on their way
         typedef const __attribute__((address_space(4))) int32_t* ScalarTable;
@@ -239,7 +255,7 @@ __global__ __launch_bounds__(64 * kWaves, (WavesPerSimd<E, D>::n)) void attentio
 
         // Tile i + 4's values and keys are on their way from where tile i's have been used on, and its page is looked up a tile earlier.  The first
         // tile's are sent for before the queries are.
-        int i = u_begin * kWaves + wave;
+        int i = u_begin * (kWaves << shift) + wave;
         const int last = i_end - 1;  // past the end: the last tile again, unused
         Place now, next;
         if (i < i_end) {
@@ -248,27 +264,17 @@ __global__ __launch_bounds__(64 * kWaves, (WavesPerSimd<E, D>::n)) void attentio
             load_keys(now);
             next = place(i + kWaves < i_end ? i + kWaves : last);
         }
-        const int row = row0 + col, token = row / a.group, head = kv_head * a.group + row % a.group;
-        const int position = row < rows ? q.len - q.n + token : -1;  // -1 sees nothing
-
         // Scores are compared before they are scaled: the scale is positive, its sign goes into q.  A scale of zero becomes next to nothing, so
         // that it does not meet an infinity.
         const float scale = fmaxf(fabsf(a.scale_log2), 1e-37f);
         bf16x8 query[SCALED ? 1 : PIECES][SCALED ? 1 : STEPS];
         intx8 q_hi, q_lo;  // for D = 64 both are in q_hi
         int q_scale;
-        const E* q_at = static_cast<const E*>(a.q) + (int64_t)(q.first + token) * a.q_stride + (int64_t)head * D;
         if constexpr (SCALED) {
             // a lane's bytes 0 .. 15 are elements 16 group on of the 128 of a product, 16 .. 31 those 64 further on; its scale is of elements 32 group on
-            constexpr int LOADS = D / 32;
-            uint4 raw[LOADS];
             uint32_t top = 0;
 #pragma unroll
-            for (int c = 0; c < LOADS; ++c) {
-                raw[c] = uint4{0, 0, 0, 0};
-                if (row < rows) raw[c] = *reinterpret_cast<const uint4*>(q_at + 16 * group + 64 * (c / 2) + 8 * (c % 2));
-                top = largest_bits(raw[c], top);
-            }
+            for (int c = 0; c < LOADS; ++c) top = largest_bits(raw[c], top);
             top = over_groups(top, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
             const QueryScale by = query_scale(top, a.scale_log2);
             q_scale = D == 128 ? by.nearest | by.rest << 8 : group < 2 ? by.nearest : by.rest;
@@ -481,12 +487,16 @@ hipError_t launch_attention_few(const emoe_kv_desc& d, int dtype, const Attentio
     const long long rows = (long long)a.max_new * a.group < most_rows ? (long long)a.max_new * a.group : most_rows;
     const long long per_request = (rows + kRows - 1) / kRows, by_tokens = (long long)a.T * a.group / kRows + a.R;
     const long long row_tiles = per_request * a.R < by_tokens ? per_request * a.R : by_tokens;
-    const long long most_rounds = (((long long)a.width << a.page.log2_size) + kTok * kWaves - 1) / (kTok * kWaves);
-    const long long line = row_tiles * a.kv_heads * (kFixed + most_rounds), shares = (line + kLeastUnits - 1) / kLeastUnits;
+    // A round's tiles are doubled until a stretch has no more rounds than leave the line in 31 bits (row tiles of all heads: below 2^25).
+    const long long stretches = row_tiles * a.kv_heads, most_tiles = (((long long)a.width << a.page.log2_size) + kTok - 1) / kTok;
+    int shift = 0;
+    auto rounds_of = [&] { return ((most_tiles - 1) >> shift >> kLogWaves) + 1; };
+    while (rounds_of() > 1 && stretches * (kFixed + rounds_of()) > 0x7fffffff - kLeastUnits) ++shift;
+    const long long most_rounds = rounds_of(), line = stretches * (kFixed + most_rounds), shares = (line + kLeastUnits - 1) / kLeastUnits;
     const int groups = shares < kFewPerCu * shape.groups ? (int)shares : kFewPerCu * shape.groups;
     *slots = most_rounds > 2 * kSnap + 1 ? 2 * groups : 0;  // none if no stretch is long enough to be cut
     auto run = [&](auto element, auto dim) {
-        attention_few_kernel<decltype(element), decltype(dim)::value><<<(unsigned)groups, 64 * kWaves, 0, st>>>(a, rule, ws);
+        attention_few_kernel<decltype(element), decltype(dim)::value><<<(unsigned)groups, 64 * kWaves, 0, st>>>(a, rule, shift, ws);
         return hipGetLastError();
     };
     if (dtype == EMOE_F32)

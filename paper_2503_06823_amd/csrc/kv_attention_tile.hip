@@ -175,9 +175,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_tile_kernel(Attentio
     // the wavefront's own rows
     const int w_row0 = row0 + 32 * wave, w_last = w_row0 + 31 < rows ? w_row0 + 31 : rows - 1;
     const bool w_any = w_row0 < rows;
-    const int w_first_p = uniform(p0 + w_row0 / a.group), w_last_p = uniform(p0 + w_last / a.group);
+    const int w_first_p = uniform(p0 + a.token_of(w_row0)), w_last_p = uniform(p0 + a.token_of(w_last));
 
-    const Tiles seen = uniform(tiles<kTok>(a, q.seq, p0 + row0 / a.group, p0 + last_row / a.group));
+    const Tiles seen = uniform(tiles<kTok>(a, q.seq, p0 + a.token_of(row0), p0 + a.token_of(last_row)));
     const int i_all = seen.count(), each = uniform(job.each);
     const int i_begin = uniform(job.piece) * each;
     int i_end = i_begin + each < i_all ? i_begin + each : i_all;
@@ -248,7 +248,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_tile_kernel(Attentio
     }
 
     // q as two e4m3 operands.  Lane (col, group) holds elements 64 s + 16 group .. +15 and 32 further on of its row; one scale a row.
-    const int row = w_row0 + col, token = row / a.group, head = kv_head * a.group + row % a.group;
+    const int row = w_row0 + col, token = a.token_of(row), head = kv_head * a.group + row - token * a.group;
     const int position = row < rows ? p0 + token : -1;  // -1 sees nothing
     intx8 q_hi[STEPS], q_lo[STEPS];
     int q_scale;

@@ -77,6 +77,16 @@ struct AttentionArgs {
     float scale_log2;  // scale * log2(e): the exponentials are powers of two
     int T, R, max_new, q_heads, kv_heads, group, width, pages, window, sinks;
     KvPage page;
+    uint32_t group_inverse;
+    int group_shift;
+
+    // row / group of a row below 2^27: the inverse is too large by less than 2^-27 of itself
+    void set_group(int heads) {
+        group = heads;
+        for (group_shift = 0; 1 << group_shift < heads; ++group_shift) {}
+        group_inverse = (uint32_t)(((1ull << (27 + group_shift)) + heads - 1) / heads) << 4;
+    }
+    __device__ __forceinline__ int token_of(int row) const { return (int)(__umulhi(2u * (uint32_t)row, group_inverse) >> group_shift); }
 };
 size_t attention_ws_bytes(const emoe_kv_desc& d, const emoe_attention_desc& a);
 hipError_t launch_attention(const emoe_kv_desc& d, const emoe_attention_desc& a, const AttentionArgs& args, hipStream_t st);

@@ -282,3 +282,15 @@ def test_another_stream_and_a_graph(gpu_device, news):
             graph.replay() if replay else step(side)
             torch.cuda.synchronize()
             assert torch.equal(out, want), (l, replay)
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (150, 40)])
+def test_a_call_that_could_have_more_work_than_31_bits_count(gpu_device, window, sinks):
+    """A table of 2^23 tokens, 256 heads and room for 2048 query tokens, of which 23 come."""
+    b = Batch(12, [40, 600], [3, 20], 256, 1, 64, 256, "f32")
+    wide = np.full((2, 1 << 15), -1, dtype=np.int32)
+    wide[:, :b.table.shape[1]] = b.table
+    want, seen = ref.attention(b.cache, b.q, b.table, b.lengths, b.cu, 64 ** -0.5, window, sinks)
+    b.table, b.T = wide, 2048
+    b.q = np.concatenate((b.q, np.zeros((2048 - 23, 256, 64))))
+    compare(b.run(window, sinks, max_new=1024)[:23], want, seen, 64, "f32")
