@@ -168,8 +168,8 @@ __device__ __forceinline__ uint32_t largest_bits(const uint4& eight, uint32_t to
     }
     return top;
 }
-// A row's scale from its largest: that comes below 2^8 (e4m3 reaches 448), what is left of it below 2^4.  `byte`: the scales of the two operands
-// as the instruction takes them; `down`: what a number is multiplied with, with the sign of the scores' scale.
+// A row's scale from its largest: that comes below 2^8 (e4m3 reaches 448), what is left of it below 2^4.  `down`: what a number is
+// multiplied with, with the sign of the scores' scale; `nearest`, `rest`: scale bytes of the two operands.
 struct QueryScale {
     float down;
     int nearest, rest;

@@ -3,7 +3,9 @@
 // Four lanes hold a block of 32 elements, eight each: one 16-byte load of bf16, the largest magnitude by two steps over the
 // lanes (as integers: a NaN is larger than all numbers), a power of two as scale, and the converters of gfx950, whose rounding is to
 // nearest even.  With the scale a power of two x / s is exact, so the codes depend on the input alone.  Bound by HBM at
-// many tokens: 2 bytes of bf16 in and 17/32 out per element, or the other way round; by the launch at a decode step's.
+// many tokens: 2 bytes of bf16 in and 17/32 out per element, or the other way round; by the launch at a decode step's.  Measured with
+// 8 heads of 128 elements: 8192 tokens 9.4 to 11.8 us for 42 MB either way, 3.6 to 4.5 TB/s where a large copy reaches 5.1; 64
+// tokens 2.9 us to write, 2.6 to read.  Two or four pieces a thread, with their loads together, took as long.
 #include "kv_cache.h"
 
 namespace emoe {
