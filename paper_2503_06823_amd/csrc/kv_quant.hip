@@ -4,8 +4,9 @@
 // lanes (as integers: a NaN is larger than all numbers), a power of two as scale, and the converters of gfx950, whose rounding is to
 // nearest even.  With the scale a power of two x / s is exact, so the codes depend on the input alone.  Bound by HBM at
 // many tokens: 2 bytes of bf16 in and 17/32 out per element, or the other way round; by the launch at a decode step's.  Measured with
-// 8 heads of 128 elements: 8192 tokens 9.4 to 11.8 us for 42 MB either way, 3.6 to 4.5 TB/s where a large copy reaches 5.1; 64
-// tokens 2.9 us to write, 2.6 to read.  Two or four pieces a thread, with their loads together, took as long.
+// 8 heads of 128 elements, as replayed graphs: 32768 tokens 36.9 us to write, 35.3 to read, 4.6 and 4.8 TB/s where a large copy reaches 5.1 (with
+// the heads of a token in a workgroup 37.6 both; 32 heads of 64: 21.0 and 20.3 us against 23.6 and 25.4); 8192 tokens 9.4 and 8.5, in scattered slots
+// 9.7 and 9.3; 64 tokens 2.2 and 2.1.  Two or four pieces a thread, with their loads together, took as long.
 #include "kv_cache.h"
 
 namespace emoe {
@@ -75,15 +76,24 @@ __device__ __forceinline__ uint32_t quantise(const float* x, uint32_t* scale_byt
     return finite ? codes : 0u;
 }
 
-// A thread: eight elements of a token's keys and the same of its values.  Pieces are numbered through, per_row of them a token; 32 bits hold them.
-// Two or four tokens' pieces a thread were no faster.
+// A thread: eight elements of a token's keys and the same of its values.  A workgroup: one head of 16 or 32 tokens, so that both sides are whole
+// lines where the slots follow each other, with its neighbours at the other heads of these tokens.
+struct Thread {
+    uint32_t token, head, piece;
+};
+__device__ __forceinline__ Thread this_thread(int kv_heads, int log_pieces) {
+    const uint32_t tokens = blockIdx.x / (uint32_t)kv_heads;
+    return {tokens * (kThreads >> log_pieces) + (threadIdx.x >> log_pieces), blockIdx.x - tokens * kv_heads, threadIdx.x & ((1u << log_pieces) - 1)};
+}
+
 template <class E>
 __global__ __launch_bounds__(kThreads) void kv_append_kernel(const E* __restrict__ k, int64_t k_stride, const E* __restrict__ v,
                                                              int64_t v_stride, const int32_t* __restrict__ slots, uint8_t* __restrict__ cache,
-                                                             uint32_t n, int kv_heads, int dim, int n_slots, KvPage page) {
-    const uint32_t per_row = (uint32_t)(kv_heads * dim / 8), per_head = (uint32_t)dim / 8, i = blockIdx.x * kThreads + threadIdx.x;
-    if (i >= n) return;  // alike in the four lanes of a block: per_row is a multiple of 8
-    const uint32_t t = i / per_row, e = i - t * per_row, head = e / per_head, piece = e % per_head;
+                                                             int T, int kv_heads, int dim, int n_slots, KvPage page) {
+    const int log_pieces = dim == 64 ? 3 : 4;
+    const auto [t, head, piece] = this_thread(kv_heads, log_pieces);
+    if (t >= (uint32_t)T) return;  // alike in the four lanes of a block
+    const uint32_t e = (head << log_pieces) + piece;
     const int slot = slots[t];
     float x[2][8];
     load8(k + (int64_t)t * k_stride + e * 8, x[0]);
@@ -119,11 +129,12 @@ __device__ __forceinline__ void store8(bf16_t* p, uint32_t codes, float scale) {
 
 template <class E>
 __global__ __launch_bounds__(kThreads) void kv_read_kernel(const uint8_t* __restrict__ cache, const int32_t* __restrict__ slots,
-                                                           E* __restrict__ k, E* __restrict__ v, uint32_t n, int kv_heads, int dim, int n_slots,
+                                                           E* __restrict__ k, E* __restrict__ v, int T, int kv_heads, int dim, int n_slots,
                                                            KvPage page) {
-    const uint32_t per_row = (uint32_t)(kv_heads * dim / 8), per_head = (uint32_t)dim / 8, i = blockIdx.x * kThreads + threadIdx.x;
-    if (i >= n) return;
-    const uint32_t t = i / per_row, e = i - t * per_row, head = e / per_head, piece = e % per_head;
+    const int log_pieces = dim == 64 ? 3 : 4;
+    const auto [t, head, piece] = this_thread(kv_heads, log_pieces);
+    if (t >= (uint32_t)T) return;
+    const size_t i = (((size_t)t * kv_heads + head) << log_pieces) + piece;
     const int slot = slots[t];
     uint32_t codes[2] = {0, 0}, byte[2] = {127, 127};
     if ((unsigned)slot < (unsigned)n_slots) {
@@ -134,15 +145,14 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(const uint8_t* __rest
             byte[w] = cache[at.scales + piece / 4];
         }
     }
-    store8(k + (size_t)i * 8, codes[0], scale_of_byte(byte[0]));
-    store8(v + (size_t)i * 8, codes[1], scale_of_byte(byte[1]));
+    store8(k + i * 8, codes[0], scale_of_byte(byte[0]));
+    store8(v + i * 8, codes[1], scale_of_byte(byte[1]));
 }
 
-template <class F>
-hipError_t over_rows(const emoe_kv_desc& d, int T, F launch) {
-    const long long n = (long long)T * (d.kv_heads * d.head_dim / 8);  // at most 2^30
-    launch((unsigned)((n + kThreads - 1) / kThreads), (uint32_t)n);
-    return hipGetLastError();
+// At most 2^33 elements (emoe.h), 2048 a workgroup.
+unsigned groups_of(const emoe_kv_desc& d, int T) {
+    const long long tokens = kThreads * 8 / d.head_dim;
+    return (unsigned)((T + tokens - 1) / tokens * d.kv_heads);
 }
 
 }  // namespace
@@ -150,10 +160,9 @@ hipError_t over_rows(const emoe_kv_desc& d, int T, F launch) {
 hipError_t launch_kv_append(const emoe_kv_desc& d, int T, int dtype, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                             const int32_t* slot, void* cache, hipStream_t st) {
     auto run = [&](auto* kp, auto* vp) {
-        return over_rows(d, T, [&](unsigned groups, uint32_t n) {
-            kv_append_kernel<<<groups, kThreads, 0, st>>>(
-                kp, k_stride, vp, v_stride, slot, static_cast<uint8_t*>(cache), n, d.kv_heads, d.head_dim, d.pages * d.page_size, kv_page(d));
-        });
+        kv_append_kernel<<<groups_of(d, T), kThreads, 0, st>>>(kp, k_stride, vp, v_stride, slot, static_cast<uint8_t*>(cache), T, d.kv_heads, d.head_dim,
+                                                               d.pages * d.page_size, kv_page(d));
+        return hipGetLastError();
     };
     if (dtype == EMOE_F32) return run(static_cast<const float*>(k), static_cast<const float*>(v));
     return run(static_cast<const bf16_t*>(k), static_cast<const bf16_t*>(v));
@@ -162,10 +171,9 @@ hipError_t launch_kv_append(const emoe_kv_desc& d, int T, int dtype, const void*
 hipError_t launch_kv_read(const emoe_kv_desc& d, int T, int dtype, const void* cache, const int32_t* slot, void* k, void* v,
                           hipStream_t st) {
     auto run = [&](auto* kp, auto* vp) {
-        return over_rows(d, T, [&](unsigned groups, uint32_t n) {
-            kv_read_kernel<<<groups, kThreads, 0, st>>>(
-                static_cast<const uint8_t*>(cache), slot, kp, vp, n, d.kv_heads, d.head_dim, d.pages * d.page_size, kv_page(d));
-        });
+        kv_read_kernel<<<groups_of(d, T), kThreads, 0, st>>>(static_cast<const uint8_t*>(cache), slot, kp, vp, T, d.kv_heads, d.head_dim,
+                                                             d.pages * d.page_size, kv_page(d));
+        return hipGetLastError();
     };
     if (dtype == EMOE_F32) return run(static_cast<float*>(k), static_cast<float*>(v));
     return run(static_cast<bf16_t*>(k), static_cast<bf16_t*>(v));
