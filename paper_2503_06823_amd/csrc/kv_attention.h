@@ -24,7 +24,7 @@ struct AttentionWs {
     size_t total;
 };
 // Which requests the kernel for few queries takes, by their rows (query tokens times the heads of a kv head): up to `always`, and up to `small` if
-// the work of all that have more than `always` is small.  The kernel for many takes the others.
+// little is gained (few_gain) on all that have more than `always`.  The kernel for many takes the others.
 struct FewRule {
     int always, small;
 };
@@ -32,12 +32,14 @@ hipError_t launch_attention_few(const emoe_kv_desc& d, int dtype, const Attentio
                                 hipStream_t st);
 hipError_t launch_attention_tile(const emoe_kv_desc& d, const AttentionArgs& a, FewRule rule, const AttentionWs& ws, hipStream_t st);
 
-// Rows of 16 times the tokens that they see, kFewStart more for a beginning and an end, up to which the kernel for few queries is faster whatever
-// the request's rows (us, few / many queries' kernel, 32 heads on 8: 128 rows on 2000 tokens 17 / 23, on 16000 35 / 36; 256 rows on 2000
-// 21 / 32, on 16000 52 / 40; four times 256 rows on 2000 32 / 46, on 16000 131 / 82): it starts sooner and cuts finer, but reads the
-// keys anew for every 16 rows.
-constexpr long long kFewWork = 1400000;
-constexpr int kFewStart = 256;
+// What the kernel for many queries saves on a request of 33 to 512 rows, in rows of 16 times tokens: it costs 3/2 such rows for a tile of 128
+// rows and 1/2 for 32 of them, and starts later.  Below kFewGain for all such requests together the other one is faster (us, few / many queries'
+// kernel, 32 heads on 8, requests times rows on tokens: 128 on 4000 20 / 23, on 16000 33 / 27; 512 on 2000 24 / 24, on 4000 32 / 28; 4 times 128 on
+// 2000 23 / 25, 256 34 / 30; 16 times 40 on 4000 43 / 51, 64 times 136 / 115; 16 times 512 on 2000 180 / 79).
+constexpr long long kFewGain = 500000;
+__host__ __device__ constexpr long long few_gain(long long rows, long long seen) {
+    return (rows + 15) / 16 * (seen + 256) - (3 * ((rows + 127) / 128) + (rows + 31) / 32) * (seen + 400) / 2;
+}
 
 namespace {
 
@@ -102,15 +104,15 @@ __device__ __forceinline__ Tiles tiles(const AttentionArgs& a, int seq, int firs
 __device__ __forceinline__ int few_rows(const AttentionArgs& a, FewRule rule) {
     if (rule.small <= rule.always) return rule.always;
     const int lane = threadIdx.x & 63;
-    long long work = 0;
+    long long gain = 0;
     for (int r = lane; r < a.R; r += 64) {
         const Request q = request(a, r);
         const long long rows = (long long)q.n * a.group, reach = (long long)a.window + a.sinks + q.n;
         const long long seen = a.window > 0 && reach < q.seq ? reach : q.seq;
-        if (rows > rule.always) work += (rows + 15) / 16 * a.kv_heads * (seen + kFewStart);
+        if (rows > rule.always) gain += few_gain(rows, seen) * a.kv_heads;
     }
-    work = readlane(wave_inclusive(work), 63);
-    return work <= kFewWork ? rule.small : rule.always;
+    gain = readlane(wave_inclusive(gain), 63);
+    return gain <= kFewGain ? rule.small : rule.always;
 }
 
 // x over the four lanes that hold one query (lane, lane ^ 16, ^ 32, ^ 48).

@@ -85,16 +85,16 @@ AttentionWs attention_ws(int dim, bool tiles) {
     return w;
 }
 
-// Requests of up to this many rows go to the kernel for few queries always, of up to the other where there is little work.
+// Requests of up to this many rows go to the kernel for few queries always, of up to the other where little is gained.
 constexpr int kAlwaysFewRows = 32, kSmallFewRows = 512;
 
-// The tile kernel is for bf16: fp32 queries would take three times the matrix work and registers there, and are for verification.  Work that is
-// small at the table's full width is small.
+// The tile kernel is for bf16: fp32 queries would take three times the matrix work and registers there, and are for verification.  A gain that is
+// small at the table's full width is small: it is at most 9/16 of the rows of 16 times what they see.
 bool with_tiles(const emoe_kv_desc& d, const emoe_attention_desc& a) {
     const long long rows = (long long)a.max_new * (a.q_heads / d.kv_heads);
     if (a.dtype != EMOE_BF16 || rows <= kAlwaysFewRows) return false;
     const long long row_tiles = ((long long)a.T * a.q_heads / d.kv_heads + 15) / 16 + d.rows;  // at most, of 16 rows
-    return rows > kSmallFewRows || row_tiles * d.kv_heads * ((long long)d.table_width * d.page_size + kFewStart) > kFewWork;
+    return rows > kSmallFewRows || row_tiles * d.kv_heads * ((long long)d.table_width * d.page_size + 256) / 16 * 9 > kFewGain;
 }
 
 }  // namespace
@@ -109,7 +109,7 @@ hipError_t launch_attention(const emoe_kv_desc& d, const emoe_attention_desc& at
     FewRule rule = {0x7fffffff, 0};
     bool few = true;
     if (tiles) {
-        const bool large = (long long)a.T * a.q_heads / 16 * kFewStart > 2 * kFewWork;  // if all the tokens are there
+        const bool large = (long long)a.T * a.q_heads / 128 * few_gain(128, 0) > kFewGain;  // if all the tokens are there, whatever they see
         rule = {kAlwaysFewRows, large ? 0 : kSmallFewRows};
         if (a.R == 1 && (large || a.max_new * (long long)a.group > kSmallFewRows)) {  // one request, which goes there whatever it brings
             rule = {0, 0};

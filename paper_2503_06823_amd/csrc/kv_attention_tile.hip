@@ -19,7 +19,8 @@
 //
 // Measured: a prompt of 8192 tokens (32 heads on 8 of 128 elements) 474 to 486 us, 1.13 to 1.16 PFLOP/s of what the mask leaves.  The matrix cores
 // are busy for 54 % of the cycles and the vector units for 49 %, next to nothing of it at the same time, at a clock of 1.85 to 2.05 GHz that power
-// sets.  Slower: scores of the next tile ahead of this one's exponentials (519 us against 504 without staging under the products), a third
+// sets.  Prompts of 512, 1024, 2048 and 4096 tokens: 20, 30, 50 and 144 us (1024: 37 if two pieces share a CU; 2048: 54 if the last of two row tiles for
+// a CU does not go with the first).  Slower: scores of the next tile ahead of this one's exponentials (519 us against 504 without staging under the products), a third
 // wavefront a SIMD (633: it spills); a higher priority in the products changes nothing.  What e4m3 leaves of q in 6 bits instead of
 // 8 is faster, but loses what strong scores need (an element-wise bound is missed by four times).
 #include <math.h>
@@ -56,11 +57,13 @@ struct Job {
     Request q;
 };
 
-// The longest piece is chosen so that the work is over soonest.  Row tiles stay whole where an equal share of all of them is twice the longest
-// or the longest is short; else the longest's key tiles are divided by 1 to 64, an estimate a lane: with pieces of c tiles there are n =
-// sum of ceil(tiles / c), which have to find places at the same time, and take c and kFixed for a beginning and an end, and kJoin
-// for the sum of pieces.  Every wavefront by itself, 64 requests a trip.
-constexpr int kFixed = 4, kJoin = 5;  // in key tiles
+// How row tiles are cut: so that the work is over soonest, in the time that a lone workgroup of a CU takes for a key tile.  Two on a CU take
+// kTwo times as long as one (one's products and the other's exponentials hardly overlap).  Whole row tiles take the longest one's tiles, or a CU's share
+// of all of them if that is more.  Else the longest is divided by 2 to 64, an estimate a lane: with pieces of c tiles there are n = sum of ceil(tiles /
+// c), which have to find places at the same time and take c, or kTwo c if some CU has two; a piece costs 64 KiB written and read again, a
+// tile's time for kPerTile of them, and kCut for the first.  Every wavefront by itself, 64 requests a trip.
+constexpr float kTwo = 1.65f, kCut = 2.0f, kPerTile = 43.0f;
+constexpr int kLeastCut = 6;  // key tiles
 __device__ __forceinline__ Job find_job(const AttentionArgs& a, int least_rows, int places, int want, bool to_the_end) {
     const int lane = threadIdx.x & 63;
     Request mine;
@@ -71,27 +74,22 @@ __device__ __forceinline__ Job find_job(const AttentionArgs& a, int least_rows, 
     };
     Rows rows;
     int longest = 0;
-    float work = 0.0f;
+    long long work = 0, row_tiles = 0;  // work: twice the key tiles of all
     for (int r0 = 0; r0 < a.R; r0 += 64) {
         rows = rows_at(r0 + lane);
-        int n = rows.longest;
-        float w = (float)rows.row_tiles * 0.5f * (float)(rows.longest + rows.shortest);
-#pragma unroll
-        for (int s = 32; s > 0; s /= 2) {
-            const int o = __shfl_xor(n, s);
-            n = o > n ? o : n;
-            w += __shfl_xor(w, s);
-        }
+        const int n = wave_top(rows.longest);
         longest = n > longest ? n : longest;
-        work += w * (float)a.kv_heads;
+        work += readlane(wave_inclusive((long long)rows.row_tiles * (rows.longest + rows.shortest)), 63) * a.kv_heads;
+        row_tiles += readlane(wave_inclusive((long long)rows.row_tiles), 63) * a.kv_heads;
     }
     Job job;
     job.found = false;
     job.all_slots = 0;
-    longest = uniform(longest);
     if (longest == 0) return job;
+    const int cus = places / 2;
     int each = longest;
-    if (longest > kFixed + kJoin && work < 2.0f * (float)longest * (float)places) {
+    long long count = row_tiles;
+    if (row_tiles < places && longest > kLeastCut) {
         const int c = (longest + lane) / (lane + 1);  // this lane's estimate
         long long pieces = 0;
         for (int r0 = 0; r0 < a.R; r0 += 64) {
@@ -102,18 +100,16 @@ __device__ __forceinline__ Job find_job(const AttentionArgs& a, int least_rows, 
                           ((__builtin_amdgcn_readlane(rows.longest, at) + c - 1) / c);
             }
         }
-        int best = lane == 0 ? (int)((pieces + places - 1) / places) * longest + kFixed : pieces <= places ? c + kFixed + kJoin : 0x7fffffff;
-        each = c;
-#pragma unroll
-        for (int s = 32; s > 0; s /= 2) {
-            const int o = __shfl_xor(best, s), e = __shfl_xor(each, s);
-            if (o < best || (o == best && e > each)) {
-                best = o;
-                each = e;
-            }
-        }
-        each = uniform(each);
+        float time = fmaxf((float)longest, 0.25f * kTwo * (float)work / (float)cus);
+        if (lane > 0) time = (pieces <= cus ? 1.0f : kTwo) * (float)c + kCut + (float)pieces / kPerTile;
+        // the longest pieces of those that take least, to an eighth of a tile's time
+        const int saved = lane > 0 && pieces > places ? 0 : 0x7fffffff - (int)fminf(8.0f * time, 1e9f);
+        const int best = __builtin_ctzll(__ballot(saved == wave_top(saved)));
+        each = __builtin_amdgcn_readlane(c, best);
+        count = readlane(pieces, best);
     }
+    // The longest row tiles come first.  With two for a CU at most the last of them comes second, for the CU with the longest.
+    if (count <= places && want >= cus) want = want < count ? (int)count - 1 - (want - cus) : 0x7fffffff;
 
     int jobs = 0, slots = 0;
     for (int r0 = 0; r0 < a.R; r0 += 64) {

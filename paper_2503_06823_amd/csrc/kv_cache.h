@@ -53,6 +53,23 @@ __device__ __forceinline__ long long readlane(long long v, int lane) {
     return ((long long)hi << 32) | (uint32_t)lo;
 }
 
+// The largest of a wavefront's values >= 0, in all lanes.
+__device__ __forceinline__ int wave_top(int v) {
+#define EMOE_TOP_STEP(ctrl, rows)                                                    \
+    {                                                                                \
+        const int o = __builtin_amdgcn_update_dpp(0, v, ctrl, rows, 0xf, false);      \
+        v = o > v ? o : v;                                                           \
+    }
+    EMOE_TOP_STEP(0x111, 0xf)
+    EMOE_TOP_STEP(0x112, 0xf)
+    EMOE_TOP_STEP(0x114, 0xf)
+    EMOE_TOP_STEP(0x118, 0xf)
+    EMOE_TOP_STEP(0x142, 0xa)
+    EMOE_TOP_STEP(0x143, 0xc)
+#undef EMOE_TOP_STEP
+    return __builtin_amdgcn_readlane(v, 63);
+}
+
 hipError_t launch_kv_plan(const emoe_kv_desc& d, int T, const int32_t* len, const int32_t* new_len, int32_t* table,
                           const int32_t* free_pages, const int64_t* counters, int32_t* cu_new, int32_t* slot, int32_t* position,
                           int32_t* seq_len, int64_t* counters_out, int32_t* refused, hipStream_t st);
