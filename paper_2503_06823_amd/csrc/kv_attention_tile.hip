@@ -85,7 +85,7 @@ __device__ __forceinline__ Job find_job(const AttentionArgs& a, int least_rows, 
     Job job;
     job.found = false;
     job.all_slots = 0;
-    if (longest == 0) return job;
+    if (longest == 0 || row_tiles > 0x7fffffff) return job;  // so many only if cu_new is not a list of offsets
     const int cus = places / 2;
     int each = longest;
     long long count = row_tiles;

@@ -126,3 +126,18 @@ def test_a_row_tile_of_every_piece_count(gpu_device):
             outs.append(out)
         assert torch.equal(outs[0], outs[1])
         compare(outs[0].double().cpu().numpy(), *plain(data, table, q, lengths, news, kv_heads, group, dim, page, window, sinks), dim, "bf16")
+
+
+@pytest.mark.parametrize("group", (1, 40))
+def test_offsets_that_are_none_reach_no_other_memory(gpu_device, group):
+    """Offsets that fall, overlap or lie outside: every request takes what lies between its two within 0 .. T, and nothing else is
+    written (Batch.run checks the rows after the last).  A request that stands alone gets what it gets otherwise."""
+    b = Batch(5, [600, 90, 70], [520, 20, 16], 1, group, 64, 16)
+    good, whole = b.cu.copy(), b.run()
+    for cu in ([0, 520, 300, 556], [-5, 520, 1 << 30, 7], [556, 0, -(1 << 31), 520], [0, 556, 0, 556]):
+        b.cu = np.array(cu, dtype=np.int32)
+        got = b.run(max_new=556)
+        if cu[1] == 520 and cu[0] <= 0 and cu[2] != 300:
+            assert np.array_equal(got[:520], whole[:520])
+    b.cu = good
+    assert np.array_equal(b.run(max_new=556), whole)
