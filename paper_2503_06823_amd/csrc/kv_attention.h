@@ -63,17 +63,23 @@ struct Request {
     int seq;    // tokens that can be seen, positions 0 .. seq-1
     int len;    // of the whole request: query i stands at len - n + i
 };
-__device__ __forceinline__ Request request(const AttentionArgs& a, int r) {
+__device__ __forceinline__ Request request(const AttentionArgs& a, int begin, int end, int len) {
     Request q;
-    int begin = a.cu_new[r], end = a.cu_new[r + 1];
     begin = begin < 0 ? 0 : begin < a.T ? begin : a.T;
     end = end < begin ? begin : end < a.T ? end : a.T;
     q.first = begin;
     q.n = end - begin < a.max_new ? end - begin : a.max_new;
-    q.len = a.seq_len[r];
+    q.len = len;
     const int most = a.width << a.page.log2_size;
     q.seq = q.len < 0 ? 0 : q.len < most ? q.len : most;
     return q;
+}
+__device__ __forceinline__ Request request(const AttentionArgs& a, int r) { return request(a, a.cu_new[r], a.cu_new[r + 1], a.seq_len[r]); }
+// r alike in a wavefront: through the scalar cache, for a vector load would wait for all that are on their way
+typedef const __attribute__((address_space(4))) int32_t* ScalarInts;
+__device__ __forceinline__ Request scalar_request(const AttentionArgs& a, int r) {
+    const ScalarInts cu_new = (ScalarInts)(a.cu_new + r), seq_len = (ScalarInts)(a.seq_len + r);
+    return request(a, cu_new[0], cu_new[1], seq_len[0]);
 }
 
 // The key tiles that queries at positions first .. last see: 0 .. sinks-1 and from .. to-1, the i-th of them.

@@ -159,7 +159,7 @@ __global__ __launch_bounds__(64 * kWaves, (WavesPerSimd<E, D>::n)) void attentio
     for (int unit = some ? start.shares.begin(blockIdx.x) : 0; unit < share_end;) {
         if (unit - before >= here.all(a.kv_heads)) {
             before += here.all(a.kv_heads);
-            q = uniform(request(a, ++r));
+            q = scalar_request(a, ++r);
             here = stretch(a, q, most_rows, shift);
             continue;
         }
@@ -195,9 +195,7 @@ __global__ __launch_bounds__(64 * kWaves, (WavesPerSimd<E, D>::n)) void attentio
         const int i_all = seen.count();
         int i_end = u_end < rounds ? u_end * (kWaves << shift) : i_all;
         while (i_end > 0 && seen.tile(i_end - 1) * kTok > p_last) --i_end;  // no row of this tile sees so far
-        // read through the scalar cache: a vector load here would wait for the tiles on their way
-        typedef const __attribute__((address_space(4))) int32_t* ScalarTable;
-        const ScalarTable table = (ScalarTable)(a.table + (size_t)r * a.width);
+        const ScalarInts table = (ScalarInts)(a.table + (size_t)r * a.width);
         const int page_mask = (1 << a.page.log2_size) - 1;
         const uint32_t head_bytes = (uint32_t)a.page.bytes(), page_stride = head_bytes * (uint32_t)a.kv_heads;
         const uint8_t* cache = a.cache + (size_t)kv_head * head_bytes;

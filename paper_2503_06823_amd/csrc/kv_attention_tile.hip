@@ -184,8 +184,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_tile_kernel(Attentio
     int i_end = i_begin + each < i_all ? i_begin + each : i_all;
     if (job.piece + 1 == job.pieces) i_end = i_all;
 
-    typedef const __attribute__((address_space(4))) int32_t* ScalarTable;
-    const ScalarTable table = (ScalarTable)(a.table + (size_t)r * a.width);
+    const ScalarInts table = (ScalarInts)(a.table + (size_t)r * a.width);
     const int page_mask = (1 << a.page.log2_size) - 1;
     const uint32_t head_bytes = (uint32_t)a.page.bytes(), page_stride = head_bytes * (uint32_t)a.kv_heads;
     const uint8_t* cache = a.cache + (size_t)kv_head * head_bytes;
