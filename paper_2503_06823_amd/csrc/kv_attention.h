@@ -111,6 +111,7 @@ __device__ __forceinline__ int few_rows(const AttentionArgs& a, FewRule rule) {
     if (rule.small <= rule.always) return rule.always;
     const int lane = threadIdx.x & 63;
     long long gain = 0;
+#pragma unroll 4
     for (int r = lane; r < a.R; r += 64) {
         const Request q = request(a, r);
         const long long rows = (long long)q.n * a.group, reach = (long long)a.window + a.sinks + q.n;

@@ -75,13 +75,16 @@ __device__ __forceinline__ Job find_job(const AttentionArgs& a, int least_rows, 
     Rows rows;
     int longest = 0;
     long long work = 0, row_tiles = 0;  // work: twice the key tiles of all
+#pragma unroll 4
     for (int r0 = 0; r0 < a.R; r0 += 64) {
         rows = rows_at(r0 + lane);
-        const int n = wave_top(rows.longest);
-        longest = n > longest ? n : longest;
-        work += readlane(wave_inclusive((long long)rows.row_tiles * (rows.longest + rows.shortest)), 63) * a.kv_heads;
-        row_tiles += readlane(wave_inclusive((long long)rows.row_tiles), 63) * a.kv_heads;
+        longest = rows.longest > longest ? rows.longest : longest;
+        work += (long long)rows.row_tiles * (rows.longest + rows.shortest);
+        row_tiles += rows.row_tiles;
     }
+    longest = wave_top(longest);
+    work = readlane(wave_inclusive(work), 63) * a.kv_heads;
+    row_tiles = readlane(wave_inclusive(row_tiles), 63) * a.kv_heads;
     Job job;
     job.found = false;
     job.all_slots = 0;
