@@ -89,6 +89,7 @@ __device__ __forceinline__ Job find_job(const AttentionArgs& a, int least_rows, 
     job.found = false;
     job.all_slots = 0;
     if (longest == 0 || row_tiles > 0x7fffffff) return job;  // so many only if cu_new is not a list of offsets
+    if (want >= places && want >= row_tiles && !to_the_end) return job;
     const int cus = places / 2;
     int each = longest;
     long long count = row_tiles;
@@ -480,8 +481,10 @@ hipError_t launch_attention_tile(const emoe_kv_desc& d, const AttentionArgs& a, 
     DeviceShape shape;
     hipError_t e = device_shape(&shape);
     if (e != hipSuccess) return e;
-    const long long per_request = ((long long)a.max_new * a.group + kRows - 1) / kRows, by_tokens = (long long)a.T * a.group / kRows + a.R;
-    const long long row_tiles = per_request * a.R < by_tokens ? per_request * a.R : by_tokens;
+    // Row tiles at most: n rows have (n - 1) / kRows + 1, and there are no more requests than of the fewest rows that come here.
+    const long long least = rule.always + 1, all_rows = (long long)a.T * a.group, requests = all_rows / least < a.R ? all_rows / least : a.R;
+    const long long per_request = ((long long)a.max_new * a.group + kRows - 1) / kRows, by_rows = requests + (all_rows - requests) / kRows;
+    const long long row_tiles = per_request * a.R < by_rows ? per_request * a.R : by_rows;
     // whole row tiles, or pieces of them that find places at the same time
     const int places = 2 * shape.groups;
     static_assert(2 * kMaxGroups <= kTileSlots, "a slot for every piece");
