@@ -167,39 +167,44 @@ __device__ __forceinline__ void to_operands(const float* x, bf16x8* out) {
 
 // bf16 queries as two e4m3 operands of the scaled matrix instructions: the nearest, and 16 times what it leaves.  A bf16 number has eight
 // significant bits, four for each, so that their sum is the number up to 2^-21 of the largest of its row.
-// The bits of the largest magnitude of eight numbers, and of `top`:
+// The magnitudes' bits are compared two a word: a larger number has larger ones, and a NaN the largest.
+typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t larger_bits(uint32_t two, uint32_t other_two) {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2v, two), __builtin_bit_cast(ushort2v, other_two)));
+}
 __device__ __forceinline__ uint32_t largest_bits(const uint4& eight, uint32_t top) {
     const uint32_t words[4] = {eight.x, eight.y, eight.z, eight.w};
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const uint32_t lower = words[e] << 16 & 0x7fff0000u, upper = words[e] & 0x7fff0000u, m = lower > upper ? lower : upper;
-        top = m > top ? m : top;
-    }
+    for (int e = 0; e < 4; ++e) top = larger_bits(top, words[e] & 0x7fff7fffu);
     return top;
 }
-// A row's scale from its largest: that comes below 2^8 (e4m3 reaches 448), what is left of it below 2^4.  `down`: what a number is
-// multiplied with, with the sign of the scores' scale; `nearest`, `rest`: scale bytes of the two operands.
+// A row's scale from its largest: that comes below 2^8 (e4m3 reaches 448), what is left of it below 2^4.
 struct QueryScale {
-    float down;
-    int nearest, rest;
+    float nearest, rest;
+    int nearest_byte, rest_byte;
+    uint32_t sign;  // of the scores' scale: it goes into the numbers
 };
 __device__ __forceinline__ QueryScale query_scale(uint32_t top, float scale) {
-    int e = (int)(top >> 23) - 127 - 7;
+    const uint32_t lower = top << 16, upper = top & 0xffff0000u;
+    int e = (int)((lower > upper ? lower : upper) >> 23) - 127 - 7;
     e = e < -118 ? -118 : e;
-    return {copysignf(__uint_as_float((uint32_t)(127 - e) << 23), scale), e + 127, e + 127 - 4};
+    return {__uint_as_float((uint32_t)(e + 127) << 23), __uint_as_float((uint32_t)(e + 127 - 4) << 23), e + 127, e + 127 - 4,
+            scale < 0.0f ? 0x80008000u : 0u};
 }
 // Four numbers, two a word.
-__device__ __forceinline__ void to_e4m3(uint32_t w0, uint32_t w1, float down, int* nearest, int* rest) {
-    const float y[4] = {__uint_as_float(w0 << 16) * down, __uint_as_float(w0 & 0xffff0000u) * down, __uint_as_float(w1 << 16) * down,
-                        __uint_as_float(w1 & 0xffff0000u) * down};
-    int hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-    hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], hi, true);
-    const float left[4] = {(y[0] - __builtin_amdgcn_cvt_f32_fp8(hi, 0)) * 16.0f, (y[1] - __builtin_amdgcn_cvt_f32_fp8(hi, 1)) * 16.0f,
-                           (y[2] - __builtin_amdgcn_cvt_f32_fp8(hi, 2)) * 16.0f, (y[3] - __builtin_amdgcn_cvt_f32_fp8(hi, 3)) * 16.0f};
-    int lo = __builtin_amdgcn_cvt_pk_fp8_f32(left[0], left[1], 0, false);
-    lo = __builtin_amdgcn_cvt_pk_fp8_f32(left[2], left[3], lo, true);
-    *nearest = hi;
-    *rest = lo;
+__device__ __forceinline__ void to_e4m3(uint32_t w0, uint32_t w1, const QueryScale& by, int* nearest, int* rest) {
+    typedef short short2v __attribute__((ext_vector_type(2)));
+    w0 ^= by.sign;
+    w1 ^= by.sign;
+    short2v hi = {0, 0}, lo = {0, 0};
+    hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_bit_cast(bf16x2, w0), by.nearest, false);
+    hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_bit_cast(bf16x2, w1), by.nearest, true);
+    *nearest = __builtin_bit_cast(int, hi);
+    const auto back0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(*nearest, by.nearest, false);
+    const auto back1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(*nearest, by.nearest, true);
+    lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, __uint_as_float(w0 << 16) - back0[0], __uint_as_float(w0 & 0xffff0000u) - back0[1], by.rest, false);
+    lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, __uint_as_float(w1 << 16) - back1[0], __uint_as_float(w1 & 0xffff0000u) - back1[1], by.rest, true);
+    *rest = __builtin_bit_cast(int, lo);
 }
 
 // Four rows (tokens) of one column (element) from row-major bf16 in LDS: of the 16 lanes of a group, lane j names the eight

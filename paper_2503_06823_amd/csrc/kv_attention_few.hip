@@ -290,14 +290,14 @@ __global__ __launch_bounds__(64 * kWaves, (WavesPerSimd<E, D>::n)) void attentio
             uint32_t top = 0;
 #pragma unroll
             for (int c = 0; c < LOADS; ++c) top = largest_bits(raw[c], top);
-            top = over_groups(top, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
+            top = over_groups(top, [](uint32_t x, uint32_t y) { return larger_bits(x, y); });
             const QueryScale by = query_scale(top, a.scale_log2);
-            q_scale = D == 128 ? by.nearest | by.rest << 8 : group < 2 ? by.nearest : by.rest;
+            q_scale = D == 128 ? by.nearest_byte | by.rest_byte << 8 : group < 2 ? by.nearest_byte : by.rest_byte;
 #pragma unroll
             for (int w = 0; w < 2 * LOADS; ++w) {
                 const uint32_t words[4] = {raw[w / 2].x, raw[w / 2].y, raw[w / 2].z, raw[w / 2].w};
                 int nearest, rest;
-                to_e4m3(words[2 * (w % 2)], words[2 * (w % 2) + 1], by.down, &nearest, &rest);
+                to_e4m3(words[2 * (w % 2)], words[2 * (w % 2) + 1], by, &nearest, &rest);
                 q_hi[w] = nearest;
                 if (D == 128) q_lo[w] = rest;
                 else q_hi[4 + w] = rest;

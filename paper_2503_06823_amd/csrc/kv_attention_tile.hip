@@ -269,16 +269,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_tile_kernel(Attentio
                 top = largest_bits(raw[s][c], top);
             }
         const uint32_t other = (uint32_t)__shfl_xor((int)top, 32);
-        top = other > top ? other : top;
+        top = larger_bits(top, other);
         const QueryScale by = query_scale(top, a.scale_log2);
-        q_scale = by.nearest | by.rest << 8;
+        q_scale = by.nearest_byte | by.rest_byte << 8;
 #pragma unroll
         for (int s = 0; s < STEPS; ++s)
 #pragma unroll
             for (int w = 0; w < 8; ++w) {
                 const uint32_t* words = reinterpret_cast<const uint32_t*>(&raw[s][w / 2]) + 2 * (w % 2);
                 int nearest, rest;
-                to_e4m3(words[0], words[1], by.down, &nearest, &rest);
+                to_e4m3(words[0], words[1], by, &nearest, &rest);
                 q_hi[s][w] = nearest;
                 q_lo[s][w] = rest;
             }
