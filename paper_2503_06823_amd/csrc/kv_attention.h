@@ -8,8 +8,11 @@ namespace emoe {
 // Work that is cut along the keys: pieces leave their outputs (fp32, not divided by the sum), maxima and sums in slots of the workspace, and
 // a launch at the end adds them.
 constexpr int kFewRows = 16;      // rows of a slot of the kernel for few queries
-constexpr int kFewPerCu = 3;      // workgroups of it that a CU holds, two slots each
-constexpr int kFewSlots = 2 * kFewPerCu * kMaxGroups;
+// Workgroups of it that a CU holds, two slots each, by their registers.  With rows of 64 elements a workgroup has half the bytes on their way: 64 decodes
+// of 500 to 8000 tokens on 16 heads 52 us with four, 56 with three, 57 with five (spills); short calls 0 to 3 % the other way.  fp32 of 128: 32 of them
+// to 4000 tokens on 8 heads 27 us with two, 35 with three, of which one waits for its place.
+constexpr int few_per_cu(int dim, bool bf16) { return dim == 64 && bf16 ? 4 : dim == 64 || bf16 ? 3 : 2; }
+constexpr int few_slots(int dim) { return 2 * few_per_cu(dim, true) * kMaxGroups; }
 constexpr int kTileRows = 128;    // of the kernel for many
 constexpr int kTileSlots = 2 * kMaxGroups;  // as many as run at the same time
 struct Piece {

@@ -75,9 +75,10 @@ size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 AttentionWs attention_ws(int dim, bool tiles) {
     AttentionWs w;
     w.few_records = 0;
-    w.few_sums = align256(kFewSlots * sizeof(Piece));
-    w.few_outputs = align256(w.few_sums + (size_t)kFewSlots * kFewRows * 8);
-    w.tile_count = align256(w.few_outputs + (size_t)kFewSlots * kFewRows * dim * 4);
+    const size_t slots = few_slots(dim);
+    w.few_sums = align256(slots * sizeof(Piece));
+    w.few_outputs = align256(w.few_sums + slots * kFewRows * 8);
+    w.tile_count = align256(w.few_outputs + slots * kFewRows * dim * 4);
     w.tile_records = w.tile_count + 256;
     w.tile_sums = align256(w.tile_records + kTileSlots * sizeof(Piece));
     w.tile_outputs = align256(w.tile_sums + (size_t)kTileSlots * kTileRows * 8);
@@ -117,7 +118,7 @@ hipError_t launch_attention(const emoe_kv_desc& d, const emoe_attention_desc& at
         }
     }
     const AttentionWs ws = attention_ws(d.head_dim, tiles);
-    static_assert((size_t)kFewSlots * (sizeof(Piece) + kFewRows * (8 + 128 * 4)) + (size_t)kTileSlots * (sizeof(Piece) + kTileRows * (8 + 128 * 4)) +
+    static_assert((size_t)few_slots(64) * (sizeof(Piece) + kFewRows * (8 + 128 * 4)) + (size_t)kTileSlots * (sizeof(Piece) + kTileRows * (8 + 128 * 4)) +
                           8 * 256 <= kAttentionWsBytes, "as include/emoe.h promises");
     int few_slots = 0;
     if (tiles) {

@@ -50,10 +50,6 @@ constexpr float kLazy = 8.0f;   // log2 of what a weight may grow to before the 
 template <class E> struct Pieces { static constexpr int n = 1; };
 template <> struct Pieces<float> { static constexpr int n = 3; };
 
-template <class E, int D> struct WavesPerSimd { static constexpr int n = 3; };
-template <> struct WavesPerSimd<float, 128> { static constexpr int n = 2; };
-template <> struct WavesPerSimd<float, 64> { static constexpr int n = 3; };
-
 // The work as one line of units: requests in order, of a request its kv heads, of a head its tiles of 16 rows, of those (a stretch) kFixed
 // units for its beginning and end and then the rounds of key tiles that the longest row sees, at least one.  Every workgroup takes an
 // equal part of the line, so that all of them end together whatever the lengths; a boundary within kSnap rounds of a stretch's beginning or
@@ -144,7 +140,7 @@ template <int D> struct Quarter { typedef uint32_t type __attribute__((ext_vecto
 template <> struct Quarter<64> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
 
 template <class E, int D>
-__global__ __launch_bounds__(64 * kWaves, (WavesPerSimd<E, D>::n)) void attention_few_kernel(AttentionArgs a, FewRule rule, int shift, AttentionWs lay) {
+__global__ __launch_bounds__(64 * kWaves, few_per_cu(D, sizeof(E) == 2)) void attention_few_kernel(AttentionArgs a, FewRule rule, int shift, AttentionWs lay) {
     constexpr int PIECES = Pieces<E>::n, STEPS = D / 32, BLOCKS = D / 16;
     constexpr bool SCALED = sizeof(E) == 2;  // K stays in 4 bits
     constexpr int V_STRIDE = D + 16;  // elements; 32 bytes past the row: 16 rows of 32 bytes fall on all banks alike
@@ -508,7 +504,7 @@ hipError_t launch_attention_few(const emoe_kv_desc& d, int dtype, const Attentio
     auto rounds_of = [&] { return ((most_tiles - 1) >> shift >> kLogWaves) + 1; };
     while (rounds_of() > 1 && stretches * (kFixed + rounds_of()) > 0x7fffffff - kLeastUnits) ++shift;
     const long long most_rounds = rounds_of(), line = stretches * (kFixed + most_rounds), shares = (line + kLeastUnits - 1) / kLeastUnits;
-    const int groups = shares < kFewPerCu * shape.groups ? (int)shares : kFewPerCu * shape.groups;
+    const int at_once = few_per_cu(d.head_dim, dtype == EMOE_BF16) * shape.groups, groups = shares < at_once ? (int)shares : at_once;
     *slots = most_rounds > 2 * kSnap + 1 ? 2 * groups : 0;  // none if no stretch is long enough to be cut
     auto run = [&](auto element, auto dim) {
         attention_few_kernel<decltype(element), decltype(dim)::value><<<(unsigned)groups, 64 * kWaves, 0, st>>>(a, rule, shift, ws);
