@@ -64,23 +64,33 @@ struct Job {
 // tile's time for kPerTile of them, and kCut for the first.  Every wavefront by itself, 64 requests a trip.
 constexpr float kTwo = 1.65f, kCut = 2.0f, kPerTile = 43.0f;
 constexpr int kLeastCut = 6;  // key tiles
-__device__ __forceinline__ Job find_job(const AttentionArgs& a, int least_rows, int places, int want, bool to_the_end) {
+// Requests come in the order of their longest row tiles where they are at most 64 with rows for this kernel (else as they are): `list` holds those of
+// this wavefront.
+__device__ __forceinline__ Job find_job(const AttentionArgs& a, int least_rows, int places, int want, bool to_the_end, int* list) {
     const int lane = threadIdx.x & 63;
     Request mine;
-    auto rows_at = [&](int r) {
+    Rows rows;
+    int id;
+    auto take = [&](int r) {
+        id = r;
         mine = {0, 0, 0, 0};
         if (r < a.R) mine = request(a, r);
-        return rows_of(a, mine, least_rows);
+        rows = rows_of(a, mine, least_rows);
     };
-    Rows rows;
-    int longest = 0;
+    int longest = 0, active = 0;
     long long work = 0, row_tiles = 0;  // work: twice the key tiles of all
 #pragma unroll 4
     for (int r0 = 0; r0 < a.R; r0 += 64) {
-        rows = rows_at(r0 + lane);
+        take(r0 + lane);
         longest = rows.longest > longest ? rows.longest : longest;
         work += (long long)rows.row_tiles * (rows.longest + rows.shortest);
         row_tiles += rows.row_tiles;
+        const unsigned long long some = __ballot(rows.row_tiles > 0);
+        if (a.R > 64 && rows.row_tiles > 0) {
+            const int at = active + __builtin_popcountll(some & ((1ull << lane) - 1));
+            if (at < 64) list[at] = id;
+        }
+        active += __builtin_popcountll(some);
     }
     longest = wave_top(longest);
     work = readlane(wave_inclusive(work), 63) * a.kv_heads;
@@ -90,14 +100,30 @@ __device__ __forceinline__ Job find_job(const AttentionArgs& a, int least_rows, 
     job.all_slots = 0;
     if (longest == 0 || row_tiles > 0x7fffffff) return job;  // so many only if cu_new is not a list of offsets
     if (want >= places && want >= row_tiles && !to_the_end) return job;
+    const bool at_hand = active <= 64;
+    if (at_hand && a.R > 64) take(lane < active ? list[lane] : a.R);
+    if (at_hand && active > 1) {
+        const unsigned long long some = __ballot(rows.row_tiles > 0), below = (1ull << lane) - 1;
+        int rank = active + __builtin_popcountll(~some & below);
+        if (rows.row_tiles > 0) rank = 0;
+        for (unsigned long long left = some; left != 0; left &= left - 1) {
+            const int at = __builtin_ctzll(left), other = __builtin_amdgcn_readlane(rows.longest, at);
+            if (rows.row_tiles > 0) rank += (other > rows.longest) | ((other == rows.longest) & (at < lane));
+        }
+        auto sorted = [&](int v) { return __builtin_amdgcn_ds_permute(4 * rank, v); };
+        id = sorted(id);
+        mine = {sorted(mine.first), sorted(mine.n), sorted(mine.seq), sorted(mine.len)};
+        rows = {sorted(rows.row_tiles), sorted(rows.longest), sorted(rows.shortest)};
+    }
+    const int end = at_hand ? 1 : a.R;  // of the trips
     const int cus = places / 2;
     int each = longest;
     long long count = row_tiles;
     if (row_tiles < places && longest > kLeastCut) {
         const int c = (longest + lane) / (lane + 1);  // this lane's estimate
         long long pieces = 0;
-        for (int r0 = 0; r0 < a.R; r0 += 64) {
-            if (a.R > 64) rows = rows_at(r0 + lane);
+        for (int r0 = 0; r0 < end; r0 += 64) {
+            if (!at_hand) take(r0 + lane);
             for (unsigned long long some = __ballot(rows.row_tiles > 0); some != 0; some &= some - 1) {
                 const int at = __builtin_ctzll(some);
                 pieces += (long long)(__builtin_amdgcn_readlane(rows.row_tiles, at) * a.kv_heads) *
@@ -116,8 +142,8 @@ __device__ __forceinline__ Job find_job(const AttentionArgs& a, int least_rows, 
     if (count <= places && want >= cus) want = want < count ? (int)count - 1 - (want - cus) : 0x7fffffff;
 
     int jobs = 0, slots = 0;
-    for (int r0 = 0; r0 < a.R; r0 += 64) {
-        if (a.R > 64) rows = rows_at(r0 + lane);
+    for (int r0 = 0; r0 < end; r0 += 64) {
+        if (!at_hand) take(r0 + lane);
         const int k = rows.row_tiles > 0 ? (rows.longest + each - 1) / each : 0;
         const int here = rows.row_tiles * a.kv_heads * k, cut_here = k > 1 ? here : 0;
         const int upto = (int)wave_inclusive((long long)here), cut_upto = (int)wave_inclusive((long long)cut_here);
@@ -132,7 +158,7 @@ __device__ __forceinline__ Job find_job(const AttentionArgs& a, int least_rows, 
             local /= a.kv_heads;
             job.row_tile = row_tiles - 1 - local % row_tiles;
             job.piece = local / row_tiles;
-            job.r = r0 + at;
+            job.r = __builtin_amdgcn_readlane(id, at);
             job.pieces = __builtin_amdgcn_readlane(k, at);
             job.each = each;
             job.slot = slots + __builtin_amdgcn_readlane(cut_upto, at) - __builtin_amdgcn_readlane(cut_here, at) +
@@ -167,10 +193,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_tile_kernel(Attentio
         unsigned long long nan[8][kWaves];
     };
     __shared__ Half halves[2];
+    __shared__ int list[kWaves][64];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const int col = lane & 31, group = lane >> 5;
 
-    const Job job = find_job(a, uniform(few_rows(a, rule)) + 1, places, blockIdx.x, blockIdx.x == 0);
+    const Job job = find_job(a, uniform(few_rows(a, rule)) + 1, places, blockIdx.x, blockIdx.x == 0, list[wave]);
     if (blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<int*>(a.ws + lay.tile_count) = job.all_slots;
     if (!job.found) return;
     const int r = uniform(job.r), kv_head = uniform(job.kv_head), row_tile = uniform(job.row_tile), pieces = uniform(job.pieces);
