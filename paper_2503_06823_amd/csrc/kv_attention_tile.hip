@@ -59,11 +59,15 @@ struct Job {
 
 // How row tiles are cut: so that the work is over soonest, in the time that a lone workgroup of a CU takes for a key tile.  Two on a CU take
 // kTwo times as long as one (one's products and the other's exponentials hardly overlap).  Whole row tiles take the longest one's tiles, or a CU's share
-// of all of them if that is more.  Else the longest is divided by 2 to 64, an estimate a lane: with pieces of c tiles there are n = sum of ceil(tiles /
-// c), which have to find places at the same time and take c, or kTwo c if some CU has two; a piece costs 64 KiB written and read again, a
-// tile's time for kPerTile of them, and kCut for the first.  Every wavefront by itself, 64 requests a trip.
-constexpr float kTwo = 1.65f, kCut = 2.0f, kPerTile = 43.0f;
+// of all of them if that is more.  Else the longest is divided by 2 to 64, an estimate a lane: pieces of c tiles take c if every CU has one at
+// most, kTwo c if it has two, and if there are more the longer of c and a CU's share, kUneven for what is not even and kBegin for a
+// second beginning; a piece of a row tile that is cut needs a slot, costs 64 KiB written and read again, a tile's time for kPerTile of them, and kCut for the first.  Every wavefront by
+// itself, 64 requests a trip.
+constexpr float kTwo = 1.65f, kCut = 3.0f, kPerTile = 43.0f, kUneven = 1.1f, kBegin = 3.0f;
 constexpr int kLeastCut = 6;  // key tiles
+// Workgroups beyond the places and the row tiles, for pieces of a row tile that is longer than all others: four prompts of 512 tokens on 100 to 8000
+// take 111 us with them, 160 without.  As they take some 1 us where none is cut, and more where each reads many lengths, only for few requests.
+__device__ __host__ __forceinline__ int extra_places(const AttentionArgs& a, int places) { return a.R <= 64 ? places / 4 : 0; }
 // Requests come in the order of their longest row tiles where they are at most 64 with rows for this kernel (else as they are): `list` holds those of
 // this wavefront.
 __device__ __forceinline__ Job find_job(const AttentionArgs& a, int least_rows, int places, int want, bool to_the_end, int* list) {
@@ -99,7 +103,11 @@ __device__ __forceinline__ Job find_job(const AttentionArgs& a, int least_rows, 
     job.found = false;
     job.all_slots = 0;
     if (longest == 0 || row_tiles > 0x7fffffff) return job;  // so many only if cu_new is not a list of offsets
-    if (want >= places && want >= row_tiles && !to_the_end) return job;
+    const int cus = places / 2;
+    const float share = 0.5f * kTwo * (float)work * 0.5f / (float)cus;
+    const bool may_cut = longest > kLeastCut && (float)longest > share;
+    const long long limit = (row_tiles > places ? row_tiles : places) + extra_places(a, places);
+    if (want >= (may_cut ? limit : row_tiles) && !to_the_end) return job;
     const bool at_hand = active <= 64;
     if (at_hand && a.R > 64) take(lane < active ? list[lane] : a.R);
     if (at_hand && active > 1) {
@@ -116,28 +124,29 @@ __device__ __forceinline__ Job find_job(const AttentionArgs& a, int least_rows, 
         rows = {sorted(rows.row_tiles), sorted(rows.longest), sorted(rows.shortest)};
     }
     const int end = at_hand ? 1 : a.R;  // of the trips
-    const int cus = places / 2;
     int each = longest;
     long long count = row_tiles;
-    if (row_tiles < places && longest > kLeastCut) {
+    if (may_cut) {
         const int c = (longest + lane) / (lane + 1);  // this lane's estimate
-        long long pieces = 0;
+        long long pieces = 0, cut = 0;
         for (int r0 = 0; r0 < end; r0 += 64) {
             if (!at_hand) take(r0 + lane);
             for (unsigned long long some = __ballot(rows.row_tiles > 0); some != 0; some &= some - 1) {
-                const int at = __builtin_ctzll(some);
-                pieces += (long long)(__builtin_amdgcn_readlane(rows.row_tiles, at) * a.kv_heads) *
-                          ((__builtin_amdgcn_readlane(rows.longest, at) + c - 1) / c);
+                const int at = __builtin_ctzll(some), k = (__builtin_amdgcn_readlane(rows.longest, at) + c - 1) / c;
+                const long long here = (long long)(__builtin_amdgcn_readlane(rows.row_tiles, at) * a.kv_heads) * k;
+                pieces += here;
+                if (k > 1) cut += here;
             }
         }
-        float time = fmaxf((float)longest, 0.25f * kTwo * (float)work / (float)cus);
-        if (lane > 0) time = (pieces <= cus ? 1.0f : kTwo) * (float)c + kCut + (float)pieces / kPerTile;
+        float time = fmaxf((float)c, share);
+        if (lane > 0) time = (pieces <= cus ? (float)c : pieces <= places ? kTwo * (float)c : kUneven * time + kBegin) + kCut + (float)cut / kPerTile;
         // the longest pieces of those that take least, to an eighth of a tile's time
-        const int saved = lane > 0 && pieces > places ? 0 : 0x7fffffff - (int)fminf(8.0f * time, 1e9f);
+        const int saved = cut > places || pieces > (limit < gridDim.x ? limit : gridDim.x) ? 0 : 0x7fffffff - (int)fminf(8.0f * time, 1e9f);
         const int best = __builtin_ctzll(__ballot(saved == wave_top(saved)));
         each = __builtin_amdgcn_readlane(c, best);
         count = readlane(pieces, best);
     }
+    if (want >= count && !to_the_end) return job;
     // The longest row tiles come first.  With two for a CU at most the last of them comes second, for the CU with the longest.
     if (count <= places && want >= cus) want = want < count ? (int)count - 1 - (want - cus) : 0x7fffffff;
 
@@ -512,10 +521,10 @@ hipError_t launch_attention_tile(const emoe_kv_desc& d, const AttentionArgs& a, 
     const long long least = rule.always + 1, all_rows = (long long)a.T * a.group, requests = all_rows / least < a.R ? all_rows / least : a.R;
     const long long per_request = ((long long)a.max_new * a.group + kRows - 1) / kRows, by_rows = requests + (all_rows - requests) / kRows;
     const long long row_tiles = per_request * a.R < by_rows ? per_request * a.R : by_rows;
-    // whole row tiles, or pieces of them that find places at the same time
+    // whole row tiles, or pieces of them
     const int places = 2 * shape.groups;
     static_assert(2 * kMaxGroups <= kTileSlots, "a slot for every piece");
-    const long long groups = row_tiles * a.kv_heads > places ? row_tiles * a.kv_heads : places;
+    const long long jobs = row_tiles * a.kv_heads, groups = jobs < places ? places : jobs + extra_places(a, places);
     if (groups > 0x7fffffff / 256) return hipErrorInvalidValue;
     if (d.head_dim == 64) attention_tile_kernel<64><<<(unsigned)groups, 64 * kWaves, 0, st>>>(a, rule, places, lay);
     else attention_tile_kernel<128><<<(unsigned)groups, 64 * kWaves, 0, st>>>(a, rule, places, lay);
