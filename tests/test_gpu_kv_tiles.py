@@ -141,3 +141,30 @@ def test_offsets_that_are_none_reach_no_other_memory(gpu_device, group):
             assert np.array_equal(got[:520], whole[:520])
     b.cu = good
     assert np.array_equal(b.run(max_new=556), whole)
+
+
+def _batches():
+    """Requests with rows for this kernel among up to 64 and among more; more than 64 of them; more row tiles than places, one request
+    far longer than the others, which is cut."""
+    g = np.random.default_rng(8)
+    few = [int(n) for n in g.integers(1, 400, 130)]
+    some = [520 if r in (3, 64, 65, 100, 129) else 1 for r in range(130)]
+    yield "five of 130", [n + m for n, m in zip(few, some)], some, 1, 2, 64, 16
+    yield "70 of 70", [int(n) for n in g.integers(40, 500, 70)], [40] * 70, 1, 16, 64, 16
+    yield "90 of 200", [int(n) for n in g.integers(40, 300, 200)], [40 if r % 20 < 9 else 1 for r in range(200)], 2, 16, 64, 32
+    yield "four of 512", [612, 4600, 812, 1500], [512] * 4, 8, 4, 128, 64
+    yield "eight, rising", [530 + 300 * r for r in range(8)], [520] * 8, 2, 2, 128, 16
+
+
+@pytest.mark.parametrize("name,lengths,news,kv_heads,group,dim,page", list(_batches()), ids=lambda v: v.replace(" ", "-") if isinstance(v, str) else "")
+def test_batches(gpu_device, name, lengths, news, kv_heads, group, dim, page):
+    from test_gpu_kv_attention import large, plain
+    data, table, q = large(len(lengths), lengths, news, kv_heads, group, dim, page)
+    kv = P.make_kv_desc(data.shape[0], page, kv_heads, dim, len(lengths), table.shape[1])
+    at = P.make_attention_desc(q.shape[0], q.shape[1], dim, "bf16", max(news))
+    n = P.emoe_kv_attention_workspace_bytes(kv, at)
+    ws, out = torch.full((n,), 255, dtype=torch.uint8, device="cuda"), torch.full_like(q, 3.0)
+    cu = torch.tensor(np.concatenate(([0], np.cumsum(news))), dtype=torch.int32, device="cuda")
+    P.emoe_kv_attention(kv, at, q, data, table, torch.tensor(lengths, dtype=torch.int32, device="cuda"), cu, out, ws, n)
+    torch.cuda.synchronize()
+    compare(out.double().cpu().numpy(), *plain(data, table, q, lengths, news, kv_heads, group, dim, page, 0, 0), dim, "bf16")
