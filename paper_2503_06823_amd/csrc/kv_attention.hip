@@ -7,7 +7,7 @@ namespace {
 // The pieces of rows that were cut, in the pieces' order.  A workgroup for every piece; those of one cut take its rows in turn.  A team of
 // lanes has four elements of a row each; where there are many pieces all teams share a row's, so that those of a long context are read side by
 // side, else every team has a row of its own.  Bound by its launch and two dependent reads: 4.8 us after 64 decodes, 5.4 after one long
-// one (96 pieces a row), 9 after two prompts of 512 tokens next to 14 decodes (33 MB of pieces).  More rows or pieces in flight a team, and 128 or 512
+// one (96 pieces a row), 9 after two prompts of 512 tokens next to 14 decodes (25 MB of pieces).  More rows or pieces in flight a team, and 128 or 512
 // threads, took as long or longer.
 constexpr int kJoinThreads = 256;
 constexpr int kOneTeam = 8;  // pieces that a team adds alone

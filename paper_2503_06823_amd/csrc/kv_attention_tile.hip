@@ -14,7 +14,7 @@
 // The tile after the next is on its way from memory while a tile is multiplied, the next one is written to the other half of LDS under the
 // scores' products; one barrier a tile.
 //
-// Split: a workgroup takes a row tile's keys whole, the longest first, where there are enough row tiles; else pieces of them (plan_tiles), which
+// Split: a workgroup takes a row tile's keys whole, the longest first, where there are enough row tiles; else pieces of them (find_job), which
 // leave fp32 outputs, maxima and sums in the workspace for a second launch to add.
 //
 // Measured: a prompt of 8192 tokens (32 heads on 8 of 128 elements) 474 to 486 us, 1.13 to 1.16 PFLOP/s of what the mask leaves.  The matrix cores
@@ -60,9 +60,9 @@ struct Job {
 // How row tiles are cut: so that the work is over soonest, in the time that a lone workgroup of a CU takes for a key tile.  Two on a CU take
 // kTwo times as long as one (one's products and the other's exponentials hardly overlap).  Whole row tiles take the longest one's tiles, or a CU's share
 // of all of them if that is more.  Else the longest is divided by 2 to 64, an estimate a lane: pieces of c tiles take c if every CU has one at
-// most, kTwo c if it has two, and if there are more the longer of c and a CU's share, kUneven for what is not even and kBegin for a
-// second beginning; a piece of a row tile that is cut needs a slot, costs 64 KiB written and read again, a tile's time for kPerTile of them, and kCut for the first.  Every wavefront by
-// itself, 64 requests a trip.
+// most, kTwo c if it has two, and if there are more the longer of c and a CU's share, kUneven for what is not even and kBegin for a second beginning; a
+// piece of a row tile that is cut needs a slot, costs 64 KiB written and read again, a tile's time for kPerTile of them, and kCut for the first.
+// Every wavefront by itself, 64 requests a trip.
 constexpr float kTwo = 1.65f, kCut = 3.0f, kPerTile = 43.0f, kUneven = 1.1f, kBegin = 3.0f;
 constexpr int kLeastCut = 6;  // key tiles
 // Workgroups beyond the places and the row tiles, for pieces of a row tile that is longer than all others: four prompts of 512 tokens on 100 to 8000
