@@ -65,6 +65,7 @@ struct Job {
 // Every wavefront by itself, 64 requests a trip.
 constexpr float kTwo = 1.65f, kCut = 3.0f, kPerTile = 43.0f, kUneven = 1.1f, kBegin = 3.0f;
 constexpr int kLeastCut = 6;  // key tiles
+constexpr int kAhead = 4;     // times 64 requests' lengths come together
 // Workgroups beyond the places and the row tiles, for pieces of a row tile that is longer than all others: four prompts of 512 tokens on 100 to 8000
 // take 111 us with them, 160 without.  As they take some 1 us where none is cut, and more where each reads many lengths, only for few requests.
 __device__ __host__ __forceinline__ int extra_places(const AttentionArgs& a, int places) { return a.R <= 64 ? places / 4 : 0; }
@@ -75,17 +76,15 @@ __device__ __forceinline__ Job find_job(const AttentionArgs& a, int least_rows, 
     Request mine;
     Rows rows;
     int id;
-    auto take = [&](int r) {
+    auto lengths = [&](int r) { return r < a.R ? request(a, r) : Request{0, 0, 0, 0}; };
+    auto take = [&](int r, const Request& q) {
         id = r;
-        mine = {0, 0, 0, 0};
-        if (r < a.R) mine = request(a, r);
-        rows = rows_of(a, mine, least_rows);
+        mine = q;
+        rows = rows_of(a, q, least_rows);
     };
     int longest = 0, active = 0;
     long long work = 0, row_tiles = 0;  // work: twice the key tiles of all
-#pragma unroll 4
-    for (int r0 = 0; r0 < a.R; r0 += 64) {
-        take(r0 + lane);
+    auto add = [&] {
         longest = rows.longest > longest ? rows.longest : longest;
         work += (long long)rows.row_tiles * (rows.longest + rows.shortest);
         row_tiles += rows.row_tiles;
@@ -95,6 +94,21 @@ __device__ __forceinline__ Job find_job(const AttentionArgs& a, int least_rows, 
             if (at < 64) list[at] = id;
         }
         active += __builtin_popcountll(some);
+    };
+    if (a.R <= 64) {
+        take(lane, lengths(lane));
+        add();
+    } else {
+        for (int r0 = 0; r0 < a.R; r0 += 64 * kAhead) {
+            Request ahead[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) ahead[k] = lengths(r0 + 64 * k + lane);
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                take(r0 + 64 * k + lane, ahead[k]);
+                add();
+            }
+        }
     }
     longest = wave_top(longest);
     work = readlane(wave_inclusive(work), 63) * a.kv_heads;
@@ -109,7 +123,10 @@ __device__ __forceinline__ Job find_job(const AttentionArgs& a, int least_rows, 
     const long long limit = (row_tiles > places ? row_tiles : places) + extra_places(a, places);
     if (want >= (may_cut ? limit : row_tiles) && !to_the_end) return job;
     const bool at_hand = active <= 64;
-    if (at_hand && a.R > 64) take(lane < active ? list[lane] : a.R);
+    if (at_hand && a.R > 64) {
+        const int r = lane < active ? list[lane] : a.R;
+        take(r, lengths(r));
+    }
     if (at_hand && active > 1) {
         const unsigned long long some = __ballot(rows.row_tiles > 0), below = (1ull << lane) - 1;
         int rank = active + __builtin_popcountll(~some & below);
@@ -130,7 +147,7 @@ __device__ __forceinline__ Job find_job(const AttentionArgs& a, int least_rows, 
         const int c = (longest + lane) / (lane + 1);  // this lane's estimate
         long long pieces = 0, cut = 0;
         for (int r0 = 0; r0 < end; r0 += 64) {
-            if (!at_hand) take(r0 + lane);
+            if (!at_hand) take(r0 + lane, lengths(r0 + lane));
             for (unsigned long long some = __ballot(rows.row_tiles > 0); some != 0; some &= some - 1) {
                 const int at = __builtin_ctzll(some), k = (__builtin_amdgcn_readlane(rows.longest, at) + c - 1) / c;
                 const long long here = (long long)(__builtin_amdgcn_readlane(rows.row_tiles, at) * a.kv_heads) * k;
@@ -152,7 +169,7 @@ __device__ __forceinline__ Job find_job(const AttentionArgs& a, int least_rows, 
 
     int jobs = 0, slots = 0;
     for (int r0 = 0; r0 < end; r0 += 64) {
-        if (!at_hand) take(r0 + lane);
+        if (!at_hand) take(r0 + lane, lengths(r0 + lane));
         const int k = rows.row_tiles > 0 ? (rows.longest + each - 1) / each : 0;
         const int here = rows.row_tiles * a.kv_heads * k, cut_here = k > 1 ? here : 0;
         const int upto = (int)wave_inclusive((long long)here), cut_upto = (int)wave_inclusive((long long)cut_here);
