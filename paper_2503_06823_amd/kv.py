@@ -78,11 +78,11 @@ class KvCache:
                             stream)
         return out
 
-    def release(self, ended: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    def release(self, ended: Optional[torch.Tensor] = None, stream=None) -> None:
         """Ends the step: rows with `ended` != 0 (int32 [rows] on the device, None: nobody) give all their pages back and start
         anew, rows that were refused keep what they held."""
         before, after = self.length
-        with torch.cuda.stream(stream):
+        with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
             torch.maximum(after, before, out=after)  # no request gets shorter: a refused row's length is 0
             B.emoe_kv_release(self.desc, before, after, ended, self.window, self.sinks, self.block_table, self.free_pages,
                               self.counters[0], self.counters[1], stream)

@@ -104,3 +104,65 @@ def test_a_refused_row_keeps_what_it_holds(gpu_device):
     assert step([0, 10])[0] == 0 and kv.length[0].tolist() == [0, 20]
     with pytest.raises(ValueError):
         kv.plan(torch.tensor([60, 60], **i32), 120)
+
+
+def test_two_steps_as_a_graph(gpu_device):
+    """Two decode steps (the counters and lengths change places) captured once and replayed with other inputs, with work of another kind
+    between the replays: the same as the calls themselves."""
+    i32 = dict(dtype=torch.int32, device="cuda")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    kvs = [P.KvCache.allocate(2, 4, 200, 40, 16, 2, 128, 256, window=90, sinks=4) for _ in range(2)]
+    prompts = [70, 3, 120, 31]
+    x = torch.randn((sum(prompts), 12, 128), generator=g, device="cuda").bfloat16()
+    for kv in kvs:
+        kv.plan(torch.tensor(prompts, **i32), sum(prompts))
+        for layer in range(2):
+            kv.append(layer, x[:, 8:10], x[:, 10:])
+        kv.release()
+    rows = torch.empty((2, 4, 12, 128), device="cuda").bfloat16()  # of two steps
+    outs = [torch.zeros((2, 2, 4, 8, 128), device="cuda").bfloat16() for _ in range(2)]
+    ones, ended = torch.ones(4, **i32), torch.zeros(4, **i32)
+
+    def steps(kv, out):
+        for s in range(2):
+            kv.plan(ones, 4)
+            for layer in range(2):
+                kv.append(layer, rows[s, :, 8:10], rows[s, :, 10:])
+                kv.attend(layer, rows[s, :, :8], out[s, layer], 1)
+            kv.release(ended)
+
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        steps(kvs[0], outs[0])
+    for n in range(8):
+        rows.copy_(torch.randn(rows.shape, generator=g, device="cuda"))
+        ended.copy_(torch.tensor([0, n == 2, 0, n == 5], **i32))
+        graph.replay()
+        torch.cuda.synchronize()
+        steps(kvs[1], outs[1])
+        (outs[1].float() @ torch.ones(128, device="cuda")).sum().item()
+        assert torch.equal(outs[0], outs[1]) and outs[0].any()
+        assert torch.equal(kvs[0].length[0], kvs[1].length[0]) and free(kvs[0]) == free(kvs[1])
+        assert torch.equal(kvs[0].block_table, kvs[1].block_table) and kvs[0].refused.item() == 0
+
+
+def test_a_step_on_another_stream(gpu_device):
+    """Everything on a stream that is not the current one, as an object and as its address."""
+    i32 = dict(dtype=torch.int32, device="cuda")
+    x = torch.randn((30, 3, 64), device="cuda").bfloat16()
+    results = []
+    for stream in (None, torch.cuda.Stream(), torch.cuda.Stream().cuda_stream):
+        kv = P.KvCache.allocate(1, 2, 64, 8, 16, 1, 64, 32)
+        new, ended, out = torch.tensor([20, 10], **i32), torch.tensor([0, 1], **i32), torch.empty((30, 1, 64), device="cuda").bfloat16()
+        torch.cuda.synchronize()
+        kv.plan(new, 30, stream)
+        kv.append(0, x[:, 1:2], x[:, 2:], stream)
+        kv.attend(0, x[:, :1], out, 20, stream=stream)
+        kv.release(ended, stream)
+        torch.cuda.synchronize()
+        results.append((out, kv.length[0].tolist(), free(kv)))
+    assert results[0][1] == [20, 0] and results[0][2] == [2, 3, 4, 5, 6, 7]
+    for r in results[1:]:
+        assert torch.equal(r[0], results[0][0]) and r[1:] == results[0][1:]
