@@ -59,6 +59,13 @@ constexpr float kLowest = -3.0e38f;  // of a running maximum: finite, so that no
 // no vector registers.
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
+// An address made of a scalar base and a lane's offset, which a load adds itself if it finds the offset in 32 bits; widened ahead of a loop, as the
+// compiler likes to, it takes 64-bit additions of the vector units (8192 tokens' prompt 477 us instead of 466, decodes 1 % more).
+__device__ __forceinline__ const uint8_t* lane_at(const uint8_t* base, uint32_t offset) {
+    asm volatile("" : "+v"(offset));
+    return base + offset;
+}
+
 // A request's queries and keys, from the lengths on the device, whatever these hold.
 struct Request {
     int first;  // its first query's token

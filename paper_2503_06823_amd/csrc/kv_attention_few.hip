@@ -246,16 +246,16 @@ __global__ __launch_bounds__(64 * kWaves, few_per_cu(D, sizeof(E) == 2)) void at
         Words k0, k1, v0, v1;
         uint32_t k_scale0, k_scale1, v_scale0, v_scale1;
         auto load_keys = [&](const Place& p) {
-            k0 = *reinterpret_cast<const Words*>(p.codes0 + in_at);
-            k1 = *reinterpret_cast<const Words*>(p.codes1 + in_at);
-            k_scale0 = p.scales0[k_scale_at];
-            k_scale1 = p.scales1[k_scale_at];
+            k0 = *reinterpret_cast<const Words*>(lane_at(p.codes0, in_at));
+            k1 = *reinterpret_cast<const Words*>(lane_at(p.codes1, in_at));
+            k_scale0 = *lane_at(p.scales0, k_scale_at);
+            k_scale1 = *lane_at(p.scales1, k_scale_at);
         };
         auto load_values = [&](const Place& p) {
-            v0 = *reinterpret_cast<const Words*>(p.codes0 + a.page.codes + in_at);
-            v1 = *reinterpret_cast<const Words*>(p.codes1 + a.page.codes + in_at);
-            v_scale0 = (p.scales0 + a.page.scales)[v_scale_at];
-            v_scale1 = (p.scales1 + a.page.scales)[v_scale_at];
+            v0 = *reinterpret_cast<const Words*>(lane_at(p.codes0 + a.page.codes, in_at));
+            v1 = *reinterpret_cast<const Words*>(lane_at(p.codes1 + a.page.codes, in_at));
+            v_scale0 = *lane_at(p.scales0 + a.page.scales, v_scale_at);
+            v_scale1 = *lane_at(p.scales1 + a.page.scales, v_scale_at);
         };
 
         floatx4 out[BLOCKS];

@@ -268,10 +268,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_tile_kernel(Attentio
     Words k_in, v_in;
     uint32_t k_byte, v_byte;
     auto load = [&](const Place& p) {
-        k_in = *reinterpret_cast<const Words*>(p.codes + in_at);
-        v_in = *reinterpret_cast<const Words*>(p.codes + a.page.codes + in_at);
-        k_byte = p.scales[scale_at];
-        v_byte = (p.scales + a.page.scales)[scale_at];
+        k_in = *reinterpret_cast<const Words*>(lane_at(p.codes, in_at));
+        v_in = *reinterpret_cast<const Words*>(lane_at(p.codes + a.page.codes, in_at));
+        k_byte = *lane_at(p.scales, scale_at);
+        v_byte = *lane_at(p.scales + a.page.scales, scale_at);
     };
     // In LDS the 64-byte piece b of V's row t lies in place b ^ v_swizzle(t), so that the four rows of a transposed read fall on all banks, and
     // in odd rows the 16-byte pieces of a pair are swapped, so that the two rows that eight lanes write do; the 16-byte chunk c of K's
