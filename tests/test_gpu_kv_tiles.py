@@ -168,3 +168,40 @@ def test_batches(gpu_device, name, lengths, news, kv_heads, group, dim, page):
     P.emoe_kv_attention(kv, at, q, data, table, torch.tensor(lengths, dtype=torch.int32, device="cuda"), cu, out, ws, n)
     torch.cuda.synchronize()
     compare(out.double().cpu().numpy(), *plain(data, table, q, lengths, news, kv_heads, group, dim, page, 0, 0), dim, "bf16")
+
+
+def test_pages_beyond_four_gib(gpu_device):
+    """A request whose pages are the last of a cache of more than 4 GiB, the same request's in a small one: the same bits."""
+    from test_gpu_kv_attention import large
+    lengths, news, page, dim = [700], [530], 256, 128
+    data, table, q = large(3, lengths, news, 1, 1, dim, page)
+    small = data.shape[0]
+    pages = (1 << 32) // data[0].numel() + 9
+    far = torch.empty((pages, *data.shape[1:]), dtype=torch.uint8, device="cuda")
+    far[-small:] = data
+    outs = []
+    for cache, at_table in ((data, table), (far, table + (pages - small))):
+        kv = P.make_kv_desc(cache.shape[0], page, 1, dim, 1, table.shape[1])
+        at = P.make_attention_desc(530, 1, dim, "bf16", 530)
+        n = P.emoe_kv_attention_workspace_bytes(kv, at)
+        ws, out = torch.empty(n, dtype=torch.uint8, device="cuda"), torch.empty_like(q)
+        i32 = dict(dtype=torch.int32, device="cuda")
+        P.emoe_kv_attention(kv, at, q, cache, at_table.contiguous(), torch.tensor(lengths, **i32), torch.tensor([0, 530], **i32), out, ws, n)
+        torch.cuda.synchronize()
+        outs.append(out)
+    assert far.numel() > 1 << 32 and torch.equal(*outs) and outs[0].any()
+
+
+@pytest.mark.parametrize("dim", (64, 128))
+def test_large_values_under_rising_scores(gpu_device, dim):
+    """Values near 2^88 while the weights climb towards where the maximum is looked for again: fp32 has room for both."""
+    b = Batch(10, [330], [17], 1, 32, dim, 16)
+    for j in range(330):
+        s = b.slot(0, j)
+        codes = np.zeros((1, dim), dtype=np.uint8)
+        codes[0, 0] = 4  # 2 * 2^k along the first axis
+        b.cache.write(s, 0, codes, np.full((1, dim // 32), 127 + j // 110, dtype=np.uint8))
+        b.cache.write(s, 1, np.full((1, dim), 6 + 8 * (j % 2), dtype=np.uint8), np.full((1, dim // 32), 127 + 85, dtype=np.uint8))
+    b.q[:, :, 0] = 3.0
+    got = b.check(scale=1.0)
+    assert np.isfinite(got).all() and np.abs(got).max() > 2.0 ** 80
