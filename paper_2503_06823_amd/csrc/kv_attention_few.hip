@@ -25,7 +25,7 @@
 // a wavefront is held in scalar registers (page numbers, addresses): in vector registers it took 16 of them and half the
 // instructions, and the lookup of a page waited for the tiles on their way.
 //
-// Measured (32 heads on 8 of 128 elements; with the sum of pieces): 64 requests of 500 to 16383 tokens 69 to 72 us (322 MB), one of 131072 37 to 39
+// Measured (32 heads on 8 of 128 elements; with the sum of pieces): 64 requests of 500 to 16383 tokens 68 to 71 us (322 MB), one of 131072 37 to 39
 // (143 MB), 32 behind windows of 4096 31 to 32 (116 MB).  The walk itself reads 6.1 to 6.9 TB/s, where a plain read stream reaches 6.9; the
 // same launches without the walk take 15 us (20 with 64 requests: more beginnings): two launches 4, from the lengths to the first tiles
 // 5, the end of a stretch 3, the sum of pieces 3.  All three wavefronts of a SIMD together spend 1.4 us of instructions on a round of

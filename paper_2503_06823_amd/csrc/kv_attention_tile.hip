@@ -17,7 +17,7 @@
 // Split: a workgroup takes a row tile's keys whole, the longest first, where there are enough row tiles; else pieces of them (find_job), which
 // leave fp32 outputs, maxima and sums in the workspace for a second launch to add.
 //
-// Measured: a prompt of 8192 tokens (32 heads on 8 of 128 elements) 474 to 486 us, 1.13 to 1.16 PFLOP/s of what the mask leaves.  The matrix cores
+// Measured: a prompt of 8192 tokens (32 heads on 8 of 128 elements) 466 to 478 us, 1.15 to 1.18 PFLOP/s of what the mask leaves.  The matrix cores
 // are busy for 54 % of the cycles and the vector units for 49 %, next to nothing of it at the same time, at a clock of 1.85 to 2.05 GHz that power
 // sets.  Prompts of 512, 1024, 2048 and 4096 tokens: 20, 30, 50 and 144 us (1024: 37 if two pieces share a CU; 2048: 54 if the last of two row tiles for
 // a CU does not go with the first).  Slower: scores of the next tile ahead of this one's exponentials (519 us against 504 without staging under the products), a third
