@@ -518,10 +518,9 @@ int emoe_kv_attention_workspace_bytes(const emoe_kv_desc *desc, const emoe_atten
  * n + i and sees the tokens j <= p with window == 0, j > p - window, or j < sinks.
  *   out[t][h] = sum_j softmax_j(scale * q[t][h] . k_j) v_j, fp32 sums; zeros where nothing is seen (p < 0).
  * q [T][q_heads][head_dim] and out dev, dtype, rows as the strides say, 16-byte aligned; block_table, seq_len, cu_new as
- * emoe_kv_plan leaves them.  Lengths are read on the device only.  bf16: the weights of the softmax are rounded to
- * bf16 for the product with the values, and scores are off by up to 2.5e-5 (8e-7 rms) of the sum of their terms'
- * magnitudes, as the matrix cores add products of 4 and 8 bits; fp32: nothing is rounded below fp32.  NaN or infinite tokens make NaN of what sees them,
- * and of nothing else.  Rows of out from cu_new[R] on are not written.  Results do not depend on the order of
+ * emoe_kv_plan leaves them.  Lengths are read on the device only.  Scores are sums in fp32 of exact products.  bf16: the weights of the
+ * softmax are rounded to bf16 for the product with the values; fp32: nothing is rounded below fp32.  NaN or infinite tokens make NaN of
+ * what sees them, and of nothing else.  Rows of out from cu_new[R] on are not written.  Results do not depend on the order of
  * execution.  ws dev, 16-byte aligned, not shared with a call that may run at the same time.
  * Limits: q_heads / kv_heads <= 256, T * q_heads < 2^31 / 16, max_new <= T.
  */

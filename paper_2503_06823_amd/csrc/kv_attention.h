@@ -51,7 +51,6 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
-typedef int intx8 __attribute__((ext_vector_type(8)));
 
 constexpr float kLowest = -3.0e38f;  // of a running maximum: finite, so that nothing minus it is a NaN
 
@@ -175,46 +174,10 @@ __device__ __forceinline__ void to_operands(const float* x, bf16x8* out) {
         }
 }
 
-// bf16 queries as two e4m3 operands of the scaled matrix instructions: the nearest, and 16 times what it leaves.  A bf16 number has eight
-// significant bits, four for each, so that their sum is the number up to 2^-21 of the largest of its row.
-// The magnitudes' bits are compared two a word: a larger number has larger ones, and a NaN the largest.
-typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ uint32_t larger_bits(uint32_t two, uint32_t other_two) {
-    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2v, two), __builtin_bit_cast(ushort2v, other_two)));
-}
-__device__ __forceinline__ uint32_t largest_bits(const uint4& eight, uint32_t top) {
-    const uint32_t words[4] = {eight.x, eight.y, eight.z, eight.w};
-#pragma unroll
-    for (int e = 0; e < 4; ++e) top = larger_bits(top, words[e] & 0x7fff7fffu);
-    return top;
-}
-// A row's scale from its largest: that comes below 2^8 (e4m3 reaches 448), what is left of it below 2^4.
-struct QueryScale {
-    float nearest, rest;
-    int nearest_byte, rest_byte;
-    uint32_t sign;  // of the scores' scale: it goes into the numbers
-};
-__device__ __forceinline__ QueryScale query_scale(uint32_t top, float scale) {
-    const uint32_t lower = top << 16, upper = top & 0xffff0000u;
-    int e = (int)((lower > upper ? lower : upper) >> 23) - 127 - 7;
-    e = e < -118 ? -118 : e;
-    return {__uint_as_float((uint32_t)(e + 127) << 23), __uint_as_float((uint32_t)(e + 127 - 4) << 23), e + 127, e + 127 - 4,
-            scale < 0.0f ? 0x80008000u : 0u};
-}
-// Four numbers, two a word.
-__device__ __forceinline__ void to_e4m3(uint32_t w0, uint32_t w1, const QueryScale& by, int* nearest, int* rest) {
-    typedef short short2v __attribute__((ext_vector_type(2)));
-    w0 ^= by.sign;
-    w1 ^= by.sign;
-    short2v hi = {0, 0}, lo = {0, 0};
-    hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_bit_cast(bf16x2, w0), by.nearest, false);
-    hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_bit_cast(bf16x2, w1), by.nearest, true);
-    *nearest = __builtin_bit_cast(int, hi);
-    const auto back0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(*nearest, by.nearest, false);
-    const auto back1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(*nearest, by.nearest, true);
-    lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, __uint_as_float(w0 << 16) - back0[0], __uint_as_float(w0 & 0xffff0000u) - back0[1], by.rest, false);
-    lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, __uint_as_float(w1 << 16) - back1[0], __uint_as_float(w1 & 0xffff0000u) - back1[1], by.rest, true);
-    *rest = __builtin_bit_cast(int, lo);
+// Eight elements of a bf16 query.  The sign of the scores' scale goes into them.
+__device__ __forceinline__ bf16x8 signed_query(const uint4& raw, float scale) {
+    const uint32_t sign = scale < 0.0f ? 0x80008000u : 0u;
+    return __builtin_bit_cast(bf16x8, uint4{raw.x ^ sign, raw.y ^ sign, raw.z ^ sign, raw.w ^ sign});
 }
 
 // Four rows (tokens) of one column (element) from row-major bf16 in LDS: of the 16 lanes of a group, lane j names the eight

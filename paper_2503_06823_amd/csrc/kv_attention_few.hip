@@ -7,12 +7,12 @@
 // its four wavefronts take tiles of 32 tokens in turn, each with a maximum, a sum and an output of its own, so that nothing waits in
 // the walk; they meet once, at its end.  The matrix instructions' token and element orders are free as long as both operands
 // agree, and are chosen so that no data moves between lanes but V's:
-//   - K of bf16 queries stays in 4 bits: v_mfma_scale_f32_16x16x128_f8f6f4 takes it with its scales, and q as two 8-bit operands (to_e4m3), for D =
-//     128 one after the other, for D = 64 side by side.  Its sums are off by 8e-7 (rms; 2.5e-5 at worst) of the sum of magnitudes.  Converting K
-//     to bf16 took a seventh of the vector instructions (64 decodes 74.4 us against 73.3, windows 34.9 against 33.6).
-//   - fp32 queries and weights are three bf16 operands each, which is exact to fp32, as a 4-bit number is in bf16.  Lane (row = lane % 16, group =
-//     lane / 16) holds D / 4 consecutive elements of one token's key, which lie in one block; step s multiplies its eight elements s, of all
-//     groups, with q's.
+//   - K becomes bf16 in registers, which is exact, and so are its products with bf16 queries; fp32 queries and weights are three bf16 operands each,
+//     exact to fp32.  Lane (row = lane % 16, group = lane / 16) holds D / 4 consecutive elements of one token's key, which lie in one
+//     block; step s multiplies its eight elements s, of all groups, with q's.  The scaled matrix instructions, which take K in 4 bits, want q in 8:
+//     two such numbers under a scale lose what a channel has 2^-14 below the largest, and are no faster (64 decodes 68.6 us either way, 1024 of 20 to
+//     600 tokens 84 with bf16, 91 with them).
+//   - Weights of bf16 calls are rounded to bf16: one product instead of three, with the bits that the result keeps.
 //   - P^T comes out of S^T in the registers in which the second product wants it: lane (query, group) holds tokens 4 group .. +3
 //     of each 16, and V's rows are taken in that order.
 //   - V: converted to bf16 where its scale is one per lane, through LDS (a wavefront's own), read back transposed.
@@ -143,7 +143,6 @@ template <> struct Quarter<64> { typedef uint32_t type __attribute__((ext_vector
 template <class E, int D, bool ONE_PAGE>
 __global__ __launch_bounds__(64 * kWaves, few_per_cu(D, sizeof(E) == 2)) void attention_few_kernel(AttentionArgs a, FewRule rule, int shift, AttentionWs lay) {
     constexpr int PIECES = Pieces<E>::n, STEPS = D / 32, BLOCKS = D / 16;
-    constexpr bool SCALED = sizeof(E) == 2;  // K stays in 4 bits
     constexpr int V_STRIDE = D + 16;  // elements; 32 bytes past the row: 16 rows of 32 bytes fall on all banks alike
     constexpr int V_BYTES = kTok * V_STRIDE * 2, WAVE_BYTES = V_BYTES + kTok * D / 2;  // V as bf16, K as it comes
     static_assert(WAVE_BYTES % 16 == 0 && BLOCKS * 1024 <= WAVE_BYTES, "the outputs take V's place at the end");
@@ -186,13 +185,13 @@ __global__ __launch_bounds__(64 * kWaves, few_per_cu(D, sizeof(E) == 2)) void at
         const int position = row < rows ? q.len - q.n + token : -1;  // -1 sees nothing
 
         const E* q_at = static_cast<const E*>(a.q) + (int64_t)(q.first + token) * a.q_stride + (int64_t)head * D;
-        constexpr int LOADS = D / 32;
-        uint4 raw[LOADS];  // of bf16 queries
-        if constexpr (SCALED) {
+        bf16x8 query[PIECES][STEPS];
+        if constexpr (PIECES == 1) {  // sent for before the first tiles are
 #pragma unroll
-            for (int c = 0; c < LOADS; ++c) {
-                raw[c] = uint4{0, 0, 0, 0};
-                if (row < rows) raw[c] = *reinterpret_cast<const uint4*>(q_at + 16 * group + 64 * (c / 2) + 8 * (c % 2));
+            for (int s = 0; s < STEPS; ++s) {
+                uint4 raw = {0, 0, 0, 0};
+                if (row < rows) raw = *reinterpret_cast<const uint4*>(q_at + group * (D / 4) + 8 * s);
+                query[0][s] = __builtin_bit_cast(bf16x8, raw);
             }
         }
 
@@ -211,14 +210,10 @@ __global__ __launch_bounds__(64 * kWaves, few_per_cu(D, sizeof(E) == 2)) void at
         // L1 cache per lane).  Keys go through LDS, where quarter q of token t lies in place q ^ swizzle(t), to lane (token, quarter).
         const int in_tok = lane >> 2, quarter = lane & 3;
         const uint32_t in_at = in_tok * (D / 2) + quarter * (D / 8), v_scale_at = in_tok * (D / 32) + quarter * (D / 4) / 32;
-        // In fp32 lane (token, group) takes quarter `group` of the token's keys; in bf16 the 32 elements of block `group`, for D = 64 of
-        // block group % 2.
-        constexpr int K_WORDS = SCALED ? 4 : D / 32, K_PARTS = D / 8 / K_WORDS;
-        const int k_part = group % K_PARTS;
-        const uint32_t k_scale_at = col * (D / 32) + k_part * K_WORDS * 8 / 32;
-        auto swizzle = [](int t) { return (t >> (D == 128 ? 2 : 3)) & (K_PARTS - 1); };
-        char* k_to = k_lds + in_tok * (D / 2) + ((quarter * K_PARTS / 4) ^ swizzle(in_tok)) * (4 * K_WORDS) + quarter % (4 / K_PARTS) * (D / 8);
-        const char* k_from = k_lds + col * (D / 2) + (k_part ^ swizzle(col)) * (4 * K_WORDS);
+        const uint32_t k_scale_at = col * (D / 32) + group * (D / 4) / 32;
+        auto swizzle = [](int t) { return (t >> (D == 128 ? 2 : 3)) & 3; };
+        char* k_to = k_lds + in_tok * (D / 2) + (quarter ^ swizzle(in_tok)) * (D / 8);
+        const char* k_from = k_lds + col * (D / 2) + (group ^ swizzle(col)) * (D / 8);
         bf16_t* v_to = v_lds + in_tok * V_STRIDE + quarter * (D / 4);
         const bf16_t* v_from = v_lds + (4 * group + (col >> 2)) * V_STRIDE + 4 * (col & 3);
 
@@ -285,26 +280,9 @@ __global__ __launch_bounds__(64 * kWaves, few_per_cu(D, sizeof(E) == 2)) void at
         // Scores are compared before they are scaled: the scale is positive, its sign goes into q.  A scale of zero becomes next to nothing, so
         // that it does not meet an infinity.
         const float scale = fmaxf(fabsf(a.scale_log2), 1e-37f);
-        bf16x8 query[SCALED ? 1 : PIECES][SCALED ? 1 : STEPS];
-        intx8 q_hi, q_lo;  // for D = 64 both are in q_hi
-        int q_scale;
-        if constexpr (SCALED) {
-            // a lane's bytes 0 .. 15 are elements 16 group on of the 128 of a product, 16 .. 31 those 64 further on; its scale is of elements 32 group on
-            uint32_t top = 0;
+        if constexpr (PIECES == 1) {
 #pragma unroll
-            for (int c = 0; c < LOADS; ++c) top = largest_bits(raw[c], top);
-            top = over_groups(top, [](uint32_t x, uint32_t y) { return larger_bits(x, y); });
-            const QueryScale by = query_scale(top, a.scale_log2);
-            q_scale = D == 128 ? by.nearest_byte | by.rest_byte << 8 : group < 2 ? by.nearest_byte : by.rest_byte;
-#pragma unroll
-            for (int w = 0; w < 2 * LOADS; ++w) {
-                const uint32_t words[4] = {raw[w / 2].x, raw[w / 2].y, raw[w / 2].z, raw[w / 2].w};
-                int nearest, rest;
-                to_e4m3(words[2 * (w % 2)], words[2 * (w % 2) + 1], by, &nearest, &rest);
-                q_hi[w] = nearest;
-                if (D == 128) q_lo[w] = rest;
-                else q_hi[4 + w] = rest;
-            }
+            for (int s = 0; s < STEPS; ++s) query[0][s] = signed_query(__builtin_bit_cast(uint4, query[0][s]), a.scale_log2);
         } else {
             float x[8];
 #pragma unroll
@@ -343,28 +321,20 @@ __global__ __launch_bounds__(64 * kWaves, few_per_cu(D, sizeof(E) == 2)) void at
             load_values(next);
             *reinterpret_cast<Words*>(k_to) = k0;
             *reinterpret_cast<Words*>(k_to + 16 * D / 2) = k1;
-            const uint32_t byte0 = k_scale0, byte1 = k_scale1;
+            const float scale0 = scale_of_byte(k_scale0), scale1 = scale_of_byte(k_scale1);
             load_keys(next);
-            auto scores = [&](const char* from, uint32_t byte) {
+            auto scores = [&](const char* from, float by) {
+                const Words words = *reinterpret_cast<const Words*>(from);
                 floatx4 s = {0.0f, 0.0f, 0.0f, 0.0f};
-                if constexpr (SCALED) {
-                    const int4 w = *reinterpret_cast<const int4*>(from);
-                    const intx8 key = {w.x, w.y, w.z, w.w, 0, 0, 0, 0};
-                    if constexpr (D == 128) s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(key, q_lo, s, 4, 0, 0, (int)byte, 1, q_scale);
-                    s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(key, q_hi, s, 4, 0, 0, (int)byte, 0, q_scale);
-                } else {
-                    const Words words = *reinterpret_cast<const Words*>(from);
-                    const float by = scale_of_byte(byte);
 #pragma unroll
-                    for (int st = 0; st < STEPS; ++st) {
-                        const bf16x8 key = from_codes(words[st], by);
+                for (int st = 0; st < STEPS; ++st) {
+                    const bf16x8 key = from_codes(words[st], by);
 #pragma unroll
-                        for (int p = PIECES - 1; p >= 0; --p) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, query[p][st], s, 0, 0, 0);
-                    }
+                    for (int p = PIECES - 1; p >= 0; --p) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, query[p][st], s, 0, 0, 0);
                 }
                 return s;
             };
-            const floatx4 z0 = scores(k_from, byte0), z1 = scores(k_from + 16 * D / 2, byte1);
+            const floatx4 z0 = scores(k_from, scale0), z1 = scores(k_from + 16 * D / 2, scale1);
             float z[8] = {z0[0], z0[1], z0[2], z0[3], z1[0], z1[1], z1[2], z1[3]};
             if (!whole) {
                 const int from = a.window > 0 && position >= a.window ? position - a.window + 1 : 0;

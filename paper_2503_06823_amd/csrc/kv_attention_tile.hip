@@ -5,24 +5,21 @@
 // Bound by the matrix cores (4 * D flop a query, head and visible token), next to them by the exponentials and by LDS.  A workgroup
 // has 128 rows (query token, query head) of one kv head, 32 a wavefront, and walks the keys in tiles of 64; two workgroups share a
 // CU, so that one's exponentials run under the other's products.
-//   - K stays in 4 bits all the way: v_mfma_scale_f32_32x32x64_f8f6f4 takes it as it lies in the cache, with its scales, and q as two
-//     8-bit operands (to_e4m3).  The product's sums are off by 8e-7 (rms; 2.5e-5 at worst) of the sum of magnitudes.  It takes the
-//     time of a product in bf16, but a quarter of the LDS bytes for K, and no conversion: with K as
-//     bf16 the fragment reads of 32 rows a wavefront take LDS as long as the products take the matrix cores.
-//   - V is converted to bf16 once for the workgroup on its way into LDS and read back transposed.
-//   - P^T comes out of S^T in the registers in which the second product wants it.
+//   - K and V are converted to bf16, exactly, once for the workgroup on their way into LDS; V is read back transposed.  K in 4 bits on the scaled
+//     matrix instructions takes a quarter of its LDS bytes and no conversion (a prompt of 8192 tokens 474 us instead of 528), but wants q in 8
+//     bits: two such numbers under a scale lose what a channel has 2^-14 below the largest, and scores far more than that where keys are weak in the large
+//     channels.
+//   - P^T comes out of S^T in the registers in which the second product wants it, rounded to bf16: one product, with the bits that the result keeps.
 // The tile after the next is on its way from memory while a tile is multiplied, the next one is written to the other half of LDS under the
 // scores' products; one barrier a tile.
 //
 // Split: a workgroup takes a row tile's keys whole, the longest first, where there are enough row tiles; else pieces of them (find_job), which
 // leave fp32 outputs, maxima and sums in the workspace for a second launch to add.
 //
-// Measured: a prompt of 8192 tokens (32 heads on 8 of 128 elements) 466 to 478 us, 1.15 to 1.18 PFLOP/s of what the mask leaves.  The matrix cores
-// are busy for 54 % of the cycles and the vector units for 49 %, next to nothing of it at the same time, at a clock of 1.85 to 2.05 GHz that power
-// sets.  Prompts of 512, 1024, 2048 and 4096 tokens: 20, 30, 50 and 144 us (1024: 37 if two pieces share a CU; 2048: 54 if the last of two row tiles for
-// a CU does not go with the first).  Slower: scores of the next tile ahead of this one's exponentials (519 us against 504 without staging under the products), a third
-// wavefront a SIMD (633: it spills); a higher priority in the products changes nothing.  What e4m3 leaves of q in 6 bits instead of
-// 8 is faster, but loses what strong scores need (an element-wise bound is missed by four times).
+// Measured: a prompt of 8192 tokens (32 heads on 8 of 128 elements) 528 us, 1.04 PFLOP/s of what the mask leaves; prompts of 512, 1024, 2048 and 4096
+// tokens: 20, 30, 51 and 151 us.  Measured before K was bf16: two pieces on one CU 37 us for 1024 tokens where 29 otherwise, 54 where 48 for 2048 if the
+// last of two row tiles for a CU does not go with the first; scores of the next tile ahead of this one's exponentials 519 where 504 for 8192, a third
+// wavefront a SIMD 633 (it spilled); a higher priority in the products changes nothing.
 #include <math.h>
 
 #include "kv_attention.h"
@@ -206,13 +203,12 @@ template <> struct Quarter<64> { typedef uint32_t type __attribute__((ext_vector
 
 template <int D>
 __global__ __launch_bounds__(64 * kWaves, 2) void attention_tile_kernel(AttentionArgs a, FewRule rule, int places, AttentionWs lay) {
-    constexpr int STEPS = D / 64, BLOCKS = D / 32, SCALES = D / 32;
-    constexpr int V_ROW = 2 * D, K_ROW = D / 2;
+    constexpr int STEPS = D / 16, BLOCKS = D / 32, SCALES = D / 32;
+    constexpr int ROW = 2 * D;  // bytes of a token's keys or values in LDS
     typedef typename Quarter<D>::type Words;
     struct Half {
-        __attribute__((aligned(16))) char v[kTok * V_ROW];  // bf16
-        __attribute__((aligned(16))) char k[kTok * K_ROW];
-        __attribute__((aligned(16))) uint8_t k_scale[kTok * SCALES];
+        __attribute__((aligned(16))) char v[kTok * ROW];  // bf16
+        __attribute__((aligned(16))) char k[kTok * ROW];
         // of a wavefront's 16 tokens: 1, some block of values is NaN; 2, their page is nobody's.  Which blocks: bit 4 t + quarter.  Eight copies,
         // so that all lanes can write without a branch.
         __attribute__((aligned(16))) int odd[8][kWaves];
@@ -275,20 +271,22 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_tile_kernel(Attentio
     };
     // In LDS the 64-byte piece b of V's row t lies in place b ^ v_swizzle(t), so that the four rows of a transposed read fall on all banks, and
     // in odd rows the 16-byte pieces of a pair are swapped, so that the two rows that eight lanes write do; the 16-byte chunk c of K's
-    // row t lies in c ^ k_swizzle(t).
+    // row t lies in k_place(c) ^ k_swizzle(t), so that a chunk of eight or sixteen rows does, and what eight lanes write (1 % faster than c ^ t % 16).
     auto v_swizzle = [](int t) { return D == 128 ? t & 3 : (t >> 1) & 1; };
-    auto k_swizzle = [](int t) { return D == 128 ? (t >> 2) & 3 : 0; };
-    const int v_to = in_tok * V_ROW + (((quarter * (D / 4) / 32) ^ v_swizzle(in_tok)) * 64) + (D == 128 ? 0 : (quarter & 1) * 32);
+    auto k_swizzle = [](int t) { return D == 128 ? (t & 1) << 2 | (t >> 1 & 3) | (t & 8) : t & 7; };
+    const int v_to = in_tok * ROW + (((quarter * (D / 4) / 32) ^ v_swizzle(in_tok)) * 64) + (D == 128 ? 0 : (quarter & 1) * 32);
     const int v_even = v_to + (in_tok & 1) * 16, v_odd = v_to + 16 - (in_tok & 1) * 16;
-    const int k_to = in_tok * K_ROW + (((quarter * (D / 8) / 16) ^ k_swizzle(in_tok)) * 16) + (D == 128 ? 0 : (quarter & 1) * 8);
+    const int k_to = in_tok * ROW, k_turn = k_swizzle(in_tok);
+    auto k_place = [](int chunk) { return D == 128 ? chunk >> 2 | (chunk & 3) << 2 : chunk; };
     auto write = [&](Half& h, const Place& p) {
         const bool there = p.owned & (p.t0 + in_tok < q.seq);
         uint32_t byte = there ? v_byte : 127u;  // never written: any number will do
         const unsigned long long nan = __ballot(byte == 255);
         h.nan[lane & 7][wave] = nan;
         h.odd[lane & 7][wave] = (nan != 0 ? 1 : 0) | (p.owned ? 0 : 2);
-        h.k_scale[in_tok * SCALES + quarter * (D / 4) / 32] = (uint8_t)k_byte;
-        *reinterpret_cast<Words*>(h.k + k_to) = k_in;
+        const float k_scale = scale_of_byte(k_byte);
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) *reinterpret_cast<bf16x8*>(h.k + k_to + ((k_place(quarter * (D / 32) + e) ^ k_turn) * 16)) = from_codes(k_in[e], k_scale);
         const float scale = scale_of_byte(byte == 255 ? 127u : byte);
 #pragma unroll
         for (int e = 0; e < D / 32; ++e) *reinterpret_cast<bf16x8*>(h.v + (e % 2 == 0 ? v_even : v_odd) + 32 * (e / 2)) = from_codes(v_in[e], scale);
@@ -304,37 +302,18 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_tile_kernel(Attentio
         after = place(i_begin + 2 < i_end ? i_begin + 2 : i_end - 1);
     }
 
-    // q as two e4m3 operands.  Lane (col, group) holds elements 64 s + 16 group .. +15 and 32 further on of its row; one scale a row.
+    // Lane (col, group) holds elements 16 s + 8 group .. +7 of its row.
     const int row = w_row0 + col, token = a.token_of(row), head = kv_head * a.group + row - token * a.group;
     const int position = row < rows ? p0 + token : -1;  // -1 sees nothing
-    intx8 q_hi[STEPS], q_lo[STEPS];
-    int q_scale;
+    bf16x8 query[STEPS];
     {
-        uint4 raw[STEPS][4];
-        const bf16_t* at = static_cast<const bf16_t*>(a.q) + (int64_t)(q.first + token) * a.q_stride + (int64_t)head * D + group * 16;
-        uint32_t top = 0;
+        const bf16_t* at = static_cast<const bf16_t*>(a.q) + (int64_t)(q.first + token) * a.q_stride + (int64_t)head * D + group * 8;
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                raw[s][c] = uint4{0, 0, 0, 0};
-                if (row < rows) raw[s][c] = *reinterpret_cast<const uint4*>(at + 64 * s + 32 * (c / 2) + 8 * (c % 2));
-                top = largest_bits(raw[s][c], top);
-            }
-        const uint32_t other = (uint32_t)__shfl_xor((int)top, 32);
-        top = larger_bits(top, other);
-        const QueryScale by = query_scale(top, a.scale_log2);
-        q_scale = by.nearest_byte | by.rest_byte << 8;
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s)
-#pragma unroll
-            for (int w = 0; w < 8; ++w) {
-                const uint32_t* words = reinterpret_cast<const uint32_t*>(&raw[s][w / 2]) + 2 * (w % 2);
-                int nearest, rest;
-                to_e4m3(words[0], words[1], by, &nearest, &rest);
-                q_hi[s][w] = nearest;
-                q_lo[s][w] = rest;
-            }
+        for (int s = 0; s < STEPS; ++s) {
+            uint4 raw = {0, 0, 0, 0};
+            if (row < rows) raw = *reinterpret_cast<const uint4*>(at + 16 * s);
+            query[s] = signed_query(raw, a.scale_log2);
+        }
     }
 
     floatx16 out[BLOCKS];
@@ -347,11 +326,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_tile_kernel(Attentio
 
     // fragment addresses: K's row is the lane's column index; V's rows 4 group + (lane % 16) / 4 of every eight, four columns each
     const int sub = (lane >> 4) & 1, v_row = 4 * group + ((lane & 15) >> 2);
-    int k_from[STEPS], v_from[BLOCKS];
+    const int k_from = col * ROW, k_from_turn = k_swizzle(col);  // 32 rows further on it is the same
+    int v_from[BLOCKS];
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) k_from[s] = col * K_ROW + (((2 * s + group) ^ k_swizzle(col)) * 16);
-#pragma unroll
-    for (int b = 0; b < BLOCKS; ++b) v_from[b] = v_row * V_ROW + ((b ^ v_swizzle(v_row)) * 64) + sub * 32 + ((((lane & 3) >> 1) ^ (v_row & 1)) * 16) + (lane & 1) * 8;
+    for (int b = 0; b < BLOCKS; ++b) v_from[b] = v_row * ROW + ((b ^ v_swizzle(v_row)) * 64) + sub * 32 + ((((lane & 3) >> 1) ^ (v_row & 1)) * 16) + (lane & 1) * 8;
 
     auto barrier = [] {
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -362,23 +340,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_tile_kernel(Attentio
     // that it does not meet an infinity.
     const float scale = fmaxf(fabsf(a.scale_log2), 1e-37f);
     auto scores = [&](const Half& h, int tb) {
-        int byte;
-        if (D == 128) byte = (int)(*reinterpret_cast<const uint32_t*>(h.k_scale + (32 * tb + col) * SCALES) >> (8 * group));
-        else byte = h.k_scale[(32 * tb + col) * SCALES + group];
         floatx16 z;
 #pragma unroll
         for (int e = 0; e < 16; ++e) z[e] = 0.0f;
 #pragma unroll
         for (int st = 0; st < STEPS; ++st) {
-            const int4 w = *reinterpret_cast<const int4*>(h.k + k_from[st] + 32 * tb * K_ROW);
-            const intx8 key = {w.x, w.y, w.z, w.w, 0, 0, 0, 0};
-            if (st == 0) {
-                z = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(key, q_lo[st], z, 4, 0, 0, byte, 1, q_scale);
-                z = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(key, q_hi[st], z, 4, 0, 0, byte, 0, q_scale);
-            } else {
-                z = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(key, q_lo[st], z, 4, 0, 2, byte, 1, q_scale);
-                z = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(key, q_hi[st], z, 4, 0, 2, byte, 0, q_scale);
-            }
+            const bf16x8 key = *reinterpret_cast<const bf16x8*>(h.k + k_from + 32 * tb * ROW + ((k_place(2 * st + group) ^ k_from_turn) * 16));
+            z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key, query[st], z, 0, 0, 0);
         }
         return z;
     };
@@ -458,8 +426,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_tile_kernel(Attentio
                     shortx4 half[2];
                     bf16x8 all;
                 } f;
-                f.half[0] = read_transposed(reinterpret_cast<const bf16_t*>(here.v + v_from[b] + (16 * k) * V_ROW));
-                f.half[1] = read_transposed(reinterpret_cast<const bf16_t*>(here.v + v_from[b] + (16 * k + 8) * V_ROW));
+                f.half[0] = read_transposed(reinterpret_cast<const bf16_t*>(here.v + v_from[b] + (16 * k) * ROW));
+                f.half[1] = read_transposed(reinterpret_cast<const bf16_t*>(here.v + v_from[b] + (16 * k + 8) * ROW));
                 out[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.all, w[k], out[b], 0, 0, 0);
             }
     };
