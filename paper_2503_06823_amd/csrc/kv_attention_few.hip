@@ -310,9 +310,9 @@ __global__ __launch_bounds__(64 * kWaves, few_per_cu(D, sizeof(E) == 2)) void at
                 if (!(t0 + in_tok < q.seq && now.owned0)) v_scale0 = 127;
                 if (!(t0 + 16 + in_tok < q.seq && now.owned1)) v_scale1 = 127;
             }
-            const unsigned long long nan0 = __ballot(v_scale0 == 255), nan1 = __ballot(v_scale1 == 255);
+            const unsigned long long nan0 = __ballot(v_scale0 > kLastScale), nan1 = __ballot(v_scale1 > kLastScale);
             auto write_values = [&](const Words& words, uint32_t byte, bf16_t* to) {
-                const float scale = scale_of_byte(byte == 255 ? 127 : byte);
+                const float scale = scale_of_byte(byte > kLastScale ? 127 : byte);
 #pragma unroll
                 for (int e = 0; e < D / 32; ++e) *reinterpret_cast<bf16x8*>(to + 8 * e) = from_codes(words[e], scale);
             };
@@ -346,7 +346,7 @@ __global__ __launch_bounds__(64 * kWaves, few_per_cu(D, sizeof(E) == 2)) void at
                 }
             }
             if ((nan0 | nan1) != 0) {
-                // bit 4 t + quarter of nan0: the value of token t.  V holds numbers there; what sees it becomes NaN at the end
+                // bit 4 t + quarter of nan0: the value of token t is none, or may be infinite.  V holds numbers there; what sees it becomes NaN at the end
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
                     bad |= z[e] != -INFINITY ? (uint32_t)((e < 4 ? nan0 : nan1) >> (16 * group + 4 * (e % 4))) & 15u : 0u;

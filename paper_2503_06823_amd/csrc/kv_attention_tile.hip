@@ -209,7 +209,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_tile_kernel(Attentio
     struct Half {
         __attribute__((aligned(16))) char v[kTok * ROW];  // bf16
         __attribute__((aligned(16))) char k[kTok * ROW];
-        // of a wavefront's 16 tokens: 1, some block of values is NaN; 2, their page is nobody's.  Which blocks: bit 4 t + quarter.  Eight copies,
+        // of a wavefront's 16 tokens: 1, some block of values is NaN or may be infinite; 2, their page is nobody's.  Which blocks: bit 4 t + quarter.  Eight copies,
         // so that all lanes can write without a branch.
         __attribute__((aligned(16))) int odd[8][kWaves];
         unsigned long long nan[8][kWaves];
@@ -281,13 +281,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_tile_kernel(Attentio
     auto write = [&](Half& h, const Place& p) {
         const bool there = p.owned & (p.t0 + in_tok < q.seq);
         uint32_t byte = there ? v_byte : 127u;  // never written: any number will do
-        const unsigned long long nan = __ballot(byte == 255);
+        const unsigned long long nan = __ballot(byte > kLastScale);
         h.nan[lane & 7][wave] = nan;
         h.odd[lane & 7][wave] = (nan != 0 ? 1 : 0) | (p.owned ? 0 : 2);
         const float k_scale = scale_of_byte(k_byte);
 #pragma unroll
         for (int e = 0; e < D / 32; ++e) *reinterpret_cast<bf16x8*>(h.k + k_to + ((k_place(quarter * (D / 32) + e) ^ k_turn) * 16)) = from_codes(k_in[e], k_scale);
-        const float scale = scale_of_byte(byte == 255 ? 127u : byte);
+        const float scale = scale_of_byte(byte > kLastScale ? 127u : byte);
 #pragma unroll
         for (int e = 0; e < D / 32; ++e) *reinterpret_cast<bf16x8*>(h.v + (e % 2 == 0 ? v_even : v_odd) + 32 * (e / 2)) = from_codes(v_in[e], scale);
     };

@@ -5,6 +5,7 @@
 namespace emoe {
 
 constexpr int kKvBlock = 32;                        // elements that share a scale
+constexpr uint32_t kLastScale = 252;                // largest scale byte whose codes all fit in fp32 and bf16: 6 * 2^125
 constexpr size_t kAttentionWsBytes = 64ull << 20;   // no call needs more
 
 // Host-side checks; EMOE_OK or an error.
