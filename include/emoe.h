@@ -484,7 +484,8 @@ int emoe_kv_release(const emoe_kv_desc *desc, const int32_t *len_before, const i
  * Keys and values of T tokens into their slots.  k, v: dev, element type dtype (emoe_dtype), row t of head h
  * at element t * stride + h * head_dim (strides of at least kv_heads * head_dim, multiples of 8: a slice of a fused
  * projection's output will do); 16-byte aligned.  slot [T] int32 dev, all different where >= 0.  A block's scale
- * is the smallest power of two s >= 2^-126 with max|x| <= 7 s; its codes are the values nearest to x / s, ties to
+ * is the smallest power of two s >= 2^-126 with max|x| <= 7 s, 2^125 if that is less (6 * 2^125 is the largest number of the format that fp32
+ * and bf16 hold, so that finite numbers stay finite); its codes are the values nearest to x / s, ties to
  * the even code, beyond 6 the 6: all of it exact, so that the bits depend on nothing but the input.  A block
  * that holds an infinity or a NaN is stored as NaN (scale byte 255).
  */

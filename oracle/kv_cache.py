@@ -12,13 +12,13 @@ CODE_VALUES = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
 
 
 def scale_exponent(amax: float) -> int:
-    """The smallest k >= -126 with amax <= 7 * 2^k."""
+    """The smallest k of -126 .. 125 with amax <= 7 * 2^k, 125 if there is none: 6 * 2^125 is below 2^128, 4 * 2^126 is not."""
     if amax == 0.0:
         return -126
     k = math.frexp(amax)[1] - 5  # amax >= 2^(k+4): too small for sure
     while amax > math.ldexp(7.0, k):
         k += 1
-    return max(k, -126)
+    return min(max(k, -126), 125)
 
 
 def code_of(x: float) -> int:

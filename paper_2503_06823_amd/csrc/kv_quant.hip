@@ -64,7 +64,7 @@ __device__ __forceinline__ uint32_t quantise(const float* x, uint32_t* scale_byt
     const bool finite = top < 0x7f800000u;
     // amax = 1.m * 2^(e - 127) <= 7 * 2^k = 1.75 * 2^(k + 2)
     int byte = (int)(top >> 23) - 2 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
-    byte = byte < 1 ? 1 : byte;
+    byte = byte < 1 ? 1 : byte > (int)kLastScale ? (int)kLastScale : byte;  // no code stands for what passes the range
     byte = finite ? byte : 255;
     const float scale = __uint_as_float((uint32_t)byte << 23);
     uint32_t codes = 0;
