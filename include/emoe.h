@@ -521,7 +521,8 @@ int emoe_kv_attention_workspace_bytes(const emoe_kv_desc *desc, const emoe_atten
  * q [T][q_heads][head_dim] and out dev, dtype, rows as the strides say, 16-byte aligned; block_table, seq_len, cu_new as
  * emoe_kv_plan leaves them.  Lengths are read on the device only.  Scores are sums in fp32 of exact products.  bf16: the weights of the
  * softmax are rounded to bf16 for the product with the values; fp32: nothing is rounded below fp32.  NaN or infinite tokens make NaN of
- * what sees them, and of nothing else; so does a block of values whose scale byte lets codes pass fp32's range (253, 254).  Rows of out from cu_new[R] on are not written.  Results do not depend on the order of
+ * what sees them, and of nothing else; so does a block of values whose scale byte lets codes pass fp32's range (253, 254).  What finite values add up to
+ * stays finite.  Rows of out from cu_new[R] on are not written.  Results do not depend on the order of
  * execution.  ws dev, 16-byte aligned, not shared with a call that may run at the same time.
  * Limits: q_heads / kv_heads <= 256, T * q_heads < 2^31 / 16, max_new <= T.
  */

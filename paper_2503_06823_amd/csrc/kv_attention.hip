@@ -11,6 +11,7 @@ namespace {
 // threads, took as long or longer.
 constexpr int kJoinThreads = 256;
 constexpr int kOneTeam = 8;  // pieces that a team adds alone
+constexpr float kRoom = 10.0f;   // log2 of more pieces than there are: their sum is no larger than the values
 constexpr int kTileJoiners = 2;  // workgroups of a piece of the kernel for many, which has eight times the rows
 template <class E, int D>
 __global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(AttentionArgs a, AttentionWs lay, int few_slots) {
@@ -39,7 +40,7 @@ __global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(AttentionA
                 const size_t at = row_of(n, row);
                 const float2 s = sums[at];
                 const floatx4 o = *reinterpret_cast<const floatx4*>(outputs + at * D + 4 * lane);
-                const float up = fmaxf(top, s.x), f = __builtin_amdgcn_exp2f(top - up), g = __builtin_amdgcn_exp2f(s.x - up);
+                const float up = fmaxf(top, s.x), f = __builtin_amdgcn_exp2f(top - up), g = __builtin_amdgcn_exp2f(s.x - up - kRoom);
                 top = up;
                 all = all * f + s.y * g;
                 v = v * f + o * g;
@@ -118,6 +119,7 @@ hipError_t launch_attention(const emoe_kv_desc& d, const emoe_attention_desc& at
         }
     }
     const AttentionWs ws = attention_ws(d.head_dim, tiles);
+    static_assert(few_slots(64) / 2 <= 1 << (int)kRoom && few_slots(128) / 2 <= 1 << (int)kRoom, "a piece a workgroup");
     static_assert((size_t)few_slots(64) * (sizeof(Piece) + kFewRows * (8 + 128 * 4)) + (size_t)kTileSlots * (sizeof(Piece) + kTileRows * (8 + 128 * 4)) +
                           8 * 256 <= kAttentionWsBytes, "as include/emoe.h promises");
     int few_slots = 0;

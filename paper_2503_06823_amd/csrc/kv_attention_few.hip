@@ -196,8 +196,10 @@ __global__ __launch_bounds__(64 * kWaves, few_per_cu(D, sizeof(E) == 2)) void at
         }
 
         const Tiles seen = uniform(tiles<kTok>(a, q.seq, q.len - q.n, q.len - 1));
-        const int i_all = seen.count();
+        const int i_begin = u_begin * (kWaves << shift), i_all = seen.count();
         int i_end = u_end < rounds ? u_end * (kWaves << shift) : i_all;
+        // What is added to the maximum, so that all weights together are below 1 and outputs no larger than the values: of at most 2^lift / 2^kLazy tokens.
+        const float lift = kLazy + 5.0f + (float)(32 - __builtin_clz((uint32_t)(i_end > i_begin ? i_end - i_begin : 1)));
         while (i_end > 0 && seen.tile(i_end - 1) * kTok > p_last) --i_end;  // no row of this tile sees so far
         const ScalarInts table = (ScalarInts)(a.table + (size_t)r * a.width);
         const int page_mask = (1 << a.page.log2_size) - 1;
@@ -268,7 +270,7 @@ __global__ __launch_bounds__(64 * kWaves, few_per_cu(D, sizeof(E) == 2)) void at
 
         // Tile i + 4's values and keys are on their way from where tile i's have been used on, and its page is looked up a tile earlier.  The first
         // tile's are sent for before the queries are.
-        int i = u_begin * (kWaves << shift) + wave;
+        int i = i_begin + wave;
         const int last = i_end - 1;  // past the end: the last tile again, unused
         Place now, next;
         if (i < i_end) {
@@ -355,8 +357,8 @@ __global__ __launch_bounds__(64 * kWaves, few_per_cu(D, sizeof(E) == 2)) void at
 #pragma unroll
             for (int e = 1; e < 8; ++e) top = fmaxf(top, z[e]);
             top = over_groups(top, [](float x, float y) { return fmaxf(x, y); }) * scale;
-            if (__any(top > most + kLazy)) {  // the weights stay below 2^8: a maximum that rises by less is not worth a pass over the output
-                const float up = fmaxf(most, top), f = __builtin_amdgcn_exp2f(most - up);
+            if (__any(top > most + (kLazy - lift))) {  // the weights stay below 2^8 of the first ones: a maximum that rises by less is not worth a pass over the output
+                const float up = fmaxf(most, top + lift), f = __builtin_amdgcn_exp2f(most - up);
                 most = up;
                 sum *= f;
 #pragma unroll

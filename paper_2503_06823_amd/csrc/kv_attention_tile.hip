@@ -32,7 +32,9 @@ typedef float floatx16 __attribute__((ext_vector_type(16)));
 constexpr int kTok = 64;    // tokens of a tile
 constexpr int kRows = kTileRows;
 constexpr int kWaves = 4;
-constexpr float kMostSum = 4294967296.0f;  // of weights, before the maximum is looked for again: outputs have room for values up to 2^95
+// Of a lane's weights, before the maximum is looked for again: a row's two lanes have 1 together, so that its outputs are no larger than the values.
+constexpr float kMostSum = 0.5f;
+constexpr float kLift = 16.0f;  // log2 of what the largest weight then is below 1: contexts of 2^15 tokens before their sum alone asks for it
 
 // A request's row tiles and the key tiles of the longest and the shortest of them.
 struct Rows {
@@ -379,7 +381,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_tile_kernel(Attentio
         return fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
     };
     // The weights are taken against the largest score of the row's first tile, whatever comes later: they are floating-point numbers, and none
-    // loses a bit until their sum comes near the end of the range.  Only then is the maximum looked for.
+    // loses a bit until their sum comes near 1.  Only then is the maximum looked for, for all rows of the wavefront.
     auto weigh = [&](const floatx16* z, bf16x8* w) {
         union {
             bf16x2 two[16];
@@ -410,7 +412,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_tile_kernel(Attentio
         if (__any(sum + added > kMostSum)) {
             const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
             const float so_far = most + __builtin_amdgcn_logf(fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])));
-            const float up = fmaxf(fmaxf(most, fmaxf(largest(z[0]), largest(z[1])) * scale), so_far), f = __builtin_amdgcn_exp2f(most - up);
+            const float up = fmaxf(most, fmaxf(fmaxf(largest(z[0]), largest(z[1])) * scale, so_far) + kLift), f = __builtin_amdgcn_exp2f(most - up);
             most = up;
             sum *= f;
 #pragma unroll

@@ -4,8 +4,9 @@ import pytest
 import torch
 
 import paper_2503_06823_amd as P
-from kv_util import Batch, as_device, bf16, page_bytes
+from kv_util import Batch, as_device, bf16, compare, page_bytes
 from oracle import kv_cache as ref
+from test_gpu_kv_attention import large, plain
 
 pytestmark = pytest.mark.gpu
 
@@ -98,3 +99,53 @@ def test_masked_tokens_of_the_largest_numbers(gpu_device, dtype, lengths, news, 
     torch.cuda.synchronize()
     b.data[:] = cache.cpu().numpy()
     assert np.array_equal(b.run(16, 1), clean)
+
+
+@pytest.mark.parametrize("exponent", (95, 110, 125))
+@pytest.mark.parametrize("dim", (64, 128))
+@pytest.mark.parametrize("dtype,group", [("bf16", 32), ("bf16", 1), ("f32", 1)])
+def test_large_values_have_a_finite_mean(gpu_device, dim, exponent, dtype, group):
+    """Values of up to 6 * 2^125 under scores that rise from token to token, stay, or fall: no sum of them on the way passes fp32's range."""
+    for steps in (0, 3, -3):
+        b = Batch(10, [330], [17], 1, group, dim, 16, dtype)
+        for j in range(330):
+            s = b.slot(0, j)
+            codes = np.zeros((1, dim), dtype=np.uint8)
+            codes[0, 0] = 4  # 2 * 2^k along the first axis
+            up = 0 if steps == 0 else j // 110 if steps > 0 else 2 - j // 110
+            b.cache.write(s, 0, codes, np.full((1, dim // 32), 127 + up, dtype=np.uint8))
+            b.cache.write(s, 1, np.full((1, dim), 7, dtype=np.uint8), np.full((1, dim // 32), 127 + exponent, dtype=np.uint8))
+        b.q[:, :, 0] = 3.0
+        got = b.check(scale=1.0)
+        assert np.isfinite(got).all() and (got >= 5.9 * 2.0 ** exponent).all()
+
+
+@pytest.mark.parametrize("lengths,news,kv_heads,group,dim,dtype", [
+    ([30001], [1], 1, 4, 128, "bf16"), ([30001, 700], [1, 1], 1, 8, 64, "bf16"), ([9001], [2], 1, 3, 64, "f32"), ([9000], [520], 1, 1, 64, "bf16"),
+    ([9000], [520], 1, 2, 128, "bf16")])
+def test_pieces_of_large_values(gpu_device, lengths, news, kv_heads, group, dim, dtype):
+    """Requests that are cut along the keys: the sum of their pieces stays in range too."""
+    page = 64
+    data, table, q = large(5, lengths, news, kv_heads, group, dim, page, dtype)
+    half, tail = page * dim // 2, page * dim // 32
+    data[:, :, 2 * half + tail:] = 127 + 125  # of values
+    kv = P.make_kv_desc(data.shape[0], page, kv_heads, dim, len(lengths), table.shape[1])
+    at = P.make_attention_desc(q.shape[0], q.shape[1], dim, dtype, max(news))
+    n = P.emoe_kv_attention_workspace_bytes(kv, at)
+    ws, out = torch.empty(n, dtype=torch.uint8, device="cuda"), torch.empty_like(q)
+    cu = torch.tensor(np.concatenate(([0], np.cumsum(news))), dtype=torch.int32, device="cuda")
+    P.emoe_kv_attention(kv, at, q, data, table, torch.tensor(lengths, dtype=torch.int32, device="cuda"), cu, out, ws, n)
+    torch.cuda.synchronize()
+    assert torch.isfinite(out).all()
+    compare(out.double().cpu().numpy(), *plain(data, table, q, lengths, news, kv_heads, group, dim, page, 0, 0), dim, dtype)
+
+
+@pytest.mark.parametrize("byte", (5, 12, 20))
+@pytest.mark.parametrize("dtype,group", [("bf16", 32), ("bf16", 1), ("f32", 1)])
+def test_the_smallest_values_are_not_lost(gpu_device, byte, dtype, group):
+    """Values of 2^-123 and more: what they are multiplied with leaves them above the last bit of a subnormal number."""
+    b = Batch(11, [330], [17], 1, group, 64, 16, dtype)
+    for j in range(330):
+        b.cache.write(b.slot(0, j), 1, np.full((1, 64), 4 + j % 4, dtype=np.uint8), np.full((1, 2), byte, dtype=np.uint8))
+    got = b.check()
+    assert (got > 2.0 ** (byte - 127)).all()
