@@ -500,7 +500,7 @@ typedef struct {
     int32_t T;          /* query tokens in this call                                             */
     int32_t q_heads;    /* a multiple of kv_heads: consecutive q_heads / kv_heads share a kv head */
     int32_t dtype;      /* emoe_dtype of q and out                                               */
-    int32_t max_new;    /* no request brings more query tokens than this                         */
+    int32_t max_new;    /* no request brings more query tokens than this; of one that does the first are answered */
     int32_t window;     /* 0: all earlier tokens are seen; else the last `window`, itself included */
     int32_t sinks;      /* with a window: the first `sinks` tokens stay visible                   */
     float scale;        /* of the scores, head_dim^-0.5 as a rule                                */

@@ -68,9 +68,9 @@ __device__ __forceinline__ const uint8_t* lane_at(const uint8_t* base, uint32_t 
 // A request's queries and keys, from the lengths on the device, whatever these hold.
 struct Request {
     int first;  // its first query's token
-    int n;      // query tokens
+    int n;      // query tokens that are answered
     int seq;    // tokens that can be seen, positions 0 .. seq-1
-    int len;    // of the whole request: query i stands at len - n + i
+    int len;    // one more than the last one's position: query i stands at len - n + i
 };
 __device__ __forceinline__ Request request(const AttentionArgs& a, int begin, int end, int len) {
     Request q;
@@ -78,9 +78,10 @@ __device__ __forceinline__ Request request(const AttentionArgs& a, int begin, in
     end = end < begin ? begin : end < a.T ? end : a.T;
     q.first = begin;
     q.n = end - begin < a.max_new ? end - begin : a.max_new;
-    q.len = len;
+    len = len < 0 ? 0 : len;
     const int most = a.width << a.page.log2_size;
-    q.seq = q.len < 0 ? 0 : q.len < most ? q.len : most;
+    q.seq = len < most ? len : most;
+    q.len = len - (end - begin - q.n);
     return q;
 }
 __device__ __forceinline__ Request request(const AttentionArgs& a, int r) { return request(a, a.cu_new[r], a.cu_new[r + 1], a.seq_len[r]); }
