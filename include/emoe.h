@@ -430,6 +430,7 @@ int emoe_generation_tick(emoe_request *request, int32_t completed, double reset_
  *
  * Limits: page_size 16, 32, 64, 128 or 256; head_dim 64 or 128; kv_heads 1..256; pages * page_size <
  * 2^31 and table_width * page_size < 2^31; rows 0..65536; T * kv_heads * head_dim <= 2^33.
+ * A call without tokens (attention: or without requests) succeeds whatever its pointers are: empty buffers may have no address.
  */
 typedef struct {
     int32_t pages;       /* pages of the cache                    */

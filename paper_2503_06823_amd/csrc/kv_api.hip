@@ -89,9 +89,9 @@ int emoe_kv_append(const emoe_kv_desc* desc, int32_t T, int32_t dtype, const voi
     const int64_t row = (int64_t)desc->kv_heads * desc->head_dim;
     if (T < 0 || k_stride < row || v_stride < row || T * row > kMostElements) return EMOE_ERR_SHAPE;
     if (k_stride % 8 != 0 || v_stride % 8 != 0) return EMOE_ERR_UNSUPPORTED;
+    if (T == 0) return EMOE_OK;  // whatever the pointers: an empty buffer may have no address
     if (!k || !v || !slot || !cache) return EMOE_ERR_NULL;
     if (unaligned(k) || unaligned(v) || unaligned(cache)) return EMOE_ERR_UNSUPPORTED;
-    if (T == 0) return EMOE_OK;
     return status_of(launch_kv_append(*desc, T, dtype, k, k_stride, v, v_stride, slot, cache, static_cast<hipStream_t>(stream)));
 }
 
@@ -101,9 +101,9 @@ int emoe_kv_read(const emoe_kv_desc* desc, int32_t T, int32_t dtype, const void*
     if (rc != EMOE_OK) return rc;
     if (dtype != EMOE_F32 && dtype != EMOE_BF16) return EMOE_ERR_UNSUPPORTED;
     if (T < 0 || (int64_t)T * desc->kv_heads * desc->head_dim > kMostElements) return EMOE_ERR_SHAPE;
+    if (T == 0) return EMOE_OK;
     if (!k || !v || !slot || !cache) return EMOE_ERR_NULL;
     if (unaligned(k) || unaligned(v) || unaligned(cache)) return EMOE_ERR_UNSUPPORTED;
-    if (T == 0) return EMOE_OK;
     return status_of(launch_kv_read(*desc, T, dtype, cache, slot, k, v, static_cast<hipStream_t>(stream)));
 }
 
@@ -120,10 +120,10 @@ int emoe_kv_attention(const emoe_kv_desc* desc, const emoe_attention_desc* atten
                       size_t ws_bytes, void* stream) {
     int rc = validate_attention(desc, attention);
     if (rc != EMOE_OK) return rc;
+    if (attention->T == 0 || desc->rows == 0) return EMOE_OK;
     if (!q || !cache || !block_table || !seq_len || !cu_new || !out) return EMOE_ERR_NULL;
     if (unaligned(q) || unaligned(cache) || unaligned(out)) return EMOE_ERR_UNSUPPORTED;
     if (!ws || unaligned(ws) || ws_bytes < attention_ws_bytes(*desc, *attention)) return EMOE_ERR_WORKSPACE;
-    if (attention->T == 0 || desc->rows == 0) return EMOE_OK;
     AttentionArgs a;
     a.q = q;
     a.cache = static_cast<const uint8_t*>(cache);

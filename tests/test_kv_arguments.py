@@ -1,0 +1,35 @@
+"""Calls of the paged 4-bit cache on a machine without a GPU: empty steps, and buffers that must not be the same."""
+import pytest
+
+import paper_2503_06823_amd as P
+
+p = 4096  # a non-NULL address that must never be dereferenced
+
+
+def kv(**kw):
+    base = dict(pages=10, page_size=64, kv_heads=8, head_dim=128, rows=4, table_width=5)
+    base.update(kw)
+    return P.make_kv_desc(**base)
+
+
+def attention(**kw):
+    base = dict(T=6, q_heads=32, head_dim=128, dtype="bf16", max_new=2)
+    base.update(kw)
+    return P.make_attention_desc(**base)
+
+
+@pytest.mark.parametrize("address", (None, p, p + 8))
+def test_steps_without_tokens_or_requests_are_successes(address):
+    """Whatever the buffers of nothing are: an empty tensor has no address."""
+    a = address
+    assert P.emoe_kv_append(kv(), 0, "bf16", a, a, a, p, stream=0) == P.EMOE_OK
+    assert P.emoe_kv_read(kv(), 0, "bf16", p, a, a, a, stream=0) == P.EMOE_OK
+    assert P.emoe_kv_attention(kv(), attention(T=0, max_new=0), a, a, a, a, a, a, a, 0, stream=0) == P.EMOE_OK
+    assert P.emoe_kv_attention(kv(rows=0), attention(), a, a, a, a, a, a, a, 0, stream=0) == P.EMOE_OK
+
+
+def test_bad_extents_are_refused_without_tokens_too():
+    assert P.emoe_kv_append(kv(page_size=8), 0, "bf16", None, None, None, p, stream=0, check=False) == P.EMOE_ERR_UNSUPPORTED
+    assert P.emoe_kv_append(kv(), 0, 7, None, None, None, p, stream=0, check=False) == P.EMOE_ERR_UNSUPPORTED
+    assert P.emoe_kv_read(kv(head_dim=80), 0, "bf16", p, None, None, None, stream=0, check=False) == P.EMOE_ERR_UNSUPPORTED
+    assert P.emoe_kv_attention(kv(), attention(T=0, max_new=1), p, p, p, p, p, p, p, 0, stream=0, check=False) == P.EMOE_ERR_SHAPE
