@@ -19,6 +19,11 @@ import torch
 from . import binding as B
 
 MOST_WORKSPACE = 64 << 20  # no call needs more
+ELEMENTS = {B.EMOE_F32: torch.float32, B.EMOE_BF16: torch.bfloat16}
+
+
+def _described(t) -> str:
+    return f"{t.dtype} {list(t.shape)} with strides {list(t.stride())} on {t.device}" if isinstance(t, torch.Tensor) else repr(t)
 
 
 @dataclass
@@ -57,10 +62,25 @@ class KvCache:
             length=[zeros(rows), zeros(rows)], cu_new=zeros(rows + 1), slot=zeros(most_new), position=zeros(most_new), refused=zeros(1),
             ws=torch.empty(MOST_WORKSPACE, dtype=torch.uint8, device=device))
 
+    # The library is handed addresses and strides: what these would not say is checked here, before anything is enqueued.
+    def _check_per_request(self, name: str, t: torch.Tensor) -> None:
+        if not isinstance(t, torch.Tensor) or t.dtype != torch.int32 or t.shape != (self.desc.rows,) or t.device != self.slot.device \
+                or not t.is_contiguous():
+            raise ValueError(f"{name}: int32 [{self.desc.rows}] on {self.slot.device}, dense, is wanted, not {_described(t)}")
+
+    def _row_stride(self, name: str, t: torch.Tensor, heads: int) -> int:
+        """Elements from one token's row to the next, of a tensor that has rows for the step's tokens."""
+        dim, element = self.desc.head_dim, ELEMENTS[B.DTYPES.get(self.dtype, self.dtype)]
+        if not isinstance(t, torch.Tensor) or t.dtype != element or t.device != self.slot.device or t.dim() != 3 or t.shape[0] < self.T \
+                or t.shape[1:] != (heads, dim) or t.stride(2) != 1 or heads > 1 and t.stride(1) != dim or self.T > 1 and t.stride(0) < heads * dim:
+            raise ValueError(f"{name}: {element} [{self.T} or more, {heads}, {dim}] on {self.slot.device} with dense rows is wanted, not {_described(t)}")
+        return t.stride(0) if self.T > 1 else heads * dim
+
     def plan(self, new_len: torch.Tensor, T: int, stream=None) -> None:
         """`new_len`: int32 [rows] on the device; `T`: their sum, at most the most_new of allocate()."""
-        if T > self.slot.numel():
+        if not 0 <= T <= self.slot.numel():
             raise ValueError(f"{T} tokens in a step for buffers of {self.slot.numel()}")
+        self._check_per_request("new_len", new_len)
         before, after = self.length
         B.emoe_kv_plan(self.desc, T, before, new_len, self.block_table, self.free_pages, self.counters[0], self.cu_new, self.slot,
                        self.position, after, self.counters[1], self.refused, stream)
@@ -69,11 +89,17 @@ class KvCache:
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, stream=None) -> None:
         """`k`, `v`: [T, kv_heads, head_dim], each a slice of a wider row if need be."""
-        B.emoe_kv_append(self.desc, self.T, self.dtype, k, v, self.slot, self.caches[layer], k.stride(0), v.stride(0), stream)
+        k_stride, v_stride = (self._row_stride(name, t, self.desc.kv_heads) for name, t in (("k", k), ("v", v)))
+        B.emoe_kv_append(self.desc, self.T, self.dtype, k, v, self.slot, self.caches[layer], k_stride, v_stride, stream)
 
     def attend(self, layer: int, q: torch.Tensor, out: torch.Tensor, max_new: int, scale: Optional[float] = None, stream=None) -> torch.Tensor:
-        """`q`, `out`: [T, q_heads, head_dim], each a slice of a wider row if need be; no request has more than `max_new` new tokens."""
-        at = B.make_attention_desc(self.T, q.shape[1], q.shape[2], self.dtype, max_new, self.window, self.sinks, scale, q.stride(0), out.stride(0))
+        """`q`, `out`: [T, q_heads, head_dim], each a slice of a wider row if need be; no request has more than `max_new` new tokens (of one that
+        does, the first are answered)."""
+        heads = q.shape[1] if isinstance(q, torch.Tensor) and q.dim() == 3 else 0
+        if heads == 0 or heads % self.desc.kv_heads != 0:
+            raise ValueError(f"q: a multiple of {self.desc.kv_heads} heads is wanted, not {_described(q)}")
+        q_stride, out_stride = (self._row_stride(name, t, heads) for name, t in (("q", q), ("out", out)))
+        at = B.make_attention_desc(self.T, heads, self.desc.head_dim, self.dtype, min(max_new, self.T), self.window, self.sinks, scale, q_stride, out_stride)
         B.emoe_kv_attention(self.desc, at, q, self.caches[layer], self.block_table, self.length[1], self.cu_new, out, self.ws, self.ws.numel(),
                             stream)
         return out
@@ -81,6 +107,8 @@ class KvCache:
     def release(self, ended: Optional[torch.Tensor] = None, stream=None) -> None:
         """Ends the step: rows with `ended` != 0 (int32 [rows] on the device, None: nobody) give all their pages back and start
         anew, rows that were refused keep what they held."""
+        if ended is not None:
+            self._check_per_request("ended", ended)
         before, after = self.length
         with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
             torch.maximum(after, before, out=after)  # no request gets shorter: a refused row's length is 0
