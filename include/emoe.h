@@ -460,7 +460,7 @@ int emoe_kv_cache_bytes(const emoe_kv_desc *desc, size_t *bytes);
  * and the rows up to it need more than tail - head together.  Its tokens have slot -1 and their positions, its
  * seq_len is 0 (nothing is seen); it keeps what it held: the caller passes the same len again later.
  * Tokens from cu_new[R] on, up to T, have slot -1 and position -1.  All pointers dev int32 but the
- * counters; counters_out is not counters.  Nothing that is read is written (but for the table's new entries): the
+ * counters.  Nothing that is read is written (but for the table's new entries), and a buffer for both is refused (EMOE_ERR_SHAPE): the
  * same call again gives the same result.
  */
 int emoe_kv_plan(const emoe_kv_desc *desc, int32_t T, const int32_t *len, const int32_t *new_len, int32_t *block_table,
@@ -475,7 +475,7 @@ int emoe_kv_plan(const emoe_kv_desc *desc, int32_t T, const int32_t *len, const 
  * have done so already.  Without one (window 0) no page leaves before its request ends, and len_before may be
  * NULL.  ended[r] != 0 (NULL: none): all pages that are left go back.  Pages go into the ring from tail on, in row order and
  * ascending within a row; counters_out = {head, tail + pages returned}.  The table is not touched.  As emoe_kv_plan,
- * counters_out is not counters.
+ * nothing that is read is written.
  */
 int emoe_kv_release(const emoe_kv_desc *desc, const int32_t *len_before, const int32_t *len, const int32_t *ended,
                     int32_t window, int32_t sinks, const int32_t *block_table, int32_t *free_pages, const int64_t *counters,

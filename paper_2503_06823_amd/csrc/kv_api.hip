@@ -2,6 +2,8 @@
 // documented in include/emoe.h.
 #include <math.h>
 
+#include <initializer_list>
+
 #include "kv_cache.h"
 
 namespace emoe {
@@ -37,6 +39,13 @@ int validate_attention(const emoe_kv_desc* d, const emoe_attention_desc* a) {
 namespace {
 constexpr int64_t kMostElements = 1ll << 33;  // of the rows of one append or read: threads of eight in a launch
 bool unaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
+// Whether some buffer of `written` is one of `read` (NULL: none).
+bool shared(std::initializer_list<const void*> written, std::initializer_list<const void*> read) {
+    for (const void* w : written)
+        for (const void* r : read)
+            if (w != nullptr && w == r) return true;
+    return false;
+}
 int status_of(hipError_t e) { return e == hipSuccess ? EMOE_OK : EMOE_ERR_DEVICE; }
 }  // namespace
 
@@ -63,7 +72,7 @@ int emoe_kv_plan(const emoe_kv_desc* desc, int32_t T, const int32_t* len, const 
     if (!free_pages || !counters || !cu_new || !counters_out || !refused) return EMOE_ERR_NULL;
     if (desc->rows > 0 && (!len || !new_len || !block_table || !seq_len)) return EMOE_ERR_NULL;
     if (T > 0 && (!slot || !position)) return EMOE_ERR_NULL;
-    if (counters == counters_out) return EMOE_ERR_SHAPE;
+    if (shared({block_table, cu_new, slot, position, seq_len, counters_out, refused}, {len, new_len, free_pages, counters})) return EMOE_ERR_SHAPE;
     return status_of(launch_kv_plan(*desc, T, len, new_len, block_table, free_pages, counters, cu_new, slot, position, seq_len,
                                     counters_out, refused, static_cast<hipStream_t>(stream)));
 }
@@ -76,7 +85,7 @@ int emoe_kv_release(const emoe_kv_desc* desc, const int32_t* len_before, const i
     if (window < 0 || sinks < 0) return EMOE_ERR_SHAPE;
     if (!free_pages || !counters || !counters_out) return EMOE_ERR_NULL;
     if (desc->rows > 0 && (!len || !block_table || (window > 0 && !len_before))) return EMOE_ERR_NULL;
-    if (counters == counters_out) return EMOE_ERR_SHAPE;
+    if (shared({free_pages, counters_out}, {len_before, len, ended, block_table, counters})) return EMOE_ERR_SHAPE;
     return status_of(launch_kv_release(*desc, len_before, len, ended, window, sinks, block_table, free_pages, counters, counters_out,
                                        static_cast<hipStream_t>(stream)));
 }

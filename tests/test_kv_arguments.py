@@ -33,3 +33,33 @@ def test_bad_extents_are_refused_without_tokens_too():
     assert P.emoe_kv_append(kv(), 0, 7, None, None, None, p, stream=0, check=False) == P.EMOE_ERR_UNSUPPORTED
     assert P.emoe_kv_read(kv(head_dim=80), 0, "bf16", p, None, None, None, stream=0, check=False) == P.EMOE_ERR_UNSUPPORTED
     assert P.emoe_kv_attention(kv(), attention(T=0, max_new=1), p, p, p, p, p, p, p, 0, stream=0, check=False) == P.EMOE_ERR_SHAPE
+
+
+PLAN = ("length", "new_len", "block_table", "free_pages", "counters", "cu_new", "slot", "position", "seq_len", "counters_out", "refused")
+RELEASE = ("len_before", "length", "ended", "block_table", "free_pages", "counters", "counters_out")
+
+
+def plan(**same):
+    at = {n: p + 64 * i for i, n in enumerate(PLAN)}
+    at.update({n: at[other] for n, other in same.items()})
+    return P.emoe_kv_plan(kv(), 6, *[at[n] for n in PLAN], stream=0, check=False)
+
+
+def release(**same):
+    at = {n: p + 64 * i for i, n in enumerate(RELEASE)}
+    at.update({n: at[other] for n, other in same.items()})
+    return P.emoe_kv_release(kv(), at["len_before"], at["length"], at["ended"], 9, 1, at["block_table"], at["free_pages"], at["counters"],
+                             at["counters_out"], stream=0, check=False)
+
+
+@pytest.mark.parametrize("read", ("length", "new_len", "free_pages", "counters"))
+@pytest.mark.parametrize("written", ("block_table", "cu_new", "slot", "position", "seq_len", "counters_out", "refused"))
+def test_plan_reads_nothing_that_it_writes(read, written):
+    """Workgroups read what another has written already or not: the lengths before and after a step have buffers of their own."""
+    assert plan(**{written: read}) == P.EMOE_ERR_SHAPE
+
+
+@pytest.mark.parametrize("read", ("len_before", "length", "ended", "block_table", "counters"))
+@pytest.mark.parametrize("written", ("free_pages", "counters_out"))
+def test_release_reads_nothing_that_it_writes(read, written):
+    assert release(**{written: read}) == P.EMOE_ERR_SHAPE
