@@ -469,7 +469,8 @@ int emoe_kv_plan(const emoe_kv_desc *desc, int32_t T, const int32_t *len, const 
 
 /*
  * Pages that nobody will read any more, back to the ring: between two steps, when request r has grown from
- * len_before[r] to len[r] tokens since the last release.  With a sliding window (see emoe_kv_attention) the
+ * len_before[r] to len[r] tokens since the last release (a len[r] below len_before[r], as emoe_kv_plan leaves it for a refused row, is taken
+ * as len_before[r]).  With a sliding window (see emoe_kv_attention) the
  * pages b that hold no sink and no token that a query at position len[r] or later sees, that is
  * ceil(sinks / page_size) <= b < floor((len - window + 1) / page_size), leave; those that had left at len_before
  * have done so already.  Without one (window 0) no page leaves before its request ends, and len_before may be
@@ -480,6 +481,13 @@ int emoe_kv_plan(const emoe_kv_desc *desc, int32_t T, const int32_t *len, const 
 int emoe_kv_release(const emoe_kv_desc *desc, const int32_t *len_before, const int32_t *len, const int32_t *ended,
                     int32_t window, int32_t sinks, const int32_t *block_table, int32_t *free_pages, const int64_t *counters,
                     int64_t *counters_out, void *stream);
+
+/*
+ * The lengths that the next step begins with, after emoe_kv_release: len[r], what request r held before the step, becomes what it holds now,
+ * the larger of len[r] and seq_len[r] (a refused row keeps what it held), and 0 where ended[r] != 0 (NULL: none).  seq_len [R] as emoe_kv_plan
+ * leaves it; len [R] (in and out) is neither of the others.
+ */
+int emoe_kv_advance(const emoe_kv_desc *desc, const int32_t *seq_len, const int32_t *ended, int32_t *len, void *stream);
 
 /*
  * Keys and values of T tokens into their slots.  k, v: dev, element type dtype (emoe_dtype), row t of head h

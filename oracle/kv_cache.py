@@ -106,6 +106,8 @@ def plan(page, width, T, length, new_len, table, ring, counters):
 def release(page, length_before, length, ended, window, sinks, table, ring, counters):
     """The ring (a copy) and the counters after emoe_kv_release."""
     ring, tail = ring.copy(), int(counters[1])
+    if length_before is not None:  # a refused row holds what it held
+        length = np.maximum(length, length_before)
 
     def dead(b, n):  # no query at position n or later sees a token of page b
         return all(j >= sinks and j <= n - window for j in range(b * page, (b + 1) * page)) and b * page >= sinks if window else False
@@ -117,6 +119,11 @@ def release(page, length_before, length, ended, window, sinks, table, ring, coun
                 ring[tail % len(ring)] = table[r, b]
                 tail += 1
     return ring, [int(counters[0]), tail]
+
+
+def advance(length, seq_len, ended):
+    """What the requests hold after a step."""
+    return [0 if ended is not None and ended[r] else max(int(length[r]), int(seq_len[r])) for r in range(len(length))]
 
 
 def attention(cache: Cache, q, table, seq_len, cu, scale, window=0, sinks=0):

@@ -9,7 +9,7 @@ from .binding import (EMOE_ACT_RELU, EMOE_ACT_SWIGLU, EMOE_BF16, EMOE_ERR_DEVICE
                       EmoeRequest, emoe_prompt_action, Loader, EMOE_PROMPT_REUSE, EMOE_PROMPT_LOAD_ALL,
                       EMOE_PROMPT_PREDICT, emoe_expected_tokens, emoe_select_experts, emoe_plan_load,
                       EmoeKvDesc, EmoeAttentionDesc, make_kv_desc, make_attention_desc, emoe_kv_cache_bytes, emoe_kv_plan,
-                      emoe_kv_release, emoe_kv_append, emoe_kv_read, emoe_kv_attention_workspace_bytes, emoe_kv_attention,
+                      emoe_kv_release, emoe_kv_advance, emoe_kv_append, emoe_kv_read, emoe_kv_attention_workspace_bytes, emoe_kv_attention,
                       emoe_workspace_bytes, lib, make_desc, make_event, status_string)
 from .kv import KvCache
 from .layer import DeviceInputs, LayerBuffers, layer_forward

@@ -31,7 +31,7 @@ EXPORTS = ("emoe_status_string", "emoe_workspace_bytes", "emoe_route", "emoe_rou
            "emoe_loader_layer_ready", "emoe_loader_residents", "emoe_loader_synchronize", "emoe_expected_latency", "emoe_schedule",
            "emoe_generation_tick", "emoe_measure_mfma_loop", "emoe_measure_read_stream",
            "emoe_measure_copy_stream", "emoe_measure_scatter_combine", "emoe_kv_cache_bytes", "emoe_kv_plan", "emoe_kv_release",
-           "emoe_kv_append", "emoe_kv_read", "emoe_kv_attention_workspace_bytes", "emoe_kv_attention")
+           "emoe_kv_advance", "emoe_kv_append", "emoe_kv_read", "emoe_kv_attention_workspace_bytes", "emoe_kv_attention")
 
 
 class EmoeLayerDesc(ctypes.Structure):
@@ -94,6 +94,7 @@ def lib() -> ctypes.CDLL:
         L.emoe_kv_cache_bytes.argtypes = [kp, ctypes.POINTER(sz)]
         L.emoe_kv_plan.argtypes = [kp, i32] + [vp] * 12
         L.emoe_kv_release.argtypes = [kp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp]
+        L.emoe_kv_advance.argtypes = [kp, vp, vp, vp, vp]
         L.emoe_kv_append.argtypes = [kp, i32, i32, vp, i64, vp, i64, vp, vp, vp]
         L.emoe_kv_read.argtypes = [kp, i32, i32, vp, vp, vp, vp, vp]
         L.emoe_kv_attention_workspace_bytes.argtypes = [kp, ap, ctypes.POINTER(sz)]
@@ -337,6 +338,11 @@ def emoe_kv_release(kv, len_before, length, ended, window, sinks, block_table, f
     rc = lib().emoe_kv_release(ctypes.byref(kv), _addr(len_before), _addr(length), _addr(ended), window, sinks, _addr(block_table),
                                _addr(free_pages), _addr(counters), _addr(counters_out), _stream_addr(stream))
     return _check(rc, "emoe_kv_release", check)
+
+
+def emoe_kv_advance(kv, seq_len, ended, length, stream=None, check=True) -> int:
+    rc = lib().emoe_kv_advance(ctypes.byref(kv), _addr(seq_len), _addr(ended), _addr(length), _stream_addr(stream))
+    return _check(rc, "emoe_kv_advance", check)
 
 
 def emoe_kv_append(kv, T, dtype, k, v, slot, cache, k_stride=None, v_stride=None, stream=None, check=True) -> int:

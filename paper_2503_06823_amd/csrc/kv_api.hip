@@ -90,6 +90,15 @@ int emoe_kv_release(const emoe_kv_desc* desc, const int32_t* len_before, const i
                                        static_cast<hipStream_t>(stream)));
 }
 
+int emoe_kv_advance(const emoe_kv_desc* desc, const int32_t* seq_len, const int32_t* ended, int32_t* len, void* stream) {
+    int rc = validate_kv_desc(desc);
+    if (rc != EMOE_OK) return rc;
+    if (desc->rows == 0) return EMOE_OK;
+    if (!seq_len || !len) return EMOE_ERR_NULL;
+    if (shared({len}, {seq_len, ended})) return EMOE_ERR_SHAPE;
+    return status_of(launch_kv_advance(*desc, seq_len, ended, len, static_cast<hipStream_t>(stream)));
+}
+
 int emoe_kv_append(const emoe_kv_desc* desc, int32_t T, int32_t dtype, const void* k, int64_t k_stride, const void* v,
                    int64_t v_stride, const int32_t* slot, void* cache, void* stream) {
     int rc = validate_kv_desc(desc);

@@ -77,6 +77,7 @@ hipError_t launch_kv_plan(const emoe_kv_desc& d, int T, const int32_t* len, cons
 hipError_t launch_kv_release(const emoe_kv_desc& d, const int32_t* len_before, const int32_t* len, const int32_t* ended, int window,
                              int sinks, const int32_t* table, int32_t* free_pages, const int64_t* counters, int64_t* counters_out,
                              hipStream_t st);
+hipError_t launch_kv_advance(const emoe_kv_desc& d, const int32_t* seq_len, const int32_t* ended, int32_t* len, hipStream_t st);
 hipError_t launch_kv_append(const emoe_kv_desc& d, int T, int dtype, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                             const int32_t* slot, void* cache, hipStream_t st);
 hipError_t launch_kv_read(const emoe_kv_desc& d, int T, int dtype, const void* cache, const int32_t* slot, void* k, void* v,

@@ -15,6 +15,7 @@ namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kReleaseRows = kWaves;
+constexpr int kAdvanceThreads = 256;
 
 // Inclusive prefix sums over the workgroup of N values a thread, and the sums of all.
 template <int N>
@@ -185,7 +186,8 @@ __global__ __launch_bounds__(kThreads) void kv_release_kernel(int R, int pages, 
         const int r = r0 + i;
         Leaving l = {0, 0, 0};
         if (r < R) {
-            l = leaving(window != 0 ? len_before[r] : 0, len[r], ended != nullptr && ended[r] != 0, window, sinks, log2_page);
+            const int held = len_before != nullptr ? len_before[r] : 0, now = len[r];
+            l = leaving(held, now > held ? now : held, ended != nullptr && ended[r] != 0, window, sinks, log2_page);
             if (l.to > width) l.to = width;  // a length that the table cannot hold
             if (l.first > width) l.first = width;
         }
@@ -210,6 +212,14 @@ __global__ __launch_bounds__(kThreads) void kv_release_kernel(int R, int pages, 
     for (int k = lane; k < n; k += 64) free_pages[ring_index(start, k, pages)] = row[k < l.first ? k : l.from + k - l.first];
 }
 
+__global__ __launch_bounds__(kAdvanceThreads) void kv_advance_kernel(int R, const int32_t* __restrict__ seq_len, const int32_t* __restrict__ ended,
+                                                                     int32_t* __restrict__ len) {
+    const int r = blockIdx.x * kAdvanceThreads + threadIdx.x;
+    if (r >= R) return;
+    const int held = len[r], now = seq_len[r];
+    len[r] = ended != nullptr && ended[r] != 0 ? 0 : now > held ? now : held;
+}
+
 }  // namespace
 
 hipError_t launch_kv_plan(const emoe_kv_desc& d, int T, const int32_t* len, const int32_t* new_len, int32_t* table,
@@ -227,6 +237,11 @@ hipError_t launch_kv_release(const emoe_kv_desc& d, const int32_t* len_before, c
     const unsigned groups = d.rows > 0 ? (unsigned)((d.rows + kReleaseRows - 1) / kReleaseRows) : 1u;
     kv_release_kernel<<<groups, kThreads, 0, st>>>(d.rows, d.pages, d.table_width, log2_of(d.page_size), window, sinks, len_before, len,
                                                    ended, table, free_pages, counters, counters_out);
+    return hipGetLastError();
+}
+
+hipError_t launch_kv_advance(const emoe_kv_desc& d, const int32_t* seq_len, const int32_t* ended, int32_t* len, hipStream_t st) {
+    kv_advance_kernel<<<(unsigned)((d.rows + kAdvanceThreads - 1) / kAdvanceThreads), kAdvanceThreads, 0, st>>>(d.rows, seq_len, ended, len);
     return hipGetLastError();
 }
 

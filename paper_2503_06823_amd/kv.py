@@ -8,6 +8,8 @@ One step of a batch, all its tensors on one stream:
         kv.append(layer, k, v)     # the step's keys and values, after the positions have been applied to them
         kv.attend(layer, q, out, max_new)
     kv.release(ended)              # pages that nobody will read again
+
+A step leaves every buffer where it was: one that was captured in a graph replays as the next one.
 """
 from __future__ import annotations
 
@@ -38,7 +40,7 @@ class KvCache:
     block_table: torch.Tensor       # int32 [rows, table_width]
     free_pages: torch.Tensor        # int32 [pages], a ring
     counters: List[torch.Tensor]    # its int64 {head, tail}, twice: every call reads one and writes the other
-    length: List[torch.Tensor]      # int32 [rows]: tokens held; before and after a step
+    length: List[torch.Tensor]      # int32 [rows], twice: tokens held between steps; in the last step, its own included (0: refused)
     cu_new: torch.Tensor
     slot: torch.Tensor
     position: torch.Tensor
@@ -81,8 +83,8 @@ class KvCache:
         if not 0 <= T <= self.slot.numel():
             raise ValueError(f"{T} tokens in a step for buffers of {self.slot.numel()}")
         self._check_per_request("new_len", new_len)
-        before, after = self.length
-        B.emoe_kv_plan(self.desc, T, before, new_len, self.block_table, self.free_pages, self.counters[0], self.cu_new, self.slot,
+        held, after = self.length
+        B.emoe_kv_plan(self.desc, T, held, new_len, self.block_table, self.free_pages, self.counters[0], self.cu_new, self.slot,
                        self.position, after, self.counters[1], self.refused, stream)
         self.counters.reverse()
         self.T = T
@@ -109,12 +111,8 @@ class KvCache:
         anew, rows that were refused keep what they held."""
         if ended is not None:
             self._check_per_request("ended", ended)
-        before, after = self.length
-        with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
-            torch.maximum(after, before, out=after)  # no request gets shorter: a refused row's length is 0
-            B.emoe_kv_release(self.desc, before, after, ended, self.window, self.sinks, self.block_table, self.free_pages,
-                              self.counters[0], self.counters[1], stream)
-            if ended is not None:
-                after.mul_(ended == 0)
+        held, after = self.length
+        B.emoe_kv_release(self.desc, held, after, ended, self.window, self.sinks, self.block_table, self.free_pages, self.counters[0],
+                          self.counters[1], stream)
+        B.emoe_kv_advance(self.desc, after, ended, held, stream)
         self.counters.reverse()
-        self.length.reverse()

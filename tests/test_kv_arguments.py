@@ -63,3 +63,13 @@ def test_plan_reads_nothing_that_it_writes(read, written):
 @pytest.mark.parametrize("written", ("free_pages", "counters_out"))
 def test_release_reads_nothing_that_it_writes(read, written):
     assert release(**{written: read}) == P.EMOE_ERR_SHAPE
+
+
+def test_advance_refuses():
+    q = p + 64
+    assert P.emoe_kv_advance(kv(page_size=8), p, p, q, stream=0, check=False) == P.EMOE_ERR_UNSUPPORTED
+    assert P.emoe_kv_advance(kv(), None, p, q, stream=0, check=False) == P.EMOE_ERR_NULL
+    assert P.emoe_kv_advance(kv(), p, p, None, stream=0, check=False) == P.EMOE_ERR_NULL
+    assert P.emoe_kv_advance(kv(), p, q, p, stream=0, check=False) == P.EMOE_ERR_SHAPE
+    assert P.emoe_kv_advance(kv(), p, q, q, stream=0, check=False) == P.EMOE_ERR_SHAPE
+    assert P.emoe_kv_advance(kv(rows=0), None, None, None, stream=0) == P.EMOE_OK

@@ -120,3 +120,19 @@ def test_fp32_rows(made):
     kv.append(0, rows(6, dtype=torch.float32), rows(6, dtype=torch.float32))
     with pytest.raises(ValueError):
         kv.append(0, rows(6), rows(6))
+
+
+def test_a_step_leaves_every_buffer_in_its_place(made):
+    """The next step reads and writes where this one did, so that a captured step replays as the next."""
+    kv, calls = made
+
+    def step():
+        calls.clear()
+        planned(kv)
+        kv.release(torch.zeros(3, **I32))
+        keep = [id(t) for t in (*kv.length, *kv.counters)]
+        return [name for name, _ in calls], keep, [[id(x) for x in a if isinstance(x, torch.Tensor) and x.numel() != 3 or x is kv.length[0]] for _, a in calls]
+
+    first = step()
+    assert first[0] == ["emoe_kv_plan", "emoe_kv_release", "emoe_kv_advance"]  # nothing of it is torch's
+    assert step() == first
