@@ -78,8 +78,8 @@ def rotate(heads, cos, sin):
 
 
 def serve(model, prompts, steps, window=0, sinks=0, pages=None):
-    """`prompts`: a list of token lists; row r generates steps - r tokens, so that requests end one after the other.  Returns the
-    tokens of every request and the cache."""
+    """`prompts`: a list of token lists; row r generates steps - r tokens, so that requests end one after the other.  `pages`: of the cache, if
+    not enough for all; requests that get none then wait until others have ended.  Returns the tokens of every request and the cache."""
     R, longest = len(prompts), max(map(len, prompts))
     page = 16
     width = -(-(longest + steps) // page)
@@ -87,22 +87,25 @@ def serve(model, prompts, steps, window=0, sinks=0, pages=None):
                             max(sum(map(len, prompts)), R), window=window, sinks=sinks, device=DEVICE)
     i32 = dict(dtype=torch.int32, device=DEVICE)
     made = [[] for _ in prompts]
-    new = [len(p) for p in prompts]
-    tokens = torch.tensor([t for p in prompts for t in p], device=DEVICE)
-    for step in range(steps):
+    pending = [list(p) for p in prompts]  # what each request brings to the next step; nothing: it has ended
+    while any(pending):
+        new = [len(p) for p in pending]
+        tokens = torch.tensor(sum(pending, []), dtype=torch.int64, device=DEVICE)
         kv.plan(torch.tensor(new, **i32), len(tokens))
         logits = model.forward(kv, tokens, max(new))
-        last = torch.tensor([sum(new[:r + 1]) - 1 for r in range(R) if new[r]], device=DEVICE)
-        chosen = logits[last].argmax(-1)
         running = [r for r in range(R) if new[r]]
+        chosen = logits[torch.tensor([sum(new[:r + 1]) - 1 for r in running], device=DEVICE)].argmax(-1)
+        held = kv.length[1].tolist()
+        ended = [0] * R
         for r, t in zip(running, chosen.tolist()):
+            if held[r] == 0:  # refused: there was no page for it, and it brings the same tokens again
+                continue
             made[r].append(t)
-        ended = [1 if new[r] and len(made[r]) >= steps - r else 0 for r in range(R)]
+            ended[r] = int(len(made[r]) >= steps - r)
+            pending[r] = [] if ended[r] else [t]
+        if not any(held[r] for r in running):
+            raise RuntimeError(f"{kv.desc.pages} pages are too few: none of requests {running} can go on")
         kv.release(torch.tensor(ended, **i32))
-        new = [1 if new[r] and not ended[r] else 0 for r in range(R)]
-        tokens = torch.tensor([made[r][-1] for r in range(R) if new[r]], dtype=torch.int64, device=DEVICE)
-        if not len(tokens):
-            break
     return made, kv
 
 
