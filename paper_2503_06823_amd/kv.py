@@ -64,19 +64,27 @@ class KvCache:
             length=[zeros(rows), zeros(rows)], cu_new=zeros(rows + 1), slot=zeros(most_new), position=zeros(most_new), refused=zeros(1),
             ws=torch.empty(MOST_WORKSPACE, dtype=torch.uint8, device=device))
 
-    # The library is handed addresses and strides: what these would not say is checked here, before anything is enqueued.
+    def __post_init__(self):
+        self._element, self._device = ELEMENTS[B.DTYPES.get(self.dtype, self.dtype)], self.slot.device
+        self._kv_heads, self._dim = self.desc.kv_heads, self.desc.head_dim
+
+    # The library is handed addresses and strides: what these would not say is checked here, before anything is enqueued.  (A microsecond a tensor:
+    # a tensor's shape and strides are asked for once.)
     def _check_per_request(self, name: str, t: torch.Tensor) -> None:
-        if not isinstance(t, torch.Tensor) or t.dtype != torch.int32 or t.shape != (self.desc.rows,) or t.device != self.slot.device \
-                or not t.is_contiguous():
-            raise ValueError(f"{name}: int32 [{self.desc.rows}] on {self.slot.device}, dense, is wanted, not {_described(t)}")
+        if not (isinstance(t, torch.Tensor) and t.dtype is torch.int32 and t.shape == (self.desc.rows,) and t.device == self._device and t.is_contiguous()):
+            raise ValueError(f"{name}: int32 [{self.desc.rows}] on {self._device}, dense, is wanted, not {_described(t)}")
 
     def _row_stride(self, name: str, t: torch.Tensor, heads: int) -> int:
         """Elements from one token's row to the next, of a tensor that has rows for the step's tokens."""
-        dim, element = self.desc.head_dim, ELEMENTS[B.DTYPES.get(self.dtype, self.dtype)]
-        if not isinstance(t, torch.Tensor) or t.dtype != element or t.device != self.slot.device or t.dim() != 3 or t.shape[0] < self.T \
-                or t.shape[1:] != (heads, dim) or t.stride(2) != 1 or heads > 1 and t.stride(1) != dim or self.T > 1 and t.stride(0) < heads * dim:
-            raise ValueError(f"{name}: {element} [{self.T} or more, {heads}, {dim}] on {self.slot.device} with dense rows is wanted, not {_described(t)}")
-        return t.stride(0) if self.T > 1 else heads * dim
+        row = heads * self._dim
+        if isinstance(t, torch.Tensor) and t.dtype is self._element and t.device == self._device and t.dim() == 3:
+            (tokens, its_heads, dim), (by_token, by_head, by_element) = t.shape, t.stride()
+            if tokens >= self.T and its_heads == heads and dim == self._dim and by_element == 1 and (by_head == dim or heads == 1):
+                if self.T <= 1:
+                    return row  # a single row's own stride says nothing
+                if by_token >= row:
+                    return by_token
+        raise ValueError(f"{name}: {self._element} [{self.T} or more, {heads}, {self._dim}] on {self._device} with dense rows is wanted, not {_described(t)}")
 
     def plan(self, new_len: torch.Tensor, T: int, stream=None) -> None:
         """`new_len`: int32 [rows] on the device; `T`: their sum, at most the most_new of allocate()."""
@@ -91,17 +99,17 @@ class KvCache:
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, stream=None) -> None:
         """`k`, `v`: [T, kv_heads, head_dim], each a slice of a wider row if need be."""
-        k_stride, v_stride = (self._row_stride(name, t, self.desc.kv_heads) for name, t in (("k", k), ("v", v)))
+        k_stride, v_stride = self._row_stride("k", k, self._kv_heads), self._row_stride("v", v, self._kv_heads)
         B.emoe_kv_append(self.desc, self.T, self.dtype, k, v, self.slot, self.caches[layer], k_stride, v_stride, stream)
 
     def attend(self, layer: int, q: torch.Tensor, out: torch.Tensor, max_new: int, scale: Optional[float] = None, stream=None) -> torch.Tensor:
         """`q`, `out`: [T, q_heads, head_dim], each a slice of a wider row if need be; no request has more than `max_new` new tokens (of one that
         does, the first are answered)."""
         heads = q.shape[1] if isinstance(q, torch.Tensor) and q.dim() == 3 else 0
-        if heads == 0 or heads % self.desc.kv_heads != 0:
-            raise ValueError(f"q: a multiple of {self.desc.kv_heads} heads is wanted, not {_described(q)}")
-        q_stride, out_stride = (self._row_stride(name, t, heads) for name, t in (("q", q), ("out", out)))
-        at = B.make_attention_desc(self.T, heads, self.desc.head_dim, self.dtype, min(max_new, self.T), self.window, self.sinks, scale, q_stride, out_stride)
+        if heads == 0 or heads % self._kv_heads != 0:
+            raise ValueError(f"q: a multiple of {self._kv_heads} heads is wanted, not {_described(q)}")
+        q_stride, out_stride = self._row_stride("q", q, heads), self._row_stride("out", out, heads)
+        at = B.make_attention_desc(self.T, heads, self._dim, self.dtype, min(max_new, self.T), self.window, self.sinks, scale, q_stride, out_stride)
         B.emoe_kv_attention(self.desc, at, q, self.caches[layer], self.block_table, self.length[1], self.cu_new, out, self.ws, self.ws.numel(),
                             stream)
         return out
