@@ -9,8 +9,8 @@ namespace emoe {
 // a launch at the end adds them.
 constexpr int kFewRows = 16;      // rows of a slot of the kernel for few queries
 // Workgroups of it that a CU holds, two slots each, by their registers.  With rows of 64 elements a workgroup has half the bytes on their way: 64 decodes
-// of 500 to 8000 tokens on 16 heads 52 us with four, 56 with three, 57 with five (spills); short calls 0 to 3 % the other way.  fp32 of 128: 32 of them
-// to 4000 tokens on 8 heads 27 us with two, 35 with three, of which one waits for its place.
+// of 500 to 8000 tokens on 16 heads 50 us with four, 52 with three; short calls 0 to 3 % the other way.  fp32 of 128: 32 of them to 4000 tokens on 8 heads 26 us
+// with two, 28 with three, of which one waits for its place.
 constexpr int few_per_cu(int dim, bool bf16) { return dim == 64 && bf16 ? 4 : dim == 64 || bf16 ? 3 : 2; }
 constexpr int few_slots(int dim) { return 2 * few_per_cu(dim, true) * kMaxGroups; }
 constexpr int kTileRows = 128;    // of the kernel for many
@@ -37,8 +37,8 @@ hipError_t launch_attention_tile(const emoe_kv_desc& d, const AttentionArgs& a, 
 
 // What the kernel for many queries saves on a request of 33 to 512 rows, in rows of 16 times tokens: it costs 3/2 such rows for a tile of 128
 // rows and 1/2 for 32 of them, and starts later.  Below kFewGain for all such requests together the other one is faster (us, few / many queries'
-// kernel, 32 heads on 8, requests times rows on tokens: 128 on 4000 20 / 23, on 16000 33 / 27; 512 on 2000 24 / 24, on 4000 32 / 28; 4 times 128 on
-// 2000 23 / 25, 256 34 / 30; 16 times 40 on 4000 43 / 51, 64 times 136 / 115; 16 times 512 on 2000 180 / 79).
+// kernel, 32 heads on 8, requests times rows on tokens: 128 on 4000 19 / 22, on 16000 32 / 26; 512 on 2000 20 / 22, on 4000 31 / 26; 4 times 128 on
+// 2000 22 / 25, 256 31 / 30; 16 times 40 on 4000 41 / 55, 64 times 128 / 128; 16 times 512 on 2000 164 / 78).
 constexpr long long kFewGain = 500000;
 __host__ __device__ constexpr long long few_gain(long long rows, long long seen) {
     return (rows + 15) / 16 * (seen + 256) - (3 * ((rows + 127) / 128) + (rows + 31) / 32) * (seen + 400) / 2;
@@ -59,7 +59,7 @@ constexpr float kLowest = -3.0e38f;  // of a running maximum: finite, so that no
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 // An address made of a scalar base and a lane's offset, which a load adds itself if it finds the offset in 32 bits; widened ahead of a loop, as the
-// compiler likes to, it takes 64-bit additions of the vector units (8192 tokens' prompt 477 us instead of 466, decodes 1 % more).
+// compiler likes to, it takes 64-bit additions of the vector units (a prompt of 2048 tokens 53 us instead of 52).
 __device__ __forceinline__ const uint8_t* lane_at(const uint8_t* base, uint32_t offset) {
     asm volatile("" : "+v"(offset));
     return base + offset;
@@ -146,6 +146,10 @@ __device__ __forceinline__ float over_groups(float x, F f) {
         return __float_as_uint(f(__uint_as_float(x), __uint_as_float(y)));
     }));
 }
+
+// What a lane loads of 16 tokens' keys or values, D / 4 elements of one row: a word holds eight.
+template <int D> struct Quarter { typedef uint32_t type __attribute__((ext_vector_type(4))); };
+template <> struct Quarter<64> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
 
 // Eight elements of 4 bits as bf16: exact, a code has two significant bits.
 __device__ __forceinline__ bf16x8 from_codes(uint32_t codes, float scale) {

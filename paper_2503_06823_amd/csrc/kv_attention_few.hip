@@ -28,7 +28,7 @@
 // Measured (32 heads on 8 of 128 elements; with the sum of pieces): 64 requests of 500 to 16383 tokens 68 to 71 us (322 MB), one of 131072 37 to 39
 // (143 MB), 32 behind windows of 4096 31 to 32 (116 MB).  The walk itself reads 6.1 to 6.9 TB/s, where a plain read stream reaches 6.9; the
 // same launches without the walk take 15 us (20 with 64 requests: more beginnings): two launches 4, from the lengths to the first tiles
-// 5, the end of a stretch 3, the sum of pieces 3.  All three wavefronts of a SIMD together spend 1.4 us of instructions on a round of
+// 5, the end of a stretch 3, the sum of pieces 3.  All three wavefronts of a SIMD together spend 1.5 us of instructions on a round of
 // tiles that memory brings in 1.9.  A fourth wavefront a SIMD, and V's fragments read before
 // the exponentials, brought nothing.
 #include <math.h>
@@ -134,10 +134,6 @@ __device__ __forceinline__ bool find_start(const AttentionArgs& a, int most_rows
     s->stretch = {__builtin_amdgcn_readlane(its.row_tiles, at), __builtin_amdgcn_readlane(its.rounds, at)};
     return true;
 }
-
-// What a lane loads of 16 tokens' keys or values, D / 4 elements of one row: a word holds eight.
-template <int D> struct Quarter { typedef uint32_t type __attribute__((ext_vector_type(4))); };
-template <> struct Quarter<64> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
 
 // ONE_PAGE: pages of kTok tokens or more, so that a tile lies in one and takes one lookup (decodes 1 % faster, with rows of 64 elements 4).
 template <class E, int D, bool ONE_PAGE>

@@ -16,10 +16,11 @@
 // Split: a workgroup takes a row tile's keys whole, the longest first, where there are enough row tiles; else pieces of them (find_job), which
 // leave fp32 outputs, maxima and sums in the workspace for a second launch to add.
 //
-// Measured: a prompt of 8192 tokens (32 heads on 8 of 128 elements) 528 us, 1.04 PFLOP/s of what the mask leaves; prompts of 512, 1024, 2048 and 4096
-// tokens: 20, 30, 51 and 151 us.  Measured before K was bf16: two pieces on one CU 37 us for 1024 tokens where 29 otherwise, 54 where 48 for 2048 if the
-// last of two row tiles for a CU does not go with the first; scores of the next tile ahead of this one's exponentials 519 where 504 for 8192, a third
-// wavefront a SIMD 633 (it spilled); a higher priority in the products changes nothing.
+// Measured: a prompt of 8192 tokens (32 heads on 8 of 128 elements) 515 to 525 us, 1.05 to 1.07 PFLOP/s of what the mask leaves.  The matrix cores are
+// busy for 49 % of the cycles, the vector units for 45 % and LDS for 46 %, the first two hardly at the same time.  Prompts of 512, 1024, 2048 and 4096
+// tokens: 20, 30, 51 and 150 us (2048: 56 if the last of two row tiles for a CU does not go with the first).  Tried with K in 4 bits: scores of the
+// next tile ahead of this one's exponentials (519 us against 504 then), a third wavefront a SIMD (633: it spilled); a higher priority in the products
+// changed nothing.
 #include <math.h>
 
 #include "kv_attention.h"
@@ -36,7 +37,8 @@ constexpr int kWaves = 4;
 constexpr float kMostSum = 0.5f;
 constexpr float kLift = 16.0f;  // log2 of what the largest weight then is below 1: contexts of 2^15 tokens before their sum alone asks for it
 
-// A request's row tiles and the key tiles of the longest and the shortest of them.
+// A request's row tiles, the key tiles that all its queries see together, which are those of its longest row tile but for a window, and those of its
+// first row tile.
 struct Rows {
     int row_tiles, longest, shortest;
 };
@@ -60,13 +62,14 @@ struct Job {
 // kTwo times as long as one (one's products and the other's exponentials hardly overlap).  Whole row tiles take the longest one's tiles, or a CU's share
 // of all of them if that is more.  Else the longest is divided by 2 to 64, an estimate a lane: pieces of c tiles take c if every CU has one at
 // most, kTwo c if it has two, and if there are more the longer of c and a CU's share, kUneven for what is not even and kBegin for a second beginning; a
-// piece of a row tile that is cut needs a slot, costs 64 KiB written and read again, a tile's time for kPerTile of them, and kCut for the first.
+// piece of a row tile that is cut needs a slot, costs 64 KiB (of 64 elements: 32) written and read again, a tile's time for kPerTile of them, and kCut
+// for the first.  The constants were fitted at 128 elements.
 // Every wavefront by itself, 64 requests a trip.
 constexpr float kTwo = 1.65f, kCut = 3.0f, kPerTile = 43.0f, kUneven = 1.1f, kBegin = 3.0f;
 constexpr int kLeastCut = 6;  // key tiles
 constexpr int kAhead = 4;     // times 64 requests' lengths come together
 // Workgroups beyond the places and the row tiles, for pieces of a row tile that is longer than all others: four prompts of 512 tokens on 100 to 8000
-// take 111 us with them, 160 without.  As they take some 1 us where none is cut, and more where each reads many lengths, only for few requests.
+// take 117 us with them, 169 without.  As they take some 1 us where none is cut, and more where each reads many lengths, only for few requests.
 __device__ __host__ __forceinline__ int extra_places(const AttentionArgs& a, int places) { return a.R <= 64 ? places / 4 : 0; }
 // Requests come in the order of their longest row tiles where they are at most 64 with rows for this kernel (else as they are): `list` holds those of
 // this wavefront.
@@ -199,9 +202,6 @@ __device__ __forceinline__ Job find_job(const AttentionArgs& a, int least_rows, 
     job.all_slots = slots;
     return job;
 }
-
-template <int D> struct Quarter { typedef uint32_t type __attribute__((ext_vector_type(4))); };
-template <> struct Quarter<64> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
 
 template <int D>
 __global__ __launch_bounds__(64 * kWaves, 2) void attention_tile_kernel(AttentionArgs a, FewRule rule, int places, AttentionWs lay) {
