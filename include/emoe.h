@@ -474,7 +474,7 @@ int emoe_kv_plan(const emoe_kv_desc *desc, int32_t T, const int32_t *len, const 
  * pages b that hold no sink and no token that a query at position len[r] or later sees, that is
  * ceil(sinks / page_size) <= b < floor((len - window + 1) / page_size), leave; those that had left at len_before
  * have done so already.  Without one (window 0) no page leaves before its request ends, and len_before may be
- * NULL.  ended[r] != 0 (NULL: none): all pages that are left go back.  Pages go into the ring from tail on, in row order and
+ * NULL if no row was refused.  ended[r] != 0 (NULL: none): all pages that are left go back.  Pages go into the ring from tail on, in row order and
  * ascending within a row; counters_out = {head, tail + pages returned}.  The table is not touched.  As emoe_kv_plan,
  * nothing that is read is written.
  */

@@ -149,3 +149,19 @@ def test_the_smallest_values_are_not_lost(gpu_device, byte, dtype, group):
         b.cache.write(b.slot(0, j), 1, np.full((1, 64), 4 + j % 4, dtype=np.uint8), np.full((1, 2), byte, dtype=np.uint8))
     got = b.check()
     assert (got > 2.0 ** (byte - 127)).all()
+
+
+@pytest.mark.parametrize("dim", (64, 128))
+@pytest.mark.parametrize("group", (32, 1))
+def test_weights_that_add_up_without_a_larger_one(gpu_device, dim, group):
+    """Many tokens whose scores are 6, after a first tile of zeros: none is far above the first maximum, their sum is.  Then the same the other way round, and
+    rows whose first tiles are behind a window."""
+    for low in (range(64), range(64, 2000)):
+        b = Batch(31, [2000], [17], 1, group, dim, 64)
+        for j in range(2000):
+            codes = np.zeros((1, dim), dtype=np.uint8)
+            codes[0, 0] = 0 if j in low else 7  # 6
+            b.cache.write(b.slot(0, j), 0, codes, np.full((1, dim // 32), 127, dtype=np.uint8))
+        b.q[:, :, 0] = 1.0
+        b.check(scale=1.0)
+        b.check(1930, 1, scale=1.0)
