@@ -17,9 +17,9 @@ LIB_PATH = os.path.join(HERE, "libemoe.so")
 EMOE_OK = 0
 EMOE_ERR_NULL, EMOE_ERR_SHAPE, EMOE_ERR_UNSUPPORTED = -1, -2, -3
 EMOE_ERR_RESIDENT, EMOE_ERR_WORKSPACE, EMOE_ERR_DEVICE = -4, -5, -6
-EMOE_F32, EMOE_BF16 = 0, 1
+EMOE_F32, EMOE_BF16, EMOE_F8 = 0, 1, 2
 EMOE_ACT_SWIGLU, EMOE_ACT_RELU = 0, 1
-DTYPES = {"f32": EMOE_F32, "bf16": EMOE_BF16}
+DTYPES = {"f32": EMOE_F32, "bf16": EMOE_BF16, "f8": EMOE_F8}
 ACTS = {"swiglu": EMOE_ACT_SWIGLU, "relu": EMOE_ACT_RELU}
 
 EXPORTS = ("emoe_status_string", "emoe_workspace_bytes", "emoe_route", "emoe_route_observe", "emoe_permute",
@@ -31,7 +31,8 @@ EXPORTS = ("emoe_status_string", "emoe_workspace_bytes", "emoe_route", "emoe_rou
            "emoe_loader_layer_ready", "emoe_loader_residents", "emoe_loader_synchronize", "emoe_expected_latency", "emoe_schedule",
            "emoe_generation_tick", "emoe_measure_mfma_loop", "emoe_measure_read_stream",
            "emoe_measure_copy_stream", "emoe_measure_scatter_combine", "emoe_kv_cache_bytes", "emoe_kv_plan", "emoe_kv_release",
-           "emoe_kv_advance", "emoe_kv_append", "emoe_kv_read", "emoe_kv_attention_workspace_bytes", "emoe_kv_attention")
+           "emoe_kv_advance", "emoe_kv_append", "emoe_kv_read", "emoe_kv_attention_workspace_bytes", "emoe_kv_attention",
+           "emoe_matrix_bytes", "emoe_matrix_pack", "emoe_matrix_unpack", "emoe_matmul_workspace_bytes", "emoe_matmul")
 
 
 class EmoeLayerDesc(ctypes.Structure):
@@ -49,6 +50,11 @@ class EmoeAttentionDesc(ctypes.Structure):
     _fields_ = [("T", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("dtype", ctypes.c_int32), ("max_new", ctypes.c_int32),
                 ("window", ctypes.c_int32), ("sinks", ctypes.c_int32), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32),
                 ("q_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64)]
+
+
+class EmoeMatmulDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("N", ctypes.c_int32), ("K", ctypes.c_int32), ("groups", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("x_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64)]
 
 
 class EmoeError(RuntimeError):
@@ -99,6 +105,12 @@ def lib() -> ctypes.CDLL:
         L.emoe_kv_read.argtypes = [kp, i32, i32, vp, vp, vp, vp, vp]
         L.emoe_kv_attention_workspace_bytes.argtypes = [kp, ap, ctypes.POINTER(sz)]
         L.emoe_kv_attention.argtypes = [kp, ap] + [vp] * 7 + [sz, vp]
+        mp = ctypes.POINTER(EmoeMatmulDesc)
+        L.emoe_matrix_bytes.argtypes = [i32, i32, ctypes.POINTER(sz)]
+        L.emoe_matrix_pack.argtypes = [i32, i32, i32, i32, vp, i64, vp, vp]
+        L.emoe_matrix_unpack.argtypes = [i32, i32, i32, i32, vp, vp, i64, vp]
+        L.emoe_matmul_workspace_bytes.argtypes = [mp, ctypes.POINTER(sz)]
+        L.emoe_matmul.argtypes = [mp] + [vp] * 5 + [sz, vp]
         for name in EXPORTS[1:]:
             getattr(L, name).restype = ctypes.c_int
         _lib = L
@@ -316,6 +328,45 @@ def make_attention_desc(T: int, q_heads: int, head_dim: int, dtype, max_new: int
     row = q_heads * head_dim
     return EmoeAttentionDesc(T, q_heads, DTYPES.get(dtype, dtype), max_new, window, sinks, head_dim ** -0.5 if scale is None else scale, 0,
                              row if q_stride is None else q_stride, row if out_stride is None else out_stride)
+
+
+def make_matmul_desc(rows: int, N: int, K: int, groups: int = 1, dtype="bf16", x_stride: Optional[int] = None,
+                     out_stride: Optional[int] = None) -> EmoeMatmulDesc:
+    """Strides in elements from row to row, dense if not given."""
+    return EmoeMatmulDesc(rows, N, K, groups, DTYPES.get(dtype, dtype), 0, K if x_stride is None else x_stride, N if out_stride is None else out_stride)
+
+
+def emoe_matrix_bytes(N: int, K: int, check=True) -> int:
+    n = ctypes.c_size_t(0)
+    rc = lib().emoe_matrix_bytes(N, K, ctypes.byref(n))
+    _check(rc, "emoe_matrix_bytes", check)
+    return n.value if rc == EMOE_OK else rc
+
+
+def emoe_matrix_pack(count, N, K, dtype, w, matrices, w_stride=None, stream=None, check=True) -> int:
+    """`w_stride`: elements from row to row, dense if not given."""
+    rc = lib().emoe_matrix_pack(count, N, K, DTYPES.get(dtype, dtype), _addr(w), K if w_stride is None else w_stride, _addr(matrices),
+                                _stream_addr(stream))
+    return _check(rc, "emoe_matrix_pack", check)
+
+
+def emoe_matrix_unpack(count, N, K, dtype, matrices, w, w_stride=None, stream=None, check=True) -> int:
+    rc = lib().emoe_matrix_unpack(count, N, K, DTYPES.get(dtype, dtype), _addr(matrices), _addr(w), K if w_stride is None else w_stride,
+                                  _stream_addr(stream))
+    return _check(rc, "emoe_matrix_unpack", check)
+
+
+def emoe_matmul_workspace_bytes(desc: EmoeMatmulDesc, check=True) -> int:
+    n = ctypes.c_size_t(0)
+    rc = lib().emoe_matmul_workspace_bytes(ctypes.byref(desc), ctypes.byref(n))
+    _check(rc, "emoe_matmul_workspace_bytes", check)
+    return n.value if rc == EMOE_OK else rc
+
+
+def emoe_matmul(desc: EmoeMatmulDesc, x, group_offsets, matrices, out, ws, ws_bytes, stream=None, check=True) -> int:
+    rc = lib().emoe_matmul(ctypes.byref(desc), _addr(x), _addr(group_offsets), _addr(matrices), _addr(out), _addr(ws), int(ws_bytes),
+                           _stream_addr(stream))
+    return _check(rc, "emoe_matmul", check)
 
 
 def emoe_kv_cache_bytes(kv: EmoeKvDesc, check=True) -> int:

@@ -2,7 +2,7 @@
 // The operations are documented in include/emoe.h.
 #include <string.h>
 
-#include "common.h"
+#include "matrix_f8.h"
 
 #include <mutex>
 
@@ -44,7 +44,7 @@ hipError_t device_shape(DeviceShape* out) {
 
 int validate_desc(const emoe_layer_desc* d) {
     if (d == nullptr) return EMOE_ERR_NULL;
-    if (d->dtype != EMOE_F32 && d->dtype != EMOE_BF16) return EMOE_ERR_UNSUPPORTED;
+    if (d->dtype != EMOE_F32 && d->dtype != EMOE_BF16 && d->dtype != EMOE_F8) return EMOE_ERR_UNSUPPORTED;
     if (d->act != EMOE_ACT_SWIGLU && d->act != EMOE_ACT_RELU) return EMOE_ERR_UNSUPPORTED;
     if (d->T < 0 || d->d_model <= 0 || d->d_ff <= 0 || d->E <= 0 || d->k <= 0 || d->S <= 0) return EMOE_ERR_SHAPE;
     if (d->k > d->S || d->S > d->E) return EMOE_ERR_SHAPE;
@@ -57,7 +57,7 @@ int validate_desc(const emoe_layer_desc* d) {
     if ((A + 2) * widest > (1ll << 31)) return EMOE_ERR_SHAPE;
     // and into one slot's weight matrix
     if ((long long)d->d_model * d->d_ff >= (1ll << 31)) return EMOE_ERR_SHAPE;
-    return EMOE_OK;
+    return d->dtype == EMOE_F8 ? validate_f8_layer(*d) : EMOE_OK;
 }
 
 PermuteWs permute_ws_layout(const emoe_layer_desc& d) {
@@ -139,6 +139,7 @@ FfnPath ffn_bf16_path(const emoe_layer_desc& d) {
 // assignments may leave more in a slot, which costs it another pass over its weights).
 FfnPath ffn_path(const emoe_layer_desc& d) {
     if (d.dtype == EMOE_F32) return kFfnF32;
+    if (d.dtype == EMOE_F8) return kFfnF8;
     return d.T <= kFewTokens ? kFfnFew : ffn_bf16_path(d);
 }
 
@@ -147,6 +148,11 @@ FfnPath ffn_path(const emoe_layer_desc& d) {
 FfnWs ffn_ws_layout(const emoe_layer_desc& d) {
     FfnWs w;
     const size_t A = (size_t)d.T * d.k;
+    if (d.dtype == EMOE_F8) {
+        w.h = 0;
+        w.partials = w.total = ffn_f8_ws_bytes(d);
+        return w;
+    }
     w.h = 0;
     w.partials = align256((A > 0 ? A : 1) * d.d_ff * elem_bytes(d));
     w.total = w.partials;
@@ -293,6 +299,10 @@ static int expert_ffn_passes(const emoe_layer_desc* desc, int passes, const void
         case kFfnTiled:
             if (sort.A > 0) return EMOE_ERR_DEVICE;  // this kernel does not sort: first_product_sorts() never asks for it
             e = launch_ffn_bf16_tiled(*desc, x_perm, gather, slot_offsets, w1_slots, w3_slots, w2_slots, y_perm, ws, passes, st);
+            break;
+        case kFfnF8:
+            if (sort.A > 0) return EMOE_ERR_DEVICE;  // nor does this one
+            e = launch_ffn_f8(*desc, x_perm, gather, slot_offsets, w1_slots, w3_slots, w2_slots, y_perm, ws, passes, st);
             break;
     }
     return e == hipSuccess ? EMOE_OK : EMOE_ERR_DEVICE;
@@ -448,19 +458,22 @@ int emoe_load_experts(const emoe_layer_desc* desc, int32_t n, const int32_t* exp
     hipStream_t st = static_cast<hipStream_t>(side_stream);
     if (wait_event && hipStreamWaitEvent(st, static_cast<hipEvent_t>(wait_event), 0) != hipSuccess)
         return EMOE_ERR_DEVICE;
-    const size_t mat_bytes = (size_t)desc->d_model * desc->d_ff * elem_bytes(*desc);
+    const bool f8 = desc->dtype == EMOE_F8;  // packed, their edges in whole blocks
+    const size_t dense = (size_t)desc->d_model * desc->d_ff * elem_bytes(*desc);
+    const size_t mat_bytes = f8 ? f8_matrix_bytes(desc->d_ff, desc->d_model) : dense;
+    const size_t mat2_bytes = f8 ? f8_matrix_bytes(desc->d_model, desc->d_ff) : dense;
     for (int i = 0; i < n; ++i) {
         const int e = expert_ids[i], s = slot_ids[i];
         if (e < 0) continue;
         uint8_t* d1 = static_cast<uint8_t*>(w1_slots) + (size_t)s * mat_bytes;
-        uint8_t* d2 = static_cast<uint8_t*>(w2_slots) + (size_t)s * mat_bytes;
+        uint8_t* d2 = static_cast<uint8_t*>(w2_slots) + (size_t)s * mat2_bytes;
         if (hipMemcpyAsync(d1, host_w1[e], mat_bytes, hipMemcpyHostToDevice, st) != hipSuccess) return EMOE_ERR_DEVICE;
         if (swiglu) {
             uint8_t* d3 = static_cast<uint8_t*>(w3_slots) + (size_t)s * mat_bytes;
             if (hipMemcpyAsync(d3, host_w3[e], mat_bytes, hipMemcpyHostToDevice, st) != hipSuccess)
                 return EMOE_ERR_DEVICE;
         }
-        if (hipMemcpyAsync(d2, host_w2[e], mat_bytes, hipMemcpyHostToDevice, st) != hipSuccess) return EMOE_ERR_DEVICE;
+        if (hipMemcpyAsync(d2, host_w2[e], mat2_bytes, hipMemcpyHostToDevice, st) != hipSuccess) return EMOE_ERR_DEVICE;
     }
     if (launch_write_maps(soe, E, eos, S, slot_of_expert, expert_of_slot, st) != hipSuccess) return EMOE_ERR_DEVICE;
     if (done_event && hipEventRecord(static_cast<hipEvent_t>(done_event), st) != hipSuccess) return EMOE_ERR_DEVICE;

@@ -61,7 +61,7 @@ FfnWs ffn_ws_layout(const emoe_layer_desc& d);
 // Which kernels a layer's FFN runs: fp32, or for bf16 those of up to 16 tokens, weight streaming (few rows per slot), tiles of
 // 128 token rows (up to a few hundred rows per slot) or tiles of 256 token rows.  The last three by the rows per slot alone:
 // ffn_bf16_path().
-enum FfnPath { kFfnStream = 0, kFfnMid = 1, kFfnTiled = 2, kFfnFew = 3, kFfnF32 = 4 };
+enum FfnPath { kFfnStream = 0, kFfnMid = 1, kFfnTiled = 2, kFfnFew = 3, kFfnF32 = 4, kFfnF8 = 5 };
 FfnPath ffn_path(const emoe_layer_desc& d);
 FfnPath ffn_bf16_path(const emoe_layer_desc& d);
 // Whether emoe_layer_forward leaves the sort of the assignments to the first product.

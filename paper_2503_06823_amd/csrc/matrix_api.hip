@@ -1,0 +1,205 @@
+// C ABI of the matrices in 8 bits and of the products with them: host-side argument checks, workspace layout, and the experts' FFN
+// in that form.  The operations are documented in include/emoe.h.
+#include "matrix_f8.h"
+
+namespace emoe {
+namespace {
+
+constexpr long long kMostExtent = 1ll << 31;
+bool unaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
+int status_of(hipError_t e) { return e == hipSuccess ? EMOE_OK : EMOE_ERR_DEVICE; }
+long long whole(long long n) { return (n + kF8Block - 1) / kF8Block * kF8Block; }
+size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
+
+int validate_matrix(int32_t N, int32_t K) {
+    if (N <= 0 || K <= 0) return EMOE_ERR_SHAPE;
+    if (N % 8 != 0 || K % 8 != 0) return EMOE_ERR_UNSUPPORTED;
+    if (whole(N) * whole(K) >= kMostExtent) return EMOE_ERR_SHAPE;
+    return EMOE_OK;
+}
+
+int validate_matrices(int32_t count, int32_t N, int32_t K, int32_t dtype, int64_t stride) {
+    int rc = validate_matrix(N, K);
+    if (rc != EMOE_OK) return rc;
+    if (dtype != EMOE_F32 && dtype != EMOE_BF16) return EMOE_ERR_UNSUPPORTED;
+    if (count < 0 || stride < K) return EMOE_ERR_SHAPE;
+    if (count > 65535 || stride % 8 != 0) return EMOE_ERR_UNSUPPORTED;
+    return EMOE_OK;
+}
+
+int validate_matmul(const emoe_matmul_desc* d) {
+    if (d == nullptr) return EMOE_ERR_NULL;
+    int rc = validate_matrix(d->N, d->K);
+    if (rc != EMOE_OK) return rc;
+    if (d->dtype != EMOE_BF16 || d->reserved != 0) return EMOE_ERR_UNSUPPORTED;
+    if (d->rows < 0 || d->groups <= 0 || d->x_stride < d->K || d->out_stride < d->N) return EMOE_ERR_SHAPE;
+    if (d->groups > kMaxExperts || d->x_stride % 8 != 0 || d->out_stride % 8 != 0) return EMOE_ERR_UNSUPPORTED;
+    if ((d->rows + 2ll) * (whole(d->N) > whole(d->K) ? whole(d->N) : whole(d->K)) > kMostExtent) return EMOE_ERR_SHAPE;
+    return EMOE_OK;
+}
+
+// Rows in 8 bits at `at`, and what follows them.
+F8Rows rows_at(uint8_t* ws, size_t* at, long long rows, int K) {
+    F8Rows r;
+    r.codes = ws + *at;
+    r.rows = (int)rows;
+    r.stride = (int)whole(K);
+    *at = align256(*at + (size_t)rows * r.stride);
+    r.scales = reinterpret_cast<uint32_t*>(ws + *at);
+    *at = align256(*at + f8_rows_scale_bytes(rows, K));
+    return r;
+}
+
+struct MatmulWs {
+    F8Rows x;
+    size_t total;
+};
+MatmulWs matmul_ws(const emoe_matmul_desc& d, void* ws) {
+    MatmulWs w;
+    w.total = 0;
+    w.x = rows_at(static_cast<uint8_t*>(ws), &w.total, d.rows, d.K);
+    return w;
+}
+
+struct FfnF8Ws {
+    F8Rows h, x;
+    size_t total;
+};
+// (x has A rows where the caller grouped them)
+FfnF8Ws ffn_ws(const emoe_layer_desc& d, void* ws) {
+    FfnF8Ws w;
+    const long long A = (long long)d.T * d.k;
+    w.total = 0;
+    w.h = rows_at(static_cast<uint8_t*>(ws), &w.total, A, d.d_ff);
+    w.x = rows_at(static_cast<uint8_t*>(ws), &w.total, A, d.d_model);
+    return w;
+}
+
+}  // namespace
+
+// Beside validate_desc(): 32-bit byte offsets into rows of whole blocks.
+int validate_f8_layer(const emoe_layer_desc& d) {
+    const long long A = (long long)d.T * d.k, m = whole(d.d_model), f = whole(d.d_ff);
+    if ((A + 2) * (m > f ? m : f) > kMostExtent || m * f >= kMostExtent) return EMOE_ERR_SHAPE;
+    return EMOE_OK;
+}
+
+size_t ffn_f8_ws_bytes(const emoe_layer_desc& d) {
+    const size_t n = ffn_ws(d, nullptr).total;
+    return n > 0 ? n : 256;
+}
+
+size_t f8_matrix_bytes(int N, int K) { return f8_layout(N, K).bytes(); }
+
+hipError_t launch_ffn_f8(const emoe_layer_desc& d, const void* x_perm, RowGather gather, const int32_t* offsets, const void* w1,
+                         const void* w3, const void* w2, void* y_perm, void* ws, int passes, hipStream_t st) {
+    const FfnF8Ws lay = ffn_ws(d, ws);
+    const int A = d.T * d.k;
+    const bool swiglu = d.act == EMOE_ACT_SWIGLU;
+    hipError_t e = hipSuccess;
+    F8Product p = {};
+    p.offsets = offsets;
+    p.groups = d.S;
+    p.rows = A;
+    p.k = 1;
+    if (passes & 1) {
+        p.x = lay.x;
+        p.x.rows = gather.perm != nullptr ? d.T : A;
+        p.perm = gather.perm;
+        p.k = gather.k;
+        p.w0 = static_cast<const uint8_t*>(w1);
+        p.w1 = static_cast<const uint8_t*>(w3);
+        p.lay = f8_layout(d.d_ff, d.d_model);
+        p.matrix_bytes = p.lay.bytes();
+        p.N = d.d_ff;
+        p.h = lay.h;
+        e = launch_f8_rows(x_perm, d.d_model, p.x.rows, d.d_model, p.x, st);
+        if (e == hipSuccess) e = launch_f8_stream(p, swiglu ? kF8Swiglu : kF8Relu, st);
+    }
+    if (e != hipSuccess || !(passes & 2)) return e;
+    p.x = lay.h;
+    p.perm = nullptr;
+    p.k = 1;
+    p.w0 = static_cast<const uint8_t*>(w2);
+    p.w1 = nullptr;
+    p.lay = f8_layout(d.d_model, d.d_ff);
+    p.matrix_bytes = p.lay.bytes();
+    p.N = d.d_model;
+    p.out = static_cast<bf16_t*>(y_perm);
+    p.out_stride = d.d_model;
+    p.out_perm = gather.out_perm;
+    return launch_f8_stream(p, kF8Plain, st);
+}
+
+}  // namespace emoe
+
+using namespace emoe;
+
+extern "C" {
+
+int emoe_matrix_bytes(int32_t N, int32_t K, size_t* bytes) {
+    int rc = validate_matrix(N, K);
+    if (rc != EMOE_OK) return rc;
+    if (!bytes) return EMOE_ERR_NULL;
+    *bytes = f8_matrix_bytes(N, K);
+    return EMOE_OK;
+}
+
+int emoe_matrix_pack(int32_t count, int32_t N, int32_t K, int32_t dtype, const void* w, int64_t w_stride, void* matrices, void* stream) {
+    int rc = validate_matrices(count, N, K, dtype, w_stride);
+    if (rc != EMOE_OK) return rc;
+    if (count == 0) return EMOE_OK;
+    if (!w || !matrices) return EMOE_ERR_NULL;
+    if (unaligned(w) || unaligned(matrices)) return EMOE_ERR_UNSUPPORTED;
+    if (w == matrices) return EMOE_ERR_SHAPE;
+    return status_of(launch_matrix_pack(count, N, K, dtype, w, w_stride, matrices, static_cast<hipStream_t>(stream)));
+}
+
+int emoe_matrix_unpack(int32_t count, int32_t N, int32_t K, int32_t dtype, const void* matrices, void* w, int64_t w_stride, void* stream) {
+    int rc = validate_matrices(count, N, K, dtype, w_stride);
+    if (rc != EMOE_OK) return rc;
+    if (count == 0) return EMOE_OK;
+    if (!w || !matrices) return EMOE_ERR_NULL;
+    if (unaligned(w) || unaligned(matrices)) return EMOE_ERR_UNSUPPORTED;
+    if (w == matrices) return EMOE_ERR_SHAPE;
+    return status_of(launch_matrix_unpack(count, N, K, dtype, matrices, w, w_stride, static_cast<hipStream_t>(stream)));
+}
+
+int emoe_matmul_workspace_bytes(const emoe_matmul_desc* desc, size_t* bytes) {
+    int rc = validate_matmul(desc);
+    if (rc != EMOE_OK) return rc;
+    if (!bytes) return EMOE_ERR_NULL;
+    *bytes = matmul_ws(*desc, nullptr).total;
+    return EMOE_OK;
+}
+
+int emoe_matmul(const emoe_matmul_desc* desc, const void* x, const int32_t* group_offsets, const void* matrices, void* out, void* ws,
+                size_t ws_bytes, void* stream) {
+    int rc = validate_matmul(desc);
+    if (rc != EMOE_OK) return rc;
+    if (desc->rows == 0) return EMOE_OK;
+    if (!x || !matrices || !out) return EMOE_ERR_NULL;
+    if (desc->groups > 1 && !group_offsets) return EMOE_ERR_NULL;
+    if (unaligned(x) || unaligned(matrices) || unaligned(out) || unaligned(ws)) return EMOE_ERR_UNSUPPORTED;
+    if (out == x || out == matrices || ws == x || ws == matrices || ws == out) return EMOE_ERR_SHAPE;
+    const MatmulWs lay = matmul_ws(*desc, ws);
+    if (!ws || ws_bytes < lay.total) return EMOE_ERR_WORKSPACE;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    hipError_t e = launch_f8_rows(x, desc->x_stride, desc->rows, desc->K, lay.x, st);
+    if (e != hipSuccess) return EMOE_ERR_DEVICE;
+    F8Product p = {};
+    p.x = lay.x;
+    p.k = 1;
+    p.offsets = group_offsets;
+    p.groups = desc->groups;
+    p.rows = desc->rows;
+    p.w0 = static_cast<const uint8_t*>(matrices);
+    p.lay = f8_layout(desc->N, desc->K);
+    p.matrix_bytes = p.lay.bytes();
+    p.N = desc->N;
+    p.out = static_cast<bf16_t*>(out);
+    p.out_stride = desc->out_stride;
+    return status_of(launch_f8_stream(p, kF8Plain, st));
+}
+
+}  // extern "C"

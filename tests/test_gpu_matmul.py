@@ -1,0 +1,151 @@
+"""emoe_matmul against products in 64 bits of the numbers that its operands stand for."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2503_06823_amd as P
+from oracle import packed as ref
+from packed_util import as_device, bf16, close, matmul, numbers, packed, tokens, weights
+
+pytestmark = pytest.mark.gpu
+
+
+def check(x, ws, offsets=None, **kw):
+    N, K = ws[0].shape
+    data = packed(ws)
+    got = matmul(as_device(x), data, N, offsets, **kw)
+    q, least, w = ref.quantise_rows(x), ref.rows_least(x), numbers(data, N, K)
+    edges = [0, x.shape[0]] if offsets is None else offsets
+    for i in range(len(ws)):
+        rows = slice(edges[i], edges[i + 1])
+        close(got[rows], q[rows] @ w[i].T, ref.product_error(q[rows], least[rows], w[i], ref.matrix_least(data[i].cpu().numpy(), N, K)))
+    assert (got[edges[-1]:] == 5.0).all()
+    return got
+
+
+@pytest.mark.parametrize("rows", (1, 2, 15, 16, 17, 33, 64, 65, 130, 257, 300))
+@pytest.mark.parametrize("N,K", [(8, 8), (128, 128), (136, 264), (264, 1032), (520, 640)])
+def test_one_matrix(gpu_device, rows, N, K):
+    g = np.random.default_rng(rows * 7 + N + K)
+    check(tokens(g, rows, K), [weights(g, N, K)])
+
+
+@pytest.mark.parametrize("rows,N,K", [(5, 6144, 4096), (64, 1024, 4096), (1, 512, 14336), (700, 768, 2048), (520, 264, 4104)])
+def test_large_extents(gpu_device, rows, N, K):
+    g = np.random.default_rng(rows)
+    check(tokens(g, rows, K), [weights(g, N, K)])
+
+
+@pytest.mark.parametrize("sizes,behind", [
+    ((3, 0, 1, 20), 0), ((0, 0, 0), 4), ((1,) * 64, 0), ((40, 0, 16, 17, 1, 0), 3), ((300, 2, 0, 129), 70), ((0, 65, 0, 64), 0), ((700, 1, 256), 1)])
+@pytest.mark.parametrize("N,K", [(136, 264), (256, 384)])
+def test_groups(gpu_device, sizes, behind, N, K):
+    g = np.random.default_rng(sum(sizes) + N)
+    offsets = np.concatenate(([0], np.cumsum(sizes))).tolist()
+    check(tokens(g, sum(sizes) + behind, K), [weights(g, N, K) for _ in sizes], offsets)
+
+
+@pytest.mark.parametrize("rows", (3, 200))
+def test_one_group_with_offsets_and_rows_behind(gpu_device, rows):
+    g = np.random.default_rng(rows)
+    check(tokens(g, rows + 9, 264), [weights(g, 136, 264)], [0, rows])
+
+
+@pytest.mark.parametrize("rows", (4, 300))
+def test_rows_of_wider_tensors(gpu_device, rows):
+    g = np.random.default_rng(rows)
+    check(tokens(g, rows, 392), [weights(g, 264, 392)], x_gap=136, out_gap=40)
+
+
+@pytest.mark.parametrize("rows", (6, 290))
+def test_infinities_and_nan_stay_in_their_rows(gpu_device, rows):
+    g = np.random.default_rng(rows)
+    x, w = tokens(g, rows, 264), weights(g, 136, 264)
+    x[1, 3], x[3, 200], x[rows - 1, 263] = np.nan, np.inf, -np.inf
+    got = check(x, [w])
+    nan = torch.isnan(got).all(1).cpu().numpy()
+    assert set(np.flatnonzero(nan)) == {1, 3, rows - 1}
+
+
+@pytest.mark.parametrize("rows", (6, 290))
+def test_magnitudes_from_the_smallest_to_the_largest(gpu_device, rows):
+    """Blocks 2^-126 to 2^119 apart in one row, and a product at the edge of fp32."""
+    g = np.random.default_rng(rows)
+    x, w = tokens(g, rows, 512), weights(g, 136, 512)
+    x[0, :128] *= 2.0 ** -120
+    x[1, 128:256] *= 2.0 ** 100
+    x[2] *= 2.0 ** -125
+    x[3] = 0.0
+    x[4] = np.where(np.arange(512) % 2, 2.0 ** -130, -2.0 ** -131)
+    w[:128, :128] *= 2.0 ** 18
+    check(bf16(x), [w])  # (row 2 is among the denormal numbers, which have fewer bits)
+
+
+@pytest.mark.parametrize("rows", (6, 290))
+def test_whole_rows_of_one_large_and_many_small_elements(gpu_device, rows):
+    g = np.random.default_rng(rows)
+    x, w = tokens(g, rows, 640), weights(g, 136, 640)
+    x[:, 5::128] *= 2.0 ** 9
+    w[:, 5::128] = 0.0
+    check(x, [w])
+
+
+def test_results_do_not_depend_on_the_rows_beside(gpu_device):
+    """The same row alone and among others, in another group's place, gives the same numbers where the same kernel multiplies it."""
+    g = np.random.default_rng(5)
+    x, w = tokens(g, 12, 520), weights(g, 264, 520)
+    data = packed([w])
+    whole = matmul(as_device(x), data, 264)
+    for r in (0, 7, 11):
+        assert torch.equal(matmul(as_device(x[r:r + 1]), data, 264)[0], whole[r])
+
+
+@pytest.mark.parametrize("rows", (5, 400))
+def test_repeats_are_the_same_bits(gpu_device, rows):
+    g = np.random.default_rng(rows)
+    x, data = as_device(tokens(g, rows, 1032)), packed([weights(g, 520, 1032)])
+    first = matmul(x, data, 520).clone()
+    for _ in range(3):
+        assert torch.equal(matmul(x, data, 520), first)
+
+
+def test_two_streams_at_once(gpu_device):
+    g = np.random.default_rng(8)
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    work = []
+    for rows in (40, 300):
+        x, w = tokens(g, rows, 776), weights(g, 392, 776)
+        work.append((as_device(x), packed([w]), matmul(as_device(x), packed([w]), 392).clone(), torch.empty((rows, 392), dtype=torch.bfloat16, device="cuda")))
+    descs = [P.make_matmul_desc(x.shape[0], 392, 776) for x, *_ in work]
+    spaces = [torch.empty(P.emoe_matmul_workspace_bytes(d), dtype=torch.uint8, device="cuda") for d in descs]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for side, d, ws, (x, m, _, out) in zip(sides, descs, spaces, work):
+            P.emoe_matmul(d, x, None, m, out, ws, ws.numel(), side)
+    torch.cuda.synchronize()
+    for x, m, want, out in work:
+        assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("rows", (7, 300))
+def test_graph_replays(gpu_device, rows):
+    g = np.random.default_rng(rows)
+    x, data = as_device(tokens(g, rows, 776)), packed([weights(g, 392, 776)])
+    other = as_device(tokens(g, rows, 776))
+    desc = P.make_matmul_desc(rows, 392, 776)
+    ws = torch.empty(P.emoe_matmul_workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+    held, out = x.clone(), torch.empty((rows, 392), dtype=torch.bfloat16, device="cuda")
+    want = [matmul(x, data, 392).clone(), matmul(other, data, 392).clone()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        P.emoe_matmul(desc, held, None, data, out, ws, ws.numel())
+    for i in (0, 1, 1, 0):
+        held.copy_((x, other)[i])
+        out.zero_()
+        ws.fill_(255 if i else 0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[i])
