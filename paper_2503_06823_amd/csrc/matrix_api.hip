@@ -50,19 +50,28 @@ F8Rows rows_at(uint8_t* ws, size_t* at, long long rows, int K) {
     return r;
 }
 
+// Which kernel multiplies: by the rows that a group has on average (their numbers live on the device).  Up to kStreamRows of them one pass
+// over a matrix does, which costs its bytes; more rows cost matrix instructions.  Tiles take at least two blocks of columns.
+constexpr long long kStreamRows = 64;
+bool is_tiled(long long rows, int groups, int K) { return rows > kStreamRows * groups && K > kF8Block; }
+
 struct MatmulWs {
     F8Rows x;
+    float* partials;  // of the tiles
     size_t total;
 };
 MatmulWs matmul_ws(const emoe_matmul_desc& d, void* ws) {
     MatmulWs w;
     w.total = 0;
     w.x = rows_at(static_cast<uint8_t*>(ws), &w.total, d.rows, d.K);
+    w.partials = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + w.total);
+    if (is_tiled(d.rows, d.groups, d.K)) w.total += kTiledPartialBytes;
     return w;
 }
 
 struct FfnF8Ws {
     F8Rows h, x;
+    float* partials;
     size_t total;
 };
 // (x has A rows where the caller grouped them)
@@ -72,7 +81,13 @@ FfnF8Ws ffn_ws(const emoe_layer_desc& d, void* ws) {
     w.total = 0;
     w.h = rows_at(static_cast<uint8_t*>(ws), &w.total, A, d.d_ff);
     w.x = rows_at(static_cast<uint8_t*>(ws), &w.total, A, d.d_model);
+    w.partials = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + w.total);
+    if (is_tiled(A, d.S, d.d_model) || is_tiled(A, d.S, d.d_ff)) w.total += kTiledPartialBytes;
     return w;
+}
+
+hipError_t multiply(const F8Product& p, int K, F8Epilogue epilogue, float* partials, hipStream_t st) {
+    return is_tiled(p.rows, p.groups, K) ? launch_f8_tiled(p, epilogue, partials, st) : launch_f8_stream(p, epilogue, st);
 }
 
 }  // namespace
@@ -114,7 +129,7 @@ hipError_t launch_ffn_f8(const emoe_layer_desc& d, const void* x_perm, RowGather
         p.N = d.d_ff;
         p.h = lay.h;
         e = launch_f8_rows(x_perm, d.d_model, p.x.rows, d.d_model, p.x, st);
-        if (e == hipSuccess) e = launch_f8_stream(p, swiglu ? kF8Swiglu : kF8Relu, st);
+        if (e == hipSuccess) e = multiply(p, d.d_model, swiglu ? kF8Swiglu : kF8Relu, lay.partials, st);
     }
     if (e != hipSuccess || !(passes & 2)) return e;
     p.x = lay.h;
@@ -128,7 +143,7 @@ hipError_t launch_ffn_f8(const emoe_layer_desc& d, const void* x_perm, RowGather
     p.out = static_cast<bf16_t*>(y_perm);
     p.out_stride = d.d_model;
     p.out_perm = gather.out_perm;
-    return launch_f8_stream(p, kF8Plain, st);
+    return multiply(p, d.d_ff, kF8Plain, lay.partials, st);
 }
 
 }  // namespace emoe
@@ -199,7 +214,7 @@ int emoe_matmul(const emoe_matmul_desc* desc, const void* x, const int32_t* grou
     p.N = desc->N;
     p.out = static_cast<bf16_t*>(out);
     p.out_stride = desc->out_stride;
-    return status_of(launch_f8_stream(p, kF8Plain, st));
+    return status_of(multiply(p, desc->K, kF8Plain, lay.partials, st));
 }
 
 }  // extern "C"

@@ -51,6 +51,8 @@ struct F8Product {
 
 hipError_t launch_f8_rows(const void* x, int64_t stride, int rows, int K, const F8Rows& to, hipStream_t st);
 hipError_t launch_f8_stream(const F8Product& p, F8Epilogue epilogue, hipStream_t st);
+// partials: kTiledPartialBytes.  At least two blocks of columns.
+hipError_t launch_f8_tiled(const F8Product& p, F8Epilogue epilogue, float* partials, hipStream_t st);
 
 hipError_t launch_matrix_pack(int count, int N, int K, int dtype, const void* w, int64_t stride, void* matrix, hipStream_t st);
 hipError_t launch_matrix_unpack(int count, int N, int K, int dtype, const void* matrix, void* w, int64_t stride, hipStream_t st);
