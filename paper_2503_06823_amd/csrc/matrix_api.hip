@@ -55,39 +55,57 @@ F8Rows rows_at(uint8_t* ws, size_t* at, long long rows, int K) {
 constexpr long long kStreamRows = 64;
 bool is_tiled(long long rows, int groups, int K) { return rows > kStreamRows * groups && K > kF8Block; }
 
+// What the kernels of a call need beside rows in 8 bits: the two need it at different times and share the place.
+struct Scratch {
+    F8StreamWs stream;
+    float* partials;  // of the tiles
+    size_t n_counters;
+};
+Scratch scratch_at(uint8_t* ws, size_t* at, size_t n_counters, bool streams, bool tiles) {
+    Scratch c;
+    c.n_counters = streams ? n_counters : 0;
+    c.stream.counters = reinterpret_cast<int*>(ws + *at);
+    *at = align256(*at + c.n_counters * sizeof(int));
+    c.stream.pieces = c.partials = reinterpret_cast<float*>(ws + *at);
+    static_assert(kTiledPartialBytes >= kF8StreamPieceBytes, "either kernel's pieces fit");
+    *at += tiles ? kTiledPartialBytes : streams ? kF8StreamPieceBytes : 0;
+    return c;
+}
+
 struct MatmulWs {
     F8Rows x;
-    float* partials;  // of the tiles
+    Scratch scratch;
     size_t total;
 };
 MatmulWs matmul_ws(const emoe_matmul_desc& d, void* ws) {
     MatmulWs w;
+    const bool tiled = is_tiled(d.rows, d.groups, d.K);
     w.total = 0;
     w.x = rows_at(static_cast<uint8_t*>(ws), &w.total, d.rows, d.K);
-    w.partials = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + w.total);
-    if (is_tiled(d.rows, d.groups, d.K)) w.total += kTiledPartialBytes;
+    w.scratch = scratch_at(static_cast<uint8_t*>(ws), &w.total, f8_stream_counters(d.rows, d.groups, d.N), !tiled, tiled);
     return w;
 }
 
 struct FfnF8Ws {
     F8Rows h, x;
-    float* partials;
+    Scratch scratch;
     size_t total;
 };
-// (x has A rows where the caller grouped them)
+// (x has A rows where the caller grouped them; the two products share the counters, each leaves them at zero)
 FfnF8Ws ffn_ws(const emoe_layer_desc& d, void* ws) {
     FfnF8Ws w;
     const long long A = (long long)d.T * d.k;
+    const bool first = is_tiled(A, d.S, d.d_model), second = is_tiled(A, d.S, d.d_ff);
     w.total = 0;
     w.h = rows_at(static_cast<uint8_t*>(ws), &w.total, A, d.d_ff);
     w.x = rows_at(static_cast<uint8_t*>(ws), &w.total, A, d.d_model);
-    w.partials = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + w.total);
-    if (is_tiled(A, d.S, d.d_model) || is_tiled(A, d.S, d.d_ff)) w.total += kTiledPartialBytes;
+    w.scratch = scratch_at(static_cast<uint8_t*>(ws), &w.total, f8_stream_counters(A, d.S, d.d_ff > d.d_model ? d.d_ff : d.d_model), !first || !second,
+                           first || second);
     return w;
 }
 
-hipError_t multiply(const F8Product& p, int K, F8Epilogue epilogue, float* partials, hipStream_t st) {
-    return is_tiled(p.rows, p.groups, K) ? launch_f8_tiled(p, epilogue, partials, st) : launch_f8_stream(p, epilogue, st);
+hipError_t multiply(const F8Product& p, int K, F8Epilogue epilogue, const Scratch& scratch, hipStream_t st) {
+    return is_tiled(p.rows, p.groups, K) ? launch_f8_tiled(p, epilogue, scratch.partials, st) : launch_f8_stream(p, epilogue, scratch.stream, st);
 }
 
 }  // namespace
@@ -128,8 +146,8 @@ hipError_t launch_ffn_f8(const emoe_layer_desc& d, const void* x_perm, RowGather
         p.matrix_bytes = p.lay.bytes();
         p.N = d.d_ff;
         p.h = lay.h;
-        e = launch_f8_rows(x_perm, d.d_model, p.x.rows, d.d_model, p.x, st);
-        if (e == hipSuccess) e = multiply(p, d.d_model, swiglu ? kF8Swiglu : kF8Relu, lay.partials, st);
+        e = launch_f8_rows(x_perm, d.d_model, p.x.rows, d.d_model, p.x, lay.scratch.stream.counters, lay.scratch.n_counters, st);
+        if (e == hipSuccess) e = multiply(p, d.d_model, swiglu ? kF8Swiglu : kF8Relu, lay.scratch, st);
     }
     if (e != hipSuccess || !(passes & 2)) return e;
     p.x = lay.h;
@@ -143,7 +161,7 @@ hipError_t launch_ffn_f8(const emoe_layer_desc& d, const void* x_perm, RowGather
     p.out = static_cast<bf16_t*>(y_perm);
     p.out_stride = d.d_model;
     p.out_perm = gather.out_perm;
-    return multiply(p, d.d_ff, kF8Plain, lay.partials, st);
+    return multiply(p, d.d_ff, kF8Plain, lay.scratch, st);
 }
 
 }  // namespace emoe
@@ -200,7 +218,7 @@ int emoe_matmul(const emoe_matmul_desc* desc, const void* x, const int32_t* grou
     const MatmulWs lay = matmul_ws(*desc, ws);
     if (!ws || ws_bytes < lay.total) return EMOE_ERR_WORKSPACE;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    hipError_t e = launch_f8_rows(x, desc->x_stride, desc->rows, desc->K, lay.x, st);
+    hipError_t e = launch_f8_rows(x, desc->x_stride, desc->rows, desc->K, lay.x, lay.scratch.stream.counters, lay.scratch.n_counters, st);
     if (e != hipSuccess) return EMOE_ERR_DEVICE;
     F8Product p = {};
     p.x = lay.x;
@@ -214,7 +232,7 @@ int emoe_matmul(const emoe_matmul_desc* desc, const void* x, const int32_t* grou
     p.N = desc->N;
     p.out = static_cast<bf16_t*>(out);
     p.out_stride = desc->out_stride;
-    return status_of(multiply(p, desc->K, kF8Plain, lay.partials, st));
+    return status_of(multiply(p, desc->K, kF8Plain, lay.scratch, st));
 }
 
 }  // extern "C"
