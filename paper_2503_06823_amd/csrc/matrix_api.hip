@@ -105,7 +105,7 @@ FfnF8Ws ffn_ws(const emoe_layer_desc& d, void* ws) {
 }
 
 hipError_t multiply(const F8Product& p, int K, F8Epilogue epilogue, const Scratch& scratch, hipStream_t st) {
-    return is_tiled(p.rows, p.groups, K) ? launch_f8_tiled(p, epilogue, scratch.partials, st) : launch_f8_stream(p, epilogue, scratch.stream, st);
+    return is_tiled(p.rows, p.groups, K) ? launch_f8_tiled(p, epilogue, scratch.partials, st) : launch_f8_stream(p, epilogue, st);
 }
 
 }  // namespace
