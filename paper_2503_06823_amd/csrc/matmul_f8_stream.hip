@@ -22,7 +22,7 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
 // Strips of a wavefront on their way, by the registers that they and the rows of x take
-constexpr int ring(int tb, int strips) { return tb == 4 && strips < 4 ? 2 * strips : 8; }
+constexpr int ring(int tb, int strips, int waves) { return tb == 4 && strips < 4 && waves > 4 ? 2 * strips : 8; }
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void* base, uint32_t bytes) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)bytes, 0x00020000);
@@ -45,7 +45,7 @@ __device__ __forceinline__ void multiply_unit(const F8Product& p, int unit, int 
                                               uint32_t (&tops)[WAVES][64]) {
     constexpr int M = matrices(EPI), H = row_groups(EPI, STRIPS), SPLIT = WAVES / (M * H);
     static_assert(SPLIT >= 1 && SPLIT * M * H == WAVES, "every wavefront has a part");
-    constexpr int DEPTH = ring(TB, STRIPS) / STRIPS;  // blocks of columns of a wavefront on their way
+    constexpr int DEPTH = ring(TB, STRIPS, WAVES) / STRIPS;  // blocks of columns of a wavefront on their way
     constexpr int ALL = STRIPS * H;       // strips of a unit, of one matrix
     constexpr int FINAL = ALL >= WAVES ? ALL / WAVES : 1;  // that a wavefront finishes
     constexpr int ROWS = 16 * TB;
@@ -241,9 +241,9 @@ hipError_t launch(const F8Product& p, hipStream_t st) {
     const bool few = p.rows <= 16;
     if constexpr (EPI == kF8Plain) {
         const long long strips = groups * ((p.N + 15) / 16);
-        if (!few) return launch_shape<EPI, 4, 4, 8>(p, st);
-        if (strips >= 2 * 256) return launch_shape<EPI, 1, 2, 8>(p, st);
-        return launch_shape<EPI, 1, 1, 8>(p, st);
+        if (strips >= 4 * 512) return few ? launch_shape<EPI, 1, 4, 4>(p, st) : launch_shape<EPI, 4, 4, 8>(p, st);
+        if (!few) return launch_shape<EPI, 4, 2, 4>(p, st);
+        return strips > 256 ? launch_shape<EPI, 1, 2, 4>(p, st) : launch_shape<EPI, 1, 1, 4>(p, st);
     } else {
         if (!few) return launch_shape<EPI, 4, 4, 8>(p, st);
         return launch_shape<EPI, 1, 4, 8>(p, st);

@@ -50,62 +50,50 @@ F8Rows rows_at(uint8_t* ws, size_t* at, long long rows, int K) {
     return r;
 }
 
-// Which kernel multiplies: by the rows that a group has on average (their numbers live on the device).  Up to kStreamRows of them one pass
-// over a matrix does, which costs its bytes; more rows cost matrix instructions.  Tiles take at least two blocks of columns.
-constexpr long long kStreamRows = 64;
-bool is_tiled(long long rows, int groups, int K) { return rows > kStreamRows * groups && K > kF8Block; }
-
-// What the kernels of a call need beside rows in 8 bits: the two need it at different times and share the place.
-struct Scratch {
-    F8StreamWs stream;
-    float* partials;  // of the tiles
-    size_t n_counters;
-};
-Scratch scratch_at(uint8_t* ws, size_t* at, size_t n_counters, bool streams, bool tiles) {
-    Scratch c;
-    c.n_counters = streams ? n_counters : 0;
-    c.stream.counters = reinterpret_cast<int*>(ws + *at);
-    *at = align256(*at + c.n_counters * sizeof(int));
-    c.stream.pieces = c.partials = reinterpret_cast<float*>(ws + *at);
-    static_assert(kTiledPartialBytes >= kF8StreamPieceBytes, "either kernel's pieces fit");
-    *at += tiles ? kTiledPartialBytes : streams ? kF8StreamPieceBytes : 0;
-    return c;
+// Which kernel multiplies: by the rows that a group has on average (their numbers live on the device).  Streaming costs a matrix's bytes for every 64 rows, and
+// more where these are over 32; tiles of 256 x 256 cost the bytes once, some 10 us for their two launches, and leave CUs without work
+// where they are few.  Measured with matrices from HBM (us, streaming / tiles): 8 groups of 14336 x 4096, 32 rows each 105 / 102, 48 127 / 106; 24 of
+// 1408 x 2048, 32 29.6 / 30.5, 48 38.6 / 31.5; 64 of 512 x 512, 32 15.6 / 17.1, 48 19.4 / 18.1; one of 6144 x 4096 (24 tiles), 64 18.1 / 25.3,
+// 128 29.0 / 30.5, 160 38.3 / 31.1; one of 1024 x 1024 (4 tiles), 128 15.9 / 18.1.  Tiles take at least two blocks of columns.
+constexpr long long kManyTiles = 64, kStreamRows = 36, kStreamRowsFewTiles = 128;
+bool is_tiled(long long rows, int groups, int N, int K) {
+    const long long tiles = (long long)groups * ((N + 255) / 256);
+    return rows > (tiles >= kManyTiles ? kStreamRows : kStreamRowsFewTiles) * groups && K > kF8Block;
 }
 
 struct MatmulWs {
     F8Rows x;
-    Scratch scratch;
+    float* partials;  // of the tiles
     size_t total;
 };
 MatmulWs matmul_ws(const emoe_matmul_desc& d, void* ws) {
     MatmulWs w;
-    const bool tiled = is_tiled(d.rows, d.groups, d.K);
     w.total = 0;
     w.x = rows_at(static_cast<uint8_t*>(ws), &w.total, d.rows, d.K);
-    w.scratch = scratch_at(static_cast<uint8_t*>(ws), &w.total, f8_stream_counters(d.rows, d.groups, d.N), !tiled, tiled);
+    w.partials = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + w.total);
+    if (is_tiled(d.rows, d.groups, d.N, d.K)) w.total += kTiledPartialBytes;
     return w;
 }
 
 struct FfnF8Ws {
     F8Rows h, x;
-    Scratch scratch;
+    float* partials;
     size_t total;
 };
-// (x has A rows where the caller grouped them; the two products share the counters, each leaves them at zero)
+// (x has A rows where the caller grouped them)
 FfnF8Ws ffn_ws(const emoe_layer_desc& d, void* ws) {
     FfnF8Ws w;
     const long long A = (long long)d.T * d.k;
-    const bool first = is_tiled(A, d.S, d.d_model), second = is_tiled(A, d.S, d.d_ff);
     w.total = 0;
     w.h = rows_at(static_cast<uint8_t*>(ws), &w.total, A, d.d_ff);
     w.x = rows_at(static_cast<uint8_t*>(ws), &w.total, A, d.d_model);
-    w.scratch = scratch_at(static_cast<uint8_t*>(ws), &w.total, f8_stream_counters(A, d.S, d.d_ff > d.d_model ? d.d_ff : d.d_model), !first || !second,
-                           first || second);
+    w.partials = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + w.total);
+    if (is_tiled(A, d.S, d.d_ff, d.d_model) || is_tiled(A, d.S, d.d_model, d.d_ff)) w.total += kTiledPartialBytes;
     return w;
 }
 
-hipError_t multiply(const F8Product& p, int K, F8Epilogue epilogue, const Scratch& scratch, hipStream_t st) {
-    return is_tiled(p.rows, p.groups, K) ? launch_f8_tiled(p, epilogue, scratch.partials, st) : launch_f8_stream(p, epilogue, st);
+hipError_t multiply(const F8Product& p, int K, F8Epilogue epilogue, float* partials, hipStream_t st) {
+    return is_tiled(p.rows, p.groups, p.N, K) ? launch_f8_tiled(p, epilogue, partials, st) : launch_f8_stream(p, epilogue, st);
 }
 
 }  // namespace
@@ -146,8 +134,8 @@ hipError_t launch_ffn_f8(const emoe_layer_desc& d, const void* x_perm, RowGather
         p.matrix_bytes = p.lay.bytes();
         p.N = d.d_ff;
         p.h = lay.h;
-        e = launch_f8_rows(x_perm, d.d_model, p.x.rows, d.d_model, p.x, lay.scratch.stream.counters, lay.scratch.n_counters, st);
-        if (e == hipSuccess) e = multiply(p, d.d_model, swiglu ? kF8Swiglu : kF8Relu, lay.scratch, st);
+        e = launch_f8_rows(x_perm, d.d_model, p.x.rows, d.d_model, p.x, st);
+        if (e == hipSuccess) e = multiply(p, d.d_model, swiglu ? kF8Swiglu : kF8Relu, lay.partials, st);
     }
     if (e != hipSuccess || !(passes & 2)) return e;
     p.x = lay.h;
@@ -161,7 +149,7 @@ hipError_t launch_ffn_f8(const emoe_layer_desc& d, const void* x_perm, RowGather
     p.out = static_cast<bf16_t*>(y_perm);
     p.out_stride = d.d_model;
     p.out_perm = gather.out_perm;
-    return multiply(p, d.d_ff, kF8Plain, lay.scratch, st);
+    return multiply(p, d.d_ff, kF8Plain, lay.partials, st);
 }
 
 }  // namespace emoe
@@ -218,7 +206,7 @@ int emoe_matmul(const emoe_matmul_desc* desc, const void* x, const int32_t* grou
     const MatmulWs lay = matmul_ws(*desc, ws);
     if (!ws || ws_bytes < lay.total) return EMOE_ERR_WORKSPACE;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    hipError_t e = launch_f8_rows(x, desc->x_stride, desc->rows, desc->K, lay.x, lay.scratch.stream.counters, lay.scratch.n_counters, st);
+    hipError_t e = launch_f8_rows(x, desc->x_stride, desc->rows, desc->K, lay.x, st);
     if (e != hipSuccess) return EMOE_ERR_DEVICE;
     F8Product p = {};
     p.x = lay.x;
@@ -232,7 +220,7 @@ int emoe_matmul(const emoe_matmul_desc* desc, const void* x, const int32_t* grou
     p.N = desc->N;
     p.out = static_cast<bf16_t*>(out);
     p.out_stride = desc->out_stride;
-    return status_of(multiply(p, desc->K, kF8Plain, lay.scratch, st));
+    return status_of(multiply(p, desc->K, kF8Plain, lay.partials, st));
 }
 
 }  // extern "C"

@@ -49,16 +49,7 @@ struct F8Product {
     F8Rows h;
 };
 
-// Workspace of the streaming kernel: pieces of units that are cut, and counters, one a unit and two, which are zero before a launch and after it.
-struct F8StreamWs {
-    float* pieces;
-    int* counters;
-};
-constexpr size_t kF8StreamPieceBytes = (size_t)4 * kMaxGroups * 64 * 1024;  // of up to twice the chunks that are wanted, 64 KiB each at most
-inline size_t f8_stream_counters(long long rows, int groups, int N) { return (size_t)(rows / 16 + groups + 1) * f8_layout(N, 8).nb + 2; }
-
-// `zeros`: of `n_zeros` counters, cleared on the way
-hipError_t launch_f8_rows(const void* x, int64_t stride, int rows, int K, const F8Rows& to, int* zeros, size_t n_zeros, hipStream_t st);
+hipError_t launch_f8_rows(const void* x, int64_t stride, int rows, int K, const F8Rows& to, hipStream_t st);
 hipError_t launch_f8_stream(const F8Product& p, F8Epilogue epilogue, hipStream_t st);
 // partials: kTiledPartialBytes.  At least two blocks of columns.
 hipError_t launch_f8_tiled(const F8Product& p, F8Epilogue epilogue, float* partials, hipStream_t st);

@@ -117,9 +117,7 @@ __global__ __launch_bounds__(256) void unpack_kernel(const uint8_t* __restrict__
 }
 
 // Rows of a product's left operand.  A wavefront takes four blocks of a row, one dword of scales: 16 lanes a block, eight elements a lane.
-__global__ __launch_bounds__(256) void rows_kernel(const bf16_t* __restrict__ x, int64_t stride, int K, F8Rows to, int kg, long long units,
-                                                   int* __restrict__ zeros, size_t n_zeros) {
-    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n_zeros; i += (size_t)gridDim.x * 256) zeros[i] = 0;
+__global__ __launch_bounds__(256) void rows_kernel(const bf16_t* __restrict__ x, int64_t stride, int K, F8Rows to, int kg, long long units) {
     const long long unit = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (unit >= units) return;
     const int lane = threadIdx.x & 63;
@@ -140,10 +138,10 @@ __global__ __launch_bounds__(256) void rows_kernel(const bf16_t* __restrict__ x,
 
 }  // namespace
 
-hipError_t launch_f8_rows(const void* x, int64_t stride, int rows, int K, const F8Rows& to, int* zeros, size_t n_zeros, hipStream_t st) {
+hipError_t launch_f8_rows(const void* x, int64_t stride, int rows, int K, const F8Rows& to, hipStream_t st) {
     const int kg = f8_layout(1, K).kg;
     const long long units = (long long)rows * kg;
-    rows_kernel<<<(unsigned)((units + 3) / 4), 256, 0, st>>>(static_cast<const bf16_t*>(x), stride, K, to, kg, units, zeros, n_zeros);
+    rows_kernel<<<(unsigned)((units + 3) / 4), 256, 0, st>>>(static_cast<const bf16_t*>(x), stride, K, to, kg, units);
     return hipGetLastError();
 }
 
