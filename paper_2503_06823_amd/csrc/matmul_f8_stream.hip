@@ -57,13 +57,13 @@ __device__ __forceinline__ void multiply_unit(const F8Product& p, int unit, int 
     const uint8_t* matrix = (M == 2 && wave >= SPLIT * H ? p.w1 : p.w0) + (size_t)group * p.matrix_bytes;
     const uint32_t codes = (uint32_t)p.lay.codes();
     const __amdgpu_buffer_rsrc_t w_rsrc = make_rsrc(matrix, codes);
-    const uint32_t x_bytes = (uint32_t)p.x.rows * (uint32_t)p.x.stride;
+    const uint32_t x_bytes = (uint32_t)p.x.rows * (uint32_t)p.lay.kb * kF8Block;
     const __amdgpu_buffer_rsrc_t x_rsrc = make_rsrc(p.x.codes, x_bytes);
     const uint32_t xs_bytes = (uint32_t)p.x.rows * (uint32_t)p.lay.kg * 4u;
     const __amdgpu_buffer_rsrc_t xs_rsrc = make_rsrc(p.x.scales, xs_bytes);
+    const uint32_t x_block = 8u * (uint32_t)p.x.piece_step;  // bytes from a block of columns to the next
     const uint32_t* w_scales = reinterpret_cast<const uint32_t*>(matrix + codes + (size_t)nb * p.lay.kg * 4);
     const uint32_t w_at = (uint32_t)nb * p.lay.kb * kF8BlockBytes + (strip0 + half * STRIPS) * kF8Strip;
-    const uint32_t divisor = p.perm != nullptr ? (uint32_t)p.k : 1u;
     const int mine = (p.lay.kb - part + SPLIT - 1) / SPLIT;  // this wavefront's blocks of columns: part, part + SPLIT, ...
 
     for (int tok0 = row0; tok0 < row_end; tok0 += ROWS) {
@@ -72,7 +72,8 @@ __device__ __forceinline__ void multiply_unit(const F8Product& p, int unit, int 
         for (int t = 0; t < TB; ++t) {
             int r = tok0 + 16 * t + tok;
             r = r < row_end ? r : row_end - 1;  // (rows past the end are multiplied and not stored)
-            xs_lane[t] = p.perm != nullptr ? (uint32_t)p.perm[r] : (uint32_t)r;
+            x_lane[t] = (uint32_t)r * p.x.row_step + (uint32_t)quad * p.x.piece_step;
+            xs_lane[t] = (uint32_t)r * 4;
         }
         intx8 w[DEPTH][STRIPS], x[DEPTH][TB];
         uint32_t xb[DEPTH][TB], wb[DEPTH];
@@ -88,24 +89,13 @@ __device__ __forceinline__ void multiply_unit(const F8Product& p, int unit, int 
             const int b = there ? part + j * SPLIT : part;
 #pragma unroll
             for (int t = 0; t < TB; ++t) {
-                x[slot][t] = two<0>(x_rsrc, there ? x_lane[t] : x_bytes, (uint32_t)b * kF8Block, 64);
+                x[slot][t] = two<0>(x_rsrc, there ? x_lane[t] : x_bytes, (uint32_t)b * x_block, (int)(x_block / 2));
                 xb[slot][t] = __builtin_amdgcn_raw_buffer_load_b32(xs_rsrc, (int)(there ? xs_lane[t] : xs_bytes), (b >> 2) * p.x.rows * 4, 0);
             }
             wb[slot] = w_scales[b >> 2];
         };
-        // (loads come back in their order: the rows' places ahead of the first strips)
-        __builtin_amdgcn_sched_barrier(0);
-        load_w(0, 0);
-        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int t = 0; t < TB; ++t) {
-            const uint32_t r = xs_lane[t] / divisor;
-            x_lane[t] = r * (uint32_t)p.x.stride + quad * 16;
-            xs_lane[t] = r * 4;
-        }
-        load_x(0, 0);
-#pragma unroll
-        for (int d = 1; d < DEPTH; ++d) {
+        for (int d = 0; d < DEPTH; ++d) {
             load_w(d, d);
             load_x(d, d);
         }
@@ -199,7 +189,7 @@ __device__ __forceinline__ void multiply_unit(const F8Product& p, int unit, int 
 #pragma unroll
                 for (int f = 0; f < FINAL; ++f) {
                     const floatx4& h = sum[0][f][t];
-                    *reinterpret_cast<uint32_t*>(p.h.codes + (size_t)r * p.h.stride + n0 + 16 * f) = f8_codes(h[0], h[1], h[2], h[3], f8_inverse(byte));
+                    *reinterpret_cast<uint32_t*>(p.h.codes + (size_t)r * p.h.row_step + (size_t)((n0 >> 4) + f) * p.h.piece_step + quad * 4) = f8_codes(h[0], h[1], h[2], h[3], f8_inverse(byte));
                 }
                 if (wave == 0 && quad == 0) reinterpret_cast<uint8_t*>(p.h.scales + (size_t)(nb >> 2) * p.h.rows + r)[nb & 3] = (uint8_t)byte;
             }

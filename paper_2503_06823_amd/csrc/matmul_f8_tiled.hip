@@ -142,12 +142,12 @@ __device__ __forceinline__ void store_h(const F8Product& p, Get get, uint32_t to
 #pragma unroll
     for (int i = 0; i < (EPI == kF8Swiglu ? 1 : 2); ++i) val[i] = codes_of(get, 4 * i, inverse);
     if (row < 0 || nb >= p.lay.nb) return;
-    uint8_t* to = p.h.codes + (size_t)row * p.h.stride + nb * kF8Block + (lane >> 4) * 16;
+    uint8_t* to = p.h.codes + (size_t)row * p.h.row_step + (size_t)(nb * 8 + (lane >> 4)) * p.h.piece_step;
     if constexpr (EPI == kF8Swiglu) {
-        *reinterpret_cast<uintx4*>(to + wn * 64) = val[0];
+        *reinterpret_cast<uintx4*>(to + (size_t)(4 * wn) * p.h.piece_step) = val[0];
     } else {
         *reinterpret_cast<uintx4*>(to) = val[0];
-        *reinterpret_cast<uintx4*>(to + 64) = val[EPI == kF8Swiglu ? 0 : 1];
+        *reinterpret_cast<uintx4*>(to + (size_t)4 * p.h.piece_step) = val[EPI == kF8Swiglu ? 0 : 1];
     }
     if ((EPI != kF8Swiglu || wn == 0) && lane < 16) reinterpret_cast<uint8_t*>(p.h.scales + (size_t)(nb >> 2) * p.h.rows + row)[nb & 3] = (uint8_t)byte;
 }
@@ -228,7 +228,7 @@ __global__ __launch_bounds__(64 * NW) void tiled_kernel(F8Product p, float* __re
     };
 
     // ---- memory -> LDS ---------------------------------------------------------------------------------------
-    const uint32_t x_bytes = (uint32_t)p.x.rows * (uint32_t)p.x.stride;
+    const uint32_t x_bytes = (uint32_t)p.x.rows * (uint32_t)p.x.row_step;
     const __amdgpu_buffer_rsrc_t x_rsrc = make_rsrc(p.x.codes, x_bytes);
     const uint32_t xs_bytes = (uint32_t)p.x.rows * (uint32_t)p.lay.kg * 4u;
     const __amdgpu_buffer_rsrc_t xs_rsrc = make_rsrc(p.x.scales, xs_bytes);
@@ -248,7 +248,7 @@ __global__ __launch_bounds__(64 * NW) void tiled_kernel(F8Product p, float* __re
         for (int i = 0; i < LPW; ++i) {
             const int tr = 64 * wave + 8 * i + (l >> 3);
             const uint32_t row = (uint32_t)__shfl((int)x_row, 8 * i + (l >> 3));
-            const int v = opaque((int)(row * (uint32_t)p.x.stride + ((l & 7) ^ ((tr >> 1) & 7)) * 16));
+            const int v = opaque((int)(row * (uint32_t)p.x.row_step + ((l & 7) ^ ((tr >> 1) & 7)) * 16));
             x_voff[i] = it.row0 + tr >= it.row_end ? x_bytes : (uint32_t)v;  // out of range: zeros without memory traffic
         }
     };

@@ -40,11 +40,10 @@ int validate_matmul(const emoe_matmul_desc* d) {
 
 // Rows in 8 bits at `at`, and what follows them.
 F8Rows rows_at(uint8_t* ws, size_t* at, long long rows, int K) {
-    F8Rows r;
+    F8Rows r = {};
     r.codes = ws + *at;
     r.rows = (int)rows;
-    r.stride = (int)whole(K);
-    *at = align256(*at + (size_t)rows * r.stride);
+    *at = align256(*at + (size_t)rows * whole(K));
     r.scales = reinterpret_cast<uint32_t*>(ws + *at);
     *at = align256(*at + f8_rows_scale_bytes(rows, K));
     return r;
@@ -59,6 +58,13 @@ constexpr long long kManyTiles = 64, kStreamRows = 36, kStreamRowsFewTiles = 128
 bool is_tiled(long long rows, int groups, int N, int K) {
     const long long tiles = (long long)groups * ((N + 255) / 256);
     return rows > (tiles >= kManyTiles ? kStreamRows : kStreamRowsFewTiles) * groups && K > kF8Block;
+}
+
+// In the order that the kernel which multiplies them reads
+F8Rows ordered(F8Rows r, int K, bool by_rows) {
+    r.row_step = by_rows ? (int)whole(K) : 16;
+    r.piece_step = by_rows ? 16 : r.rows * 16;
+    return r;
 }
 
 struct MatmulWs {
@@ -117,6 +123,7 @@ hipError_t launch_ffn_f8(const emoe_layer_desc& d, const void* x_perm, RowGather
     const FfnF8Ws lay = ffn_ws(d, ws);
     const int A = d.T * d.k;
     const bool swiglu = d.act == EMOE_ACT_SWIGLU;
+    const F8Rows h = ordered(lay.h, d.d_ff, is_tiled(A, d.S, d.d_model, d.d_ff));
     hipError_t e = hipSuccess;
     F8Product p = {};
     p.offsets = offsets;
@@ -124,21 +131,26 @@ hipError_t launch_ffn_f8(const emoe_layer_desc& d, const void* x_perm, RowGather
     p.rows = A;
     p.k = 1;
     if (passes & 1) {
+        const bool tiled = is_tiled(A, d.S, d.d_ff, d.d_model);
         p.x = lay.x;
-        p.x.rows = gather.perm != nullptr ? d.T : A;
-        p.perm = gather.perm;
-        p.k = gather.k;
+        // tiles gather the rows themselves, so that each is read and converted once
+        if (tiled && gather.perm != nullptr) {
+            p.x.rows = d.T;
+            p.perm = gather.perm;
+            p.k = gather.k;
+        }
+        p.x = ordered(p.x, d.d_model, tiled);
         p.w0 = static_cast<const uint8_t*>(w1);
         p.w1 = static_cast<const uint8_t*>(w3);
         p.lay = f8_layout(d.d_ff, d.d_model);
         p.matrix_bytes = p.lay.bytes();
         p.N = d.d_ff;
-        p.h = lay.h;
-        e = launch_f8_rows(x_perm, d.d_model, p.x.rows, d.d_model, p.x, st);
+        p.h = h;
+        e = launch_f8_rows(x_perm, d.d_model, d.d_model, p.x, tiled ? nullptr : gather.perm, gather.k, offsets + d.S, st);
         if (e == hipSuccess) e = multiply(p, d.d_model, swiglu ? kF8Swiglu : kF8Relu, lay.partials, st);
     }
     if (e != hipSuccess || !(passes & 2)) return e;
-    p.x = lay.h;
+    p.x = h;
     p.perm = nullptr;
     p.k = 1;
     p.w0 = static_cast<const uint8_t*>(w2);
@@ -206,10 +218,9 @@ int emoe_matmul(const emoe_matmul_desc* desc, const void* x, const int32_t* grou
     const MatmulWs lay = matmul_ws(*desc, ws);
     if (!ws || ws_bytes < lay.total) return EMOE_ERR_WORKSPACE;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    hipError_t e = launch_f8_rows(x, desc->x_stride, desc->rows, desc->K, lay.x, st);
-    if (e != hipSuccess) return EMOE_ERR_DEVICE;
     F8Product p = {};
-    p.x = lay.x;
+    p.x = ordered(lay.x, desc->K, is_tiled(desc->rows, desc->groups, desc->N, desc->K));
+    if (launch_f8_rows(x, desc->x_stride, desc->K, p.x, nullptr, 1, nullptr, st) != hipSuccess) return EMOE_ERR_DEVICE;
     p.k = 1;
     p.offsets = group_offsets;
     p.groups = desc->groups;

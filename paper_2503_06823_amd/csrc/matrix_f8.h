@@ -19,12 +19,15 @@ inline F8Layout f8_layout(int N, int K) {
     return {nb, kb, (kb + 3) / 4};
 }
 
-// Rows in 8 bits: codes [rows][stride], scales [kg][rows], a dword for four blocks of 128 elements.
+// Rows in 8 bits: codes, in pieces of 16 in one of two orders, and scales [kg][rows], a dword for four blocks of 128 elements.
+// By rows, [rows][kb 8][16], as tiles are brought to LDS; by pieces, [kb 8][rows][16], where a matrix instruction's operand goes from
+// memory to registers: neighbouring lanes, which hold neighbouring rows, then read neighbouring bytes (64 rows times 6144 x 4096: 15.3 us
+// by rows, where each lane of a load has a line of its own, 12.5 by pieces).
 struct F8Rows {
     uint8_t* codes;
     uint32_t* scales;
     int rows;
-    int stride;  // bytes, K in whole blocks
+    int row_step, piece_step;  // bytes from a row to the next, and from a piece of a row to the next
 };
 inline size_t f8_rows_scale_bytes(long long rows, int K) { return (size_t)rows * f8_layout(1, K).kg * 4; }
 
@@ -33,7 +36,7 @@ inline size_t f8_rows_scale_bytes(long long rows, int K) { return (size_t)rows *
 enum F8Epilogue { kF8Plain = 0, kF8Swiglu = 1, kF8Relu = 2 };
 struct F8Product {
     F8Rows x;
-    const int32_t* perm;  // grouped row r is row perm[r] / k of x; NULL: r
+    const int32_t* perm;  // (tiles) grouped row r is row perm[r] / k of x; NULL: r
     int k;
     const int32_t* offsets;
     int groups;
@@ -49,9 +52,11 @@ struct F8Product {
     F8Rows h;
 };
 
-hipError_t launch_f8_rows(const void* x, int64_t stride, int rows, int K, const F8Rows& to, hipStream_t st);
+// Row r of `to` is row r of x, or with perm row perm[r] / k; of these only the rows before *end.
+hipError_t launch_f8_rows(const void* x, int64_t stride, int K, const F8Rows& to, const int32_t* perm, int k, const int32_t* end, hipStream_t st);
+// x by pieces, a row of it for each grouped row
 hipError_t launch_f8_stream(const F8Product& p, F8Epilogue epilogue, hipStream_t st);
-// partials: kTiledPartialBytes.  At least two blocks of columns.
+// partials: kTiledPartialBytes.  x by rows; at least two blocks of columns.
 hipError_t launch_f8_tiled(const F8Product& p, F8Epilogue epilogue, float* partials, hipStream_t st);
 
 hipError_t launch_matrix_pack(int count, int N, int K, int dtype, const void* w, int64_t stride, void* matrix, hipStream_t st);

@@ -117,19 +117,26 @@ __global__ __launch_bounds__(256) void unpack_kernel(const uint8_t* __restrict__
 }
 
 // Rows of a product's left operand.  A wavefront takes four blocks of a row, one dword of scales: 16 lanes a block, eight elements a lane.
-__global__ __launch_bounds__(256) void rows_kernel(const bf16_t* __restrict__ x, int64_t stride, int K, F8Rows to, int kg, long long units) {
+__global__ __launch_bounds__(256) void rows_kernel(const bf16_t* __restrict__ x, int64_t stride, int K, F8Rows to, int kb, int kg, long long units,
+                                                   const int32_t* __restrict__ perm, int k_of, const int32_t* __restrict__ end) {
     const long long unit = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (unit >= units) return;
     const int lane = threadIdx.x & 63;
     const int row = (int)(unit / kg), group = (int)(unit % kg);
+    long long from = row;
+    if (perm != nullptr) {
+        if (row >= *end) return;  // (perm is not set there)
+        from = (uint32_t)perm[row] / (uint32_t)k_of;
+    }
     const int k = group * 4 * kF8Block + lane * 8;
     float v[8];
-    load8(x + (size_t)row * stride + (k < K ? k : 0), k < K, v);
+    load8(x + from * stride + (k < K ? k : 0), k < K, v);
     uint32_t top = top_of(v);
 #pragma unroll
     for (int o = 1; o < 16; o <<= 1) top = umax(top, (uint32_t)__shfl_xor((int)top, o));
     uint32_t byte = f8_scale_byte(top);
-    if (k < to.stride) *reinterpret_cast<uint2*>(to.codes + (size_t)row * to.stride + k) = codes_of(v, f8_inverse(byte));
+    if (k < kb * kF8Block)
+        *reinterpret_cast<uint2*>(to.codes + (size_t)row * to.row_step + (size_t)(k >> 4) * to.piece_step + (k & 8)) = codes_of(v, f8_inverse(byte));
     byte <<= 8 * (lane >> 4);
     byte |= (uint32_t)__shfl_xor((int)byte, 16);
     byte |= (uint32_t)__shfl_xor((int)byte, 32);
@@ -138,10 +145,10 @@ __global__ __launch_bounds__(256) void rows_kernel(const bf16_t* __restrict__ x,
 
 }  // namespace
 
-hipError_t launch_f8_rows(const void* x, int64_t stride, int rows, int K, const F8Rows& to, hipStream_t st) {
-    const int kg = f8_layout(1, K).kg;
-    const long long units = (long long)rows * kg;
-    rows_kernel<<<(unsigned)((units + 3) / 4), 256, 0, st>>>(static_cast<const bf16_t*>(x), stride, K, to, kg, units);
+hipError_t launch_f8_rows(const void* x, int64_t stride, int K, const F8Rows& to, const int32_t* perm, int k, const int32_t* end, hipStream_t st) {
+    const F8Layout lay = f8_layout(1, K);
+    const long long units = (long long)to.rows * lay.kg;
+    rows_kernel<<<(unsigned)((units + 3) / 4), 256, 0, st>>>(static_cast<const bf16_t*>(x), stride, K, to, lay.kb, lay.kg, units, perm, k, end);
     return hipGetLastError();
 }
 
