@@ -84,6 +84,10 @@ __global__ __launch_bounds__(256) void pack_kernel(const E* __restrict__ w, int6
     // the scale, and zeros for the columns behind the last block that share its dword
     if ((int)threadIdx.x < 4 && (kb == lay.kb - 1 || threadIdx.x == 0) && kb + (int)threadIdx.x < 4 * lay.kg)
         to[codes + (size_t)nb * 4 * lay.kg + kb + threadIdx.x] = threadIdx.x == 0 ? (uint8_t)byte : 0;
+    if (blockIdx.x == gridDim.x - 1) {  // and to whole 256 bytes
+        const size_t scales = codes + (size_t)lay.nb * 4 * lay.kg;
+        if (scales + threadIdx.x < bytes) to[scales + threadIdx.x] = 0;
+    }
 }
 
 template <class E>

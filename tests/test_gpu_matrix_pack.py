@@ -5,7 +5,7 @@ import torch
 
 import paper_2503_06823_amd as P
 from oracle import packed as ref
-from packed_util import bf16
+from packed_util import as_device, bf16, weights
 
 pytestmark = pytest.mark.gpu
 
@@ -95,3 +95,13 @@ def test_a_block_with_an_infinity_or_nan_is_nan_and_no_other_is(gpu_device, valu
 def test_bytes(gpu_device):
     for N, K in ((8, 8), (128, 128), (136, 520), (14336, 4096), (1032, 2808)):
         assert P.emoe_matrix_bytes(N, K) == ref.matrix_bytes(N, K)
+
+
+@pytest.mark.parametrize("N,K,count", [(136, 264, 2), (8, 8, 3), (128, 128 * 64, 1), (264, 8208, 2)])
+def test_every_byte_of_a_matrix_is_written(gpu_device, N, K, count):
+    """Whatever the room held: the bytes depend on the input only."""
+    w = np.stack([weights(np.random.default_rng(N + i), N, K) for i in range(count)])
+    room = torch.full((count * P.emoe_matrix_bytes(N, K) + 256,), 171, dtype=torch.uint8, device="cuda")
+    P.emoe_matrix_pack(count, N, K, "bf16", as_device(w), room)
+    got = room.cpu().numpy()
+    assert np.array_equal(got[:-256], np.concatenate([ref.pack(m) for m in w])) and (got[-256:] == 171).all()
