@@ -1,9 +1,9 @@
 """Serves a few requests on a small mixture-of-experts model with random weights: prompts first, then one token each a step, until
 all have what they asked for.  Every layer is attention over the paged 4-bit cache, then a MoE layer over the resident experts.
 
-    python examples/serve_moe.py [--steps N]
+    python examples/serve_moe.py [--steps N] [--packed]
 
-What is not the library's (projections, norms, rotary positions, the choice of the next token) is plain torch.
+With --packed the experts and all projections are matrices in 8 bits.  What is not the library's (projections in bf16, norms, rotary positions, the choice of the next token) is plain torch.
 """
 from __future__ import annotations
 
@@ -23,7 +23,7 @@ DEVICE = "cuda:0"
 class Model:
     """Random weights, four of eight experts resident in every layer."""
 
-    def __init__(self, layers=2, d=512, q_heads=8, kv_heads=2, head_dim=64, d_ff=1024, experts=8, resident=4, top_k=2, vocab=1000, seed=1):
+    def __init__(self, layers=2, d=512, q_heads=8, kv_heads=2, head_dim=64, d_ff=1024, experts=8, resident=4, top_k=2, vocab=1000, seed=1, packed=False):
         self.layers, self.d, self.q_heads, self.kv_heads, self.head_dim = layers, d, q_heads, kv_heads, head_dim
         self.d_ff, self.experts, self.resident, self.top_k = d_ff, experts, resident, top_k
         g = torch.Generator(device=DEVICE)
@@ -41,13 +41,25 @@ class Model:
                 qkv=normal((q_heads + 2 * kv_heads) * head_dim, d, std=d ** -0.5), out=normal(d, q_heads * head_dim, std=d ** -0.5),
                 moe=(normal(experts, d, std=d ** -0.5), None, slots, normal(resident, d_ff, d, std=d ** -0.5),
                      normal(resident, d_ff, d, std=d ** -0.5), normal(resident, d, d_ff, std=d_ff ** -0.5))))
-        self.buffers = {}
+        self.buffers, self.packed, self.ws = {}, packed, None
+        if packed:
+            self.head = P.PackedMatrices.pack(self.head)
+            for block in self.blocks:
+                block.update({name: P.PackedMatrices.pack(block[name]) for name in ("qkv", "out")})
+                block["moe"] = block["moe"][:3] + tuple(P.PackedMatrices.pack(w).data for w in block["moe"][3:])
+
+    def product(self, x, w):
+        if not self.packed:
+            return x @ w.t()
+        if self.ws is None or self.ws.numel() < w.workspace_bytes(len(x)):
+            self.ws = w.workspace(len(x))
+        return w.matmul(x, torch.empty((len(x), w.N), dtype=x.dtype, device=DEVICE), self.ws)
 
     def moe(self, block, x):
         T = x.shape[0]
         if T not in self.buffers:  # once per batch size
             self.buffers[T] = P.LayerBuffers.allocate(
-                P.make_desc(T, self.d, self.d_ff, self.experts, self.top_k, self.resident, "bf16", "swiglu"), DEVICE)
+                P.make_desc(T, self.d, self.d_ff, self.experts, self.top_k, self.resident, "f8" if self.packed else "bf16", "swiglu"), DEVICE)
         return P.layer_forward(self.buffers[T], x, *block["moe"], one_call=True)
 
     def forward(self, kv, tokens, max_new):
@@ -57,13 +69,13 @@ class Model:
         angle = kv.position[:T, None].float() * 10000.0 ** (-torch.arange(0, n, 2, device=DEVICE) / n)
         cos, sin = angle.cos()[:, None], angle.sin()[:, None]
         for i, block in enumerate(self.blocks):
-            heads = (norm(x) @ block["qkv"].t()).view(T, q + 2 * k, n)
+            heads = self.product(norm(x), block["qkv"]).view(T, q + 2 * k, n)
             rotate(heads[:, :q + k], cos, sin)
             kv.append(i, heads[:, q:q + k], heads[:, q + k:])
             attended = kv.attend(i, heads[:, :q], torch.empty((T, q, n), dtype=x.dtype, device=DEVICE), max_new)
-            x = x + attended.view(T, q * n) @ block["out"].t()
+            x = x + self.product(attended.view(T, q * n), block["out"])
             x = x + self.moe(block, norm(x))
-        return norm(x) @ self.head.t()
+        return self.product(norm(x), self.head)
 
 
 def norm(x):
@@ -112,8 +124,10 @@ def serve(model, prompts, steps, window=0, sinks=0, pages=None):
 def main():
     parser = argparse.ArgumentParser()
     parser.add_argument("--steps", type=int, default=24)
-    steps = max(parser.parse_args().steps, 6)
-    model = Model()
+    parser.add_argument("--packed", action="store_true")
+    args = parser.parse_args()
+    steps = max(args.steps, 6)
+    model = Model(packed=args.packed)
     g = torch.Generator().manual_seed(2)
     prompts = [torch.randint(0, 1000, (n,), generator=g).tolist() for n in (5, 130, 37, 1)]
     serve(model, prompts, steps)  # builds the buffers

@@ -14,3 +14,4 @@ from .binding import (EMOE_ACT_RELU, EMOE_ACT_SWIGLU, EMOE_BF16, EMOE_ERR_DEVICE
                       emoe_workspace_bytes, lib, make_desc, make_event, status_string)
 from .kv import KvCache
 from .layer import DeviceInputs, LayerBuffers, layer_forward
+from .packed import PackedMatrices
