@@ -6,7 +6,8 @@
 // matrix instruction (v_mfma_scale_f32_16x16x128_f8f6f4) wants them, so they go from memory to registers and nowhere else, a contiguous
 // KiB a load, eight strips (16 KiB) on their way a wavefront, and no wavefront waits for another before the end of K.  The matrix's rows
 // are the instruction's row operand, 16 rows of x its columns; the powers of two are operands of the instruction.
-// The partial sums meet in LDS, added in wavefront order.
+// The partial sums meet in LDS, added in wavefront order.  Few short rows are converted to 8 bits here, by each workgroup for itself, while the matrix's
+// first strips are on their way; other rows by a launch before.
 //
 // The instruction adds the products of eight consecutive elements in units of 2^-13 of the largest pair's power of two, and all else in
 // fp32: 1.5e-5 of a sum of random products, a hundredth of the rounding of the result to bf16.  (The bf16 instruction, on exact
@@ -39,10 +40,68 @@ __device__ __forceinline__ intx8 two(__amdgpu_buffer_rsrc_t from, uint32_t lane,
 constexpr int row_groups(int epilogue, int strips) { return epilogue == kF8Plain ? 1 : 8 / strips; }
 constexpr int matrices(int epilogue) { return epilogue == kF8Swiglu ? 2 : 1; }
 
-// Rows row0 .. row_end - 1 of x times a unit of their group's matrix, 16 TB at a time.
-template <int EPI, int TB, int STRIPS, int WAVES, int POLICY>
+// A workgroup's rows of x where it converts them itself: codes [row][kb][128], and the powers [row][kb] as bytes
+struct OwnRows {
+    uint8_t codes[kF8OwnBlocks * kF8Block];
+    uint8_t powers[kF8OwnBlocks];
+};
+// Their conversion, 16 lanes a block and eight elements a lane, in two parts: the loads, and once the matrix's first loads are on their way the rest
+template <int WAVES>
+struct RowsInFlight {
+    static constexpr int kRounds = kF8OwnBlocks * 16 / (64 * WAVES);
+    uint4 raw[kRounds];
+    __device__ __forceinline__ void request(const F8Product& p, int row0, int row_end) {
+        const int kb = p.lay.kb, units = (row_end - row0) * kb * 16;
+        const uint32_t inverse = 65536u / (uint32_t)kb + 1u;  // (block * inverse) >> 16 is block / kb up to kF8OwnBlocks
+        uint32_t row[kRounds];
+        int k[kRounds];
+#pragma unroll
+        for (int i = 0; i < kRounds; ++i) {
+            const int u = i * 64 * WAVES + threadIdx.x, block = u >> 4, r = (int)((uint32_t)block * inverse >> 16);
+            k[i] = u < units ? (block - r * kb) * kF8Block + (u & 15) * 8 : p.K;
+            row[i] = u < units ? row0 + r : row0;
+        }
+        if (p.perm != nullptr) {
+#pragma unroll
+            for (int i = 0; i < kRounds; ++i) row[i] = (uint32_t)p.perm[row[i]];
+#pragma unroll
+            for (int i = 0; i < kRounds; ++i) row[i] /= (uint32_t)p.k;
+        }
+#pragma unroll
+        for (int i = 0; i < kRounds; ++i) {
+            raw[i] = make_uint4(0, 0, 0, 0);
+            if (k[i] < p.K) raw[i] = *reinterpret_cast<const uint4*>(p.from + (int64_t)row[i] * p.from_stride + k[i]);
+        }
+    }
+    __device__ __forceinline__ void convert(const F8Product& p, int row0, int row_end, OwnRows& own) const {
+        const int units = (row_end - row0) * p.lay.kb * 16;
+#pragma unroll
+        for (int i = 0; i < kRounds; ++i) {
+            if (i * 64 * WAVES >= units) break;
+            const int u = i * 64 * WAVES + threadIdx.x;
+            float v[8];
+            f8_widened(raw[i], v);
+            uint32_t top = f8_top(v);
+#pragma unroll
+            for (int o = 1; o < 16; o <<= 1) top = umax(top, (uint32_t)__shfl_xor((int)top, o));
+            const uint32_t byte = f8_scale_byte(top);
+            if (u < units) {
+                *reinterpret_cast<uint2*>(own.codes + u * 8) = f8_codes(v, f8_inverse(byte));
+                if ((u & 15) == 0) own.powers[u >> 4] = (uint8_t)byte;
+            }
+        }
+        // a barrier for LDS alone: the matrix's loads stay on their way
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+    }
+};
+
+// Rows row0 .. row_end - 1 of x times a unit of their group's matrix, 16 TB at a time, with TB < 4 all of them.  OWN: x is converted here.
+template <int EPI, int TB, int STRIPS, int WAVES, int POLICY, bool OWN>
 __device__ __forceinline__ void multiply_unit(const F8Product& p, int unit, int group, int row0, int row_end, floatx4 (&red)[WAVES][STRIPS][64],
-                                              uint32_t (&tops)[WAVES][64]) {
+                                              uint32_t (&tops)[WAVES][64], OwnRows* own) {
+    static_assert(!OWN || TB == 1, "at most 16 rows");
     constexpr int M = matrices(EPI), H = row_groups(EPI, STRIPS), SPLIT = WAVES / (M * H);
     static_assert(SPLIT >= 1 && SPLIT * M * H == WAVES, "every wavefront has a part");
     constexpr int DEPTH = ring(TB, STRIPS, WAVES) / STRIPS;  // blocks of columns of a wavefront on their way
@@ -72,8 +131,13 @@ __device__ __forceinline__ void multiply_unit(const F8Product& p, int unit, int 
         for (int t = 0; t < TB; ++t) {
             int r = tok0 + 16 * t + tok;
             r = r < row_end ? r : row_end - 1;  // (rows past the end are multiplied and not stored)
-            x_lane[t] = (uint32_t)r * p.x.row_step + (uint32_t)quad * p.x.piece_step;
-            xs_lane[t] = (uint32_t)r * 4;
+            if constexpr (OWN) {
+                xs_lane[t] = (uint32_t)((r - row0) * p.lay.kb);  // its first block
+                x_lane[t] = xs_lane[t] * kF8Block + quad * 16;
+            } else {
+                x_lane[t] = (uint32_t)r * p.x.row_step + (uint32_t)quad * p.x.piece_step;
+                xs_lane[t] = (uint32_t)r * 4;
+            }
         }
         intx8 w[DEPTH][STRIPS], x[DEPTH][TB];
         uint32_t xb[DEPTH][TB], wb[DEPTH];
@@ -83,20 +147,36 @@ __device__ __forceinline__ void multiply_unit(const F8Product& p, int unit, int 
             const uint32_t b = there ? part + j * SPLIT : part, lane_at = there ? lane * 16u : codes;
 #pragma unroll
             for (int i = 0; i < STRIPS; ++i) w[slot][i] = two<POLICY>(w_rsrc, lane_at, w_at + b * kF8BlockBytes + i * kF8Strip, 1024);
+            wb[slot] = w_scales[b >> 2];
         };
         auto load_x = [&](int slot, int j) {
             const bool there = j < mine;
             const int b = there ? part + j * SPLIT : part;
 #pragma unroll
             for (int t = 0; t < TB; ++t) {
+                if constexpr (OWN) {  // (behind the last block the first one again: its products are with zeros)
+                    const int at = there ? b : 0;
+                    const uintx4* from = reinterpret_cast<const uintx4*>(own->codes + x_lane[t] + at * kF8Block);
+                    x[slot][t] = __builtin_bit_cast(intx8, __builtin_shufflevector(from[0], from[4], 0, 1, 2, 3, 4, 5, 6, 7));
+                    xb[slot][t] = own->powers[xs_lane[t] + at];
+                    continue;
+                }
                 x[slot][t] = two<0>(x_rsrc, there ? x_lane[t] : x_bytes, (uint32_t)b * x_block, (int)(x_block / 2));
                 xb[slot][t] = __builtin_amdgcn_raw_buffer_load_b32(xs_rsrc, (int)(there ? xs_lane[t] : xs_bytes), (b >> 2) * p.x.rows * 4, 0);
             }
-            wb[slot] = w_scales[b >> 2];
         };
+        if constexpr (OWN) {
+            RowsInFlight<WAVES> rows;
+            rows.request(p, row0, row_end);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int d = 0; d < DEPTH; ++d) load_w(d, d);
+            __builtin_amdgcn_sched_barrier(0);
+            rows.convert(p, row0, row_end, *own);
+        }
 #pragma unroll
         for (int d = 0; d < DEPTH; ++d) {
-            load_w(d, d);
+            if constexpr (!OWN) load_w(d, d);
             load_x(d, d);
         }
         floatx4 acc[STRIPS][TB];
@@ -112,7 +192,7 @@ __device__ __forceinline__ void multiply_unit(const F8Product& p, int unit, int 
                 uint32_t xbc[TB];
                 const uint32_t wbc = j + d < mine ? wb[d] >> shift : 127u;  // (zeros times any power but NaN)
 #pragma unroll
-                for (int t = 0; t < TB; ++t) xbc[t] = xb[d][t] >> shift;
+                for (int t = 0; t < TB; ++t) xbc[t] = OWN ? xb[d][t] : xb[d][t] >> shift;
 #pragma unroll
                 for (int i = 0; i < STRIPS; ++i)
 #pragma unroll
@@ -195,14 +275,20 @@ __device__ __forceinline__ void multiply_unit(const F8Product& p, int unit, int 
             }
             __syncthreads();  // tops are free again
         }
+        if constexpr (TB < 4) break;  // (no loop for the compiler: the matrix's powers are scalar loads)
     }
 }
 
 // MOST: blocks of 16 rows that a group has at most, or those of a pass
-template <int EPI, int MOST, int STRIPS, int WAVES>
+template <int EPI, int MOST, int STRIPS, int WAVES, bool OWN>
 __global__ __launch_bounds__(64 * WAVES) void stream_kernel(F8Product p, int n_units) {
     __shared__ floatx4 red[WAVES][STRIPS][64];
     __shared__ uint32_t tops[WAVES][64];
+    OwnRows* own = nullptr;
+    if constexpr (OWN) {
+        __shared__ __align__(16) OwnRows rows;
+        own = &rows;
+    }
     const int unit = blockIdx.x % n_units, group = blockIdx.x / n_units;
     int row0 = 0, row_end = p.rows;
     if (p.offsets != nullptr) {
@@ -212,16 +298,23 @@ __global__ __launch_bounds__(64 * WAVES) void stream_kernel(F8Product p, int n_u
         row_end = row_end < p.rows ? row_end : p.rows;
     }
     if (row_end <= row0) return;  // its matrix is never touched
-    if (MOST == 1 || row_end - row0 <= 16) multiply_unit<EPI, 1, STRIPS, WAVES, 2>(p, unit, group, row0, row_end, red, tops);
-    else if (MOST == 2 || row_end - row0 <= 32) multiply_unit<EPI, MOST < 2 ? 1 : 2, STRIPS, WAVES, 2>(p, unit, group, row0, row_end, red, tops);
-    else multiply_unit<EPI, MOST, STRIPS, WAVES, 2>(p, unit, group, row0, row_end, red, tops);
+    if (MOST == 1 || row_end - row0 <= 16) multiply_unit<EPI, 1, STRIPS, WAVES, 2, OWN>(p, unit, group, row0, row_end, red, tops, own);
+    else if (MOST == 2 || row_end - row0 <= 32) multiply_unit<EPI, MOST < 2 ? 1 : 2, STRIPS, WAVES, 2, OWN>(p, unit, group, row0, row_end, red, tops, own);
+    else multiply_unit<EPI, MOST, STRIPS, WAVES, 2, OWN>(p, unit, group, row0, row_end, red, tops, own);
 }
 
 template <int EPI, int MOST, int STRIPS, int WAVES>
 hipError_t launch_shape(const F8Product& p, hipStream_t st) {
     constexpr int all = STRIPS * row_groups(EPI, STRIPS);
     const int n_units = (p.N + 16 * all - 1) / (16 * all);
-    stream_kernel<EPI, MOST, STRIPS, WAVES><<<(unsigned)(p.groups * n_units), 64 * WAVES, 0, st>>>(p, n_units);
+    const unsigned grid = (unsigned)(p.groups * n_units);
+    if constexpr (MOST == 1) {
+        if (p.from != nullptr) {
+            stream_kernel<EPI, MOST, STRIPS, WAVES, true><<<grid, 64 * WAVES, 0, st>>>(p, n_units);
+            return hipGetLastError();
+        }
+    }
+    stream_kernel<EPI, MOST, STRIPS, WAVES, false><<<grid, 64 * WAVES, 0, st>>>(p, n_units);
     return hipGetLastError();
 }
 

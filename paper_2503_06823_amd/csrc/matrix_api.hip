@@ -98,6 +98,12 @@ FfnF8Ws ffn_ws(const emoe_layer_desc& d, void* ws) {
     return w;
 }
 
+void own_rows(F8Product& p, const void* x, int64_t stride, int K) {
+    p.from = static_cast<const bf16_t*>(x);
+    p.from_stride = stride;
+    p.K = K;
+}
+
 hipError_t multiply(const F8Product& p, int K, F8Epilogue epilogue, float* partials, hipStream_t st) {
     return is_tiled(p.rows, p.groups, p.N, K) ? launch_f8_tiled(p, epilogue, partials, st) : launch_f8_stream(p, epilogue, st);
 }
@@ -146,11 +152,18 @@ hipError_t launch_ffn_f8(const emoe_layer_desc& d, const void* x_perm, RowGather
         p.matrix_bytes = p.lay.bytes();
         p.N = d.d_ff;
         p.h = h;
-        e = launch_f8_rows(x_perm, d.d_model, d.d_model, p.x, tiled ? nullptr : gather.perm, gather.k, offsets + d.S, st);
+        if (!tiled && f8_own_rows(A, d.d_model)) {
+            own_rows(p, x_perm, d.d_model, d.d_model);
+            p.perm = gather.perm;
+            p.k = gather.k;
+        } else {
+            e = launch_f8_rows(x_perm, d.d_model, d.d_model, p.x, tiled ? nullptr : gather.perm, gather.k, offsets + d.S, st);
+        }
         if (e == hipSuccess) e = multiply(p, d.d_model, swiglu ? kF8Swiglu : kF8Relu, lay.partials, st);
     }
     if (e != hipSuccess || !(passes & 2)) return e;
     p.x = h;
+    p.from = nullptr;
     p.perm = nullptr;
     p.k = 1;
     p.w0 = static_cast<const uint8_t*>(w2);
@@ -219,8 +232,10 @@ int emoe_matmul(const emoe_matmul_desc* desc, const void* x, const int32_t* grou
     if (!ws || ws_bytes < lay.total) return EMOE_ERR_WORKSPACE;
     hipStream_t st = static_cast<hipStream_t>(stream);
     F8Product p = {};
-    p.x = ordered(lay.x, desc->K, is_tiled(desc->rows, desc->groups, desc->N, desc->K));
-    if (launch_f8_rows(x, desc->x_stride, desc->K, p.x, nullptr, 1, nullptr, st) != hipSuccess) return EMOE_ERR_DEVICE;
+    const bool tiled = is_tiled(desc->rows, desc->groups, desc->N, desc->K);
+    p.x = ordered(lay.x, desc->K, tiled);
+    if (!tiled && f8_own_rows(desc->rows, desc->K)) own_rows(p, x, desc->x_stride, desc->K);
+    else if (launch_f8_rows(x, desc->x_stride, desc->K, p.x, nullptr, 1, nullptr, st) != hipSuccess) return EMOE_ERR_DEVICE;
     p.k = 1;
     p.offsets = group_offsets;
     p.groups = desc->groups;

@@ -36,7 +36,7 @@ inline size_t f8_rows_scale_bytes(long long rows, int K) { return (size_t)rows *
 enum F8Epilogue { kF8Plain = 0, kF8Swiglu = 1, kF8Relu = 2 };
 struct F8Product {
     F8Rows x;
-    const int32_t* perm;  // (tiles) grouped row r is row perm[r] / k of x; NULL: r
+    const int32_t* perm;  // (tiles, and `from`) grouped row r is row perm[r] / k of x; NULL: r
     int k;
     const int32_t* offsets;
     int groups;
@@ -50,11 +50,19 @@ struct F8Product {
     int64_t out_stride;
     const int32_t* out_perm;  // row r is stored as row out_perm[r]; NULL: r
     F8Rows h;
+    const bf16_t* from;  // (streaming) NULL, or the rows themselves, x not being there: workgroups convert them
+    int64_t from_stride;
+    int K;
 };
+// Whether streaming converts the rows itself, every workgroup all of its own: what a launch costs, against work that each repeats.  Measured in a graph
+// (us, converted by the workgroups / by a launch before): 6144 x 4096, 1 row 7.5 / 9.7, 4 rows 9.2 / 9.9; 6144 x 1024, 16 rows 6.8 / 6.8; 4096 x 14336, 1 row
+// 13.4 / 15.9; 16 rows of 16 groups of 2816 x 1024 10.7 / 13.3; one token's experts of 14336 x 4096 60.2 / 62.9.
+constexpr int kF8OwnBlocks = 128;
+inline bool f8_own_rows(long long rows, int K) { return rows <= 16 && rows * f8_layout(1, K).kb <= kF8OwnBlocks; }
 
 // Row r of `to` is row r of x, or with perm row perm[r] / k; of these only the rows before *end.
 hipError_t launch_f8_rows(const void* x, int64_t stride, int K, const F8Rows& to, const int32_t* perm, int k, const int32_t* end, hipStream_t st);
-// x by pieces, a row of it for each grouped row
+// x by pieces, a row of it for each grouped row; or `from`
 hipError_t launch_f8_stream(const F8Product& p, F8Epilogue epilogue, hipStream_t st);
 // partials: kTiledPartialBytes.  x by rows; at least two blocks of columns.
 hipError_t launch_f8_tiled(const F8Product& p, F8Epilogue epilogue, float* partials, hipStream_t st);
@@ -88,6 +96,24 @@ __device__ __forceinline__ uint32_t f8_codes(float a, float b, float c, float d,
 }
 __device__ __forceinline__ uint32_t f8_magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 __device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
+// The same of eight at once
+__device__ __forceinline__ void f8_widened(uint4 bf16s, float (&v)[8]) {
+    const uint32_t w[4] = {bf16s.x, bf16s.y, bf16s.z, bf16s.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ uint32_t f8_top(const float (&v)[8]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = umax(m, f8_magnitude(v[i]));
+    return m;
+}
+__device__ __forceinline__ uint2 f8_codes(const float (&v)[8], float inverse) {
+    return make_uint2(f8_codes(v[0], v[1], v[2], v[3], inverse), f8_codes(v[4], v[5], v[6], v[7], inverse));
+}
 #endif
 
 }  // namespace emoe

@@ -8,13 +8,7 @@ namespace {
 
 // Eight elements from memory, as numbers; zeros where there are none.
 __device__ __forceinline__ void load8(const bf16_t* p, bool there, float (&v)[8]) {
-    uint4 r = there ? *reinterpret_cast<const uint4*>(p) : make_uint4(0, 0, 0, 0);
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
+    f8_widened(there ? *reinterpret_cast<const uint4*>(p) : make_uint4(0, 0, 0, 0), v);
 }
 __device__ __forceinline__ void load8(const float* p, bool there, float (&v)[8]) {
 #pragma unroll
@@ -32,16 +26,6 @@ __device__ __forceinline__ void store8(bf16_t* p, const float (&v)[8]) {
 __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
     *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
     *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
-}
-
-__device__ __forceinline__ uint32_t top_of(const float (&v)[8]) {
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = umax(m, f8_magnitude(v[i]));
-    return m;
-}
-__device__ __forceinline__ uint2 codes_of(const float (&v)[8], float inverse) {
-    return make_uint2(f8_codes(v[0], v[1], v[2], v[3], inverse), f8_codes(v[4], v[5], v[6], v[7], inverse));
 }
 
 // A workgroup takes a block.  Pass i covers rows 16 i .. 16 i + 15, a thread eight columns of one row: reads are whole
@@ -70,7 +54,7 @@ __global__ __launch_bounds__(256) void pack_kernel(const E* __restrict__ w, int6
     for (int i = 0; i < 8; ++i) {
         const int n = n0 + 16 * i;
         load8(from + (size_t)(n < N ? n : 0) * stride + (k < K ? k : 0), n < N && k < K, v[i]);
-        top = umax(top, top_of(v[i]));
+        top = umax(top, f8_top(v[i]));
     }
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) top = umax(top, (uint32_t)__shfl_xor((int)top, o));
@@ -80,7 +64,7 @@ __global__ __launch_bounds__(256) void pack_kernel(const E* __restrict__ w, int6
     const float inverse = f8_inverse(byte);
     uint8_t* block = to + (size_t)(nb * lay.kb + kb) * kF8BlockBytes + at.code;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) *reinterpret_cast<uint2*>(block + i * kF8Strip) = codes_of(v[i], inverse);
+    for (int i = 0; i < 8; ++i) *reinterpret_cast<uint2*>(block + i * kF8Strip) = f8_codes(v[i], inverse);
     // the scale, and zeros for the columns behind the last block that share its dword
     if ((int)threadIdx.x < 4 && (kb == lay.kb - 1 || threadIdx.x == 0) && kb + (int)threadIdx.x < 4 * lay.kg)
         to[codes + (size_t)nb * 4 * lay.kg + kb + threadIdx.x] = threadIdx.x == 0 ? (uint8_t)byte : 0;
@@ -135,12 +119,12 @@ __global__ __launch_bounds__(256) void rows_kernel(const bf16_t* __restrict__ x,
     const int k = group * 4 * kF8Block + lane * 8;
     float v[8];
     load8(x + from * stride + (k < K ? k : 0), k < K, v);
-    uint32_t top = top_of(v);
+    uint32_t top = f8_top(v);
 #pragma unroll
     for (int o = 1; o < 16; o <<= 1) top = umax(top, (uint32_t)__shfl_xor((int)top, o));
     uint32_t byte = f8_scale_byte(top);
     if (k < kb * kF8Block)
-        *reinterpret_cast<uint2*>(to.codes + (size_t)row * to.row_step + (size_t)(k >> 4) * to.piece_step + (k & 8)) = codes_of(v, f8_inverse(byte));
+        *reinterpret_cast<uint2*>(to.codes + (size_t)row * to.row_step + (size_t)(k >> 4) * to.piece_step + (k & 8)) = f8_codes(v, f8_inverse(byte));
     byte <<= 8 * (lane >> 4);
     byte |= (uint32_t)__shfl_xor((int)byte, 16);
     byte |= (uint32_t)__shfl_xor((int)byte, 32);

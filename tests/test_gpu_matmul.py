@@ -149,3 +149,22 @@ def test_graph_replays(gpu_device, rows):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want[i])
+
+
+@pytest.mark.parametrize("groups", (1, 4))
+def test_rows_converted_by_a_launch_or_by_the_product_are_the_same(gpu_device, groups):
+    """12 rows of ten blocks are still converted by the product, 13 are not; both take a row of any distance."""
+    g = np.random.default_rng(groups)
+    x, data = as_device(tokens(g, 16, 1160)), packed([weights(g, 264, 1160) for _ in range(groups)])
+    edges = lambda rows: None if groups == 1 else [0, 2, 2, 11, rows]
+    many = matmul(x, data, 264, edges(16))
+    for rows in (12, 13):
+        assert torch.equal(matmul(x[:rows], data, 264, edges(rows)), many[:rows])
+        assert torch.equal(matmul(x[:rows], data, 264, edges(rows), x_gap=24), many[:rows])
+
+
+@pytest.mark.parametrize("rows,K", [(1, 16384), (2, 8192), (4, 4096), (3, 5376), (5, 3200), (16, 1024), (15, 1016), (16, 8), (7, 2296)])
+def test_the_most_that_a_product_converts(gpu_device, rows, K):
+    g = np.random.default_rng(K)
+    check(tokens(g, rows, K), [weights(g, 136, K)])
+    check(tokens(g, rows, K), [weights(g, 136, K) for _ in range(3)], [0, rows // 2, rows // 2, rows])

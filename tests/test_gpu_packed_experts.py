@@ -236,3 +236,19 @@ def test_packed_experts_are_loaded(gpu_device):
     P.layer_forward(want, x, gate, None, soe, *[w[[4, 1, 5]].contiguous() for w in m])
     torch.cuda.synchronize()
     assert torch.equal(b.out, want.out)
+
+
+@pytest.mark.parametrize("T,k", [(1, 2), (3, 2), (4, 2), (16, 1), (8, 1), (2, 4)])
+@pytest.mark.parametrize("d,act", [(2056, "swiglu"), (1024, "relu")])
+def test_few_tokens_whose_rows_the_first_product_converts(gpu_device, T, k, d, act):
+    a = Layer(T, d, 264, 5, k, act)
+    want, off = a.experts()
+    a.gather()
+    torch.cuda.synchronize()
+    close(a.y[:T * k], want, off)
+    # the same from rows that the caller has grouped
+    y = torch.full_like(a.y, 5.0)
+    grouped = a.dev["x"][torch.from_numpy(a.perm // k).cuda()].contiguous()
+    P.emoe_expert_ffn(a.desc, grouped, a.dev["offsets"], a.m1, a.m3, a.m2, y, a.ws, a.ws.numel())
+    torch.cuda.synchronize()
+    assert torch.equal(y, a.y)
