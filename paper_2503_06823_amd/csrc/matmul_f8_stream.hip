@@ -22,8 +22,7 @@ typedef unsigned int uintx4 __attribute__((ext_vector_type(4)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
-// Strips of a wavefront on their way, by the registers that they and the rows of x take
-constexpr int ring(int tb, int strips, int waves) { return tb == 4 && strips < 4 && waves > 4 ? 2 * strips : 8; }
+constexpr int kRing = 8;  // strips of a wavefront on their way
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void* base, uint32_t bytes) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)bytes, 0x00020000);
@@ -104,7 +103,7 @@ __device__ __forceinline__ void multiply_unit(const F8Product& p, int unit, int 
     static_assert(!OWN || TB == 1, "at most 16 rows");
     constexpr int M = matrices(EPI), H = row_groups(EPI, STRIPS), SPLIT = WAVES / (M * H);
     static_assert(SPLIT >= 1 && SPLIT * M * H == WAVES, "every wavefront has a part");
-    constexpr int DEPTH = ring(TB, STRIPS, WAVES) / STRIPS;  // blocks of columns of a wavefront on their way
+    constexpr int DEPTH = kRing / STRIPS;  // blocks of columns of a wavefront on their way
     constexpr int ALL = STRIPS * H;       // strips of a unit, of one matrix
     constexpr int FINAL = ALL >= WAVES ? ALL / WAVES : 1;  // that a wavefront finishes
     constexpr int ROWS = 16 * TB;
@@ -318,18 +317,22 @@ hipError_t launch_shape(const F8Product& p, hipStream_t st) {
     return hipGetLastError();
 }
 
+// A wavefront's strips by the strips that there are: more of them a wavefront read x less often, fewer leave no CU without work.  Measured with matrices from
+// HBM, plain products of 17 to 64 rows a group (us, two strips / four, four wavefronts): 384 strips 15.7 / 17.1 (6144 x 4096), 256 14.7 / 16.6, 768
+// 25.8 / 19.7, 1040 12.7 / 10.3 (16 groups of 1032 x 776), 2048 96 / 89 (8 of 4096 x 14336), 7168 126 / 97; eight wavefronts of four strips 18.2, 17.3, 20.7,
+// 12.4, 89, 102.  The activations' products, which want 128 rows a unit, with four wavefronts / eight: 20 rows of 6 groups of 14336 x 4096 121 / 121 (SwiGLU),
+// 71 / 74 (ReLU), of 16 of 2816 x 1032 30.7 / 31.1, 21.2 / 22.0, one row of 32 of 512 x 512 9.5 / 10.2, 7.9 / 9.0; with eight strips a wavefront 130, 72, 32.5, 21.6, 9.9, 7.9.
 template <int EPI>
 hipError_t launch(const F8Product& p, hipStream_t st) {
     const long long groups = p.groups < p.rows ? p.groups : p.rows;  // that can have rows
     const bool few = p.rows <= 16;
     if constexpr (EPI == kF8Plain) {
         const long long strips = groups * ((p.N + 15) / 16);
-        if (strips >= 4 * 512) return few ? launch_shape<EPI, 1, 4, 4>(p, st) : launch_shape<EPI, 4, 4, 8>(p, st);
-        if (!few) return launch_shape<EPI, 4, 2, 4>(p, st);
+        if (!few) return strips > 512 ? launch_shape<EPI, 4, 4, 4>(p, st) : launch_shape<EPI, 4, 2, 4>(p, st);
+        if (strips >= 4 * 512) return launch_shape<EPI, 1, 4, 4>(p, st);
         return strips > 256 ? launch_shape<EPI, 1, 2, 4>(p, st) : launch_shape<EPI, 1, 1, 4>(p, st);
     } else {
-        if (!few) return launch_shape<EPI, 4, 4, 8>(p, st);
-        return launch_shape<EPI, 1, 4, 8>(p, st);
+        return few ? launch_shape<EPI, 1, 4, 4>(p, st) : launch_shape<EPI, 4, 4, 4>(p, st);
     }
 }
 

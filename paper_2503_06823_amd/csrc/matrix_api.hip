@@ -49,16 +49,25 @@ F8Rows rows_at(uint8_t* ws, size_t* at, long long rows, int K) {
     return r;
 }
 
-// Which kernel multiplies: by the rows that a group has on average (their numbers live on the device).  Streaming costs a matrix's bytes for every 64 rows, and
-// more where these are over 32; tiles of 256 x 256 cost the bytes once, some 10 us for their two launches, and leave CUs without work
-// where they are few.  Measured with matrices from HBM (us, streaming / tiles): 8 groups of 14336 x 4096, 32 rows each 105 / 102, 48 127 / 106; 24 of
-// 1408 x 2048, 32 29.6 / 30.5, 48 38.6 / 31.5; 64 of 512 x 512, 32 15.6 / 17.1, 48 19.4 / 18.1; one of 6144 x 4096 (24 tiles), 64 18.1 / 25.3,
-// 128 29.0 / 30.5, 160 38.3 / 31.1; one of 1024 x 1024 (4 tiles), 128 15.9 / 18.1.  Tiles take at least two blocks of columns.
-constexpr long long kManyTiles = 64, kStreamRows = 36, kStreamRowsFewTiles = 128;
-bool is_tiled(long long rows, int groups, int N, int K) {
-    const long long tiles = (long long)groups * ((N + 255) / 256);
-    return rows > (tiles >= kManyTiles ? kStreamRows : kStreamRowsFewTiles) * groups && K > kF8Block;
+// Which kernel multiplies: by the rows that a group has on average (their numbers live on the device).  Streaming reads a matrix once for every 64 rows, the
+// second time half from caches; tiles of 256 x 256 read it once, but cost some 10 us more, and leave CUs without work where they are few.  So few tiles of small
+// matrices take over where 128 rows end, other matrices where 64 do, and several, of which some have more rows than others, from 48 on.  Measured with
+// matrices from HBM (us, streaming / tiles): 6144 x 4096 (24 tiles) 64 rows 15.8 / 25.4, 128 25.4 / 29.4, 160 33.3 / 30.2; 8 groups of 2048 x 2048 (64), 128
+// rows each 25.9 / 33.2, 160 34.4 / 34.3; 32000 x 4096 (125) 64 rows 36.0 / 47.8, 80 57.3 / 48.5; 8 of 4096 x 14336 (128) 64 109 / 122, 80 195 / 128; 8 of
+// 14336 x 4096 (448) 36 108 / 103, 64 114 / 106; 24 of 2048 x 1408 (192) 36 29.7 / 26.3, 64 33.1 / 28.7; SwiGLU's two of 6 groups of 14336 x 4096 (672) 36
+// 138 / 144, 64 155 / 144, of 16 of 2816 x 1032 (352) 64 40.1 / 43.5, 80 69 / 46; one ReLU product of 14336 x 4096 (56) 64 26.7 / 32.9, 80 43.8 / 33.6.
+// Tiles take at least two blocks of columns.
+constexpr long long kFewTiles = 64, kSmallMatrices = 48ll << 20;
+bool is_tiled(long long rows, int groups, int N, int K, int matrices) {
+    const long long tiles = (long long)groups * ((matrices * (long long)N + 255) / 256);
+    const bool small = tiles <= kFewTiles && (long long)groups * matrices * N * K <= kSmallMatrices;
+    const long long streamed = small ? 128 : groups == 1 ? 64 : 48;
+    return rows > streamed * groups && K > kF8Block;
 }
+bool first_is_tiled(const emoe_layer_desc& d) {
+    return is_tiled((long long)d.T * d.k, d.S, d.d_ff, d.d_model, d.act == EMOE_ACT_SWIGLU ? 2 : 1);
+}
+bool second_is_tiled(const emoe_layer_desc& d) { return is_tiled((long long)d.T * d.k, d.S, d.d_model, d.d_ff, 1); }
 
 // In the order that the kernel which multiplies them reads
 F8Rows ordered(F8Rows r, int K, bool by_rows) {
@@ -77,7 +86,7 @@ MatmulWs matmul_ws(const emoe_matmul_desc& d, void* ws) {
     w.total = 0;
     w.x = rows_at(static_cast<uint8_t*>(ws), &w.total, d.rows, d.K);
     w.partials = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + w.total);
-    if (is_tiled(d.rows, d.groups, d.N, d.K)) w.total += kTiledPartialBytes;
+    if (is_tiled(d.rows, d.groups, d.N, d.K, 1)) w.total += kTiledPartialBytes;
     return w;
 }
 
@@ -94,7 +103,7 @@ FfnF8Ws ffn_ws(const emoe_layer_desc& d, void* ws) {
     w.h = rows_at(static_cast<uint8_t*>(ws), &w.total, A, d.d_ff);
     w.x = rows_at(static_cast<uint8_t*>(ws), &w.total, A, d.d_model);
     w.partials = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + w.total);
-    if (is_tiled(A, d.S, d.d_ff, d.d_model) || is_tiled(A, d.S, d.d_model, d.d_ff)) w.total += kTiledPartialBytes;
+    if (first_is_tiled(d) || second_is_tiled(d)) w.total += kTiledPartialBytes;
     return w;
 }
 
@@ -104,8 +113,8 @@ void own_rows(F8Product& p, const void* x, int64_t stride, int K) {
     p.K = K;
 }
 
-hipError_t multiply(const F8Product& p, int K, F8Epilogue epilogue, float* partials, hipStream_t st) {
-    return is_tiled(p.rows, p.groups, p.N, K) ? launch_f8_tiled(p, epilogue, partials, st) : launch_f8_stream(p, epilogue, st);
+hipError_t multiply(bool tiled, const F8Product& p, F8Epilogue epilogue, float* partials, hipStream_t st) {
+    return tiled ? launch_f8_tiled(p, epilogue, partials, st) : launch_f8_stream(p, epilogue, st);
 }
 
 }  // namespace
@@ -129,7 +138,8 @@ hipError_t launch_ffn_f8(const emoe_layer_desc& d, const void* x_perm, RowGather
     const FfnF8Ws lay = ffn_ws(d, ws);
     const int A = d.T * d.k;
     const bool swiglu = d.act == EMOE_ACT_SWIGLU;
-    const F8Rows h = ordered(lay.h, d.d_ff, is_tiled(A, d.S, d.d_model, d.d_ff));
+    const bool second_tiled = second_is_tiled(d);
+    const F8Rows h = ordered(lay.h, d.d_ff, second_tiled);
     hipError_t e = hipSuccess;
     F8Product p = {};
     p.offsets = offsets;
@@ -137,7 +147,7 @@ hipError_t launch_ffn_f8(const emoe_layer_desc& d, const void* x_perm, RowGather
     p.rows = A;
     p.k = 1;
     if (passes & 1) {
-        const bool tiled = is_tiled(A, d.S, d.d_ff, d.d_model);
+        const bool tiled = first_is_tiled(d);
         p.x = lay.x;
         // tiles gather the rows themselves, so that each is read and converted once
         if (tiled && gather.perm != nullptr) {
@@ -159,7 +169,7 @@ hipError_t launch_ffn_f8(const emoe_layer_desc& d, const void* x_perm, RowGather
         } else {
             e = launch_f8_rows(x_perm, d.d_model, d.d_model, p.x, tiled ? nullptr : gather.perm, gather.k, offsets + d.S, st);
         }
-        if (e == hipSuccess) e = multiply(p, d.d_model, swiglu ? kF8Swiglu : kF8Relu, lay.partials, st);
+        if (e == hipSuccess) e = multiply(tiled, p, swiglu ? kF8Swiglu : kF8Relu, lay.partials, st);
     }
     if (e != hipSuccess || !(passes & 2)) return e;
     p.x = h;
@@ -174,7 +184,7 @@ hipError_t launch_ffn_f8(const emoe_layer_desc& d, const void* x_perm, RowGather
     p.out = static_cast<bf16_t*>(y_perm);
     p.out_stride = d.d_model;
     p.out_perm = gather.out_perm;
-    return multiply(p, d.d_ff, kF8Plain, lay.partials, st);
+    return multiply(second_tiled, p, kF8Plain, lay.partials, st);
 }
 
 }  // namespace emoe
@@ -232,7 +242,7 @@ int emoe_matmul(const emoe_matmul_desc* desc, const void* x, const int32_t* grou
     if (!ws || ws_bytes < lay.total) return EMOE_ERR_WORKSPACE;
     hipStream_t st = static_cast<hipStream_t>(stream);
     F8Product p = {};
-    const bool tiled = is_tiled(desc->rows, desc->groups, desc->N, desc->K);
+    const bool tiled = is_tiled(desc->rows, desc->groups, desc->N, desc->K, 1);
     p.x = ordered(lay.x, desc->K, tiled);
     if (!tiled && f8_own_rows(desc->rows, desc->K)) own_rows(p, x, desc->x_stride, desc->K);
     else if (launch_f8_rows(x, desc->x_stride, desc->K, p.x, nullptr, 1, nullptr, st) != hipSuccess) return EMOE_ERR_DEVICE;
@@ -246,7 +256,7 @@ int emoe_matmul(const emoe_matmul_desc* desc, const void* x, const int32_t* grou
     p.N = desc->N;
     p.out = static_cast<bf16_t*>(out);
     p.out_stride = desc->out_stride;
-    return status_of(multiply(p, desc->K, kF8Plain, lay.partials, st));
+    return status_of(multiply(tiled, p, kF8Plain, lay.partials, st));
 }
 
 }  // extern "C"

@@ -11,9 +11,9 @@ from test_gpu_matmul import check
 pytestmark = pytest.mark.gpu
 
 
-@pytest.mark.parametrize("each", (36, 37))
+@pytest.mark.parametrize("each", (36, 37, 48, 49, 128, 129))
 def test_many_tiles(gpu_device, each):
-    """64 groups of one tile in N: rows for streaming at most, and one more a group."""
+    """64 groups of one tile in N."""
     g = np.random.default_rng(each)
     sizes = np.full(64, each)
     sizes[3], sizes[4], sizes[9], sizes[10] = 0, 2 * each, 1, 2 * each - 1
@@ -96,3 +96,18 @@ def test_the_most_rows(gpu_device):
         sample(x, m.data[0], N, K, out, [0, 1, rows // 2, rows // 2 + 255, rows - 2, rows - 1], nb)
     with pytest.raises(P.EmoeError):
         m.workspace(rows + 1)
+
+
+@pytest.mark.parametrize("each", (47, 48, 49, 64, 65))
+def test_more_tiles(gpu_device, each):
+    """65 tiles in all, several matrices: rows for streaming at most, and one more a group, groups with more and with less."""
+    g = np.random.default_rng(each)
+    sizes = np.array([each, each + 30, 0, each - 30, each])
+    offsets = np.concatenate(([0], np.cumsum(sizes))).tolist()
+    check(tokens(g, int(sizes.sum()), 264), [weights(g, 3208, 264) for _ in sizes], offsets)
+
+
+@pytest.mark.parametrize("rows", (64, 65, 128, 129))
+def test_one_matrix_of_many_tiles(gpu_device, rows):
+    g = np.random.default_rng(rows)
+    check(tokens(g, rows, 136), [weights(g, 16648, 136)])
