@@ -75,7 +75,7 @@ const char *emoe_status_string(int status);
  * (either output pointer may be NULL).  Pure host arithmetic.  The FFN workspace is
  * h [A,f] in dtype plus, for bf16 layers with more than 22 rows per slot on average,
  * 32 or 64 MiB of fp32 partial sums of output tiles cut along K; for EMOE_F8 layers h and
- * x's rows in 8 bits, and 64 MiB of such sums with more than 48 rows per slot.  Neither workspace
+ * x's rows in 8 bits, and 64 MiB of such sums where there are many rows.  Neither workspace
  * needs initialising, and nothing in them outlives a call except h between the two
  * passes of emoe_expert_ffn_pass.  Calls that may run at the same time (different
  * streams) need workspaces of their own. */

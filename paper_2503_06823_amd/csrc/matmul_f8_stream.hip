@@ -1,13 +1,17 @@
 // Products in 8 bits for few rows a group (a decode step): the cost is reading each matrix that has rows once.
 //
 // A workgroup takes a unit: the rows of a group's matrix that share a power of two, 128, of the SwiGLU product those of both matrices -
-// whole blocks of 128 outputs, which is what the activation's result needs to be brought to 8 bits - or fewer of a plain product, and all of K.  A wavefront
-// has STRIPS strips of 16 of these rows and every SPLIT-th block of 128 columns.  Matrices lie in memory in the order in which the
-// matrix instruction (v_mfma_scale_f32_16x16x128_f8f6f4) wants them, so they go from memory to registers and nowhere else, a contiguous
-// KiB a load, eight strips (16 KiB) on their way a wavefront, and no wavefront waits for another before the end of K.  The matrix's rows
-// are the instruction's row operand, 16 rows of x its columns; the powers of two are operands of the instruction.
+// whole blocks of 128 outputs, which is what the activation's result needs to be brought to 8 bits - or fewer of a plain product, and all of K, times
+// up to 64 rows of x.  A wavefront has STRIPS strips of 16 of the matrix's rows and every SPLIT-th block of 128 columns.  Matrices lie in memory in the
+// order in which the matrix instruction (v_mfma_scale_f32_16x16x128_f8f6f4) wants them, so they go from memory to registers and nowhere else, a
+// contiguous KiB a load, eight strips (16 KiB) on their way a wavefront, and no wavefront waits for another before the end of K.  The matrix's rows are
+// the instruction's row operand, 16 rows of x its columns; the powers of two are operands of the instruction.
 // The partial sums meet in LDS, added in wavefront order.  Few short rows are converted to 8 bits here, by each workgroup for itself, while the matrix's
 // first strips are on their way; other rows by a launch before.
+//
+// One token's experts (two of 14336 x 4096, SwiGLU): 234 MB in 36 us, 6.5 TB/s, and 117 MB in 21 (the read stream: 6.9 TB/s, with some 2 us to begin and
+// end); a whole matrix of 6144 x 4096 in 6.8.  64 rows: x, read once by each workgroup, is what bounds: 50 MB through the L1 caches for a matrix
+// of 25 MB, 15 us with the conversion's launch.
 //
 // The instruction adds the products of eight consecutive elements in units of 2^-13 of the largest pair's power of two, and all else in
 // fp32: 1.5e-5 of a sum of random products, a hundredth of the rounding of the result to bf16.  (The bf16 instruction, on exact
@@ -22,7 +26,8 @@ typedef unsigned int uintx4 __attribute__((ext_vector_type(4)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kRing = 8;  // strips of a wavefront on their way
+// Blocks of columns of a wavefront on their way, eight strips: with the rows of x what the registers of two wavefronts a SIMD hold
+constexpr int ring(int tb, int strips) { return tb == 4 && strips == 2 ? 3 : 8 / strips; }
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void* base, uint32_t bytes) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)bytes, 0x00020000);
@@ -96,17 +101,16 @@ struct RowsInFlight {
     }
 };
 
-// Rows row0 .. row_end - 1 of x times a unit of their group's matrix, 16 TB at a time, with TB < 4 all of them.  OWN: x is converted here.
+// Rows row0 .. row_end - 1 of x, 16 TB at most, times a unit of their group's matrix.  OWN: x is converted here.
 template <int EPI, int TB, int STRIPS, int WAVES, int POLICY, bool OWN>
 __device__ __forceinline__ void multiply_unit(const F8Product& p, int unit, int group, int row0, int row_end, floatx4 (&red)[WAVES][STRIPS][64],
                                               uint32_t (&tops)[WAVES][64], OwnRows* own) {
     static_assert(!OWN || TB == 1, "at most 16 rows");
     constexpr int M = matrices(EPI), H = row_groups(EPI, STRIPS), SPLIT = WAVES / (M * H);
     static_assert(SPLIT >= 1 && SPLIT * M * H == WAVES, "every wavefront has a part");
-    constexpr int DEPTH = kRing / STRIPS;  // blocks of columns of a wavefront on their way
+    constexpr int DEPTH = ring(TB, STRIPS);
     constexpr int ALL = STRIPS * H;       // strips of a unit, of one matrix
     constexpr int FINAL = ALL >= WAVES ? ALL / WAVES : 1;  // that a wavefront finishes
-    constexpr int ROWS = 16 * TB;
     const int lane = threadIdx.x & 63, tok = lane & 15, quad = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int part = wave % SPLIT, half = wave / SPLIT % H;
@@ -124,163 +128,160 @@ __device__ __forceinline__ void multiply_unit(const F8Product& p, int unit, int 
     const uint32_t w_at = (uint32_t)nb * p.lay.kb * kF8BlockBytes + (strip0 + half * STRIPS) * kF8Strip;
     const int mine = (p.lay.kb - part + SPLIT - 1) / SPLIT;  // this wavefront's blocks of columns: part, part + SPLIT, ...
 
-    for (int tok0 = row0; tok0 < row_end; tok0 += ROWS) {
-        uint32_t x_lane[TB], xs_lane[TB];
+    uint32_t x_lane[TB], xs_lane[TB];
+#pragma unroll
+    for (int t = 0; t < TB; ++t) {
+        int r = row0 + 16 * t + tok;
+        r = r < row_end ? r : row_end - 1;  // (rows past the end are multiplied and not stored)
+        if constexpr (OWN) {
+            xs_lane[t] = (uint32_t)((r - row0) * p.lay.kb);  // its first block
+            x_lane[t] = xs_lane[t] * kF8Block + quad * 16;
+        } else {
+            x_lane[t] = (uint32_t)r * p.x.row_step + (uint32_t)quad * p.x.piece_step;
+            xs_lane[t] = (uint32_t)r * 4;
+        }
+    }
+    intx8 w[DEPTH][STRIPS], x[DEPTH][TB];
+    uint32_t xb[DEPTH][TB], wb[DEPTH];
+    // the wavefront's j-th block of columns; behind its last one out of range: zeros, and nothing is read
+    auto load_w = [&](int slot, int j) {
+        const bool there = j < mine;
+        const uint32_t b = there ? part + j * SPLIT : part, lane_at = there ? lane * 16u : codes;
+#pragma unroll
+        for (int i = 0; i < STRIPS; ++i) w[slot][i] = two<POLICY>(w_rsrc, lane_at, w_at + b * kF8BlockBytes + i * kF8Strip, 1024);
+        wb[slot] = w_scales[b >> 2];
+    };
+    auto load_x = [&](int slot, int j) {
+        const bool there = j < mine;
+        const int b = there ? part + j * SPLIT : part;
 #pragma unroll
         for (int t = 0; t < TB; ++t) {
-            int r = tok0 + 16 * t + tok;
-            r = r < row_end ? r : row_end - 1;  // (rows past the end are multiplied and not stored)
-            if constexpr (OWN) {
-                xs_lane[t] = (uint32_t)((r - row0) * p.lay.kb);  // its first block
-                x_lane[t] = xs_lane[t] * kF8Block + quad * 16;
-            } else {
-                x_lane[t] = (uint32_t)r * p.x.row_step + (uint32_t)quad * p.x.piece_step;
-                xs_lane[t] = (uint32_t)r * 4;
+            if constexpr (OWN) {  // (behind the last block the first one again: its products are with zeros)
+                const int at = there ? b : 0;
+                const uintx4* from = reinterpret_cast<const uintx4*>(own->codes + x_lane[t] + at * kF8Block);
+                x[slot][t] = __builtin_bit_cast(intx8, __builtin_shufflevector(from[0], from[4], 0, 1, 2, 3, 4, 5, 6, 7));
+                xb[slot][t] = own->powers[xs_lane[t] + at];
+                continue;
             }
+            x[slot][t] = two<0>(x_rsrc, there ? x_lane[t] : x_bytes, (uint32_t)b * x_block, (int)(x_block / 2));
+            xb[slot][t] = __builtin_amdgcn_raw_buffer_load_b32(xs_rsrc, (int)(there ? xs_lane[t] : xs_bytes), (b >> 2) * p.x.rows * 4, 0);
         }
-        intx8 w[DEPTH][STRIPS], x[DEPTH][TB];
-        uint32_t xb[DEPTH][TB], wb[DEPTH];
-        // the wavefront's j-th block of columns; behind its last one out of range: zeros, and nothing is read
-        auto load_w = [&](int slot, int j) {
-            const bool there = j < mine;
-            const uint32_t b = there ? part + j * SPLIT : part, lane_at = there ? lane * 16u : codes;
+    };
+    if constexpr (OWN) {
+        RowsInFlight<WAVES> rows;
+        rows.request(p, row0, row_end);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int i = 0; i < STRIPS; ++i) w[slot][i] = two<POLICY>(w_rsrc, lane_at, w_at + b * kF8BlockBytes + i * kF8Strip, 1024);
-            wb[slot] = w_scales[b >> 2];
-        };
-        auto load_x = [&](int slot, int j) {
-            const bool there = j < mine;
-            const int b = there ? part + j * SPLIT : part;
+        for (int d = 0; d < DEPTH; ++d) load_w(d, d);
+        __builtin_amdgcn_sched_barrier(0);
+        rows.convert(p, row0, row_end, *own);
+    }
 #pragma unroll
-            for (int t = 0; t < TB; ++t) {
-                if constexpr (OWN) {  // (behind the last block the first one again: its products are with zeros)
-                    const int at = there ? b : 0;
-                    const uintx4* from = reinterpret_cast<const uintx4*>(own->codes + x_lane[t] + at * kF8Block);
-                    x[slot][t] = __builtin_bit_cast(intx8, __builtin_shufflevector(from[0], from[4], 0, 1, 2, 3, 4, 5, 6, 7));
-                    xb[slot][t] = own->powers[xs_lane[t] + at];
-                    continue;
-                }
-                x[slot][t] = two<0>(x_rsrc, there ? x_lane[t] : x_bytes, (uint32_t)b * x_block, (int)(x_block / 2));
-                xb[slot][t] = __builtin_amdgcn_raw_buffer_load_b32(xs_rsrc, (int)(there ? xs_lane[t] : xs_bytes), (b >> 2) * p.x.rows * 4, 0);
-            }
-        };
-        if constexpr (OWN) {
-            RowsInFlight<WAVES> rows;
-            rows.request(p, row0, row_end);
-            __builtin_amdgcn_sched_barrier(0);
+    for (int d = 0; d < DEPTH; ++d) {
+        if constexpr (!OWN) load_w(d, d);
+        load_x(d, d);
+    }
+    floatx4 acc[STRIPS][TB];
 #pragma unroll
-            for (int d = 0; d < DEPTH; ++d) load_w(d, d);
-            __builtin_amdgcn_sched_barrier(0);
-            rows.convert(p, row0, row_end, *own);
-        }
+    for (int i = 0; i < STRIPS; ++i)
+#pragma unroll
+        for (int t = 0; t < TB; ++t) acc[i][t] = floatx4{0, 0, 0, 0};
+    for (int j = 0; j < mine; j += DEPTH) {
 #pragma unroll
         for (int d = 0; d < DEPTH; ++d) {
-            if constexpr (!OWN) load_w(d, d);
-            load_x(d, d);
+            __builtin_amdgcn_sched_barrier(0);
+            const int shift = 8 * ((part + (j + d) * SPLIT) & 3);
+            uint32_t xbc[TB];
+            const uint32_t wbc = j + d < mine ? wb[d] >> shift : 127u;  // (zeros times any power but NaN)
+#pragma unroll
+            for (int t = 0; t < TB; ++t) xbc[t] = OWN ? xb[d][t] : xb[d][t] >> shift;
+#pragma unroll
+            for (int i = 0; i < STRIPS; ++i)
+#pragma unroll
+                for (int t = 0; t < TB; ++t)
+                    acc[i][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[d][i], x[d][t], acc[i][t], 0, 0, 0, (int)wbc, 0, (int)xbc[t]);
+            load_w(d, j + d + DEPTH);
+            load_x(d, j + d + DEPTH);
         }
-        floatx4 acc[STRIPS][TB];
-#pragma unroll
-        for (int i = 0; i < STRIPS; ++i)
-#pragma unroll
-            for (int t = 0; t < TB; ++t) acc[i][t] = floatx4{0, 0, 0, 0};
-        for (int j = 0; j < mine; j += DEPTH) {
-#pragma unroll
-            for (int d = 0; d < DEPTH; ++d) {
-                __builtin_amdgcn_sched_barrier(0);
-                const int shift = 8 * ((part + (j + d) * SPLIT) & 3);
-                uint32_t xbc[TB];
-                const uint32_t wbc = j + d < mine ? wb[d] >> shift : 127u;  // (zeros times any power but NaN)
-#pragma unroll
-                for (int t = 0; t < TB; ++t) xbc[t] = OWN ? xb[d][t] : xb[d][t] >> shift;
-#pragma unroll
-                for (int i = 0; i < STRIPS; ++i)
-#pragma unroll
-                    for (int t = 0; t < TB; ++t)
-                        acc[i][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[d][i], x[d][t], acc[i][t], 0, 0, 0, (int)wbc, 0, (int)xbc[t]);
-                load_w(d, j + d + DEPTH);
-                load_x(d, j + d + DEPTH);
-            }
-        }
+    }
 
-        // ---- the partial sums, 16 rows of x at a time; wavefront q finishes the strips from q FINAL on ------------------
-        floatx4 sum[M][FINAL][TB];
+    // ---- the partial sums, 16 rows of x at a time; wavefront q finishes the strips from q FINAL on ------------------
+    floatx4 sum[M][FINAL][TB];
 #pragma unroll
-        for (int t = 0; t < TB; ++t) {
+    for (int t = 0; t < TB; ++t) {
 #pragma unroll
-            for (int i = 0; i < STRIPS; ++i) red[wave][i][lane] = acc[i][t];
-            __syncthreads();
-            if (ALL >= WAVES || wave < ALL) {
+        for (int i = 0; i < STRIPS; ++i) red[wave][i][lane] = acc[i][t];
+        __syncthreads();
+        if (ALL >= WAVES || wave < ALL) {
 #pragma unroll
-                for (int m = 0; m < M; ++m)
-#pragma unroll
-                    for (int f = 0; f < FINAL; ++f) {
-                        const int i = wave * FINAL + f, from = (m * H + i / STRIPS) * SPLIT;
-                        floatx4 v = red[from][i % STRIPS][lane];
-#pragma unroll
-                        for (int o = 1; o < SPLIT; ++o) v += red[from + o][i % STRIPS][lane];
-                        sum[m][f][t] = v;
-                    }
-            }
-            __syncthreads();
-        }
-
-        // a lane holds row tok of x and outputs 4 quad .. 4 quad + 3 of its wavefront's strips
-        const int n0 = nb * kF8Block + (strip0 + wave * FINAL) * 16 + quad * 4;
-        if constexpr (EPI == kF8Plain) {
-            if (ALL >= WAVES || wave < ALL) {
-#pragma unroll
-                for (int t = 0; t < TB; ++t) {
-                    const int r = tok0 + 16 * t + tok;
-                    if (r >= row_end) continue;
-                    bf16_t* to = p.out + (size_t)(p.out_perm != nullptr ? p.out_perm[r] : r) * p.out_stride + n0;
-#pragma unroll
-                    for (int f = 0; f < FINAL; ++f)
-                        if (n0 + 16 * f < p.N) *reinterpret_cast<bf16x4*>(to + 16 * f) = __builtin_convertvector(sum[0][f][t], bf16x4);
-                }
-            }
-        } else {
-#pragma unroll
-            for (int t = 0; t < TB; ++t) {
-                uint32_t top = 0;
-#pragma unroll
-                for (int f = 0; f < FINAL; ++f)
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) {
-                        float g = sum[0][f][t][v];
-                        if constexpr (EPI == kF8Swiglu) g = g / (1.0f + __expf(-g)) * sum[M - 1][f][t][v];
-                        else g = g < 0.0f ? 0.0f : g;  // (NaN stays)
-                        sum[0][f][t][v] = g;
-                        top = umax(top, f8_magnitude(g));
-                    }
-                top = umax(top, (uint32_t)__shfl_xor((int)top, 16));
-                top = umax(top, (uint32_t)__shfl_xor((int)top, 32));
-                if (quad == 0) tops[wave][16 * t + tok] = top;
-            }
-            __syncthreads();
-#pragma unroll
-            for (int t = 0; t < TB; ++t) {
-                const int r = tok0 + 16 * t + tok, c = 16 * t + tok;
-                uint32_t top = tops[0][c];
-#pragma unroll
-                for (int o = 1; o < WAVES; ++o) top = umax(top, tops[o][c]);
-                const uint32_t byte = f8_scale_byte(top);
-                if (r >= row_end) continue;
+            for (int m = 0; m < M; ++m)
 #pragma unroll
                 for (int f = 0; f < FINAL; ++f) {
-                    const floatx4& h = sum[0][f][t];
-                    *reinterpret_cast<uint32_t*>(p.h.codes + (size_t)r * p.h.row_step + (size_t)((n0 >> 4) + f) * p.h.piece_step + quad * 4) = f8_codes(h[0], h[1], h[2], h[3], f8_inverse(byte));
+                    const int i = wave * FINAL + f, from = (m * H + i / STRIPS) * SPLIT;
+                    floatx4 v = red[from][i % STRIPS][lane];
+#pragma unroll
+                    for (int o = 1; o < SPLIT; ++o) v += red[from + o][i % STRIPS][lane];
+                    sum[m][f][t] = v;
                 }
-                if (wave == 0 && quad == 0) reinterpret_cast<uint8_t*>(p.h.scales + (size_t)(nb >> 2) * p.h.rows + r)[nb & 3] = (uint8_t)byte;
-            }
-            __syncthreads();  // tops are free again
         }
-        if constexpr (TB < 4) break;  // (no loop for the compiler: the matrix's powers are scalar loads)
+        __syncthreads();
+    }
+
+    // a lane holds row tok of x and outputs 4 quad .. 4 quad + 3 of its wavefront's strips
+    const int n0 = nb * kF8Block + (strip0 + wave * FINAL) * 16 + quad * 4;
+    if constexpr (EPI == kF8Plain) {
+        if (ALL >= WAVES || wave < ALL) {
+#pragma unroll
+            for (int t = 0; t < TB; ++t) {
+                const int r = row0 + 16 * t + tok;
+                if (r >= row_end) continue;
+                bf16_t* to = p.out + (size_t)(p.out_perm != nullptr ? p.out_perm[r] : r) * p.out_stride + n0;
+#pragma unroll
+                for (int f = 0; f < FINAL; ++f)
+                    if (n0 + 16 * f < p.N) *reinterpret_cast<bf16x4*>(to + 16 * f) = __builtin_convertvector(sum[0][f][t], bf16x4);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int t = 0; t < TB; ++t) {
+            uint32_t top = 0;
+#pragma unroll
+            for (int f = 0; f < FINAL; ++f)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    float g = sum[0][f][t][v];
+                    if constexpr (EPI == kF8Swiglu) g = g / (1.0f + __expf(-g)) * sum[M - 1][f][t][v];
+                    else g = g < 0.0f ? 0.0f : g;  // (NaN stays)
+                    sum[0][f][t][v] = g;
+                    top = umax(top, f8_magnitude(g));
+                }
+            top = umax(top, (uint32_t)__shfl_xor((int)top, 16));
+            top = umax(top, (uint32_t)__shfl_xor((int)top, 32));
+            if (quad == 0) tops[wave][16 * t + tok] = top;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < TB; ++t) {
+            const int r = row0 + 16 * t + tok, c = 16 * t + tok;
+            uint32_t top = tops[0][c];
+#pragma unroll
+            for (int o = 1; o < WAVES; ++o) top = umax(top, tops[o][c]);
+            const uint32_t byte = f8_scale_byte(top);
+            if (r >= row_end) continue;
+#pragma unroll
+            for (int f = 0; f < FINAL; ++f) {
+                const floatx4& h = sum[0][f][t];
+                *reinterpret_cast<uint32_t*>(p.h.codes + (size_t)r * p.h.row_step + (size_t)((n0 >> 4) + f) * p.h.piece_step + quad * 4) = f8_codes(h[0], h[1], h[2], h[3], f8_inverse(byte));
+            }
+            if (wave == 0 && quad == 0) reinterpret_cast<uint8_t*>(p.h.scales + (size_t)(nb >> 2) * p.h.rows + r)[nb & 3] = (uint8_t)byte;
+        }
     }
 }
 
-// MOST: blocks of 16 rows that a group has at most, or those of a pass
+// MOST: blocks of 16 rows that a workgroup has at most.  Workgroups go through the units of an item, then of the next: with MOST 1 items are groups, otherwise
+// 64 rows of a group or what is left of it, counted through the groups (there are fewer than there are workgroups for).
 template <int EPI, int MOST, int STRIPS, int WAVES, bool OWN>
-__global__ __launch_bounds__(64 * WAVES) void stream_kernel(F8Product p, int n_units) {
+__global__ __launch_bounds__(64 * WAVES, 2) void stream_kernel(F8Product p, int n_units) {
     __shared__ floatx4 red[WAVES][STRIPS][64];
     __shared__ uint32_t tops[WAVES][64];
     OwnRows* own = nullptr;
@@ -288,15 +289,41 @@ __global__ __launch_bounds__(64 * WAVES) void stream_kernel(F8Product p, int n_u
         __shared__ __align__(16) OwnRows rows;
         own = &rows;
     }
-    const int unit = blockIdx.x % n_units, group = blockIdx.x / n_units;
-    int row0 = 0, row_end = p.rows;
-    if (p.offsets != nullptr) {
-        row0 = p.offsets[group];
-        row_end = p.offsets[group + 1];
-        row0 = row0 > 0 ? row0 : 0;
-        row_end = row_end < p.rows ? row_end : p.rows;
+    const int unit = blockIdx.x % n_units, item = blockIdx.x / n_units;
+    int group = 0, row0 = 0, row_end = p.rows;
+    if (MOST == 1 || p.groups == 1) {
+        if (MOST == 1) group = item;
+        if (p.offsets != nullptr) {
+            row0 = p.offsets[group];
+            row_end = p.offsets[group + 1];
+            row0 = row0 > 0 ? row0 : 0;
+            row_end = row_end < p.rows ? row_end : p.rows;
+        }
+        if (MOST > 1) row0 += item * 16 * MOST;
+    } else {
+        const int lane = threadIdx.x & 63;
+        int begin = 0, end = 0;
+        if (lane < p.groups) {
+            begin = p.offsets[lane];
+            end = p.offsets[lane + 1];
+            begin = begin > 0 ? begin : 0;
+            end = end < p.rows ? end : p.rows;
+        }
+        const int items = end > begin ? (end - begin + 16 * MOST - 1) / (16 * MOST) : 0;
+        int upto = items;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int below = __shfl_up(upto, o);
+            upto += lane >= o ? below : 0;
+        }
+        const uint64_t behind = __ballot(upto > item);
+        if (behind == 0) return;
+        group = __builtin_amdgcn_readfirstlane(__builtin_ctzll(behind));
+        row0 = __builtin_amdgcn_readlane(begin, group) + (item - __builtin_amdgcn_readlane(upto - items, group)) * 16 * MOST;
+        row_end = __builtin_amdgcn_readlane(end, group);
     }
     if (row_end <= row0) return;  // its matrix is never touched
+    if (MOST > 1) row_end = row_end < row0 + 16 * MOST ? row_end : row0 + 16 * MOST;
     if (MOST == 1 || row_end - row0 <= 16) multiply_unit<EPI, 1, STRIPS, WAVES, 2, OWN>(p, unit, group, row0, row_end, red, tops, own);
     else if (MOST == 2 || row_end - row0 <= 32) multiply_unit<EPI, MOST < 2 ? 1 : 2, STRIPS, WAVES, 2, OWN>(p, unit, group, row0, row_end, red, tops, own);
     else multiply_unit<EPI, MOST, STRIPS, WAVES, 2, OWN>(p, unit, group, row0, row_end, red, tops, own);
@@ -306,7 +333,8 @@ template <int EPI, int MOST, int STRIPS, int WAVES>
 hipError_t launch_shape(const F8Product& p, hipStream_t st) {
     constexpr int all = STRIPS * row_groups(EPI, STRIPS);
     const int n_units = (p.N + 16 * all - 1) / (16 * all);
-    const unsigned grid = (unsigned)(p.groups * n_units);
+    const long long chunks = MOST == 1 ? p.groups : p.groups == 1 ? (p.rows + 16 * MOST - 1) / (16 * MOST) : p.groups + p.rows / (16 * MOST);
+    const unsigned grid = (unsigned)(chunks * n_units);
     if constexpr (MOST == 1) {
         if (p.from != nullptr) {
             stream_kernel<EPI, MOST, STRIPS, WAVES, true><<<grid, 64 * WAVES, 0, st>>>(p, n_units);
@@ -318,16 +346,16 @@ hipError_t launch_shape(const F8Product& p, hipStream_t st) {
 }
 
 // A wavefront's strips by the strips that there are: more of them a wavefront read x less often, fewer leave no CU without work.  Measured with matrices from
-// HBM, plain products of 17 to 64 rows a group (us, two strips / four, four wavefronts): 384 strips 15.7 / 17.1 (6144 x 4096), 256 14.7 / 16.6, 768
-// 25.8 / 19.7, 1040 12.7 / 10.3 (16 groups of 1032 x 776), 2048 96 / 89 (8 of 4096 x 14336), 7168 126 / 97; eight wavefronts of four strips 18.2, 17.3, 20.7,
-// 12.4, 89, 102.  The activations' products, which want 128 rows a unit, with four wavefronts / eight: 20 rows of 6 groups of 14336 x 4096 121 / 121 (SwiGLU),
-// 71 / 74 (ReLU), of 16 of 2816 x 1032 30.7 / 31.1, 21.2 / 22.0, one row of 32 of 512 x 512 9.5 / 10.2, 7.9 / 9.0; with eight strips a wavefront 130, 72, 32.5, 21.6, 9.9, 7.9.
+// HBM, plain products of 17 to 64 rows a stretch (us, two strips / four): 128 strips 13.1 / 14.3 (64 rows times 2048 x 4096), 384 15.5 / 16.7 (6144 x 4096), 512
+// 16.4 / 17.4, 768 23.8 / 19.6, two stretches of 384 23.8 / 18.5, 1040 12.0 / 10.0 (16 groups of 1032 x 776), 2048 103 / 100 (8 of 4096 x 14336); eight wavefronts
+// of four strips were up to a fifth slower.  The activations' products want 128 rows a unit; four wavefronts / eight: 20 rows of 6 groups of 14336 x 4096 121 / 121
+// (SwiGLU), 71 / 74 (ReLU), one row of 32 of 512 x 512 9.5 / 10.2, 7.9 / 9.0; with eight strips a wavefront 130, 72, 9.9, 7.9.
 template <int EPI>
 hipError_t launch(const F8Product& p, hipStream_t st) {
     const long long groups = p.groups < p.rows ? p.groups : p.rows;  // that can have rows
     const bool few = p.rows <= 16;
     if constexpr (EPI == kF8Plain) {
-        const long long strips = groups * ((p.N + 15) / 16);
+        const long long stretches = (p.rows + 63) / 64, strips = (groups > stretches ? groups : stretches) * ((p.N + 15) / 16);
         if (!few) return strips > 512 ? launch_shape<EPI, 4, 4, 4>(p, st) : launch_shape<EPI, 4, 2, 4>(p, st);
         if (strips >= 4 * 512) return launch_shape<EPI, 1, 4, 4>(p, st);
         return strips > 256 ? launch_shape<EPI, 1, 2, 4>(p, st) : launch_shape<EPI, 1, 1, 4>(p, st);

@@ -49,25 +49,25 @@ F8Rows rows_at(uint8_t* ws, size_t* at, long long rows, int K) {
     return r;
 }
 
-// Which kernel multiplies: by the rows that a group has on average (their numbers live on the device).  Streaming reads a matrix once for every 64 rows, the
-// second time half from caches; tiles of 256 x 256 read it once, but cost some 10 us more, and leave CUs without work where they are few.  So few tiles of small
-// matrices take over where 128 rows end, other matrices where 64 do, and several, of which some have more rows than others, from 48 on.  Measured with
-// matrices from HBM (us, streaming / tiles): 6144 x 4096 (24 tiles) 64 rows 15.8 / 25.4, 128 25.4 / 29.4, 160 33.3 / 30.2; 8 groups of 2048 x 2048 (64), 128
-// rows each 25.9 / 33.2, 160 34.4 / 34.3; 32000 x 4096 (125) 64 rows 36.0 / 47.8, 80 57.3 / 48.5; 8 of 4096 x 14336 (128) 64 109 / 122, 80 195 / 128; 8 of
-// 14336 x 4096 (448) 36 108 / 103, 64 114 / 106; 24 of 2048 x 1408 (192) 36 29.7 / 26.3, 64 33.1 / 28.7; SwiGLU's two of 6 groups of 14336 x 4096 (672) 36
-// 138 / 144, 64 155 / 144, of 16 of 2816 x 1032 (352) 64 40.1 / 43.5, 80 69 / 46; one ReLU product of 14336 x 4096 (56) 64 26.7 / 32.9, 80 43.8 / 33.6.
-// Tiles take at least two blocks of columns.
-constexpr long long kFewTiles = 64, kSmallMatrices = 48ll << 20;
-bool is_tiled(long long rows, int groups, int N, int K, int matrices) {
-    const long long tiles = (long long)groups * ((matrices * (long long)N + 255) / 256);
-    const bool small = tiles <= kFewTiles && (long long)groups * matrices * N * K <= kSmallMatrices;
-    const long long streamed = small ? 128 : groups == 1 ? 64 : 48;
-    return rows > streamed * groups && K > kF8Block;
+// Which kernel multiplies, by the rows (how many each group has lives on the device: half a stretch of 64 more than they fill is what groups of unequal
+// sizes have on average).  Streaming reads a matrix once for every 64 rows of a group, from caches after the first; tiles of 256 x 256 read it once, but cost some 10 us
+// more and leave CUs without work where they are few.  So streaming it is where one reading does, and where its workgroups are few or short.  Measured with matrices
+// from HBM (us, streaming / tiles): one of 6144 x 4096 64 rows 15.5 / 25.8, 100 18.6 / 28.7, 256 28.3 / 36.9; 32000 x 4096 64 rows
+// 35.7 / 48.6, 80 55.9 / 47.9; 1024 x 1024 320 rows 10.2 / 19.0; 8 of 14336 x 4096 64 rows each 112 / 108, 80 184 / 109; 8 of 2048 x 2048 128 24.1 / 32.8, 256
+// 35.4 / 41.9, 320 46.6 / 40.1; 24 of 2048 x 1408 64 31.0 / 28.6, 80 41.3 / 29.9.  SwiGLU's two: 6 groups of 14336 x 4096 64 rows 143 / 146, 80 243 / 151; 4 of
+// 4096 x 1024 128 19.3 / 32.6; one of 14336 x 4096 128 48.0 / 47.5, 160 77 / 49; ReLU 128 28.6 / 36.1, 160 42.0 / 37.5; 16 of 2816 x 1032 64
+// 23.9 / 24.9, 80 35.0 / 26.4.  Tiles take at least two blocks of columns.
+bool is_tiled(long long rows, int groups, int N, int K, F8Epilogue epilogue) {
+    if (K <= kF8Block || rows <= (groups == 1 ? 64ll : 48ll) * groups) return false;
+    const bool plain = epilogue == kF8Plain;
+    const long long stretches = groups == 1 ? (rows + 63) / 64 : (rows + 32ll * groups) / 64;
+    const long long workgroups = stretches * (plain ? (N + 63) / 64 : (N + 127) / 128);
+    return plain ? workgroups > 512 || workgroups * K > 1ll << 21 : workgroups > 384 || workgroups * K > 1ll << 20;
 }
 bool first_is_tiled(const emoe_layer_desc& d) {
-    return is_tiled((long long)d.T * d.k, d.S, d.d_ff, d.d_model, d.act == EMOE_ACT_SWIGLU ? 2 : 1);
+    return is_tiled((long long)d.T * d.k, d.S, d.d_ff, d.d_model, d.act == EMOE_ACT_SWIGLU ? kF8Swiglu : kF8Relu);
 }
-bool second_is_tiled(const emoe_layer_desc& d) { return is_tiled((long long)d.T * d.k, d.S, d.d_model, d.d_ff, 1); }
+bool second_is_tiled(const emoe_layer_desc& d) { return is_tiled((long long)d.T * d.k, d.S, d.d_model, d.d_ff, kF8Plain); }
 
 // In the order that the kernel which multiplies them reads
 F8Rows ordered(F8Rows r, int K, bool by_rows) {
@@ -86,7 +86,7 @@ MatmulWs matmul_ws(const emoe_matmul_desc& d, void* ws) {
     w.total = 0;
     w.x = rows_at(static_cast<uint8_t*>(ws), &w.total, d.rows, d.K);
     w.partials = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + w.total);
-    if (is_tiled(d.rows, d.groups, d.N, d.K, 1)) w.total += kTiledPartialBytes;
+    if (is_tiled(d.rows, d.groups, d.N, d.K, kF8Plain)) w.total += kTiledPartialBytes;
     return w;
 }
 
@@ -242,7 +242,7 @@ int emoe_matmul(const emoe_matmul_desc* desc, const void* x, const int32_t* grou
     if (!ws || ws_bytes < lay.total) return EMOE_ERR_WORKSPACE;
     hipStream_t st = static_cast<hipStream_t>(stream);
     F8Product p = {};
-    const bool tiled = is_tiled(desc->rows, desc->groups, desc->N, desc->K, 1);
+    const bool tiled = is_tiled(desc->rows, desc->groups, desc->N, desc->K, kF8Plain);
     p.x = ordered(lay.x, desc->K, tiled);
     if (!tiled && f8_own_rows(desc->rows, desc->K)) own_rows(p, x, desc->x_stride, desc->K);
     else if (launch_f8_rows(x, desc->x_stride, desc->K, p.x, nullptr, 1, nullptr, st) != hipSuccess) return EMOE_ERR_DEVICE;

@@ -5,7 +5,7 @@ import torch
 
 import paper_2503_06823_amd as P
 from oracle import packed as ref
-from packed_util import close, tokens, weights
+from packed_util import as_device, close, matmul, packed, tokens, weights
 from test_gpu_matmul import check
 
 pytestmark = pytest.mark.gpu
@@ -111,3 +111,36 @@ def test_more_tiles(gpu_device, each):
 def test_one_matrix_of_many_tiles(gpu_device, rows):
     g = np.random.default_rng(rows)
     check(tokens(g, rows, 136), [weights(g, 16648, 136)])
+
+
+@pytest.mark.parametrize("sizes", [(64, 128, 65, 0, 1), (63, 0, 0, 127, 192), (0, 0, 191, 1, 1), (16, 17, 32, 33, 96, 80)])
+@pytest.mark.parametrize("behind", (0, 70))
+def test_stretches_of_rows(gpu_device, sizes, behind):
+    """Rows of a group in stretches of 64: whole ones, one more and one less, groups without any between them; what lies behind the last stays."""
+    g = np.random.default_rng(len(sizes) + behind)
+    offsets = np.concatenate(([0], np.cumsum(sizes))).tolist()
+    check(tokens(g, sum(sizes) + behind, 520), [weights(g, 200, 520) for _ in sizes], offsets)
+
+
+@pytest.mark.parametrize("rows", (600, 1024, 1100))
+def test_many_stretches_of_one_small_matrix(gpu_device, rows):
+    g = np.random.default_rng(rows)
+    check(tokens(g, rows, 264), [weights(g, 264, 264)])
+    check(tokens(g, rows, 264), [weights(g, 264, 264)], [0, rows - 65])
+
+
+@pytest.mark.parametrize("rows,K", [(700, 128), (1000, 8), (5000, 64)])
+def test_one_block_of_columns(gpu_device, rows, K):
+    """All rows are streamed, whatever their number."""
+    g = np.random.default_rng(rows)
+    check(tokens(g, rows, K), [weights(g, 264, K)])
+    check(tokens(g, rows, K), [weights(g, 72, K) for _ in range(3)], [0, rows // 2 + 3, rows // 2 + 3, rows - 10])
+
+
+def test_offsets_out_of_range_stay_in_bounds(gpu_device):
+    """Negative, descending and too large ones: nothing outside of out is written."""
+    g = np.random.default_rng(1)
+    x, data = as_device(tokens(g, 200, 264)), packed([weights(g, 136, 264) for _ in range(4)])
+    for at in ([-5, 3, 2, 100, 1 << 30], [0, 1 << 30, -(1 << 30), 50, 60], [200, 200, 300, 100, 7]):
+        out = matmul(x, data, 136, at)  # (looks at what lies around)
+        assert out.shape == (200, 136)
