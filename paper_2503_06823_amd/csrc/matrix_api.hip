@@ -52,11 +52,11 @@ F8Rows rows_at(uint8_t* ws, size_t* at, long long rows, int K) {
 // Which kernel multiplies, by the rows (how many each group has lives on the device: half a stretch of 64 more than they fill is what groups of unequal
 // sizes have on average).  Streaming reads a matrix once for every 64 rows of a group, from caches after the first; tiles of 256 x 256 read it once, but cost some 10 us
 // more and leave CUs without work where they are few.  So streaming it is where one reading does, and where its workgroups are few or short.  Measured with matrices
-// from HBM (us, streaming / tiles): one of 6144 x 4096 64 rows 15.5 / 25.8, 100 18.6 / 28.7, 256 28.3 / 36.9; 32000 x 4096 64 rows
-// 35.7 / 48.6, 80 55.9 / 47.9; 1024 x 1024 320 rows 10.2 / 19.0; 8 of 14336 x 4096 64 rows each 112 / 108, 80 184 / 109; 8 of 2048 x 2048 128 24.1 / 32.8, 256
-// 35.4 / 41.9, 320 46.6 / 40.1; 24 of 2048 x 1408 64 31.0 / 28.6, 80 41.3 / 29.9.  SwiGLU's two: 6 groups of 14336 x 4096 64 rows 143 / 146, 80 243 / 151; 4 of
-// 4096 x 1024 128 19.3 / 32.6; one of 14336 x 4096 128 48.0 / 47.5, 160 77 / 49; ReLU 128 28.6 / 36.1, 160 42.0 / 37.5; 16 of 2816 x 1032 64
-// 23.9 / 24.9, 80 35.0 / 26.4.  Tiles take at least two blocks of columns.
+// from HBM (us, streaming / tiles): one of 6144 x 4096 64 rows 15.7 / 25.9, 256 28.4 / 37.6, 512 40.1 / 41.1; 32000 x 4096 64 rows 33.0 / 47.9, 80
+// 53.8 / 47.7; 1024 x 1024 1024 rows 10.9 / 23.4; 8 of 14336 x 4096 64 rows each 104 / 109, 80 185 / 109; 8 of 2048 x 2048 128 23.8 / 29.2, 256 35.1 / 36.5, 320
+// 47.0 / 32.3; 24 of 2048 x 1408 64 31.0 / 27.0, 80 41.0 / 28.0.  SwiGLU's two: 6 groups of 14336 x 4096 64 rows 144 / 146, 80 254 / 156; 4 of 4096 x 1024
+// 128 21.0 / 23.6; one of 14336 x 4096 128 51.3 / 50.2, 160 79.5 / 50.0; ReLU 128 30.7 / 36.8, 160 43.6 / 37.9; 16 of 2816 x 1032 64 24.3 / 23.1, 80
+// 35.1 / 24.4.  Tiles take at least two blocks of columns.
 bool is_tiled(long long rows, int groups, int N, int K, F8Epilogue epilogue) {
     if (K <= kF8Block || rows <= (groups == 1 ? 64ll : 48ll) * groups) return false;
     const bool plain = epilogue == kF8Plain;

@@ -252,3 +252,23 @@ def test_few_tokens_whose_rows_the_first_product_converts(gpu_device, T, k, d, a
     P.emoe_expert_ffn(a.desc, grouped, a.dev["offsets"], a.m1, a.m3, a.m2, y, a.ws, a.ws.numel())
     torch.cuda.synchronize()
     assert torch.equal(y, a.y)
+
+
+@pytest.mark.parametrize("T,d,f,S,k,act", [
+    (3000, 392, 520, 4, 2, "swiglu"), (3000, 392, 1160, 4, 2, "relu"), (6000, 392, 520, 3, 1, "swiglu"), (6000, 264, 1032, 2, 1, "relu"),
+    (1500, 520, 3208, 2, 2, "swiglu"), (4000, 136, 1032, 6, 2, "swiglu"), (5000, 1032, 136, 8, 1, "swiglu")])
+def test_experts_of_many_rows(gpu_device, T, d, f, S, k, act):
+    """Products in tiles, both or one of the two; of one expert a token the second writes the tokens' rows."""
+    a = Layer(T, d, f, S, k, act)
+    want, off = a.experts()
+    if k == 1:
+        a.combine()
+        torch.cuda.synchronize()
+        scale = a.weight.double().numpy()[:, :1]
+        y, o = want[a.inverse], off[a.inverse]
+        close(a.out[:T], y * scale, (o + (np.abs(y) + o) * HALF_STEP) * scale)
+        assert (a.out[T:] == 5.0).all()
+    a.gather()
+    torch.cuda.synchronize()
+    close(a.y[:T * k], want, off)
+    assert (a.y[T * k:] == 5.0).all()
