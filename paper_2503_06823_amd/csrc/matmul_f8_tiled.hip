@@ -628,15 +628,19 @@ __global__ __launch_bounds__(64 * NW) void fixup_kernel(F8Product p, const float
 template <int EPI>
 hipError_t launch(const F8Product& p, float* partials, hipStream_t st) {
     auto kern = tiled_kernel<EPI>;
-    static std::atomic<bool> attr_set{false};  // set once per kernel; setting it twice from two threads is harmless
-    if (!attr_set.load(std::memory_order_acquire)) {
-        hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)LDS_BYTES);
+    static std::atomic<uint64_t> devices_set{0};  // set once per kernel and device; setting it twice from two threads is harmless
+    int device = 0;
+    hipError_t e = hipGetDevice(&device);
+    if (e != hipSuccess) return e;
+    const uint64_t bit = 1ull << (device & 63);
+    if (!(devices_set.load(std::memory_order_acquire) & bit)) {
+        e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)LDS_BYTES);
         if (e != hipSuccess) return e;
-        attr_set.store(true, std::memory_order_release);
+        devices_set.fetch_or(bit, std::memory_order_release);
     }
     DeviceShape shape;
-    hipError_t es = device_shape(&shape);
-    if (es != hipSuccess) return es;
+    e = device_shape(&shape);
+    if (e != hipSuccess) return e;
     const int n_tiles = EPI == kF8Swiglu ? p.lay.nb : (p.lay.nb + 1) / 2;
     kern<<<shape.groups, 64 * NW, LDS_BYTES, st>>>(p, partials, n_tiles, shape.xcds);
     if (p.lay.kb >= kLeastCut) fixup_kernel<EPI><<<kFixupGroups, 64 * NW, 0, st>>>(p, partials, n_tiles, shape.groups);

@@ -272,3 +272,38 @@ def test_experts_of_many_rows(gpu_device, T, d, f, S, k, act):
     torch.cuda.synchronize()
     close(a.y[:T * k], want, off)
     assert (a.y[T * k:] == 5.0).all()
+
+
+def test_packed_experts_through_the_periodic_loader(gpu_device):
+    """All experts for the first prompts, then the chosen ones, loaded on the loader's stream."""
+    E, k, T, d, f = 6, 2, 90, 136, 264
+    x, gate, m, _ = layer_inputs(T, d, f, E, E, k)
+    host = [[w[e].cpu().pin_memory() for e in range(E)] for w in m]
+    desc = P.make_desc(T, d, f, E, k, E, "f8", "swiglu")
+    slots = [torch.full(tuple(w.shape), 255, dtype=torch.uint8, device="cuda") for w in m]
+    soe, eos = (torch.full((E,), -1, dtype=torch.int32, device="cuda") for _ in range(2))
+    b, want = P.LayerBuffers.allocate(desc), P.LayerBuffers.allocate(desc)
+    torch.cuda.synchronize()
+    loader = P.Loader([dict(desc=desc, host_w1=host[0], host_w3=host[1], host_w2=host[2], w1_slots=slots[0], w3_slots=slots[1], w2_slots=slots[2],
+                            slot_of_expert=soe, expert_of_slot=eos)], 2)
+    for prompt in range(4):
+        _, action = loader.next_prompt()
+        if action == P.EMOE_PROMPT_PREDICT:
+            loader.update([[5, 1, 2]])
+        loader.layer_begin(0)
+        P.layer_forward(b, x, gate, None, soe, *slots, one_call=True)
+        loader.layer_end(0)
+        torch.cuda.synchronize()
+        here = loader.residents(0)
+        assert sorted(e for e in here if e >= 0) == (list(range(E)) if prompt < 2 else [1, 2, 5])
+        own = torch.full((E,), -1, dtype=torch.int32)
+        for s, e in enumerate(here):
+            if e >= 0:
+                own[e] = s
+                assert all(torch.equal(a[s], w[e]) for a, w in zip(slots, m))
+        resident = [w[[max(e, 0) for e in here]].contiguous() for w in m]
+        P.layer_forward(want, x, gate, None, own.cuda(), *resident)
+        torch.cuda.synchronize()
+        assert torch.equal(b.out, want.out)
+    loader.synchronize()
+    loader.close()
