@@ -348,7 +348,9 @@ hipError_t launch_shape(const F8Product& p, hipStream_t st) {
 // A wavefront's strips by the strips that there are: more of them a wavefront read x less often, fewer leave no CU without work.  Measured with matrices from
 // HBM, plain products of 17 to 64 rows a stretch (us, two strips / four): 128 strips 13.1 / 14.3 (64 rows times 2048 x 4096), 384 15.5 / 16.7 (6144 x 4096), 512
 // 16.4 / 17.4, 768 23.8 / 19.6, two stretches of 384 23.8 / 18.5, 1040 12.0 / 10.0 (16 groups of 1032 x 776), 2048 103 / 100 (8 of 4096 x 14336); eight wavefronts
-// of four strips were up to a fifth slower.  The activations' products want 128 rows a unit; four wavefronts / eight: 20 rows of 6 groups of 14336 x 4096 121 / 121
+// of four strips were up to a fifth slower.  Up to 16 rows (one strip / two / four): 64 strips 4.5 / 5.3 / 6.7 (one row times 1024 x 4096), 256 5.9 / 7.1 / 8.7, 384
+// 8.3 / 7.5 / 9.3, 512 27.2 / 25.8 / 29.6 (2 of 4096 x 14336), 520 6.3 / 5.6 / 4.5 (8 of 1032 x 776), 768 12.4 / 12.7 / 11.6, 2000 28.0 / 27.6 / 26.2, 2048 23.9 / 15.1 /
+// 13.4 (16 rows of 16 of 2048 x 1408); with eight wavefronts one or two strips 10.1 and 7.2 at 384, 36.9 and 27.7 at 2000.  The activations' products want 128 rows a unit; four wavefronts / eight: 20 rows of 6 groups of 14336 x 4096 121 / 121
 // (SwiGLU), 71 / 74 (ReLU), one row of 32 of 512 x 512 9.5 / 10.2, 7.9 / 9.0; with eight strips a wavefront 130, 72, 9.9, 7.9.
 template <int EPI>
 hipError_t launch(const F8Product& p, hipStream_t st) {
@@ -356,8 +358,8 @@ hipError_t launch(const F8Product& p, hipStream_t st) {
     const bool few = p.rows <= 16;
     if constexpr (EPI == kF8Plain) {
         const long long stretches = (p.rows + 63) / 64, strips = (groups > stretches ? groups : stretches) * ((p.N + 15) / 16);
-        if (!few) return strips > 512 ? launch_shape<EPI, 4, 4, 4>(p, st) : launch_shape<EPI, 4, 2, 4>(p, st);
-        if (strips >= 4 * 512) return launch_shape<EPI, 1, 4, 4>(p, st);
+        if (strips > 512) return few ? launch_shape<EPI, 1, 4, 4>(p, st) : launch_shape<EPI, 4, 4, 4>(p, st);
+        if (!few) return launch_shape<EPI, 4, 2, 4>(p, st);
         return strips > 256 ? launch_shape<EPI, 1, 2, 4>(p, st) : launch_shape<EPI, 1, 1, 4>(p, st);
     } else {
         return few ? launch_shape<EPI, 1, 4, 4>(p, st) : launch_shape<EPI, 4, 4, 4>(p, st);
