@@ -1,6 +1,7 @@
 // Conversions to and from 8 bits under a power of two a block of 128: matrices once when a model is read, rows of activations
 // before every product.  All of it is exact but the one rounding to a code, so the bits depend on nothing but the input.
-// Bound by memory: an element is read and written once.
+// Bound by memory: an element is read and written once.  Packing 14336 x 4096 of bf16 takes 42 us (4.2 TB/s) and reading it back 27 (6.5 TB/s, of it what was packed
+// from caches), rows of 8192 x 4096 21 to 24 us (4.2 to 4.8 TB/s); a copy reaches 5.1.
 #include "matrix_f8.h"
 
 namespace emoe {

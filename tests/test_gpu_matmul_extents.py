@@ -29,8 +29,7 @@ def test_few_tiles(gpu_device, rows, N):
 
 @pytest.mark.parametrize("kb", (1, 2, 3, 4, 5, 7, 8, 9, 10, 13, 16, 17, 31, 33))
 def test_blocks_of_columns(gpu_device, kb):
-    """Pieces of tiles along K begin at whole fours, rows' powers come in fours: every remainder, with the last block cut too; groups
-    start at different blocks."""
+    """A wavefront takes every fourth block, rows' powers come in fours: every remainder, with the last block cut too."""
     g = np.random.default_rng(kb)
     sizes = (150, 0, 257, 3, 130, 300)
     offsets = np.concatenate(([0], np.cumsum(sizes))).tolist()

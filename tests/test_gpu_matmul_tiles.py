@@ -38,8 +38,8 @@ def test_groups(gpu_device, sizes, behind, K):
 
 @pytest.mark.parametrize("kb", (2, 3, 4, 5, 6, 7, 8, 9, 13, 17, 23, 24, 25, 26, 27, 31, 33))
 def test_blocks_of_columns(gpu_device, kb):
-    """Tiles are cut along K from 24 blocks on, at whole fours, and rows' powers come in fours: every remainder, with the last block cut too;
-    groups start at different blocks."""
+    """Tiles are cut along K from 24 blocks on, at whole fours, and rows' powers come in fours: every remainder, with the last block
+    cut too."""
     g = np.random.default_rng(kb)
     sizes = (150, 0, 257, 3, 130, 1560)
     offsets = np.concatenate(([0], np.cumsum(sizes))).tolist()
