@@ -159,6 +159,15 @@ def _addr(t) -> Optional[int]:
         return _ptr(t).value
 
 
+def _device_addr(name: str, t) -> Optional[int]:
+    """_addr() of memory that kernels read or write.  A tensor or array that says where it lies has to lie on a GPU: an address of the
+    host's, handed to a kernel, is a fault of the GPU.  (An int says nothing and is taken as it is.)"""
+    there = getattr(t, "is_cuda", None)
+    if there or (there is None and not hasattr(t, "ctypes")):
+        return _addr(t)
+    raise ValueError(f"{name}: memory of a GPU is wanted, not of {getattr(t, 'device', 'cpu')}")
+
+
 def _stream_addr(stream) -> Optional[int]:
     """_stream() without the wrapping."""
     if stream is None:
@@ -345,14 +354,14 @@ def emoe_matrix_bytes(N: int, K: int, check=True) -> int:
 
 def emoe_matrix_pack(count, N, K, dtype, w, matrices, w_stride=None, stream=None, check=True) -> int:
     """`w_stride`: elements from row to row, dense if not given."""
-    rc = lib().emoe_matrix_pack(count, N, K, DTYPES.get(dtype, dtype), _addr(w), K if w_stride is None else w_stride, _addr(matrices),
-                                _stream_addr(stream))
+    rc = lib().emoe_matrix_pack(count, N, K, DTYPES.get(dtype, dtype), _device_addr("w", w), K if w_stride is None else w_stride,
+                                _device_addr("matrices", matrices), _stream_addr(stream))
     return _check(rc, "emoe_matrix_pack", check)
 
 
 def emoe_matrix_unpack(count, N, K, dtype, matrices, w, w_stride=None, stream=None, check=True) -> int:
-    rc = lib().emoe_matrix_unpack(count, N, K, DTYPES.get(dtype, dtype), _addr(matrices), _addr(w), K if w_stride is None else w_stride,
-                                  _stream_addr(stream))
+    rc = lib().emoe_matrix_unpack(count, N, K, DTYPES.get(dtype, dtype), _device_addr("matrices", matrices), _device_addr("w", w),
+                                  K if w_stride is None else w_stride, _stream_addr(stream))
     return _check(rc, "emoe_matrix_unpack", check)
 
 
@@ -364,8 +373,8 @@ def emoe_matmul_workspace_bytes(desc: EmoeMatmulDesc, check=True) -> int:
 
 
 def emoe_matmul(desc: EmoeMatmulDesc, x, group_offsets, matrices, out, ws, ws_bytes, stream=None, check=True) -> int:
-    rc = lib().emoe_matmul(ctypes.byref(desc), _addr(x), _addr(group_offsets), _addr(matrices), _addr(out), _addr(ws), int(ws_bytes),
-                           _stream_addr(stream))
+    rc = lib().emoe_matmul(ctypes.byref(desc), _device_addr("x", x), _device_addr("group_offsets", group_offsets),
+                           _device_addr("matrices", matrices), _device_addr("out", out), _device_addr("ws", ws), int(ws_bytes), _stream_addr(stream))
     return _check(rc, "emoe_matmul", check)
 
 

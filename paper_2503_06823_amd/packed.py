@@ -32,7 +32,7 @@ class PackedMatrices:
 
     @staticmethod
     def pack(w: torch.Tensor, stream=None) -> "PackedMatrices":
-        """`w`: [N, K] or [count, N, K], fp32 or bf16."""
+        """`w`: [N, K] or [count, N, K], fp32 or bf16, in a GPU's memory (as every tensor here: the calls refuse the host's)."""
         if not (isinstance(w, torch.Tensor) and w.dim() in (2, 3)):
             raise ValueError(f"w: [N, K] or [count, N, K] is wanted, not {_described(w)}")
         m = PackedMatrices.allocate(w.shape[0] if w.dim() == 3 else 1, w.shape[-2], w.shape[-1], w.device)
