@@ -75,10 +75,10 @@ const char *emoe_status_string(int status);
  * (either output pointer may be NULL).  Pure host arithmetic.  The FFN workspace is
  * h [A,f] in dtype plus, for bf16 layers with more than 22 rows per slot on average,
  * 32 or 64 MiB of fp32 partial sums of output tiles cut along K; for EMOE_F8 layers h and
- * x's rows in 8 bits, and 64 MiB of such sums where there are many rows.  Neither workspace
- * needs initialising, and nothing in them outlives a call except h between the two
- * passes of emoe_expert_ffn_pass.  Calls that may run at the same time (different
- * streams) need workspaces of their own. */
+ * x's rows in 8 bits, and where there are many rows 64 MiB of such sums and, with d_ff up to
+ * 2560, a bit for each element of h.  Neither workspace needs initialising, and nothing in
+ * them outlives a call except h between the two passes of emoe_expert_ffn_pass.  Calls that
+ * may run at the same time (different streams) need workspaces of their own. */
 int emoe_workspace_bytes(const emoe_layer_desc *desc, size_t *permute_ws_bytes, size_t *ffn_ws_bytes);
 
 /*
@@ -563,6 +563,9 @@ int emoe_kv_attention(const emoe_kv_desc *desc, const emoe_attention_desc *atten
  * bf16, and emoe_route, emoe_permute and emoe_combine do what they do for bf16.  The expert FFN brings x's rows and h's, which is
  * never rounded to anything else, to 8 bits as above:
  *   h = q(act(q(x) W1^T) (* q(x) W3^T)),  y = bf16(h W2^T).
+ * Products are summed as in emoe_matmul.  What the sums lose, 1e-5 to 1e-4 of an element of h as a rule, may give an element that is as near to a tie of
+ * two codes either of them.  With d_ff up to 2560, elements within 1e-4 of a tie whose two codes are more than 1 / 32 of their row of h apart (a row being taken
+ * for the root of the sum of the squares of its blocks' largest elements) are summed again in fp32, whichever kernel makes h.
  */
 
 /* Bytes of a packed matrix; a multiple of 256.  Pure host arithmetic. */

@@ -18,7 +18,7 @@ LIB = os.path.join(HERE, "libemoe.so")
 
 SOURCES = ["api.hip", "maps.hip", "select.hip", "loader.hip", "schedule.hip", "route.hip", "route_mfma.hip", "route_f32.hip", "permute.hip", "combine.hip", "ffn_f32.hip", "ffn_bf16_tiled.hip", "ffn_bf16_mid.hip",
            "ffn_bf16_stream.hip", "ffn_bf16_few.hip", "peaks.hip", "kv_api.hip", "kv_tables.hip", "kv_quant.hip", "kv_attention.hip", "kv_attention_few.hip", "kv_attention_tile.hip",
-           "matrix_api.hip", "matrix_pack.hip", "matmul_f8_stream.hip", "matmul_f8_tiled.hip"]
+           "matrix_api.hip", "matrix_pack.hip", "matmul_f8_stream.hip", "matmul_f8_tiled.hip", "matmul_f8_ties.hip"]
 FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-function",
          # packed fp32 VALU forms are kept out of all device code
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -56,7 +56,7 @@ def compile_objects(obj_dir: str, extra_flags=(), jobs: int = 8):
 def build_library(force: bool = True, jobs: int = 8, extra_flags=()) -> str:
     """Compile every HIP source and link libemoe.so; returns its path."""
     os.makedirs(OBJ, exist_ok=True)
-    headers = [os.path.join(CSRC, "common.h"), os.path.join(CSRC, "mfma_agpr.h"), os.path.join(CSRC, "block_sort.h"), os.path.join(CSRC, "mid_work.h"), os.path.join(CSRC, "route_topk.h"), os.path.join(CSRC, "wave_max.h"), os.path.join(CSRC, "kv_cache.h"), os.path.join(CSRC, "kv_attention.h"), os.path.join(CSRC, "matrix_f8.h"), os.path.join(CSRC, "tile_plan.h"),
+    headers = [os.path.join(CSRC, "common.h"), os.path.join(CSRC, "mfma_agpr.h"), os.path.join(CSRC, "block_sort.h"), os.path.join(CSRC, "mid_work.h"), os.path.join(CSRC, "route_topk.h"), os.path.join(CSRC, "wave_max.h"), os.path.join(CSRC, "kv_cache.h"), os.path.join(CSRC, "kv_attention.h"), os.path.join(CSRC, "matrix_f8.h"), os.path.join(CSRC, "tile_plan.h"), os.path.join(CSRC, "matmul_f8_tiles.h"),
                os.path.join(ROOT, "include", "emoe.h")]
     newest_hdr = max(os.path.getmtime(h) for h in headers)
 

@@ -101,44 +101,12 @@ struct RowsInFlight {
     }
 };
 
-// Output n of row r once more, by a whole wavefront, its products exact and its sums in fp32 (see kNearTie)
-template <bool OWN>
-__device__ __forceinline__ float sum_again(const F8Product& p, const uint8_t* matrix, int n, int r, int row0, const OwnRows* own) {
-    const int column = 2 * (threadIdx.x & 63), nb = n >> 7, kb = p.lay.kb;
-    const size_t codes = p.lay.codes();
-    const uint8_t* w = matrix + (size_t)nb * kb * kF8BlockBytes + ((n >> 4) & 7) * kF8Strip + (column >> 6) * 1024 + ((column >> 4) & 3) * 256 + (n & 15) * 16 +
-                       (column & 15);
-    const uint8_t* w_powers = matrix + codes + (size_t)nb * p.lay.kg * 4;
-    float sum = 0.0f;
-#pragma unroll 2
-    for (int b = 0; b < kb; ++b) {
-        const int wc = *reinterpret_cast<const uint16_t*>(w + (size_t)b * kF8BlockBytes);
-        int xc, power = w_powers[b];
-        if constexpr (OWN) {
-            xc = *reinterpret_cast<const uint16_t*>(own->codes + ((r - row0) * kb + b) * kF8Block + column);
-            power += own->powers[(r - row0) * kb + b];
-        } else {
-            xc = *reinterpret_cast<const uint16_t*>(p.x.codes + (size_t)r * p.x.row_step + (size_t)(b * 8 + (column >> 4)) * p.x.piece_step + (column & 15));
-            power += (p.x.scales[(size_t)(b >> 2) * p.x.rows + r] >> (8 * (b & 3))) & 255u;
-        }
-        const float two = __builtin_amdgcn_cvt_f32_fp8(wc, 0) * __builtin_amdgcn_cvt_f32_fp8(xc, 0) + __builtin_amdgcn_cvt_f32_fp8(wc, 1) * __builtin_amdgcn_cvt_f32_fp8(xc, 1);
-        sum += ldexpf(two, power - 254);
-    }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
-    return sum;
-}
-// A number under its block's power is near a tie of two codes if it is within kNearTie steps of it.  The instruction's error, 1e-5 to 5e-5 of a result, is
-// a thousandth of a step and decides there, and of the elements that are large in their block (kLargeCode and more, of up to 448) the code is up to an eighth of
-// the element: where such an element is most of its row, 9 % of an output row have come of it (1368 tokens, d 1216, f 200: 5.8e-3 of all outputs, 2.5e-3 without).
-// So of the large ones those near a tie, one in some thousands, are summed again, in rows of up to kFewBlocks blocks: in longer ones (f 14336) no element is
-// much of its row, and the workgroups that have one take 2 us more for it (64 tokens' experts 196 -> 233 us if they were summed there).
-constexpr float kNearTie = 0.0015f, kLargeCode = 128.0f;
-constexpr int kFewBlocks = 16;
-__device__ __forceinline__ bool near_tie(float scaled) {
-    const float s = fabsf(scaled), steps = s * (s >= 256.0f ? 1.0f / 32 : 1.0f / 16);
-    return s >= kLargeCode && s < 448.0f && fabsf(steps - floorf(steps) - 0.5f) < kNearTie;
-}
+// As F8RowInMemory, of OwnRows
+struct OwnRow {
+    const uint8_t *codes, *powers;
+    __device__ uint4 piece(int q) const { return *reinterpret_cast<const uint4*>(codes + q * 16); }
+    __device__ int power(int b) const { return powers[b]; }
+};
 
 // Rows row0 .. row_end - 1 of x, 16 TB at most, times a unit of their group's matrix.  OWN: x is converted here.
 template <int EPI, int TB, int STRIPS, int WAVES, int POLICY, bool OWN>
@@ -299,6 +267,7 @@ __device__ __forceinline__ void multiply_unit(const F8Product& p, int unit, int 
             if (quad == 0) tops[wave][16 * t + tok] = top;
         }
         __syncthreads();
+        uint32_t near[TB], top_of[TB];
 #pragma unroll
         for (int t = 0; t < TB; ++t) {
             const int r = row0 + 16 * t + tok, c = 16 * t + tok;
@@ -307,30 +276,42 @@ __device__ __forceinline__ void multiply_unit(const F8Product& p, int unit, int 
             for (int o = 1; o < WAVES; ++o) top = umax(top, tops[o][c]);
             const uint32_t byte = f8_scale_byte(top);
             const float inverse = f8_inverse(byte);
-            int again = -1;  // which of the lane's numbers of this row is to be summed again
-#pragma unroll
-            for (int f = 0; f < FINAL; ++f)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) again = near_tie(sum[0][f][t][v] * inverse) ? 4 * f + v : again;
-            if (r >= row_end || byte == 255u || p.lay.nb > kFewBlocks) again = -1;
-            for (uint64_t left = __ballot(again >= 0); left != 0; left &= left - 1) {
-                const int who = __builtin_amdgcn_readfirstlane(__builtin_ctzll(left)), which = __builtin_amdgcn_readlane(again, who);
-                const int n = nb * kF8Block + (strip0 + wave * FINAL + (which >> 2)) * 16 + (who >> 4) * 4 + (which & 3), row = row0 + 16 * t + (who & 15);
-                float g = sum_again<OWN>(p, p.w0 + (size_t)group * p.matrix_bytes, n, row, row0, own);
-                if constexpr (EPI == kF8Swiglu) g = g / (1.0f + __expf(-g)) * sum_again<OWN>(p, p.w1 + (size_t)group * p.matrix_bytes, n, row, row0, own);
-                else g = g < 0.0f ? 0.0f : g;
-#pragma unroll
-                for (int f = 0; f < FINAL; ++f)
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) sum[0][f][t][v] = lane == who && which == 4 * f + v ? g : sum[0][f][t][v];
-            }
+            near[t] = 0;
+            top_of[t] = top;
             if (r >= row_end) continue;
 #pragma unroll
-            for (int f = 0; f < FINAL; ++f) {
+            for (int f = FINAL - 1; f >= 0; --f) {
                 const floatx4& h = sum[0][f][t];
                 *reinterpret_cast<uint32_t*>(p.h.codes + (size_t)r * p.h.row_step + (size_t)((n0 >> 4) + f) * p.h.piece_step + quad * 4) = f8_codes(h[0], h[1], h[2], h[3], inverse);
+#pragma unroll
+                for (int v = 3; v >= 0; --v) near[t] = f8_near_ties(near[t], h[v] * inverse);
             }
+            if (byte == 255u || p.lay.nb > kTieBlocks) near[t] = 0;
             if (wave == 0 && quad == 0) reinterpret_cast<uint8_t*>(p.h.scales + (size_t)(nb >> 2) * p.h.rows + r)[nb & 3] = (uint8_t)byte;
+        }
+#pragma unroll 1
+        for (int t = 0; t < TB; ++t) {
+            uint32_t its_near = near[0], its_top = top_of[0];
+#pragma unroll
+            for (int i = 1; i < TB; ++i) {
+                its_near = t == i ? near[i] : its_near;
+                its_top = t == i ? top_of[i] : its_top;
+            }
+            for (uint64_t left = __ballot(its_near != 0); left != 0; left &= left - 1) {
+                const int who = __builtin_amdgcn_readfirstlane(__builtin_ctzll(left)), row = row0 + 16 * t + (who & 15);
+                const float inverse = f8_inverse(f8_scale_byte((uint32_t)__builtin_amdgcn_readlane((int)its_top, who)));
+                const uint8_t* both[M];
+                both[0] = p.w0 + (size_t)group * p.matrix_bytes;
+                if constexpr (M == 2) both[1] = p.w1 + (size_t)group * p.matrix_bytes;
+                for (uint32_t bits = (uint32_t)__builtin_amdgcn_readlane((int)its_near, who); bits != 0; bits &= bits - 1) {
+                    const int bit = __builtin_ctz(bits), n = nb * kF8Block + (strip0 + wave * FINAL + (bit >> 2)) * 16 + (who >> 4) * 4 + (bit & 3);
+                    float h;
+                    if constexpr (OWN) h = f8_h<M, 64>(p.lay, both, n, OwnRow{own->codes + (row - row0) * p.lay.kb * kF8Block, own->powers + (row - row0) * p.lay.kb});
+                    else h = f8_h<M, 64>(p.lay, both, n, F8RowInMemory(p.x, row));
+                    if (lane == who)  // (which stored the element before)
+                        p.h.codes[(size_t)row * p.h.row_step + (size_t)(n >> 4) * p.h.piece_step + (n & 15)] = (uint8_t)f8_codes(h, 0.0f, 0.0f, 0.0f, inverse);
+                }
+            }
         }
     }
 }

@@ -92,6 +92,7 @@ MatmulWs matmul_ws(const emoe_matmul_desc& d, void* ws) {
 
 struct FfnF8Ws {
     F8Rows h, x;
+    uint16_t* near;  // of the tiles, see F8Product
     float* partials;
     size_t total;
 };
@@ -102,6 +103,8 @@ FfnF8Ws ffn_ws(const emoe_layer_desc& d, void* ws) {
     w.total = 0;
     w.h = rows_at(static_cast<uint8_t*>(ws), &w.total, A, d.d_ff);
     w.x = rows_at(static_cast<uint8_t*>(ws), &w.total, A, d.d_model);
+    w.near = reinterpret_cast<uint16_t*>(static_cast<uint8_t*>(ws) + w.total);
+    if (first_is_tiled(d) && whole(d.d_ff) <= kTieBlocks * kF8Block) w.total = align256(w.total + (size_t)A * whole(d.d_ff) / 8);
     w.partials = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + w.total);
     if (first_is_tiled(d) || second_is_tiled(d)) w.total += kTiledPartialBytes;
     return w;
@@ -162,6 +165,7 @@ hipError_t launch_ffn_f8(const emoe_layer_desc& d, const void* x_perm, RowGather
         p.matrix_bytes = p.lay.bytes();
         p.N = d.d_ff;
         p.h = h;
+        p.near = lay.near;
         if (!tiled && f8_own_rows(A, d.d_model)) {
             own_rows(p, x_perm, d.d_model, d.d_model);
             p.perm = gather.perm;

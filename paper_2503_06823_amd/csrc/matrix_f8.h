@@ -33,6 +33,7 @@ inline size_t f8_rows_scale_bytes(long long rows, int K) { return (size_t)rows *
 
 // The product of grouped rows with their group's matrix (offsets NULL: one group of all rows), and what becomes of it:
 // plain: bf16 rows of out; SwiGLU, ReLU: the activation's result as rows in 8 bits, h.
+constexpr int kTieBlocks = 20;  // blocks of a row of h up to which elements near ties of two codes are summed again, see kNearTie
 enum F8Epilogue { kF8Plain = 0, kF8Swiglu = 1, kF8Relu = 2 };
 struct F8Product {
     F8Rows x;
@@ -50,6 +51,7 @@ struct F8Product {
     int64_t out_stride;
     const int32_t* out_perm;  // row r is stored as row out_perm[r]; NULL: r
     F8Rows h;
+    uint16_t* near;  // (tiles) which elements of h are near ties of two codes, [lay.nb][2][rows][4], see near_ties_kernel
     const bf16_t* from;  // (streaming) NULL, or the rows themselves, x not being there: workgroups convert them
     int64_t from_stride;
     int K;
@@ -66,6 +68,7 @@ hipError_t launch_f8_rows(const void* x, int64_t stride, int K, const F8Rows& to
 hipError_t launch_f8_stream(const F8Product& p, F8Epilogue epilogue, hipStream_t st);
 // partials: kTiledPartialBytes.  x by rows; at least two blocks of columns.
 hipError_t launch_f8_tiled(const F8Product& p, F8Epilogue epilogue, float* partials, hipStream_t st);
+hipError_t launch_f8_ties(const F8Product& p, F8Epilogue epilogue, float* partials, hipStream_t st);  // (its part for activations into short rows of h)
 
 hipError_t launch_matrix_pack(int count, int N, int K, int dtype, const void* w, int64_t stride, void* matrix, hipStream_t st);
 hipError_t launch_matrix_unpack(int count, int N, int K, int dtype, const void* matrix, void* w, int64_t stride, hipStream_t st);
@@ -113,6 +116,84 @@ __device__ __forceinline__ uint32_t f8_top(const float (&v)[8]) {
 }
 __device__ __forceinline__ uint2 f8_codes(const float (&v)[8], float inverse) {
     return make_uint2(f8_codes(v[0], v[1], v[2], v[3], inverse), f8_codes(v[4], v[5], v[6], v[7], inverse));
+}
+
+// ---- elements of h near a tie of two codes ------------------------------------------------------------------------------
+// The matrix cores' sums are 1e-5 to 5e-5 off (see matmul_f8_stream.hip), a thousandth of a code's step, and of an element that near a tie of two codes
+// they decide which of the two it gets.  Of the elements that are large in their block (128 and more, of up to 448) the codes are up to an eighth of the
+// element apart: where such an element is most of its row of h, an output row changes by as much (1368 tokens, d 1216, f 200: one row 9 %, all outputs 5.8e-3;
+// with those elements summed again 0.8 % and 2.5e-3).  So a large element within kNearTie of a tie whose step is more than 1 / 32 of its row gets its sums once more,
+// products exact and added in fp32, and the code of these, whichever kernel makes h: some 1e-4 of all elements are near ties, 2e-5 matter.
+// Rows of up to kTieBlocks blocks: where blocks share a power, a step is at most 1 / 32 of a longer row (a block's largest element is 224 or more under its
+// power, a step 32).  In longer ones a block that stands out by more than its neighbours' powers is left as it is: looking for these cost 64 tokens' experts of
+// f 14336 190 -> 203 us and 4096 tokens' 1172 -> 1215.
+// A call takes longer for it with such elements: a microsecond or two of a half or whole wavefront each, which is felt where most rows have many.
+// What is left: one in some 100 sums of large elements is off by more than kNearTie (2e-4 to 1e-4 of the element, where terms of the sum cancel); smaller elements
+// have what the matrix cores say, a step of theirs being at most a thirtieth of the block's largest.
+constexpr uint32_t kNearTie = 1573;  // 0.0015 steps, a step being 2^20 of a float's last places
+// near * 2 + whether a number under its block's factor is one of them.  Codes have three places after the point: a tie is where the other 20 say one half, from
+// 136 on, the first of the large ones; smaller numbers leave bit 30.  (By signs: a comparison would take scalar registers, and two wait states.)
+__device__ __forceinline__ uint32_t f8_near_ties(uint32_t near, float scaled) {
+    const uint32_t over = __float_as_uint(scaled) - (0x43080000u - kNearTie);
+    return __builtin_amdgcn_alignbit(near, (over & 0x400fffffu) - 2 * kNearTie, 31);
+}
+
+// 16 products of codes, exact, and their sum
+__device__ __forceinline__ float f8_dot16(uint4 a, uint4 b) {
+    const int u[4] = {(int)a.x, (int)a.y, (int)a.z, (int)a.w}, v[4] = {(int)b.x, (int)b.y, (int)b.z, (int)b.w};
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        sum = fmaf(__builtin_amdgcn_cvt_f32_fp8(u[i], 0), __builtin_amdgcn_cvt_f32_fp8(v[i], 0), sum);
+        sum = fmaf(__builtin_amdgcn_cvt_f32_fp8(u[i], 1), __builtin_amdgcn_cvt_f32_fp8(v[i], 1), sum);
+        sum = fmaf(__builtin_amdgcn_cvt_f32_fp8(u[i], 2), __builtin_amdgcn_cvt_f32_fp8(v[i], 2), sum);
+        sum = fmaf(__builtin_amdgcn_cvt_f32_fp8(u[i], 3), __builtin_amdgcn_cvt_f32_fp8(v[i], 3), sum);
+    }
+    return sum;
+}
+// A row of x in 8 bits: its pieces of 16 codes and its powers
+struct F8RowInMemory {
+    const uint8_t* codes;
+    const uint8_t* powers;
+    size_t piece_step, fours_step;  // bytes from a piece to the next; from four powers to the next four
+    __device__ F8RowInMemory(const F8Rows& x, size_t row)
+        : codes(x.codes + row * x.row_step), powers(reinterpret_cast<const uint8_t*>(x.scales + row)), piece_step(x.piece_step), fours_step((size_t)x.rows * 4) {}
+    __device__ uint4 piece(int q) const { return *reinterpret_cast<const uint4*>(codes + q * piece_step); }
+    __device__ int power(int b) const { return powers[(b >> 2) * fours_step + (b & 3)]; }
+};
+// Element n of h for row x, by LANES lanes that stand together: a lane takes pieces lane, lane + LANES, ...  M: 2 for SwiGLU, 1 for ReLU.
+template <int M, int LANES, class Row>
+__device__ __forceinline__ float f8_h(const F8Layout& lay, const uint8_t* const (&matrix)[M], int n, const Row& x) {
+    const size_t w_at = (size_t)(n >> 7) * lay.kb * kF8BlockBytes + ((n >> 4) & 7) * kF8Strip + (n & 15) * 16;
+    const size_t power_at = lay.codes() + (size_t)(n >> 7) * lay.kg * 4;
+    constexpr int AHEAD = 4;  // a lane's pieces on their way together
+    const int pieces = lay.kb * 8;
+    float sum[M] = {};
+    for (int q0 = threadIdx.x & (LANES - 1); q0 < pieces; q0 += AHEAD * LANES) {
+        uint4 xc[AHEAD], wc[M][AHEAD];
+        int power[M][AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int q = q0 + i * LANES < pieces ? q0 + i * LANES : q0, b = q >> 3;
+            xc[i] = x.piece(q);
+            const int x_power = x.power(b);
+#pragma unroll
+            for (int m = 0; m < M; ++m) {
+                wc[m][i] = *reinterpret_cast<const uint4*>(matrix[m] + w_at + (size_t)b * kF8BlockBytes + ((q >> 2) & 1) * 1024 + (q & 3) * 256);
+                power[m][i] = x_power + matrix[m][power_at + b];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+            for (int m = 0; m < M; ++m) sum[m] += q0 + i * LANES < pieces ? ldexpf(f8_dot16(wc[m][i], xc[i]), power[m][i] - 254) : 0.0f;
+    }
+#pragma unroll
+    for (int o = 1; o < LANES; o <<= 1)
+#pragma unroll
+        for (int m = 0; m < M; ++m) sum[m] += __shfl_xor(sum[m], o);
+    if constexpr (M == 2) return sum[0] / (1.0f + __expf(-sum[0])) * sum[M - 1];
+    else return sum[0] < 0.0f ? 0.0f : sum[0];
 }
 #endif
 
