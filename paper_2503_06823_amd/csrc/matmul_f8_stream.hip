@@ -33,7 +33,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void* base, ui
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)bytes, 0x00020000);
 }
 // 16 bytes at `lane + at` and 16 at `second` bytes from there: an offset of the lane's, and a scalar one
-template <int POLICY>
+template <int POLICY>  // of caches: 2, not kept: a matrix is read once; 0
 __device__ __forceinline__ intx8 two(__amdgpu_buffer_rsrc_t from, uint32_t lane, uint32_t at, int second) {
     const uintx4 a = __builtin_amdgcn_raw_buffer_load_b128(from, (int)lane, (int)at, POLICY);
     const uintx4 b = __builtin_amdgcn_raw_buffer_load_b128(from, (int)lane + second, (int)at, POLICY);
@@ -109,7 +109,7 @@ struct OwnRow {
 };
 
 // Rows row0 .. row_end - 1 of x, 16 TB at most, times a unit of their group's matrix.  OWN: x is converted here.
-template <int EPI, int TB, int STRIPS, int WAVES, int POLICY, bool OWN>
+template <int EPI, int TB, int STRIPS, int WAVES, bool OWN>
 __device__ __forceinline__ void multiply_unit(const F8Product& p, int unit, int group, int row0, int row_end, floatx4 (&red)[WAVES][STRIPS][64],
                                               uint32_t (&tops)[WAVES][64], OwnRows* own) {
     static_assert(!OWN || TB == 1, "at most 16 rows");
@@ -155,7 +155,7 @@ __device__ __forceinline__ void multiply_unit(const F8Product& p, int unit, int 
         const bool there = j < mine;
         const uint32_t b = there ? part + j * SPLIT : part, lane_at = there ? lane * 16u : codes;
 #pragma unroll
-        for (int i = 0; i < STRIPS; ++i) w[slot][i] = two<POLICY>(w_rsrc, lane_at, w_at + b * kF8BlockBytes + i * kF8Strip, 1024);
+        for (int i = 0; i < STRIPS; ++i) w[slot][i] = two<2>(w_rsrc, lane_at, w_at + b * kF8BlockBytes + i * kF8Strip, 1024);
         wb[slot] = w_scales[b >> 2];
     };
     auto load_x = [&](int slot, int j) {
@@ -316,7 +316,7 @@ __device__ __forceinline__ void multiply_unit(const F8Product& p, int unit, int 
     }
 }
 
-// MOST: blocks of 16 rows that a workgroup has at most.  Workgroups go through the units of an item, then of the next: with MOST 1 items are groups, otherwise
+// MOST: blocks of 16 rows that a workgroup has at most, 1 or 4.  Workgroups go through the units of an item, then of the next: with MOST 1 items are groups, otherwise
 // 64 rows of a group or what is left of it, counted through the groups (there are fewer than there are workgroups for).
 template <int EPI, int MOST, int STRIPS, int WAVES, bool OWN>
 __global__ __launch_bounds__(64 * WAVES, 2) void stream_kernel(F8Product p, int n_units) {
@@ -362,9 +362,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void stream_kernel(F8Product p, int 
     }
     if (row_end <= row0) return;  // its matrix is never touched
     if (MOST > 1) row_end = row_end < row0 + 16 * MOST ? row_end : row0 + 16 * MOST;
-    if (MOST == 1 || row_end - row0 <= 16) multiply_unit<EPI, 1, STRIPS, WAVES, 2, OWN>(p, unit, group, row0, row_end, red, tops, own);
-    else if (MOST == 2 || row_end - row0 <= 32) multiply_unit<EPI, MOST < 2 ? 1 : 2, STRIPS, WAVES, 2, OWN>(p, unit, group, row0, row_end, red, tops, own);
-    else multiply_unit<EPI, MOST, STRIPS, WAVES, 2, OWN>(p, unit, group, row0, row_end, red, tops, own);
+    if (MOST == 1 || row_end - row0 <= 16) multiply_unit<EPI, 1, STRIPS, WAVES, OWN>(p, unit, group, row0, row_end, red, tops, own);
+    else if (row_end - row0 <= 32) multiply_unit<EPI, MOST == 1 ? 1 : 2, STRIPS, WAVES, OWN>(p, unit, group, row0, row_end, red, tops, own);
+    else multiply_unit<EPI, MOST, STRIPS, WAVES, OWN>(p, unit, group, row0, row_end, red, tops, own);
 }
 
 template <int EPI, int MOST, int STRIPS, int WAVES>

@@ -325,28 +325,12 @@ __device__ __forceinline__ void tiles(const F8Product& p, float* __restrict__ pa
         __builtin_amdgcn_global_load_lds((global_void*)s, (lds_void*)(lds + kMatrixScalesAt + (parity * NW + wave) * 256), 4, 0, 0);
     };
 
-    // Where an item's requests stand in its K tiles
-    struct Cursor {
-        int at, begin, end;
-    };
-    auto cursor_of = [&](const Item& it) INLINE {
-        Cursor u;
-        u.begin = it.kb;
-        u.end = it.kb + it.kt;
-        u.at = u.begin;
-        return u;
-    };
-    auto advance = [](Cursor& u) INLINE {
-        ++u.at;
-        u.at = u.at == u.end ? u.begin : u.at;
-    };
-
     Item cur, nxt;
     if (!item_at(0, cur)) return;
     int perm_entry = load_perm(cur);
     row_addr(cur, perm_entry);
     Panel panel = panel_of(cur);
-    Cursor cursor = cursor_of(cur);
+    int wanted = cur.kb;                // the K tile that is requested next: of this item up to its last, then of the next one
     bool there = true;                  // whether there is a tile to request
     int scale_put = 0, scale_get = 1;   // which of two places the next group of powers takes, and which the last one that was read has
     int kb_next = 0;                    // the K tile after the one that is multiplied
@@ -354,7 +338,7 @@ __device__ __forceinline__ void tiles(const F8Product& p, float* __restrict__ pa
     // the first two tiles
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-        const int kb = __builtin_amdgcn_readfirstlane(cursor.at);
+        const int kb = __builtin_amdgcn_readfirstlane(wanted);
         if ((kb & 3) == 0) {
             issue_scales(panel, scale_put, kb);
             scale_put ^= 1;
@@ -366,7 +350,7 @@ __device__ __forceinline__ void tiles(const F8Product& p, float* __restrict__ pa
 #pragma unroll
         for (int i = 0; i < LPW / 2; ++i) issue_w(panel, Second{}, i, t * TILE_BYTES, kb);
         kb_next = kb;
-        advance(cursor);
+        ++wanted;
     }
     barrier_keep_loads<0>();
 
@@ -450,7 +434,7 @@ __device__ __forceinline__ void tiles(const F8Product& p, float* __restrict__ pa
             auto k_tile = [&](auto first_c, auto now_c, bool last) INLINE {
                 constexpr int now = decltype(now_c)::value, other = now ^ 1;
                 const auto nothing = [](auto) INLINE {};
-                const int kb = __builtin_amdgcn_readfirstlane(cursor.at);
+                const int kb = __builtin_amdgcn_readfirstlane(wanted);
                 if (there && (kb & 3) == 0) {
                     issue_scales(panel, scale_put, kb);
                     scale_put ^= 1;
@@ -483,7 +467,7 @@ __device__ __forceinline__ void tiles(const F8Product& p, float* __restrict__ pa
                 const int kb_then = kb_next;
                 kb_next = kb;
                 place ^= TILE_BYTES;
-                advance(cursor);
+                ++wanted;
                 barrier_keep_loads<kPending>();
                 __builtin_amdgcn_sched_barrier(0);
                 shift_scales(kb_then);
@@ -492,12 +476,12 @@ __device__ __forceinline__ void tiles(const F8Product& p, float* __restrict__ pa
             };
             // the last two K tiles request the next item's first two
             auto turn_to_next = [&]() INLINE {
-                cursor = Cursor{0, 0, 4};
+                wanted = 0;
                 there = have_nxt;
                 if (have_nxt) {
                     row_addr(nxt, perm_entry);
                     panel = panel_of(nxt);
-                    cursor = cursor_of(nxt);
+                    wanted = nxt.kb;
                 } else {  // none: they go on, out of range: zeros land where nobody reads any more
 #pragma unroll
                     for (int i = 0; i < LPW; ++i) x_voff[i] = x_bytes;
