@@ -20,14 +20,16 @@
  *     fixed array behind emoe_permute_static, and the number of compute units
  *     and XCDs of each device, which are looked up once and remembered.
  *   - Tensors are dense row-major.  Element type is desc->dtype: fp32, or
- *     bf16 stored as 16-bit patterns.  Pointers must be 16-byte aligned.
+ *     bf16 stored as 16-bit patterns; of layers with EMOE_F8 bf16, and the experts'
+ *     matrices packed (see "Matrices in 8 bits").  Pointers must be 16-byte aligned.
  *   - `stream` is a hipStream_t (NULL = the null stream).  Calls only enqueue
  *     work on it; none synchronises with the host.
  *   - Return value: EMOE_OK or a negative emoe_status.  Arguments are checked
  *     on the host before anything is enqueued; on a validation error nothing
  *     is enqueued and no output is touched.  T == 0 is a successful no-op.
  *   - Limits of the layer's calls: 1 <= k <= S <= E <= 64; d_model and d_ff multiples of 8;
- *     (T*k + 2) * max(d_model, d_ff) <= 2^31.  The cache's and the attention's stand with them.
+ *     (T*k + 2) * max(d_model, d_ff) <= 2^31 and d_model * d_ff < 2^31, with EMOE_F8 the extents
+ *     taken in whole 128.  The cache's and the attention's stand with them.
  */
 #ifndef EMOE_H
 #define EMOE_H
@@ -59,14 +61,15 @@ typedef struct {
     int32_t E;       /* experts the gate scores                     */
     int32_t k;       /* experts per token                           */
     int32_t S;       /* expert slots in GPU memory (see note below) */
-    int32_t dtype;   /* emoe_dtype of x, weights, x_perm, y_perm, out */
+    int32_t dtype;   /* emoe_dtype of x, weights, x_perm, y_perm, out; EMOE_F8: weights packed, the others bf16 */
     int32_t act;     /* emoe_act                                    */
 } emoe_layer_desc;
 
 /* Note on S: the row counts of the slots live on the device, so the expert FFN picks its kernels
  * (weight streaming, small or large tiles) on the host from T*k / S, the average rows per slot if
- * every slot is occupied.  Results do not depend on it, speed does: size S to the resident budget
- * (the L of Section 3.4), not to E, when far fewer experts are resident than exist. */
+ * every slot is occupied.  Results depend on it through the order of fp32 sums alone (EMOE_F8: and
+ * through the codes of elements of h that lie near a tie, see there), speed does: size S to the
+ * resident budget (the L of Section 3.4), not to E, when far fewer experts are resident than exist. */
 
 /* Static description of a status code; never NULL, never freed. */
 const char *emoe_status_string(int status);
@@ -153,9 +156,11 @@ int emoe_permute_static(const emoe_layer_desc *desc, const void *x, const int32_
  * is less to compute and less to read from GPU memory).  For slot s and rows r in [slot_offsets[s], slot_offsets[s+1]):
  *   SwiGLU: h = silu(x_perm[r] W1_s^T) * (x_perm[r] W3_s^T),  y_perm[r] = h W2_s^T
  *   ReLU  : h = max(x_perm[r] W1_s^T, 0),                      y_perm[r] = h W2_s^T
- * Products accumulate in fp32; h and y_perm are rounded once to dtype.
+ * Products accumulate in fp32; h and y_perm are rounded once to dtype (EMOE_F8: the matrices, sums
+ * and h as in "Matrices in 8 bits", y_perm is bf16).
  * x_perm [A,d] dev; slot_offsets [S+1] dev; w1_slots, w3_slots [S,f,d] dev
- * (w3_slots must be NULL for ReLU and non-NULL for SwiGLU); w2_slots [S,d,f] dev;
+ * (w3_slots must be NULL for ReLU and non-NULL for SwiGLU); w2_slots [S,d,f] dev, with EMOE_F8 packed
+ * matrices one behind the other;
  * y_perm [A,d] dev (out); ws dev, ws_bytes >= ffn_ws_bytes.
  */
 int emoe_expert_ffn(const emoe_layer_desc *desc, const void *x_perm, const int32_t *slot_offsets,
@@ -191,7 +196,7 @@ int emoe_expert_ffn_gather_pass(const emoe_layer_desc *desc, int32_t pass, const
 /*
  * Gate-weighted combine back to token order (Section 1):
  *   out[t,:] = sum_{j<k} topk_weight[t,j] * y_perm[inv_perm[t*k+j], :], j ascending,
- * fp32 accumulation, one rounding to dtype.  out [T,d] dev.
+ * fp32 accumulation, one rounding to dtype (EMOE_F8: bf16).  out [T,d] dev.
  */
 int emoe_combine(const emoe_layer_desc *desc, const void *y_perm, const int32_t *inv_perm,
                  const float *topk_weight, void *out, void *stream);
@@ -245,7 +250,8 @@ int emoe_layer_forward(const emoe_layer_desc *desc, const void *x, const void *w
  * are read; they must stay valid and unchanged until done_event (or the stream)
  * completes, and should be pinned for the copy to be asynchronous.  host_w3 may
  * be NULL for ReLU.
- * w1_slots/w3_slots/w2_slots: dev slot buffers [S,f,d], [S,f,d], [S,d,f].
+ * w1_slots/w3_slots/w2_slots: dev slot buffers [S,f,d], [S,f,d], [S,d,f].  With EMOE_F8 all of
+ * them are packed matrices, one of emoe_matrix_bytes for each expert or slot.
  * slot_of_expert [E] dev, expert_of_slot [S] dev: the device maps (out).
  * expert_of_slot_host [S] host (in/out): the caller's mirror of expert_of_slot
  * (-1 = empty); read to validate the change, updated on success.
