@@ -78,10 +78,11 @@ const char *emoe_status_string(int status);
  * (either output pointer may be NULL).  Pure host arithmetic.  The FFN workspace is
  * h [A,f] in dtype plus, for bf16 layers with more than 22 rows per slot on average,
  * 32 or 64 MiB of fp32 partial sums of output tiles cut along K; for EMOE_F8 layers h and
- * x's rows in 8 bits, and where there are many rows 64 MiB of such sums and, with d_ff up to
- * 2560, a bit for each element of h.  Neither workspace needs initialising, and nothing in
- * them outlives a call except h between the two passes of emoe_expert_ffn_pass.  Calls that
- * may run at the same time (different streams) need workspaces of their own. */
+ * x's rows in 8 bits, and where there are many rows 64 MiB of such sums (d_model or d_ff
+ * above 2944) and, with d_ff up to 2560, a bit for each element of h.  Neither workspace
+ * needs initialising, and nothing in them outlives a call except h between the two
+ * passes of emoe_expert_ffn_pass.  Calls that may run at the same time (different
+ * streams) need workspaces of their own. */
 int emoe_workspace_bytes(const emoe_layer_desc *desc, size_t *permute_ws_bytes, size_t *ffn_ws_bytes);
 
 /*

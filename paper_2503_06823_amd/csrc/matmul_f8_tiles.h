@@ -59,10 +59,6 @@ constexpr int kMatrixScalesAt = kScalesAt + 2 * kScaleGroup;  // 256 bytes a wav
 constexpr int kTopsAt = kMatrixScalesAt + 2 * NW * 256;       // magnitudes of 128 rows a wavefront
 constexpr size_t LDS_BYTES = kTopsAt + NW * 128 * 4;
 constexpr int kPieceTiles = 4;                // K tiles (512 elements) of a piece of a leftover tile, at least
-// K tiles from which leftover tiles are cut into pieces: the pieces' sums and the launch that adds them cost as much as the rest of a round of 23.
-// (Cut / not, us: 24 groups of 300 rows times 2048 x 1408 57.7 / 48.2, 2048 rows times 4096 x 1024 39.4 / 27.3, 8 groups of 300 times 2048 x 2048 39.8 /
-// 31.8, of 512 SwiGLU rows times 4096 x 2944 101.2 / 99.4, 24 of 300 times 1408 x 2048 82.4 / 84.2.)
-constexpr int kLeastCut = 24;
 constexpr int kFixupGroups = (kMaxGroups - 1) * TS;  // workgroups of the fix-up launch: the most units there can be
 constexpr int kPlanFloats = kTiledPlanBytes / 4;     // the plan sits ahead of the partial sums
 
@@ -218,7 +214,7 @@ __device__ __forceinline__ void tiles(const F8Product& p, float* __restrict__ pa
     const int KB = p.lay.kb;  // K tiles, at least two
     const int G = gridDim.x;
     const SlotTable table = group_table(p, n_tiles, lane);
-    const Plan plan = make_plan(table.total, KB, G, KB < kLeastCut ? KB : kPieceTiles);
+    const Plan plan = make_plan(table.total, KB, G, KB < kF8LeastCut ? KB : kPieceTiles);
     if (blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<int4*>(partials) = make_int4(plan.tiles, plan.rounds, plan.left, plan.splits);
     const int xcd = blockIdx.x % XCDS, cu = blockIdx.x / XCDS, per_xcd = G / XCDS;
     const int sk_item = xcd * per_xcd + cu;
@@ -641,7 +637,7 @@ hipError_t launch_tiles(const F8Product& p, float* partials, const DeviceShape& 
     }
     const int n_tiles = EPI == kF8Swiglu ? p.lay.nb : (p.lay.nb + 1) / 2;
     KERNEL<<<shape.groups, 64 * NW, LDS_BYTES, st>>>(p, partials, n_tiles, shape.xcds);
-    if (p.lay.kb >= kLeastCut) fixup_kernel<EPI, TIES><<<kFixupGroups, 64 * NW, 0, st>>>(p, partials, n_tiles, shape.groups);
+    if (p.lay.kb >= kF8LeastCut) fixup_kernel<EPI, TIES><<<kFixupGroups, 64 * NW, 0, st>>>(p, partials, n_tiles, shape.groups);
     return hipGetLastError();
 }
 

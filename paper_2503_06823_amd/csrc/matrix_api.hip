@@ -86,7 +86,7 @@ MatmulWs matmul_ws(const emoe_matmul_desc& d, void* ws) {
     w.total = 0;
     w.x = rows_at(static_cast<uint8_t*>(ws), &w.total, d.rows, d.K);
     w.partials = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + w.total);
-    if (is_tiled(d.rows, d.groups, d.N, d.K, kF8Plain)) w.total += kTiledPartialBytes;
+    if (is_tiled(d.rows, d.groups, d.N, d.K, kF8Plain)) w.total += f8_partial_bytes(f8_layout(d.N, d.K).kb);
     return w;
 }
 
@@ -106,7 +106,9 @@ FfnF8Ws ffn_ws(const emoe_layer_desc& d, void* ws) {
     w.near = reinterpret_cast<uint16_t*>(static_cast<uint8_t*>(ws) + w.total);
     if (first_is_tiled(d) && whole(d.d_ff) <= kTieBlocks * kF8Block) w.total = align256(w.total + (size_t)A * whole(d.d_ff) / 8);
     w.partials = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + w.total);
-    if (first_is_tiled(d) || second_is_tiled(d)) w.total += kTiledPartialBytes;
+    const size_t first = first_is_tiled(d) ? f8_partial_bytes(f8_layout(d.d_ff, d.d_model).kb) : 0;
+    const size_t second = second_is_tiled(d) ? f8_partial_bytes(f8_layout(d.d_model, d.d_ff).kb) : 0;
+    w.total += first > second ? first : second;  // (one after the other)
     return w;
 }
 

@@ -66,7 +66,13 @@ inline bool f8_own_rows(long long rows, int K) { return rows <= 16 && rows * f8_
 hipError_t launch_f8_rows(const void* x, int64_t stride, int K, const F8Rows& to, const int32_t* perm, int k, const int32_t* end, hipStream_t st);
 // x by pieces, a row of it for each grouped row; or `from`
 hipError_t launch_f8_stream(const F8Product& p, F8Epilogue epilogue, hipStream_t st);
-// partials: kTiledPartialBytes.  x by rows; at least two blocks of columns.
+// K tiles (blocks of columns) from which leftover tiles are cut into pieces: the pieces' sums and the launch that adds them cost as much as some 24 of them.
+// Cut / not, us: 8 blocks 39.4 / 27.3 (2048 rows times 4096 x 1024); 11 57.7 / 48.2 (24 groups of 300 rows times 2048 x 1408); 16 82.4 / 84.2, 39.8 / 31.8; 23 101.2 /
+// 99.4; 25 49.9 / 48.8 (1024 rows times 6144 x 3200), 57.2 / 52.0 (2048 times 4096 x 3200); 26 46.7 / 49.4 (2100 times 1040 x 3208); 32 56.3 / 58.3 (1024 times
+// 6144 x 4096), 63.6 / 62.1, 106.5 / 112.8 (5120 times 4096 x 4096), of experts 177.9 / 173.0; 112 1186 / 1227 (4096 tokens' experts of 14336).
+constexpr int kF8LeastCut = 24;
+// partials: f8_partial_bytes(p.lay.kb).  x by rows; at least two blocks of columns.
+inline size_t f8_partial_bytes(int kb) { return kb >= kF8LeastCut ? kTiledPartialBytes : kTiledPlanBytes; }
 hipError_t launch_f8_tiled(const F8Product& p, F8Epilogue epilogue, float* partials, hipStream_t st);
 hipError_t launch_f8_ties(const F8Product& p, F8Epilogue epilogue, float* partials, hipStream_t st);  // (its part for activations into short rows of h)
 

@@ -7,13 +7,12 @@ import torch
 
 import paper_2503_06823_amd as P
 import test_gpu_packed_experts as streamed
-from packed_paths import CUT_FROM, blocks, experts_take_tiles
+from packed_paths import CUT_FROM, SHORT, blocks, experts_take_tiles
 from packed_util import HALF_STEP, as_device, close, packed, tokens
 
 pytestmark = pytest.mark.gpu
 
 COMPUTE_UNITS = 256
-SHORT = 20  # blocks of a row of h up to which tiles note elements near ties
 
 
 def tiles(rows, S, N, swiglu):

@@ -5,9 +5,10 @@ import itertools
 import pytest
 
 import paper_2503_06823_amd as P
-from packed_paths import blocks, experts_take_tiles, takes_tiles
+from packed_paths import CUT_FROM, SHORT, blocks, experts_take_tiles, takes_tiles
 
-LEAST_SUMS = 1 << 20  # of partial sums; rows alone are counted to the byte
+PLAN = 256  # bytes of a product in tiles; rows are counted to the byte
+SUMS = PLAN + (64 << 20)  # and of one that is cut along K
 
 
 def row_bytes(at, rows, K):
@@ -25,8 +26,7 @@ def test_products(groups):
     for N, K, rows in itertools.product(EXTENTS, EXTENTS, (1, 16, 64, 65, 200, 48 * groups, 48 * groups + 1, 1000, 1025, 3000, 8192, 20000)):
         if (rows + 2) * max(blocks(N), blocks(K)) * 128 <= 1 << 31:
             more = P.emoe_matmul_workspace_bytes(P.make_matmul_desc(rows, N, K, groups)) - row_bytes(0, rows, K)
-            assert more == 0 or more >= LEAST_SUMS
-            assert (more > 0) == takes_tiles(rows, groups, N, K), (rows, groups, N, K)
+            assert more == (0 if not takes_tiles(rows, groups, N, K) else SUMS if blocks(K) >= CUT_FROM else PLAN), (rows, groups, N, K)
             tiled += more > 0
     assert tiled > 100
 
@@ -38,9 +38,11 @@ def test_experts(S, k, act):
     for d, f, T in itertools.product(EXTENTS, EXTENTS, (1, 16, 64, 65, 48 * S, 600, 1000, 1500, 3000, 4100, 8192)):
         if (T * k + 2) * max(blocks(d), blocks(f)) * 128 <= 1 << 31:
             n = P.emoe_workspace_bytes(P.make_desc(T, d, f, S, k, S, "f8", act))[1]
-            more = n - row_bytes(row_bytes(0, T * k, f), T * k, d)
+            at = row_bytes(row_bytes(0, T * k, f), T * k, d)
             both = experts_take_tiles(T, d, f, S, k)
-            assert more == 0 or more >= LEAST_SUMS
-            assert (more > 0) == any(both), (T, d, f, S, k)
+            if both[0] and blocks(f) <= SHORT:
+                at = -(-(at + T * k * blocks(f) * 16) // 256) * 256
+            cut = any(tiled and blocks(K) >= CUT_FROM for tiled, K in zip(both, (d, f)))
+            assert n - at == (SUMS if cut else PLAN if any(both) else 0), (T, d, f, S, k)
             seen.add(both)
     assert len(seen) == 4
