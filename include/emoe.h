@@ -79,7 +79,7 @@ const char *emoe_status_string(int status);
  * h [A,f] in dtype plus, for bf16 layers with more than 22 rows per slot on average,
  * 32 or 64 MiB of fp32 partial sums of output tiles cut along K; for EMOE_F8 layers h and
  * x's rows in 8 bits, and where there are many rows 64 MiB of such sums (d_model or d_ff
- * above 2944) and, with d_ff up to 2560, a bit for each element of h.  Neither workspace
+ * above 2944) and, with d_ff up to 640, a bit for each element of h.  Neither workspace
  * needs initialising, and nothing in them outlives a call except h between the two
  * passes of emoe_expert_ffn_pass.  Calls that may run at the same time (different
  * streams) need workspaces of their own. */
@@ -571,8 +571,9 @@ int emoe_kv_attention(const emoe_kv_desc *desc, const emoe_attention_desc *atten
  * never rounded to anything else, to 8 bits as above:
  *   h = q(act(q(x) W1^T) (* q(x) W3^T)),  y = bf16(h W2^T).
  * Products are summed as in emoe_matmul.  What the sums lose, 1e-5 to 1e-4 of an element of h as a rule, may give an element that is as near to a tie of
- * two codes either of them.  With d_ff up to 2560, elements within 1e-4 of a tie whose two codes are more than 1 / 32 of their row of h apart (a row being taken
- * for the root of the sum of the squares of its blocks' largest elements) are summed again in fp32, whichever kernel makes h.
+ * two codes either of them.  With d_ff up to 640, elements within 1e-4 of a tie whose two codes are more than 1 / 16 of their row of h apart (a row being taken
+ * for the root of the sum of the squares of its blocks' largest elements) are summed again in fp32, whichever kernel makes h; longer rows have such elements only
+ * where a block is far above the others, and products of few rows a slot look for them up to 2560.
  */
 
 /* Bytes of a packed matrix; a multiple of 256.  Pure host arithmetic. */

@@ -1,4 +1,4 @@
-// Products in 8 bits for many rows a group, activations into rows of h of up to kTieBlocks blocks: the kernels of matmul_f8_tiles.h, which also note the
+// Products in 8 bits for many rows a group, activations into rows of h of up to kTieBlocksTiled blocks: the kernels of matmul_f8_tiles.h, which also note the
 // elements near ties of two codes (see kNearTie), and a launch that sums those once more.
 #include "matmul_f8_tiles.h"
 
@@ -14,9 +14,8 @@ __global__ __launch_bounds__(64 * NW) void tiled_ties(F8Product p, float* __rest
 // other blocks of a row are not known.  A thread looks at 64 outputs of a row at a time; of what a workgroup finds a thread each asks whether it matters,
 // and half wavefronts sum what does.  All of it is memory latencies, one after the other: so workgroups are large, and no more than there are CUs.
 // A row is at least as large as the square root of the sum of the squares of its blocks' largest elements, each 224 and more under its power.  An element matters
-// if its two codes, 32 apart from 256 on and 16 below, are more than 1 / 32 of that apart: what does not changes its row by less than the rounding of the
-// row's elements to four bits.
-constexpr float kMatters32 = 20.9f, kMatters16 = 5.22f;  // (32 * 32 / 224)^2, (16 * 32 / 224)^2: what the row's squares have to stay below, in this block's power
+// if its two codes, 32 apart from 256 on and 16 below, are more than 1 / 16 of that apart.
+constexpr float kMatters32 = 5.22f, kMatters16 = 1.306f;  // (32 * 16 / 224)^2, (16 * 16 / 224)^2: what the row's squares have to stay below, in this block's power
 constexpr int kNearThreads = 512, kNearAtOnce = 16;      // of a workgroup; words of 64 outputs that a thread looks at in one go
 constexpr int kNearList = 2048;                          // elements that a workgroup lists at once
 struct NearElement {  // of a list: (round * threads + thread) * 64 + bit
@@ -87,12 +86,12 @@ __global__ __launch_bounds__(kNearThreads) void near_ties_kernel(F8Product p) {
                 const NearElement e(list[i], word0, stride, (uint32_t)p.rows);
                 const uint32_t code = *code_of(e) & 127u;
                 const int power = (int)power_of(e);
-                uint32_t powers[(kTieBlocks + 3) / 4];
+                uint32_t powers[(kTieBlocksTiled + 3) / 4];
 #pragma unroll
-                for (int j = 0; j < (kTieBlocks + 3) / 4; ++j) powers[j] = 4 * j < p.lay.nb ? p.h.scales[(size_t)j * p.h.rows + e.row] : 0;
+                for (int j = 0; j < (kTieBlocksTiled + 3) / 4; ++j) powers[j] = 4 * j < p.lay.nb ? p.h.scales[(size_t)j * p.h.rows + e.row] : 0;
                 float squares = 0.0f;  // of the row's blocks' powers, over this one's
 #pragma unroll
-                for (int j = 0; j < kTieBlocks; ++j)
+                for (int j = 0; j < kTieBlocksTiled; ++j)
                     if (j < p.lay.nb) squares += ldexpf(1.0f, 2 * ((int)((powers[j >> 2] >> (8 * (j & 3))) & 255u) - power));
                 if (squares < (code >= 0x78u ? kMatters32 : kMatters16)) matters[atomicAdd(&how_many, 1)] = list[i];  // (0x78: 256.  In any order: each is one's own)
             }

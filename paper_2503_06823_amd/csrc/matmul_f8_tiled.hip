@@ -12,7 +12,7 @@ __global__ __launch_bounds__(64 * NW) void tiled_kernel(F8Product p, float* __re
 }  // namespace
 
 hipError_t launch_f8_tiled(const F8Product& p, F8Epilogue epilogue, float* partials, hipStream_t st) {
-    if (epilogue != kF8Plain && p.lay.nb <= kTieBlocks) return launch_f8_ties(p, epilogue, partials, st);
+    if (epilogue != kF8Plain && p.lay.nb <= kTieBlocksTiled) return launch_f8_ties(p, epilogue, partials, st);
     DeviceShape shape;
     const hipError_t e = device_shape(&shape);
     if (e != hipSuccess) return e;

@@ -104,7 +104,7 @@ FfnF8Ws ffn_ws(const emoe_layer_desc& d, void* ws) {
     w.h = rows_at(static_cast<uint8_t*>(ws), &w.total, A, d.d_ff);
     w.x = rows_at(static_cast<uint8_t*>(ws), &w.total, A, d.d_model);
     w.near = reinterpret_cast<uint16_t*>(static_cast<uint8_t*>(ws) + w.total);
-    if (first_is_tiled(d) && whole(d.d_ff) <= kTieBlocks * kF8Block) w.total = align256(w.total + (size_t)A * whole(d.d_ff) / 8);
+    if (first_is_tiled(d) && whole(d.d_ff) <= kTieBlocksTiled * kF8Block) w.total = align256(w.total + (size_t)A * whole(d.d_ff) / 8);
     w.partials = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + w.total);
     const size_t first = first_is_tiled(d) ? f8_partial_bytes(f8_layout(d.d_ff, d.d_model).kb) : 0;
     const size_t second = second_is_tiled(d) ? f8_partial_bytes(f8_layout(d.d_model, d.d_ff).kb) : 0;

@@ -33,7 +33,8 @@ inline size_t f8_rows_scale_bytes(long long rows, int K) { return (size_t)rows *
 
 // The product of grouped rows with their group's matrix (offsets NULL: one group of all rows), and what becomes of it:
 // plain: bf16 rows of out; SwiGLU, ReLU: the activation's result as rows in 8 bits, h.
-constexpr int kTieBlocks = 20;  // blocks of a row of h up to which elements near ties of two codes are summed again, see kNearTie
+// Blocks of a row of h up to which elements near ties of two codes are summed again (see kNearTie), by tiles and by streaming
+constexpr int kTieBlocksTiled = 5, kTieBlocks = 20;
 enum F8Epilogue { kF8Plain = 0, kF8Swiglu = 1, kF8Relu = 2 };
 struct F8Product {
     F8Rows x;
@@ -128,11 +129,13 @@ __device__ __forceinline__ uint2 f8_codes(const float (&v)[8], float inverse) {
 // The matrix cores' sums are 1e-5 to 5e-5 off (see matmul_f8_stream.hip), a thousandth of a code's step, and of an element that near a tie of two codes
 // they decide which of the two it gets.  Of the elements that are large in their block (128 and more, of up to 448) the codes are up to an eighth of the
 // element apart: where such an element is most of its row of h, an output row changes by as much (1368 tokens, d 1216, f 200: one row 9 %, all outputs 5.8e-3;
-// with those elements summed again 0.8 % and 2.5e-3).  So a large element within kNearTie of a tie whose step is more than 1 / 32 of its row gets its sums once more,
-// products exact and added in fp32, and the code of these, whichever kernel makes h: some 1e-4 of all elements are near ties, 2e-5 matter.
-// Rows of up to kTieBlocks blocks: where blocks share a power, a step is at most 1 / 32 of a longer row (a block's largest element is 224 or more under its
-// power, a step 32).  In longer ones a block that stands out by more than its neighbours' powers is left as it is: looking for these cost 64 tokens' experts of
-// f 14336 190 -> 203 us and 4096 tokens' 1172 -> 1215.
+// with those elements summed again 0.8 % and 2.5e-3).  So a large element within kNearTie of a tie that matters to its row, its step being more than 1 / 16 of it,
+// gets its sums once more, products exact and added in fp32, and the code of these, whichever kernel makes h.  (1e-4 to 3e-4 of all elements are near ties.)
+// Where blocks share a power, a step is at most 1 / 16 of rows of more than five blocks (a block's largest element is 224 or more under its power, a step 32), and a
+// code on the other side of a tie changes them by no more than the rounding of each of their elements to four bits.  So tiles look for such elements in rows of up to
+// five blocks, at 10 us a call (16384 rows of d 1216, f 200 78 -> 88; 6000 of f 640, ReLU, 56 -> 66), and streaming, where few rows are much of a call's result, up to
+// 20 (64 tokens' 24 experts of f 1408 63.3 -> 65.1, 500 tokens' of f 512 32.4 -> 36.1, 1368 of f 200 44.4 -> 49.0; beyond, 64 tokens' of f 14336 190 -> 203).
+// Tiles up to 20 blocks: 8192 tokens' 24 experts of f 1408 472 -> 505 us; of any length: 4096 tokens' of 14336 1172 -> 1215.
 // A call takes longer for it with such elements: a microsecond or two of a half or whole wavefront each, which is felt where most rows have many.
 // What is left: one in some 100 sums of large elements is off by more than kNearTie (2e-4 to 1e-4 of the element, where terms of the sum cancel); smaller elements
 // have what the matrix cores say, a step of theirs being at most a thirtieth of the block's largest.

@@ -3,7 +3,7 @@ test_packed_paths.py holds what is said here to the library's workspaces."""
 BLOCK = 128
 CUT_FROM = 24  # blocks of columns from which tiles that leave compute units idle are cut along K
 
-SHORT = 20     # blocks of a row of h up to which tiles note elements near ties of two codes
+SHORT = 5      # blocks of a row of h up to which tiles note elements near ties of two codes
 
 
 def blocks(n):

@@ -24,11 +24,13 @@ def tiles(rows, S, N, swiglu):
 CASES = [
     (3100, 264, 1032, 1, 1, "swiglu", (True, False)), (3100, 264, 1160, 2, 2, "relu", (True, False)), (1200, 520, 136, 8, 6, "swiglu", (False, True)),
     (3000, 392, 2056, 3, 2, "relu", (True, True)), (1500, 648, 1416, 8, 4, "swiglu", (True, True)),
+    # rows of h of up to five blocks
+    (5300, 264, 520, 1, 1, "swiglu", (True, False)), (8300, 392, 264, 2, 1, "relu", (True, True)),
     # more than a round of tiles, of an odd number of blocks of columns
     (6000, 520, 1160, 2, 2, "swiglu", (True, True)), (9000, 392, 2184, 1, 1, "relu", (True, True)),
     # cut along K: the first product, the second, both; behind a round of whole tiles
-    (4300, 3208, 520, 1, 1, "swiglu", (True, True)), (2300, 3208, 648, 3, 2, "relu", (True, True)), (1500, 648, 3336, 2, 2, "swiglu", (True, True)),
-    (1100, 3336, 3208, 2, 1, "relu", (True, True)), (2100, 3208, 2184, 2, 2, "swiglu", (True, True)),
+    (4300, 3208, 520, 1, 1, "swiglu", (True, True)), (2800, 3208, 520, 3, 2, "relu", (True, True)), (2300, 3208, 648, 3, 2, "relu", (True, True)),
+    (1500, 648, 3336, 2, 2, "swiglu", (True, True)), (1100, 3336, 3208, 2, 1, "relu", (True, True)), (2100, 3208, 2184, 2, 2, "swiglu", (True, True)),
     (1100, 3208, 3336, 2, 2, "swiglu", (True, True)), (2600, 392, 3208, 2, 2, "relu", (True, True)),
 ]
 
@@ -52,11 +54,11 @@ def test_the_cases_are_of_every_kind():
     assert {(True, 1, False), (True, 0, False), (False, 1, False), (False, 0, False), (True, 0, True), (False, 1, True)} <= rounds
 
 
-@pytest.mark.parametrize("sizes,d", [((0, 4000, 0, 17, 1, 2500, 64), 392), ((1, 257, 5000, 0), 264), ((0, 0, 2500, 15, 241), 3208)])
-@pytest.mark.parametrize("act", ("swiglu", "relu"))
-def test_uneven_slots(gpu_device, sizes, d, act):
-    assert experts_take_tiles(sum(sizes), d, 1160, len(sizes), 1)[0]
-    a = streamed.Layer(sum(sizes), d, 1160, len(sizes), 1, act, sizes=sizes)
+@pytest.mark.parametrize("sizes,d", [((0, 4000, 0, 17, 1, 2500, 64), 392), ((1, 257, 5500, 0), 264), ((0, 0, 4000, 15, 241), 3208)])
+@pytest.mark.parametrize("f,act", [(520, "swiglu"), (520, "relu"), (1160, "swiglu"), (1160, "relu")])
+def test_uneven_slots(gpu_device, sizes, d, f, act):
+    assert experts_take_tiles(sum(sizes), d, f, len(sizes), 1)[0]
+    a = streamed.Layer(sum(sizes), d, f, len(sizes), 1, act, sizes=sizes)
     want, off = a.experts()
     a.gather()
     torch.cuda.synchronize()
@@ -69,11 +71,11 @@ def test_uneven_slots(gpu_device, sizes, d, act):
     assert (scale == 1).all() and torch.equal(a.out[:-1], y[:-1][torch.from_numpy(a.inverse).cuda()])
 
 
-@pytest.mark.parametrize("T,d", [(4000, 392), (2200, 3208)])
+@pytest.mark.parametrize("T,d,f", [(4000, 392, 1160), (2200, 3208, 1160), (5300, 392, 520), (4300, 3208, 520)])
 @pytest.mark.parametrize("act", ("swiglu", "relu"))
-def test_nan_and_infinity_stay_in_their_rows(gpu_device, T, d, act):
-    assert experts_take_tiles(T, d, 1160, 2, 1)[0]
-    a = streamed.Layer(T, d, 1160, 2, 1, act)
+def test_nan_and_infinity_stay_in_their_rows(gpu_device, T, d, f, act):
+    assert experts_take_tiles(T, d, f, 2, 1)[0]
+    a = streamed.Layer(T, d, f, 2, 1, act)
     a.combine()
     torch.cuda.synchronize()
     before = a.out[:-1].clone()
@@ -90,11 +92,10 @@ def test_nan_and_infinity_stay_in_their_rows(gpu_device, T, d, act):
     assert torch.equal(a.out[:-1][others], before[others])
 
 
-@pytest.mark.parametrize("T,d", [(3300, 264), (4300, 3208)])
+@pytest.mark.parametrize("T,d,f", [(3300, 264, 1032), (4300, 3208, 1032), (5300, 264, 520)])
 @pytest.mark.parametrize("act", ("swiglu", "relu"))
-def test_h_beyond_fp32_is_nan_and_large_h_is_not(gpu_device, T, d, act):
+def test_h_beyond_fp32_is_nan_and_large_h_is_not(gpu_device, T, d, f, act):
     """h passes fp32's range in one row, and only there is the result NaN."""
-    f = 1032
     assert experts_take_tiles(T, d, f, 1, 1)[0]
     a = streamed.Layer(T, d, f, 1, 1, act)
     x = np.zeros((T, d))
@@ -112,7 +113,7 @@ def test_h_beyond_fp32_is_nan_and_large_h_is_not(gpu_device, T, d, act):
     assert nan[1].all() and int(nan.sum()) == d and torch.isfinite(a.out[2]).all()
 
 
-@pytest.mark.parametrize("T,d,f,S,k,act", [(2100, 264, 1160, 3, 2, "swiglu"), (2300, 3208, 648, 3, 2, "relu"), (4300, 3208, 520, 1, 1, "swiglu")])
+@pytest.mark.parametrize("T,d,f,S,k,act", [(2100, 264, 1160, 3, 2, "swiglu"), (2800, 3208, 520, 3, 2, "relu"), (4300, 3208, 520, 1, 1, "swiglu")])
 def test_graph_replays_with_eager_work_between(gpu_device, T, d, f, S, k, act):
     assert experts_take_tiles(T, d, f, S, k)[0]
     a = streamed.Layer(T, d, f, S, k, act)
@@ -143,7 +144,7 @@ def test_graph_replays_with_eager_work_between(gpu_device, T, d, f, S, k, act):
         assert torch.equal(a.out[:-1], want[i ^ 1][:-1])
 
 
-@pytest.mark.parametrize("T,d,f,S,k,act", [(3000, 392, 2056, 3, 2, "relu"), (2100, 3208, 2184, 2, 2, "swiglu")])
+@pytest.mark.parametrize("T,d,f,S,k,act", [(3000, 392, 2056, 3, 2, "relu"), (2100, 3208, 2184, 2, 2, "swiglu"), (2800, 3208, 520, 3, 2, "swiglu")])
 def test_the_same_bits_every_time(gpu_device, T, d, f, S, k, act):
     assert experts_take_tiles(T, d, f, S, k) == (True, True)
     a = streamed.Layer(T, d, f, S, k, act)

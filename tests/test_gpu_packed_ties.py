@@ -88,10 +88,9 @@ def check(a, grouped=False):
 # T, d, f, S, k: streaming with rows that it converts itself, and with converted ones of one to four blocks of 16 a stretch
 STREAMED = [(4, 264, 520, 3, 2), (16, 1032, 264, 1, 1), (8, 2056, 136, 2, 1), (12, 2056, 1032, 2, 2), (40, 264, 136, 3, 1), (64, 264, 520, 1, 1), (150, 1032, 392, 2, 1),
             (200, 392, 2312, 2, 2)]
-# tiles: whole ones, of several groups, of few rows a group, of many columns; cut along K.  There an element has to matter to its row: in more than five
-# blocks it does if the others are smaller
-TILED = [(3200, 264, 1032, 1, 1), (1500, 392, 1160, 2, 2), (800, 520, 2056, 8, 4), (1400, 264, 2504, 3, 1), (4200, 3208, 520, 1, 1), (2200, 3208, 648, 3, 2),
-         (5100, 264, 520, 2, 1), (8200, 520, 136, 3, 2)]
+# tiles: whole ones, of several groups, of few rows a group; cut along K.  There an element has to matter to its row, which it does if the other blocks are smaller
+TILED = [(5300, 264, 520, 1, 1), (8300, 392, 264, 2, 1), (3200, 520, 392, 8, 4), (26000, 136, 104, 1, 1), (5300, 1160, 640, 3, 1), (4300, 3208, 520, 1, 1),
+         (2800, 3208, 392, 3, 2), (8200, 520, 136, 3, 2)]
 
 
 @pytest.mark.parametrize("kinds", (KINDS, TIES + KINDS[:1]), ids=("beside", "on"))
@@ -109,12 +108,12 @@ def test_streamed(gpu_device, T, d, f, S, k, act, kinds):
 @pytest.mark.parametrize("T,d,f,S,k", TILED)
 def test_tiled(gpu_device, T, d, f, S, k, act, grouped):
     assert experts_take_tiles(T, d, f, S, k)[0]
-    check(Beside(T, d, f, S, k, act, KINDS + (TIES if act == "relu" else TIES[:1]), one_block=blocks(f) > 5), grouped)
+    check(Beside(T, d, f, S, k, act, KINDS + (TIES if act == "relu" else TIES[:1]), one_block=blocks(f) > 1), grouped)
 
 
 def test_many_more_elements_than_a_list_holds(gpu_device):
     """All elements of all rows of a block: one workgroup finds tens of thousands."""
-    a = Beside(5100, 264, 520, 1, 1, "relu", KINDS)
+    a = Beside(26000, 136, 104, 1, 1, "relu", KINDS)
     assert experts_take_tiles(a.T, a.d, a.f, a.S, a.k)[0]
     for w, _, second, columns in a.experts:
         w[:, 8:] = np.where(w[:, 8:] != 0, np.tile([16.0, 4.0, 2.0 ** -4, 0, 0, 0, 0, 0], a.d // 8 - 1), 0)
@@ -127,7 +126,7 @@ def test_the_sizes_are_of_every_kind():
 
 
 def test_the_same_tokens_have_the_same_codes_however_many_stand_beside_them(gpu_device):
-    few, many = (Beside(T, 264, 1032, 1, 1, "swiglu", KINDS, one_block=True) for T in (40, 3200))
-    assert not experts_take_tiles(40, 264, 1032, 1, 1)[0] and experts_take_tiles(3200, 264, 1032, 1, 1)[0]
+    few, many = (Beside(T, 264, 520, 1, 1, "swiglu", KINDS, one_block=True) for T in (40, 5300))
+    assert not experts_take_tiles(40, 264, 520, 1, 1)[0] and experts_take_tiles(5300, 264, 520, 1, 1)[0]
     assert (few.x == many.x[:40]).all() and (few.perm == np.arange(40)).all()
     assert (few.run() == many.run()[:40]).all()
