@@ -17,10 +17,11 @@
 // Rows are spread evenly over a group's tiles in blocks of 16, and the K loop is compiled for 0 .. 8 blocks a wavefront (tile_plan.h).  Tiles that
 // do not fill a round of the chip are cut along K, and a second launch adds the pieces in order.
 //
-// 8192 rows times 6144 x 4096 in 152 us, 2.7 PFLOP/s (a library's product of the same extents, with one factor a matrix, 162 to 171), the SwiGLU product of
-// 8192 assignments over four experts of 14336 x 4096 in 737 us, 2.6 PFLOP/s.  What bounds it is the power that the matrix cores draw: they are busy in 63 to 71 % of
-// the cycles at a clock that they push down to 1.9 to 2.0 GHz; without any LDS reads it would be 7 to 10 % faster.  LDS is busy in 19 % of the cycles.  A tile of K
-// takes 1.3 to 1.5 us; an item's end 4 us, of the SwiGLU product 10 (activation 5.6, codes and stores 3.4, the next item's beginning 1).
+// 8192 rows times 6144 x 4096: 177 us a call, 22 to 25 of them the conversion, so some 152 for the product, 2.7 PFLOP/s (under the tracer 158 to 184; a library's
+// product of the same extents, with one factor a matrix, 164 to 171).  The SwiGLU product of 8192 assignments over four experts of 14336 x 4096 in 745 to 777 us, 2.5
+// PFLOP/s.  What bounds it is the power that the matrix cores draw: they are busy in 63 to 71 % of the cycles at a clock that they push down to 1.9 to 2.0 GHz; without
+// any LDS reads it would be 7 to 10 % faster.  LDS is busy in 19 % of the cycles.  A tile of K takes 1.3 to 1.5 us; an item's end 4 us, of the SwiGLU product 10 (activation
+// 5.6, codes and stores 3.4, the next item's beginning 1).
 //
 // The activation's result leaves as rows in 8 bits: h replaces the gate's accumulators, its largest magnitude over the 128 columns is joined between
 // lanes and, of SwiGLU, between the two wavefronts that share the columns, and a lane's codes are exchanged so that 16 of a row are stored at once.

@@ -56,7 +56,8 @@ F8Rows rows_at(uint8_t* ws, size_t* at, long long rows, int K) {
 // 53.8 / 47.7; 1024 x 1024 1024 rows 10.9 / 23.4; 8 of 14336 x 4096 64 rows each 104 / 109, 80 185 / 109; 8 of 2048 x 2048 128 23.8 / 29.2, 256 35.1 / 36.5, 320
 // 47.0 / 32.3; 24 of 2048 x 1408 64 31.0 / 27.0, 80 41.0 / 28.0.  SwiGLU's two: 6 groups of 14336 x 4096 64 rows 144 / 146, 80 254 / 156; 4 of 4096 x 1024
 // 128 21.0 / 23.6; one of 14336 x 4096 128 51.3 / 50.2, 160 79.5 / 50.0; ReLU 128 30.7 / 36.8, 160 43.6 / 37.9; 16 of 2816 x 1032 64 24.3 / 23.1, 80
-// 35.1 / 24.4.  Tiles take at least two blocks of columns.
+// 35.1 / 24.4.  Tiles take at least two blocks of columns.  What goes by averages is wrong about a group that has most of the rows: 3000 of 64 groups of 6144 x
+// 4096 stream in 371 us spread evenly, in 426 with half of them in one group, in 226 with all of them there, which tiles of one group take 91 for.
 bool is_tiled(long long rows, int groups, int N, int K, F8Epilogue epilogue) {
     if (K <= kF8Block || rows <= (groups == 1 ? 64ll : 48ll) * groups) return false;
     const bool plain = epilogue == kF8Plain;
