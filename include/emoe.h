@@ -581,7 +581,7 @@ int emoe_matrix_bytes(int32_t N, int32_t K, size_t *bytes);
 
 /*
  * `count` matrices [N][K] of dtype (EMOE_F32 or EMOE_BF16), rows w_stride elements apart (at least K, a multiple of 8) and matrices N rows, packed one
- * behind the other; and the numbers that packed matrices hold, which both types hold exactly.  w, matrices: dev, 16-byte aligned, different;
+ * behind the other; and the numbers that packed matrices hold, which both types hold exactly.  w, matrices: dev, 16-byte aligned, not overlapping;
  * count at most 65535.  What lies between the rows of w is neither read nor written.
  */
 int emoe_matrix_pack(int32_t count, int32_t N, int32_t K, int32_t dtype, const void *w, int64_t w_stride, void *matrices,
@@ -610,8 +610,8 @@ int emoe_matmul_workspace_bytes(const emoe_matmul_desc *desc, size_t *bytes);
  * last group are not written.  Matrices of groups without rows are not read.
  * Sums are in fp32, but the products of eight elements that follow each other come together in units of 2^-13 of the power of two of the
  * largest, as the matrix cores add numbers of 8 bits; the result is rounded to bf16 once.  A NaN in a row makes NaN of that row of out only.  Results do
- * not depend on the order of execution.  x, out, matrices, ws: dev, 16-byte aligned, all different; ws not shared with a call that may
- * run at the same time.
+ * not depend on the order of execution.  x, out, matrices, ws: dev, 16-byte aligned, none overlapping another (rows of x and of out may lie side by side in
+ * wider rows); ws not shared with a call that may run at the same time.
  */
 int emoe_matmul(const emoe_matmul_desc *desc, const void *x, const int32_t *group_offsets, const void *matrices, void *out, void *ws,
                 size_t ws_bytes, void *stream);

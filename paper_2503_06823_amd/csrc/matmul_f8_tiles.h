@@ -120,7 +120,7 @@ __device__ __forceinline__ uint32_t activate(Get get, Put put) {
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
             float g = get(b, v);
-            if constexpr (EPI == kF8Swiglu) g = g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)) * get(b + NB, v);
+            if constexpr (EPI == kF8Swiglu) g = g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)) * get(b + NB, v);  // (rcp: an ulp, 2^-20 of a code's step)
             else g = g < 0.0f ? 0.0f : g;  // (NaN stays)
             put(b, v, g);
             top = umax(top, f8_magnitude(g));
